@@ -263,6 +263,88 @@ ff_status_t ff_get_tap(const ff_plan_t *plan, int32_t which, const void **dev_pt
  * tensor-core attention launch from 128 pooled tokens on.  Every other configuration runs on the generic fp32 kernels. */
 ff_status_t ff_plan_set_attention_impl(ff_plan_t *plan, int32_t impl);
 
+/* ---- queries and keys between the projections and the attention ------------------------------------
+ *
+ * Rotary positions, and the norm of every head row with the rotation in the same pass; for layers whose
+ * Q and K carry positions or are normalised before ff_forward.  (No counterpart in the paper, which takes
+ * Q and K as given.)
+ *
+ *   rotation  of the rot_dim / 2 channel pairs (a, b) of a row at position s:
+ *             (m (a cos t - b sin t), m (a sin t + b cos t)),  t = s theta_i;  channels from rot_dim on stay
+ *   norm      z = x r w,  r = 1 / sqrt(mean(x^2) + eps) over the head_dim channels of a row
+ *
+ * theta_i = base^(-i / P), i = 0 .. P-1, for P = rot_dim / 2 pairs; scaled for contexts longer than the
+ * trained one:
+ *   LINEAR    theta_i / factor (position interpolation)
+ *   NTK       base replaced by base * factor^(P / (P - 1)): the slowest pair as LINEAR, the fastest unchanged
+ *   BY_PARTS  theta_i (g + (1 - g) / factor), g = clamp((u_i - 1) / 31, 0, 1) with the turns u_i =
+ *             original_length theta_i / 2 pi that the pair makes within the original length, and
+ *             m = 0.1 ln(factor) + 1 (m = 1 otherwise); Peng et al., "YaRN", 2023
+ * With axis_pairs the pairs are divided over the axes of a grid: the first axis_pairs[0] turn with t, the
+ * next axis_pairs[1] with h, the others with w, each axis with its own i and P.
+ *
+ * A handle holds host memory only and serves any device; calls run on the current one.  Like a plan it is
+ * not thread-safe (its error message), and its calls are asynchronous on the given stream. */
+typedef struct ff_rotary ff_rotary_t; /* opaque */
+
+enum { FF_ROTARY_HALF = 0,          /* pair i = channels (i, i + rot_dim / 2) */
+       FF_ROTARY_INTERLEAVED = 1 }; /* pair i = channels (2i, 2i + 1) */
+enum { FF_ROTARY_SCALE_NONE = 0, FF_ROTARY_SCALE_LINEAR = 1, FF_ROTARY_SCALE_NTK = 2, FF_ROTARY_SCALE_BY_PARTS = 3 };
+
+typedef struct {
+  int32_t head_dim;        /* multiple of 8, <= 256 */
+  int32_t rot_dim;         /* even, 2 .. head_dim: the first rot_dim channels are turned */
+  int32_t dtype;           /* FF_BF16 or FF_FP32: the tensors; all arithmetic is fp32 */
+  int32_t layout, scaling;
+  int32_t axis_pairs[3];   /* pairs that turn with t, h, w; {0, 0, 0}: one position per token */
+  int32_t grid[3];         /* T, H, W of calls without positions (axis_pairs needed), or {0, 0, 0} */
+  int32_t original_length; /* BY_PARTS */
+  double base, factor;     /* base >= 1; 1 <= factor <= 1e9 (not used by NONE) */
+} ff_rotary_config_t;
+
+/* One tensor of head rows: element (b, h, n, c) lies at data[b stride_batch + h stride_head + n stride_token
+ * + c].  Strides in elements, >= 0, any order; rows that are wider aligned move in wider pieces (16 bytes at
+ * most).  An output may be its own input (the same address and strides); otherwise outputs overlap nothing. */
+typedef struct {
+  void *data;              /* device */
+  int64_t stride_batch, stride_head, stride_token;
+  int32_t heads;
+} ff_heads_t;
+
+ff_status_t ff_rotary_create(const ff_rotary_config_t *cfg, ff_rotary_t **out);
+ff_status_t ff_rotary_destroy(ff_rotary_t *rotary);   /* NULL is allowed */
+
+/* Message of the last failing call on this handle; NULL: as ff_last_error(NULL). */
+const char *ff_rotary_last_error(const ff_rotary_t *rotary);
+
+/* The handle's frequencies, theta[rot_dim / 2] in radians per position, and the magnitude m.  Host only. */
+ff_status_t ff_rotary_frequencies(const ff_rotary_t *rotary, double *theta, double *magnitude);
+
+/* The rotation of q and (unless k is NULL) k; `inverse` non-zero: its transpose, which is the backward pass.
+ *   positions  device, int32: positions of sample b at positions + b position_stride, [tokens] or, with
+ *              axis_pairs, [tokens][3] (t, h, w).  NULL: 0 .. tokens-1, or the cells of the grid in order */
+ff_status_t ff_rotary_apply(const ff_rotary_t *rotary, int64_t batch, int64_t tokens, const int32_t *positions,
+                            int64_t position_stride, const ff_heads_t *q, const ff_heads_t *k, int32_t inverse,
+                            const ff_heads_t *q_out, const ff_heads_t *k_out, void *cuda_stream);
+
+/* Norm of every row of q and k, then the rotation, in one pass.
+ *   wq, wk  device, float [head_dim], or NULL for ones;  eps > 0 */
+ff_status_t ff_qk_norm(const ff_rotary_t *rotary, int64_t batch, int64_t tokens, const int32_t *positions,
+                       int64_t position_stride, const ff_heads_t *q, const ff_heads_t *k, const float *wq,
+                       const float *wk, float eps, const ff_heads_t *q_out, const ff_heads_t *k_out, void *cuda_stream);
+
+/* Its backward pass: from the inputs q, k and the gradients of the outputs, the gradients of the inputs (dq may
+ * be dq_out, or q) and of the weights (device, float [head_dim]; NULL: not wanted).  The weights' sums run over
+ * all rows in an order that depends on the sizes alone: the same call gives the same bits.
+ *   workspace  device, 16-byte aligned, ff_qk_norm_workspace_bytes; calls that may run at the same time need
+ *              one each */
+ff_status_t ff_qk_norm_backward(const ff_rotary_t *rotary, int64_t batch, int64_t tokens, const int32_t *positions,
+                                int64_t position_stride, const ff_heads_t *q, const ff_heads_t *k, const float *wq,
+                                const float *wk, float eps, const ff_heads_t *dq_out, const ff_heads_t *dk_out,
+                                const ff_heads_t *dq, const ff_heads_t *dk, float *dwq, float *dwk, void *workspace,
+                                size_t workspace_bytes, void *cuda_stream);
+ff_status_t ff_qk_norm_workspace_bytes(const ff_rotary_t *rotary, size_t *bytes);
+
 /* ---- for callers that cannot allocate device memory ---------------------------------------------
  *
  * The paper has no counterpart of this entry point; it exists for integration reasons only.

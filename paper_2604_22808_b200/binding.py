@@ -12,7 +12,7 @@ from typing import Optional, Sequence
 
 import numpy as np
 
-from .configs import FFConfig
+from .configs import FFConfig, RotaryConfig
 
 # FF_LIBRARY_VARIANT=debug loads the build with device-side range checks (python -m paper_2604_22808_b200.build --debug),
 # =clocks the one with cycle sums (--clocks)
@@ -32,7 +32,8 @@ EXPORTS = ("ff_config_validate", "ff_band_sizes", "ff_band_rank", "ff_workspace_
            "ff_plan_create", "ff_plan_workspace_bytes", "ff_band_info", "ff_plan_set_workspace", "ff_destroy", "ff_last_error",
            "ff_route", "ff_forward", "ff_forward_host", "ff_forward_projected", "ff_plan_device_status", "ff_plan_last_launches", "ff_plan_kernel_info",
            "ff_get_tap", "ff_plan_set_attention_impl", "ff_plan_set_profiling", "ff_plan_stage_times", "ff_high_attention_noalloc",
-           "ff_plan_selftest_bounded_wait")
+           "ff_plan_selftest_bounded_wait", "ff_rotary_create", "ff_rotary_destroy", "ff_rotary_last_error", "ff_rotary_frequencies",
+           "ff_rotary_apply", "ff_qk_norm", "ff_qk_norm_backward", "ff_qk_norm_workspace_bytes")
 STAGES = ("transform", "router", "attention", "summary", "inverse")
 
 
@@ -46,6 +47,17 @@ class ff_config_t(C.Structure):
 
 class ff_weights_t(C.Structure):
     _fields_ = [("W1", C.c_void_p), ("b1", C.c_void_p), ("W2", C.c_void_p), ("b2", C.c_void_p), ("U", C.c_void_p)]
+
+
+class ff_rotary_config_t(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("dtype", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("axis_pairs", C.c_int32 * 3), ("grid", C.c_int32 * 3), ("original_length", C.c_int32), ("base", C.c_double),
+                ("factor", C.c_double)]
+
+
+class ff_heads_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_batch", C.c_int64), ("stride_head", C.c_int64), ("stride_token", C.c_int64),
+                ("heads", C.c_int32)]
 
 
 class FFError(RuntimeError):
@@ -64,8 +76,10 @@ def library() -> C.CDLL:
         lib = C.CDLL(_LIB_PATH)
         lib.ff_last_error.restype = C.c_char_p
         lib.ff_last_error.argtypes = [C.c_void_p]
+        lib.ff_rotary_last_error.restype = C.c_char_p
+        lib.ff_rotary_last_error.argtypes = [C.c_void_p]
         for name in EXPORTS:
-            if name != "ff_last_error":
+            if not name.endswith("last_error"):
                 getattr(lib, name).restype = C.c_int32
         lib.ff_plan_create.argtypes = [C.POINTER(ff_config_t), C.POINTER(ff_weights_t), C.POINTER(C.c_void_p)]
         lib.ff_plan_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
@@ -85,6 +99,15 @@ def library() -> C.CDLL:
         lib.ff_plan_stage_times.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_int64)]
         lib.ff_high_attention_noalloc.argtypes = [C.c_void_p] * 4 + [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p]
         lib.ff_plan_selftest_bounded_wait.argtypes = [C.c_void_p, C.c_int64, C.POINTER(C.c_int32), C.c_void_p]
+        heads, place = C.POINTER(ff_heads_t), [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64]
+        lib.ff_rotary_create.argtypes = [C.POINTER(ff_rotary_config_t), C.POINTER(C.c_void_p)]
+        lib.ff_rotary_destroy.argtypes = [C.c_void_p]
+        lib.ff_rotary_frequencies.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double)]
+        lib.ff_rotary_apply.argtypes = place + [heads, heads, C.c_int32, heads, heads, C.c_void_p]
+        lib.ff_qk_norm.argtypes = place + [heads, heads, C.c_void_p, C.c_void_p, C.c_float, heads, heads, C.c_void_p]
+        lib.ff_qk_norm_backward.argtypes = (place + [heads, heads, C.c_void_p, C.c_void_p, C.c_float] + [heads] * 4
+                                            + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p])
+        lib.ff_qk_norm_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
         lib.ff_config_validate.argtypes = [C.POINTER(ff_config_t)]
         lib.ff_band_sizes.argtypes = [C.POINTER(ff_config_t), C.POINTER(C.c_int64)]
         lib.ff_band_rank.argtypes = [C.POINTER(ff_config_t), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32),
@@ -348,6 +371,139 @@ class Plan:
                   TAP_PI: (torch.float32, (cfg.batch, 3))}
         dt, shape = shapes[which]
         return raw.view(dt).view(shape)
+
+
+# ---- queries and keys between the projections and the attention ---------------------------------------
+class Rotary:
+    """Rotary positions of queries and keys, alone or with the norm of every head row in the same pass.
+
+    q, k and the tensors written are CUDA tensors [batch][heads][tokens][head_dim] of the configuration's type, with
+    contiguous channels and any strides for the rest (a transposed view of [batch][tokens][heads][head_dim] is one); q and k
+    may have different numbers of heads, and k and its output may be None.  An output may be its own input.  positions: an
+    int32 CUDA tensor [tokens] or [batch][tokens], with a last dimension of 3 (t, h, w) where the configuration divides the
+    pairs over axes; None: the token's index, or its cell in the configuration's grid."""
+
+    def __init__(self, cfg: RotaryConfig):
+        import torch
+        self.cfg = cfg
+        self._torch = torch
+        self.handle = C.c_void_p()
+        c = ff_rotary_config_t()
+        c.head_dim, c.rot_dim, c.original_length = cfg.head_dim, cfg.rot_dim, cfg.original_length
+        c.base, c.factor = cfg.base, cfg.factor
+        try:
+            c.dtype = {"bf16": FF_BF16, "fp32": FF_FP32}[cfg.dtype]
+            c.layout = {"half": 0, "interleaved": 1}[cfg.layout]
+            c.scaling = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3}[cfg.scaling]
+        except KeyError as e:
+            raise FFError(1, f"unknown dtype, layout or scaling: {e}") from None
+        c.axis_pairs = (C.c_int32 * 3)(*cfg.axis_pairs)
+        c.grid = (C.c_int32 * 3)(*cfg.grid)
+        _check(library().ff_rotary_create(C.byref(c), C.byref(self.handle)))
+        self._dtype = torch.float32 if cfg.dtype == "fp32" else torch.bfloat16
+        self._axes = 3 if any(cfg.axis_pairs) else 1
+        self._raw_stream = _stream_getter(torch)
+        n = C.c_size_t()
+        _check(library().ff_qk_norm_workspace_bytes(self.handle, C.byref(n)))
+        self.workspace_bytes = n.value
+
+    def destroy(self):
+        if self.handle:
+            library().ff_rotary_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def frequencies(self):
+        """(radians per position of every pair, magnitude of the rotation)"""
+        theta, m = (C.c_double * (self.cfg.rot_dim // 2))(), C.c_double()
+        self._status(library().ff_rotary_frequencies(self.handle, theta, C.byref(m)))
+        return np.array(theta), m.value
+
+    def _status(self, status: int):
+        if status != FF_OK:
+            raise FFError(status, library().ff_rotary_last_error(self.handle).decode())
+
+    def _heads(self, t, shape, device):
+        """The ff_heads_t of a tensor of that shape on that device."""
+        if t.shape != shape or t.dtype != self._dtype or t.device != device or not t.is_cuda:
+            raise FFError(1, f"expected a {self._dtype} tensor of shape {tuple(shape)} on {device}")
+        s = t.stride()
+        if s[3] != 1:
+            raise FFError(1, "the channels of a head must be contiguous")
+        return C.byref(ff_heads_t(t.data_ptr(), s[0], s[1], s[2], shape[1]))
+
+    def _place(self, q, k, positions):
+        """(batch, tokens, positions, stride between the samples' positions) and the shape of k, all checked."""
+        if q.dim() != 4 or q.shape[3] != self.cfg.head_dim:
+            raise FFError(1, f"expected q of shape [batch][heads][tokens][{self.cfg.head_dim}]")
+        B, _, N, d = q.shape
+        if k is not None and (k.dim() != 4 or k.shape[0] != B or k.shape[2] != N or k.shape[3] != d):
+            raise FFError(1, f"expected k of shape [{B}][heads][{N}][{d}]")
+        if positions is None:
+            return B, N, None, 0
+        p, tail = positions, (N,) if self._axes == 1 else (N, 3)
+        if p.dtype != self._torch.int32 or p.device != q.device or not p.is_contiguous() or (p.shape != tail and p.shape != (B,) + tail):
+            raise FFError(1, f"expected contiguous int32 positions of shape {tail} or {(B,) + tail} on {q.device}")
+        return B, N, p.data_ptr(), N * self._axes if p.dim() > len(tail) else 0
+
+    def _weight(self, w, device):
+        if w is None:
+            return None
+        if w.dtype != self._torch.float32 or w.shape != (self.cfg.head_dim,) or not w.is_contiguous() or w.device != device:
+            raise FFError(1, f"expected contiguous fp32 weights of shape [{self.cfg.head_dim}] on {device}")
+        return w.data_ptr()
+
+    def _call(self, device, fn, *args):
+        """The call on the tensors' device (made current for it where another one is) and its current stream."""
+        torch = self._torch
+        if torch.cuda.current_device() == device.index:
+            return self._status(fn(self.handle, *args, self._raw_stream(device.index)))
+        with torch.cuda.device(device):
+            return self._status(fn(self.handle, *args, self._raw_stream(device.index)))
+
+    def apply(self, q, q_out, k=None, k_out=None, positions=None, inverse: bool = False):
+        """The rotation of q and k; inverse: its transpose, the backward pass."""
+        B, N, pos, ps = self._place(q, k, positions)
+        dev = q.device
+        if (k is None) != (k_out is None):
+            raise FFError(1, "k comes with its output, or neither does")
+        ks = None if k is None else k.shape
+        self._call(dev, library().ff_rotary_apply, B, N, pos, ps, self._heads(q, q.shape, dev), None if ks is None else self._heads(k, ks, dev),
+                   int(inverse), self._heads(q_out, q.shape, dev), None if ks is None else self._heads(k_out, ks, dev))
+        return q_out, k_out
+
+    def qk_norm(self, q, k, wq, wk, q_out, k_out, eps: float = 1e-6, positions=None):
+        """Norm of every row, times wq / wk (fp32 [head_dim], None: ones), then the rotation."""
+        B, N, pos, ps = self._place(q, k, positions)
+        dev = q.device
+        if (k is None) != (k_out is None):
+            raise FFError(1, "k comes with its output, or neither does")
+        ks = None if k is None else k.shape
+        self._call(dev, library().ff_qk_norm, B, N, pos, ps, self._heads(q, q.shape, dev), None if ks is None else self._heads(k, ks, dev),
+                   self._weight(wq, dev), self._weight(wk, dev), eps, self._heads(q_out, q.shape, dev),
+                   None if ks is None else self._heads(k_out, ks, dev))
+        return q_out, k_out
+
+    def qk_norm_backward(self, q, k, wq, wk, dq_out, dk_out, dq, dk, dwq=None, dwk=None, eps: float = 1e-6, positions=None):
+        """Gradients of q, k (and of the weights, fp32 [head_dim], where given) from those of qk_norm's outputs."""
+        B, N, pos, ps = self._place(q, k, positions)
+        dev = q.device
+        if (k is None) != (dk_out is None) or (k is None) != (dk is None):
+            raise FFError(1, "k comes with its gradients, or neither does")
+        ks = None if k is None else k.shape
+        # (a workspace per call: calls on different streams and captured graphs share none)
+        ws = self._torch.empty(self.workspace_bytes, dtype=self._torch.uint8, device=dev)
+        self._call(dev, library().ff_qk_norm_backward, B, N, pos, ps, self._heads(q, q.shape, dev), None if ks is None else self._heads(k, ks, dev),
+                   self._weight(wq, dev), self._weight(wk, dev), eps, self._heads(dq_out, q.shape, dev),
+                   None if ks is None else self._heads(dk_out, ks, dev), self._heads(dq, q.shape, dev),
+                   None if ks is None else self._heads(dk, ks, dev), self._weight(dwq, dev), self._weight(dwk, dev),
+                   ws.data_ptr(), self.workspace_bytes)
+        return dq, dk
 
 
 # Same names as the C entry points, for callers that prefer the flat API.

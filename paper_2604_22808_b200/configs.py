@@ -60,6 +60,21 @@ class FFConfig:
         return replace(self, name=name, **kw)
 
 
+@dataclass(frozen=True)
+class RotaryConfig:
+    """Rotary positions of queries and keys (include/freqformer.h, ff_rotary_config_t)."""
+    head_dim: int
+    rot_dim: int                                    # the first rot_dim channels of a head are turned
+    dtype: str = "bf16"                             # "bf16" or "fp32"
+    layout: str = "half"                            # pairs (i, i + rot_dim / 2), or "interleaved": (2i, 2i + 1)
+    base: float = 10000.0
+    scaling: str = "none"                           # "none", "linear", "ntk", "by_parts"
+    factor: float = 1.0
+    original_length: int = 0                        # "by_parts"
+    axis_pairs: Tuple[int, int, int] = (0, 0, 0)    # pairs that turn with t, h, w; zeros: one position per token
+    grid: Tuple[int, int, int] = (0, 0, 0)          # T, H, W of calls without positions
+
+
 def _cuts(grid, c_low_num, c_low_den):
     """L_a = n_a * c_low, M_a = n_a * (c_low + 1/2), both exact integers here."""
     low = tuple(n * c_low_num // c_low_den for n in grid)

@@ -1,0 +1,592 @@
+// Queries and keys between the projections and the attention: rotary positions, and the norm of every head row with the
+// rotation in the same pass, forward and backward.
+//
+//   rotation   (a, b) of pair p -> m (a cos t - b sin t, a sin t + b cos t),   t = position * theta_p
+//   norm       z = x r w,  r = 1 / sqrt(mean(x^2) + eps) over the row's head_dim channels,  y = rotation of z
+//   backward   dz = the rotation's transpose of dy;  n = x r;  g = dz w;  dx = r (g - n mean(g n));  dw = sum over rows of dz n
+//
+// All of it is one pass over the rows: a row of head_dim channels is read once, stays in registers in fp32 and is written
+// once, so the bound is memory: 2 (backward 3) tensors.  What could exceed that are the angles, one sine and cosine per
+// token and pair; they do not depend on the head, so a thread that owns the same pairs of one token computes them once and
+// keeps them in registers while it walks over the heads.
+//
+// Angles: theta_p / 2 pi is kept as a 64-bit fraction of a turn.  position * fraction modulo 2^64 is then the angle modulo a
+// whole turn, exact to 2^-33 turns for any 32-bit position, and its high word is what sincospi is asked for: no floating-point
+// product of a far position ever has to be reduced.
+//
+// Threads: a row is cut in chunks of CH channels (16 bytes where strides, rot_dim and head_dim allow, else 8, 4 or 2), and a
+// thread owns two chunks of it so that both channels of a pair are its own: no exchange between threads for the rotation.
+//   half layout          chunk j of the first half of the turned channels and chunk j of the second; the channels that are not
+//                        turned follow in neighbouring chunks
+//   interleaved layout   chunk j of the first half of the row and chunk j of the second: pairs lie inside a chunk
+// A row takes L = 2^k lanes (8 for 128 bf16 channels), a warp 32 / L tokens at a time.
+#include <math.h>
+#include <stdio.h>
+
+#include <new>
+
+#include "ff_internal.h"
+
+struct ff_rotary {
+  ff_rotary_config_t cfg;
+  int pairs;                       // rot_dim / 2
+  int axis_end[2];                 // pairs below the first turn with axis t, below the second with h, then w
+  int axes;                        // position components of a token: 1 or 3
+  double theta[128];               // radians per position
+  unsigned long long phase[128];   // the same as a 64-bit fraction of a turn
+  float magnitude;
+  char err[512];
+};
+
+namespace {
+
+enum { ROTATE = 0, NORM = 1, NORM_BACKWARD = 2 };
+constexpr int H_THREADS = 256, H_WARPS = H_THREADS / 32;
+constexpr int PARTIAL_ROWS = 2 * FF_B200_SMS;     // rows of partial weight gradients at most: one wave of two blocks per SM
+
+struct HeadsView { char* p; long long sb, sh, st; };   // strides in bytes
+
+struct HeadsParams {
+  HeadsView x[2], y[2], g[2];      // q and k: input, output, (backward) the gradient of the forward pass's output
+  const float* w[2];               // norm weights or NULL
+  float* partial;                  // backward: [blocks of q, then of k][head_dim]
+  const int* positions;
+  long long pos_stride;            // elements between the samples' positions
+  int rows;                        // batch * tokens
+  FFFastDiv tokens, gw, gh;        // tokens per sample; the grid's W and H
+  int heads[2], chunk, nchunk0;    // heads of q and k, heads a block walks over, blocks in y that belong to q
+  int d, rot, np, lanes_log2;      // channels, turned channels, chunk pairs of a row, log2 of the lanes of a row
+  int axis_end0, axis_end1, axes;
+  int inverse;
+  float magnitude, eps;
+  unsigned long long phase[128];
+};
+
+template <int BYTES> struct Word;
+template <> struct Word<16> { using type = uint4; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<4> { using type = unsigned; };
+template <> struct Word<2> { using type = unsigned short; };
+template <class T, int CH> using Chunk = typename Word<sizeof(T) * CH>::type;
+
+template <class T, int CH>
+__device__ __forceinline__ void unpack(const Chunk<T, CH>& c, float (&v)[CH]) {
+  if constexpr (sizeof(T) == 4) {
+    const float* f = reinterpret_cast<const float*>(&c);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) v[i] = f[i];
+  } else {
+    const unsigned short* h = reinterpret_cast<const unsigned short*>(&c);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) v[i] = __uint_as_float((unsigned)h[i] << 16);
+  }
+}
+// (the one rounding of the operators with bf16 tensors)
+template <class T, int CH>
+__device__ __forceinline__ Chunk<T, CH> pack(const float (&v)[CH]) {
+  Chunk<T, CH> c;
+  T* t = reinterpret_cast<T*>(&c);
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    if constexpr (sizeof(T) == 4) t[i] = v[i];
+    else t[i] = __float2bfloat16_rn(v[i]);
+  }
+  return c;
+}
+
+// The pairs of two chunks turned by (c, s).  Interleaved: the first half of c, s belongs to `a`.
+template <int CH, bool INTER>
+__device__ __forceinline__ void turn(float (&a)[CH], float (&b)[CH], const float (&c)[CH], const float (&s)[CH], bool turned_a, bool turned_b) {
+  if constexpr (INTER) {
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+      const float a0 = a[2 * i], a1 = a[2 * i + 1], b0 = b[2 * i], b1 = b[2 * i + 1];
+      if (turned_a) { a[2 * i] = a0 * c[i] - a1 * s[i]; a[2 * i + 1] = a0 * s[i] + a1 * c[i]; }
+      if (turned_b) { b[2 * i] = b0 * c[CH / 2 + i] - b1 * s[CH / 2 + i]; b[2 * i + 1] = b0 * s[CH / 2 + i] + b1 * c[CH / 2 + i]; }
+    }
+  } else if (turned_a) {            // (both chunks of a half-layout pair are turned or neither is)
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const float x = a[i], y = b[i];
+      a[i] = x * c[i] - y * s[i];
+      b[i] = x * s[i] + y * c[i];
+    }
+  }
+}
+
+// 1 / sqrt(mean of squares + eps) of a row whose values the lanes of a group hold.  Rows whose squares leave fp32 are summed
+// again scaled by 2^-70 (eps is far below their mean).
+template <int CH, int PER>
+__device__ __forceinline__ float row_rms(const float (&a)[PER][CH], const float (&b)[PER][CH], int lanes, float inv_d, float eps) {
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+#pragma unroll
+    for (int c = 0; c < CH; ++c) ss += a[i][c] * a[i][c] + b[i][c] * b[i][c];
+  for (int m = 1; m < lanes; m <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+  const bool big = !(ss < 3.0e38f);
+  if (!__any_sync(0xffffffffu, big)) return rsqrtf(ss * inv_d + eps);
+  const float down = 8.4703294725430034e-22f;   // 2^-70
+  float sc = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const float u = a[i][c] * down, v = b[i][c] * down;
+      sc += u * u + v * v;
+    }
+  for (int m = 1; m < lanes; m <<= 1) sc += __shfl_xor_sync(0xffffffffu, sc, m);
+  return big ? rsqrtf(sc * inv_d) * down : rsqrtf(ss * inv_d + eps);
+}
+
+template <class T, int CH, int PER, bool INTER, int MODE>
+__global__ void __launch_bounds__(H_THREADS, 2) heads_kernel(const __grid_constant__ HeadsParams P) {
+  constexpr int U = MODE == NORM_BACKWARD ? 2 : 4;            // heads whose rows are in flight together
+  using C = Chunk<T, CH>;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int lanes = 1 << P.lanes_log2, lig = lane & (lanes - 1);
+  const int per_warp = 32 >> P.lanes_log2;                    // tokens of a warp
+  const int t = blockIdx.y >= (unsigned)P.nchunk0;            // 0: q, 1: k
+  const int h0 = ((int)blockIdx.y - (t ? P.nchunk0 : 0)) * P.chunk;
+  const int h1 = min(h0 + P.chunk, P.heads[t]);
+  const float inv_d = 1.f / (float)P.d;
+
+  // the thread's chunks
+  int oa[PER], ob[PER];
+  bool have[PER], ta[PER], tb[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = lig + i * lanes;
+    have[i] = j < P.np;
+    if (INTER) {
+      oa[i] = j * CH; ob[i] = (j + P.np) * CH;
+      ta[i] = have[i] && oa[i] < P.rot; tb[i] = have[i] && ob[i] < P.rot;
+    } else {
+      const int turned = P.rot / (2 * CH);
+      ta[i] = tb[i] = have[i] && j < turned;
+      oa[i] = j < turned ? j * CH : P.rot + 2 * (j - turned) * CH;
+      ob[i] = j < turned ? P.rot / 2 + j * CH : oa[i] + CH;
+    }
+  }
+  ff_pdl_wait();
+
+  float wa[PER][CH], wb[PER][CH];
+  if constexpr (MODE != ROTATE) {
+    const float* w = P.w[t];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        wa[i][c] = have[i] ? (w ? w[oa[i] + c] : 1.f) : 0.f;
+        wb[i][c] = have[i] ? (w ? w[ob[i] + c] : 1.f) : 0.f;
+      }
+  }
+  float da[PER][CH], db[PER][CH];                             // backward: the thread's share of dw
+  if constexpr (MODE == NORM_BACKWARD) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int c = 0; c < CH; ++c) da[i][c] = db[i][c] = 0.f;
+  }
+
+  const long long step = (long long)gridDim.x * H_WARPS * per_warp;
+  for (long long r0 = ((long long)blockIdx.x * H_WARPS + warp) * per_warp; r0 < P.rows; r0 += step) {
+    const long long row = r0 + (lane >> P.lanes_log2);
+    const bool live = row < P.rows;
+    const unsigned ru = live ? (unsigned)row : 0u;
+    const unsigned b = ff_div(ru, P.tokens), n = ru - b * P.tokens.d;
+    // angles of the token
+    float cs[PER][CH], sn[PER][CH];
+    {
+      int pos[3];
+      if (P.positions) {
+        const int* at = P.positions + b * P.pos_stride + (long long)n * P.axes;
+        pos[0] = live ? at[0] : 0;
+        pos[1] = live && P.axes == 3 ? at[1] : 0;
+        pos[2] = live && P.axes == 3 ? at[2] : 0;
+      } else if (P.axes == 3) {
+        const unsigned line = ff_div(n, P.gw);
+        pos[2] = (int)(n - line * P.gw.d);
+        pos[0] = (int)ff_div(line, P.gh);
+        pos[1] = (int)(line - pos[0] * P.gh.d);
+      } else {
+        pos[0] = (int)n; pos[1] = pos[2] = 0;
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const int p = INTER ? (c < CH / 2 ? oa[i] / 2 + c : ob[i] / 2 + c - CH / 2) : oa[i] + c;
+          const bool on = INTER && c >= CH / 2 ? tb[i] : ta[i];
+          cs[i][c] = sn[i][c] = 0.f;
+          if (on) {
+            const int at = p < P.axis_end0 ? pos[0] : (p < P.axis_end1 ? pos[1] : pos[2]);
+            const unsigned long long turns = (unsigned long long)(long long)at * P.phase[p];
+            float s, co;
+            sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &s, &co);     // 2^-31: half turns
+            cs[i][c] = co * P.magnitude;
+            sn[i][c] = (P.inverse ? -s : s) * P.magnitude;
+          }
+        }
+    }
+    const char* xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st;
+    char* yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st;
+    const char* gp = MODE == NORM_BACKWARD ? P.g[t].p + b * P.g[t].sb + n * P.g[t].st : nullptr;
+#pragma unroll 1
+    for (int h = h0; h < h1; h += U) {
+      C xa[U][PER], xb[U][PER], ga[U][PER], gb[U][PER];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const bool on = live && have[i] && h + u < h1;
+          const char* src = xp + (long long)(h + u) * P.x[t].sh;
+          xa[u][i] = on ? __ldcs((const C*)(src + oa[i] * sizeof(T))) : C{};
+          xb[u][i] = on ? __ldcs((const C*)(src + ob[i] * sizeof(T))) : C{};
+          if constexpr (MODE == NORM_BACKWARD) {
+            const char* gs = gp + (long long)(h + u) * P.g[t].sh;
+            ga[u][i] = on ? __ldcs((const C*)(gs + oa[i] * sizeof(T))) : C{};
+            gb[u][i] = on ? __ldcs((const C*)(gs + ob[i] * sizeof(T))) : C{};
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float a[PER][CH], c[PER][CH];                         // the two chunks
+#pragma unroll
+        for (int i = 0; i < PER; ++i) { unpack<T, CH>(xa[u][i], a[i]); unpack<T, CH>(xb[u][i], c[i]); }
+        if constexpr (MODE == NORM) {
+          const float r = row_rms<CH, PER>(a, c, lanes, inv_d, P.eps);
+#pragma unroll
+          for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int k = 0; k < CH; ++k) { a[i][k] = a[i][k] * r * wa[i][k]; c[i][k] = c[i][k] * r * wb[i][k]; }
+        }
+        if constexpr (MODE != NORM_BACKWARD) {
+#pragma unroll
+          for (int i = 0; i < PER; ++i) turn<CH, INTER>(a[i], c[i], cs[i], sn[i], ta[i], tb[i]);
+        } else {
+          const float r = row_rms<CH, PER>(a, c, lanes, inv_d, P.eps);
+          float g0[PER][CH], g1[PER][CH], dot = 0.f;
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            unpack<T, CH>(ga[u][i], g0[i]); unpack<T, CH>(gb[u][i], g1[i]);
+            turn<CH, INTER>(g0[i], g1[i], cs[i], sn[i], ta[i], tb[i]);
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+              a[i][k] *= r; c[i][k] *= r;                     // n
+              da[i][k] += g0[i][k] * a[i][k]; db[i][k] += g1[i][k] * c[i][k];
+              g0[i][k] *= wa[i][k]; g1[i][k] *= wb[i][k];     // g
+              dot += g0[i][k] * a[i][k] + g1[i][k] * c[i][k];
+            }
+          }
+          for (int m = 1; m < lanes; m <<= 1) dot += __shfl_xor_sync(0xffffffffu, dot, m);
+          dot *= inv_d;
+#pragma unroll
+          for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int k = 0; k < CH; ++k) { a[i][k] = r * (g0[i][k] - a[i][k] * dot); c[i][k] = r * (g1[i][k] - c[i][k] * dot); }
+        }
+        if (live && h + u < h1) {
+          char* dst = yp + (long long)(h + u) * P.y[t].sh;
+#pragma unroll
+          for (int i = 0; i < PER; ++i)
+            if (have[i]) {
+              *(C*)(dst + oa[i] * sizeof(T)) = pack<T, CH>(a[i]);
+              *(C*)(dst + ob[i] * sizeof(T)) = pack<T, CH>(c[i]);
+            }
+        }
+      }
+    }
+  }
+
+  if constexpr (MODE == NORM_BACKWARD) {
+    // the block's rows of dw: lanes that own the same channels, then the warps, in a fixed order
+    __shared__ float sum[H_WARPS][256];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        for (int m = lanes; m < 32; m <<= 1) {
+          da[i][k] += __shfl_xor_sync(0xffffffffu, da[i][k], m);
+          db[i][k] += __shfl_xor_sync(0xffffffffu, db[i][k], m);
+        }
+        if (lane < lanes && have[i]) { sum[warp][oa[i] + k] = da[i][k]; sum[warp][ob[i] + k] = db[i][k]; }
+      }
+    __syncthreads();
+    for (int c = threadIdx.x; c < P.d; c += H_THREADS) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < H_WARPS; ++w) s += sum[w][c];
+      P.partial[((long long)blockIdx.y * gridDim.x + blockIdx.x) * P.d + c] = s;
+    }
+  }
+}
+
+// dw[t][c] = sum of the partial rows of q (t = 0) or k, in a fixed order.  One block: 32 columns of one of them.
+__global__ void __launch_bounds__(1024) weight_gradient_kernel(const float* partial, int rows_q, int rows_k, int d, float* dwq, float* dwk) {
+  __shared__ float sum[32][33];
+  ff_pdl_wait();
+  const int t = blockIdx.y, c = blockIdx.x * 32 + (threadIdx.x & 31), ty = threadIdx.x >> 5;
+  const float* p = partial + (t ? (long long)rows_q * d : 0);
+  const int rows = t ? rows_k : rows_q;
+  float s = 0.f;
+  if (c < d)
+#pragma unroll 4
+    for (int r = ty; r < rows; r += 32) s += p[(long long)r * d + c];
+  sum[ty][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (ty == 0) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += sum[i][threadIdx.x];
+    float* out = t ? dwk : dwq;
+    if (c < d && out) out[c] = s;
+  }
+}
+
+ff_status_t fail(ff_rotary* h, ff_status_t code, const char* msg) {
+  if (h) snprintf(h->err, sizeof h->err, "%s", msg);
+  else ff_set_thread_error(msg);
+  return code;
+}
+ff_status_t cuda_fail(ff_rotary* h, cudaError_t e) {
+  char msg[256];
+  snprintf(msg, sizeof msg, "CUDA error: %s", cudaGetErrorString(e));
+  return fail(h, FF_ERR_CUDA, msg);
+}
+
+// What a call's tensors have to fulfil; the greatest common divisor of their strides and addresses decides the chunk.
+struct Call {
+  ff_rotary* h;
+  int64_t batch, tokens;
+  int e;                            // bytes of an element
+  uint64_t bits;                    // all addresses and strides in bytes, or-ed
+};
+ff_status_t check_view(Call& c, const ff_heads_t* v, int heads, bool written) {
+  if (!v || !v->data) return fail(c.h, FF_ERR_INVALID_ARG, "a tensor is NULL");
+  if (v->heads != heads) return fail(c.h, FF_ERR_INVALID_ARG, "tensors of one kind must have the same number of heads");
+  if (written && ((c.batch > 1 && v->stride_batch == 0) || (c.tokens > 1 && v->stride_token == 0) || (heads > 1 && v->stride_head == 0)))
+    return fail(c.h, FF_ERR_INVALID_ARG, "an output's stride is 0: rows would be written over one another");
+  if (v->stride_batch < 0 || v->stride_head < 0 || v->stride_token < 0) return fail(c.h, FF_ERR_INVALID_ARG, "strides must not be negative");
+  // (strides that no second element uses do not count)
+  c.bits |= (uint64_t)(uintptr_t)v->data;
+  if (c.batch > 1) c.bits |= (uint64_t)v->stride_batch * c.e;
+  if (c.tokens > 1) c.bits |= (uint64_t)v->stride_token * c.e;
+  if (heads > 1) c.bits |= (uint64_t)v->stride_head * c.e;
+  if ((uintptr_t)v->data % c.e) return fail(c.h, FF_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
+  return FF_OK;
+}
+HeadsView view(const ff_heads_t* v, int e) {
+  return HeadsView{(char*)v->data, (long long)v->stride_batch * e, (long long)v->stride_head * e, (long long)v->stride_token * e};
+}
+
+template <class T, int CH, int PER, int MODE>
+cudaError_t launch_layout(bool inter, dim3 grid, cudaStream_t st, const HeadsParams& P) {
+  if constexpr (CH > 1)
+    if (inter) return ff_launch(heads_kernel<T, CH, PER, true, MODE>, grid, dim3(H_THREADS), 0, st, P);
+  return ff_launch(heads_kernel<T, CH, PER, false, MODE>, grid, dim3(H_THREADS), 0, st, P);
+}
+template <class T, int MODE>
+cudaError_t launch_chunk(int ch, bool inter, dim3 grid, cudaStream_t st, const HeadsParams& P) {
+  if constexpr (sizeof(T) == 2)
+    if (ch == 8) return launch_layout<T, 8, 1, MODE>(inter, grid, st, P);
+  if (ch == 4) return launch_layout<T, 4, 1, MODE>(inter, grid, st, P);
+  if (ch == 2) return launch_layout<T, 2, 2, MODE>(inter, grid, st, P);
+  return launch_layout<T, 1, 4, MODE>(inter, grid, st, P);
+}
+
+// Common to the three entry points.  `mode` NORM_BACKWARD: g = gradients of the forward outputs, y = dq / dk.
+ff_status_t run(const ff_rotary_t* handle, int mode, int64_t batch, int64_t tokens, const int32_t* positions, int64_t position_stride,
+                const ff_heads_t* const x[2], const ff_heads_t* const y[2], const ff_heads_t* const g[2], const float* const w[2], float eps,
+                int inverse, float* dwq, float* dwk, void* ws, size_t ws_bytes, void* stream) {
+  ff_rotary* h = const_cast<ff_rotary*>(handle);
+  if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "the rotary handle is NULL");
+  const ff_rotary_config_t& c = h->cfg;
+  if (batch < 0 || tokens < 0) return fail(h, FF_ERR_INVALID_ARG, "batch and tokens must not be negative");
+  if (!x[0] || !y[0]) return fail(h, FF_ERR_INVALID_ARG, "q is NULL");
+  if (!x[1] != !y[1]) return fail(h, FF_ERR_INVALID_ARG, "k comes with its output, or neither does");
+  if (mode != ROTATE && !(eps > 0.f && eps < 3.0e38f)) return fail(h, FF_ERR_INVALID_ARG, "eps must be positive and finite");
+  if (batch > 0x7fffffff || tokens > 0x7fffffff || batch * tokens > 0x7fffffff) return fail(h, FF_ERR_UNSUPPORTED, "batch * tokens must be below 2^31");
+  if (!positions && h->axes == 3) {
+    const int64_t cells = (int64_t)c.grid[0] * c.grid[1] * c.grid[2];
+    if (cells == 0) return fail(h, FF_ERR_INVALID_ARG, "without a grid the positions along its axes have to be given");
+    if (cells != tokens) return fail(h, FF_ERR_INVALID_ARG, "without positions the tokens are the grid's cells: T * H * W of them");
+  }
+  if (positions && (((uintptr_t)positions) & 3)) return fail(h, FF_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+  if (positions && position_stride < 0) return fail(h, FF_ERR_INVALID_ARG, "the positions' stride must not be negative");
+  HeadsParams P{};
+  Call call{h, batch, tokens, c.dtype == FF_FP32 ? 4 : 2, 0};
+  const int kinds = x[1] ? 2 : 1;
+  for (int t = 0; t < kinds; ++t) {
+    if (x[t]->heads < 1) return fail(h, FF_ERR_INVALID_ARG, "a tensor has no heads");
+    if (x[t]->heads > 65536) return fail(h, FF_ERR_UNSUPPORTED, "at most 65536 heads are supported");
+    P.heads[t] = x[t]->heads;
+    if (batch * tokens == 0) continue;
+    ff_status_t s = check_view(call, x[t], x[t]->heads, false);
+    if (s == FF_OK) s = check_view(call, y[t], x[t]->heads, true);
+    if (s == FF_OK && mode == NORM_BACKWARD) s = g[t] ? check_view(call, g[t], x[t]->heads, false) : fail(h, FF_ERR_INVALID_ARG, "a gradient is NULL");
+    if (s != FF_OK) return s;
+    P.x[t] = view(x[t], call.e);
+    P.y[t] = view(y[t], call.e);
+    if (mode == NORM_BACKWARD) P.g[t] = view(g[t], call.e);
+  }
+  const bool want_dw = mode == NORM_BACKWARD && (dwq || dwk);
+  size_t need = 0;
+  if (mode == NORM_BACKWARD) {
+    ff_qk_norm_workspace_bytes(handle, &need);
+    if (!ws || ws_bytes < need) return fail(h, FF_ERR_WORKSPACE, "the workspace is missing or smaller than ff_qk_norm_workspace_bytes");
+    if (((uintptr_t)ws) & 15) return fail(h, FF_ERR_WORKSPACE, "the workspace must be 16-byte aligned");
+  }
+  cudaStream_t st = (cudaStream_t)stream;
+  if (batch * tokens == 0) {        // nothing to turn; sums over no rows are zero
+    cudaError_t e = cudaSuccess;
+    if (mode == NORM_BACKWARD && dwq) e = cudaMemsetAsync(dwq, 0, sizeof(float) * c.head_dim, st);
+    if (e == cudaSuccess && mode == NORM_BACKWARD && dwk && kinds == 2) e = cudaMemsetAsync(dwk, 0, sizeof(float) * c.head_dim, st);
+    return e == cudaSuccess ? FF_OK : cuda_fail(h, e);
+  }
+
+  // the widest chunk that alignment and the channels' division allow
+  const int half = c.rot_dim / 2, d = c.head_dim;
+  const bool inter = c.layout == FF_ROTARY_INTERLEAVED;
+  int ch = c.dtype == FF_FP32 ? 4 : 8;
+  for (; ch > 1; ch >>= 1) {
+    const bool fits = inter ? (c.rot_dim % ch == 0 && d % (2 * ch) == 0) : (half % ch == 0 && (d - c.rot_dim) % (2 * ch) == 0);
+    if (fits && call.bits % ((uint64_t)ch * call.e) == 0) break;
+  }
+  if (inter && ch < 2) return fail(h, FF_ERR_UNSUPPORTED, "interleaved pairs need tensors aligned to two elements");
+  P.np = d / (2 * ch);
+  int lg = 0;
+  while ((1 << lg) < P.np && lg < 5) ++lg;
+  P.lanes_log2 = lg;
+  P.rows = (int)(batch * tokens);
+  P.tokens = ff_fast_div((unsigned)tokens);
+  P.gw = ff_fast_div(c.grid[2] > 0 ? c.grid[2] : 1);
+  P.gh = ff_fast_div(c.grid[1] > 0 ? c.grid[1] : 1);
+  P.positions = positions; P.pos_stride = position_stride;
+  P.d = d; P.rot = c.rot_dim;
+  P.axis_end0 = h->axis_end[0]; P.axis_end1 = h->axis_end[1]; P.axes = h->axes;
+  P.inverse = inverse; P.magnitude = h->magnitude; P.eps = eps;
+  P.w[0] = w[0]; P.w[1] = w[1];
+  memcpy(P.phase, h->phase, sizeof P.phase);
+
+  const int most = P.heads[0] > P.heads[1] ? P.heads[0] : P.heads[1];
+  const long long blocks_x = (P.rows + (long long)H_WARPS * (32 >> lg) - 1) / ((long long)H_WARPS * (32 >> lg));
+  // Heads a block walks over with the same angles: up to 8, fewer where the launch would not fill the device.
+  int chunk = 8;
+  while (chunk > 1 && blocks_x * ((P.heads[0] + chunk - 1) / chunk + (P.heads[1] + chunk - 1) / chunk) < 2 * FF_B200_SMS) chunk >>= 1;
+  if (mode == NORM_BACKWARD && most > 64 * chunk) chunk = (most + 63) / 64;
+  P.chunk = chunk;
+  P.nchunk0 = (P.heads[0] + chunk - 1) / chunk;
+  const int nchunk1 = kinds == 2 ? (P.heads[1] + chunk - 1) / chunk : 0;
+  const int ny = P.nchunk0 + nchunk1;
+  long long nx = blocks_x;
+  if (mode == NORM_BACKWARD && nx * ny > PARTIAL_ROWS) nx = PARTIAL_ROWS / ny > 0 ? PARTIAL_ROWS / ny : 1;
+  P.partial = (float*)ws;
+  const dim3 grid((unsigned)nx, (unsigned)ny);
+  cudaError_t e;
+  if (mode == ROTATE) e = call.e == 4 ? launch_chunk<float, ROTATE>(ch, inter, grid, st, P) : launch_chunk<__nv_bfloat16, ROTATE>(ch, inter, grid, st, P);
+  else if (mode == NORM) e = call.e == 4 ? launch_chunk<float, NORM>(ch, inter, grid, st, P) : launch_chunk<__nv_bfloat16, NORM>(ch, inter, grid, st, P);
+  else e = call.e == 4 ? launch_chunk<float, NORM_BACKWARD>(ch, inter, grid, st, P) : launch_chunk<__nv_bfloat16, NORM_BACKWARD>(ch, inter, grid, st, P);
+  if (e == cudaSuccess && want_dw)
+    e = ff_launch(weight_gradient_kernel, dim3((d + 31) / 32, kinds), dim3(1024), 0, st, (const float*)P.partial, (int)(nx * P.nchunk0),
+                  (int)(nx * nchunk1), d, dwq, dwk);
+  return e == cudaSuccess ? FF_OK : cuda_fail(h, e);
+}
+
+}  // namespace
+
+extern "C" ff_status_t ff_rotary_create(const ff_rotary_config_t* cfg, ff_rotary_t** out) {
+  if (!cfg || !out) return fail(nullptr, FF_ERR_INVALID_ARG, "cfg or out is NULL");
+  *out = nullptr;
+  const ff_rotary_config_t& c = *cfg;
+  if (c.dtype != FF_BF16 && c.dtype != FF_FP32) return fail(nullptr, FF_ERR_INVALID_ARG, "dtype must be FF_BF16 or FF_FP32");
+  if (c.layout != FF_ROTARY_HALF && c.layout != FF_ROTARY_INTERLEAVED) return fail(nullptr, FF_ERR_INVALID_ARG, "layout must be FF_ROTARY_HALF or FF_ROTARY_INTERLEAVED");
+  if (c.scaling < FF_ROTARY_SCALE_NONE || c.scaling > FF_ROTARY_SCALE_BY_PARTS) return fail(nullptr, FF_ERR_INVALID_ARG, "unknown scaling");
+  if (c.head_dim < 1 || c.rot_dim < 2 || (c.rot_dim & 1) || c.rot_dim > c.head_dim)
+    return fail(nullptr, FF_ERR_INVALID_ARG, "rot_dim must be even and between 2 and head_dim");
+  if (c.head_dim % 8 != 0 || c.head_dim > 256) return fail(nullptr, FF_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 and <= 256");
+  if (!(c.base >= 1.0) || !(c.base < 1e300)) return fail(nullptr, FF_ERR_INVALID_ARG, "base must be finite and at least 1");
+  if (c.scaling != FF_ROTARY_SCALE_NONE && (!(c.factor >= 1.0) || !(c.factor < 1e9))) return fail(nullptr, FF_ERR_INVALID_ARG, "the scaling factor must be between 1 and 1e9");
+  if (c.scaling == FF_ROTARY_SCALE_BY_PARTS && c.original_length < 1) return fail(nullptr, FF_ERR_INVALID_ARG, "scaling by parts needs the original length");
+  const int32_t* a = c.axis_pairs;
+  const bool axes = a[0] || a[1] || a[2];
+  if (a[0] < 0 || a[1] < 0 || a[2] < 0 || (axes && (int64_t)a[0] + a[1] + a[2] != c.rot_dim / 2))
+    return fail(nullptr, FF_ERR_INVALID_ARG, "the pairs of the axes must add up to rot_dim / 2");
+  const int32_t* n = c.grid;
+  if (n[0] < 0 || n[1] < 0 || n[2] < 0 || ((n[0] || n[1] || n[2]) && !(n[0] && n[1] && n[2])))
+    return fail(nullptr, FF_ERR_INVALID_ARG, "a grid has three positive axis lengths");
+  if (n[0] && !axes) return fail(nullptr, FF_ERR_INVALID_ARG, "a grid needs the pairs of its axes");
+  if ((double)n[0] * n[1] * n[2] > 2147483647.0) return fail(nullptr, FF_ERR_UNSUPPORTED, "a grid has fewer than 2^31 cells");
+  ff_rotary* h = new (std::nothrow) ff_rotary();
+  if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "out of host memory");
+  h->cfg = c;
+  h->pairs = c.rot_dim / 2;
+  h->axes = axes ? 3 : 1;
+  const int count[3] = {axes ? a[0] : h->pairs, axes ? a[1] : 0, axes ? a[2] : 0};
+  h->axis_end[0] = count[0];
+  h->axis_end[1] = count[0] + count[1];
+  const long double tau = 6.283185307179586476925286766559005768L, s = c.scaling == FF_ROTARY_SCALE_NONE ? 1.0L : (long double)c.factor;
+  for (int axis = 0, p = 0; axis < 3; ++axis)
+    for (int i = 0; i < count[axis]; ++i, ++p) {
+      const int P = count[axis];
+      long double base = c.base;
+      if (c.scaling == FF_ROTARY_SCALE_NTK && P > 1) base *= powl(s, (long double)P / (P - 1));
+      long double th = powl(base, -(long double)i / P);
+      if (c.scaling == FF_ROTARY_SCALE_LINEAR) th /= s;
+      if (c.scaling == FF_ROTARY_SCALE_BY_PARTS) {
+        long double keep = (c.original_length * th / tau - 1.0L) / 31.0L;
+        keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+        th *= keep + (1 - keep) / s;
+      }
+      h->theta[p] = (double)th;
+      h->phase[p] = (unsigned long long)ldexpl(th / tau, 64);      // theta <= 1: below 0.16 of a turn
+    }
+  h->magnitude = c.scaling == FF_ROTARY_SCALE_BY_PARTS ? (float)(0.1L * logl(s) + 1.0L) : 1.0f;
+  *out = h;
+  return FF_OK;
+}
+
+extern "C" ff_status_t ff_rotary_destroy(ff_rotary_t* h) {
+  delete h;
+  return FF_OK;
+}
+
+extern "C" const char* ff_rotary_last_error(const ff_rotary_t* h) { return h ? h->err : ff_last_error(nullptr); }
+
+extern "C" ff_status_t ff_rotary_frequencies(const ff_rotary_t* h, double* theta, double* magnitude) {
+  if (!h || !theta || !magnitude) return fail(const_cast<ff_rotary*>(h), FF_ERR_INVALID_ARG, "handle, theta or magnitude is NULL");
+  for (int p = 0; p < h->pairs; ++p) theta[p] = h->theta[p];
+  *magnitude = h->magnitude;
+  return FF_OK;
+}
+
+extern "C" ff_status_t ff_qk_norm_workspace_bytes(const ff_rotary_t* h, size_t* bytes) {
+  if (!h || !bytes) return fail(const_cast<ff_rotary*>(h), FF_ERR_INVALID_ARG, "handle or bytes is NULL");
+  *bytes = (size_t)(PARTIAL_ROWS + 128) * h->cfg.head_dim * sizeof(float);   // (at least one row for each of the 2 x 64 blocks of heads)
+  return FF_OK;
+}
+
+extern "C" ff_status_t ff_rotary_apply(const ff_rotary_t* h, int64_t batch, int64_t tokens, const int32_t* positions, int64_t position_stride,
+                                       const ff_heads_t* q, const ff_heads_t* k, int32_t inverse, const ff_heads_t* q_out,
+                                       const ff_heads_t* k_out, void* stream) {
+  const ff_heads_t *x[2] = {q, k}, *y[2] = {q_out, k_out}, *g[2] = {};
+  const float* w[2] = {};
+  return run(h, ROTATE, batch, tokens, positions, position_stride, x, y, g, w, 0.f, inverse != 0, nullptr, nullptr, nullptr, 0, stream);
+}
+
+extern "C" ff_status_t ff_qk_norm(const ff_rotary_t* h, int64_t batch, int64_t tokens, const int32_t* positions, int64_t position_stride,
+                                  const ff_heads_t* q, const ff_heads_t* k, const float* wq, const float* wk, float eps,
+                                  const ff_heads_t* q_out, const ff_heads_t* k_out, void* stream) {
+  const ff_heads_t *x[2] = {q, k}, *y[2] = {q_out, k_out}, *g[2] = {};
+  const float* w[2] = {wq, wk};
+  return run(h, NORM, batch, tokens, positions, position_stride, x, y, g, w, eps, 0, nullptr, nullptr, nullptr, 0, stream);
+}
+
+extern "C" ff_status_t ff_qk_norm_backward(const ff_rotary_t* h, int64_t batch, int64_t tokens, const int32_t* positions, int64_t position_stride,
+                                           const ff_heads_t* q, const ff_heads_t* k, const float* wq, const float* wk, float eps,
+                                           const ff_heads_t* dq_out, const ff_heads_t* dk_out, const ff_heads_t* dq, const ff_heads_t* dk,
+                                           float* dwq, float* dwk, void* workspace, size_t workspace_bytes, void* stream) {
+  const ff_heads_t *x[2] = {q, k}, *y[2] = {dq, dk}, *g[2] = {dq_out, dk_out};
+  const float* w[2] = {wq, wk};
+  return run(h, NORM_BACKWARD, batch, tokens, positions, position_stride, x, y, g, w, eps, 1, dwq, dwk, workspace, workspace_bytes, stream);
+}
