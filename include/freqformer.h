@@ -345,6 +345,52 @@ ff_status_t ff_qk_norm_backward(const ff_rotary_t *rotary, int64_t batch, int64_
                                 size_t workspace_bytes, void *cuda_stream);
 ff_status_t ff_qk_norm_workspace_bytes(const ff_rotary_t *rotary, size_t *bytes);
 
+/* ---- the gated feed-forward block ---------------------------------------------------------------------
+ *
+ * The other half of a transformer layer, behind ff_forward_projected (no counterpart in the paper):
+ *     out = (act(X Wg) * (X Wu)) Wd
+ * bf16 tensors, fp32 accumulation, all contiguous and 16-byte aligned, weights as y = x W:
+ *   X, out          [tokens][dim]
+ *   Wg, Wu          [dim][hidden]
+ *   Wd              [hidden][dim]
+ *   gate, up        [tokens][hidden]: X Wg and X Wu, kept by a training forward for the backward pass
+ * The hidden activations (and, backward, the gradients of gate and up) are rounded to bf16 between the products; the
+ * accumulators and the activation are fp32.  Any number of tokens, one and zero included.
+ *
+ * A handle belongs to the device that was current at ff_ffn_create and holds a status word there; calls are
+ * asynchronous on the given stream, which has to be one of that device, the current one.  The caller owns the workspace
+ * (device, 256-byte aligned); calls that may run at the same time need one each. */
+typedef struct ff_ffn ff_ffn_t; /* opaque */
+
+enum { FF_ACT_SILU = 0,      /* g / (1 + e^-g) */
+       FF_ACT_GELU_TANH = 1, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+       FF_ACT_GELU = 2 };    /* g (1 + erf(g / sqrt 2)) / 2 */
+
+typedef struct {
+  int32_t dim, hidden;       /* multiples of 8 */
+  int32_t activation;
+} ff_ffn_config_t;
+
+ff_status_t ff_ffn_validate(const ff_ffn_config_t *cfg);
+/* Workspace of a forward (training = 0) or backward (1) call with that many tokens. */
+ff_status_t ff_ffn_workspace_bytes(const ff_ffn_config_t *cfg, int64_t tokens, int32_t training, size_t *bytes);
+ff_status_t ff_ffn_create(const ff_ffn_config_t *cfg, ff_ffn_t **out);
+ff_status_t ff_ffn_destroy(ff_ffn_t *ffn);            /* NULL is allowed */
+const char *ff_ffn_last_error(const ff_ffn_t *ffn);   /* as ff_last_error */
+
+/* gate, up: both, to keep them for ff_ffn_backward, or both NULL. */
+ff_status_t ff_ffn_forward(ff_ffn_t *ffn, int64_t tokens, const void *X, const void *Wg, const void *Wu, const void *Wd,
+                           void *gate, void *up, void *out, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* The gradients of X and of the weights from that of out; dX, dWd, or dWg and dWu together may be NULL.  They
+ * overwrite what was there and are the same bits in every call with the same inputs. */
+ff_status_t ff_ffn_backward(ff_ffn_t *ffn, int64_t tokens, const void *X, const void *Wg, const void *Wu, const void *Wd,
+                            const void *gate, const void *up, const void *dout, void *dX, void *dWg, void *dWu,
+                            void *dWd, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Synchronises the stream, returns the device status word (FF_OK or FF_ERR_TIMEOUT) and clears it. */
+ff_status_t ff_ffn_device_status(ff_ffn_t *ffn, void *cuda_stream);
+
 /* ---- for callers that cannot allocate device memory ---------------------------------------------
  *
  * The paper has no counterpart of this entry point; it exists for integration reasons only.

@@ -12,7 +12,7 @@ from typing import Optional, Sequence
 
 import numpy as np
 
-from .configs import FFConfig, RotaryConfig
+from .configs import FFConfig, FFNConfig, RotaryConfig
 
 # FF_LIBRARY_VARIANT=debug loads the build with device-side range checks (python -m paper_2604_22808_b200.build --debug),
 # =clocks the one with cycle sums (--clocks)
@@ -33,7 +33,9 @@ EXPORTS = ("ff_config_validate", "ff_band_sizes", "ff_band_rank", "ff_workspace_
            "ff_route", "ff_forward", "ff_forward_host", "ff_forward_projected", "ff_plan_device_status", "ff_plan_last_launches", "ff_plan_kernel_info",
            "ff_get_tap", "ff_plan_set_attention_impl", "ff_plan_set_profiling", "ff_plan_stage_times", "ff_high_attention_noalloc",
            "ff_plan_selftest_bounded_wait", "ff_rotary_create", "ff_rotary_destroy", "ff_rotary_last_error", "ff_rotary_frequencies",
-           "ff_rotary_apply", "ff_qk_norm", "ff_qk_norm_backward", "ff_qk_norm_workspace_bytes")
+           "ff_rotary_apply", "ff_qk_norm", "ff_qk_norm_backward", "ff_qk_norm_workspace_bytes", "ff_ffn_validate",
+           "ff_ffn_workspace_bytes", "ff_ffn_create", "ff_ffn_destroy", "ff_ffn_last_error", "ff_ffn_forward", "ff_ffn_backward",
+           "ff_ffn_device_status")
 STAGES = ("transform", "router", "attention", "summary", "inverse")
 
 
@@ -53,6 +55,10 @@ class ff_rotary_config_t(C.Structure):
     _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("dtype", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
                 ("axis_pairs", C.c_int32 * 3), ("grid", C.c_int32 * 3), ("original_length", C.c_int32), ("base", C.c_double),
                 ("factor", C.c_double)]
+
+
+class ff_ffn_config_t(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("hidden", C.c_int32), ("activation", C.c_int32)]
 
 
 class ff_heads_t(C.Structure):
@@ -76,8 +82,9 @@ def library() -> C.CDLL:
         lib = C.CDLL(_LIB_PATH)
         lib.ff_last_error.restype = C.c_char_p
         lib.ff_last_error.argtypes = [C.c_void_p]
-        lib.ff_rotary_last_error.restype = C.c_char_p
-        lib.ff_rotary_last_error.argtypes = [C.c_void_p]
+        for name in ("ff_rotary_last_error", "ff_ffn_last_error"):
+            getattr(lib, name).restype = C.c_char_p
+            getattr(lib, name).argtypes = [C.c_void_p]
         for name in EXPORTS:
             if not name.endswith("last_error"):
                 getattr(lib, name).restype = C.c_int32
@@ -108,6 +115,13 @@ def library() -> C.CDLL:
         lib.ff_qk_norm_backward.argtypes = (place + [heads, heads, C.c_void_p, C.c_void_p, C.c_float] + [heads] * 4
                                             + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p])
         lib.ff_qk_norm_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
+        lib.ff_ffn_validate.argtypes = [C.POINTER(ff_ffn_config_t)]
+        lib.ff_ffn_workspace_bytes.argtypes = [C.POINTER(ff_ffn_config_t), C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
+        lib.ff_ffn_create.argtypes = [C.POINTER(ff_ffn_config_t), C.POINTER(C.c_void_p)]
+        lib.ff_ffn_destroy.argtypes = [C.c_void_p]
+        lib.ff_ffn_forward.argtypes = [C.c_void_p, C.c_int64] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
+        lib.ff_ffn_backward.argtypes = [C.c_void_p, C.c_int64] + [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p]
+        lib.ff_ffn_device_status.argtypes = [C.c_void_p, C.c_void_p]
         lib.ff_config_validate.argtypes = [C.POINTER(ff_config_t)]
         lib.ff_band_sizes.argtypes = [C.POINTER(ff_config_t), C.POINTER(C.c_int64)]
         lib.ff_band_rank.argtypes = [C.POINTER(ff_config_t), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32),
@@ -504,6 +518,89 @@ class Rotary:
                    None if ks is None else self._heads(dk, ks, dev), self._weight(dwq, dev), self._weight(dwk, dev),
                    ws.data_ptr(), self.workspace_bytes)
         return dq, dk
+
+
+# ---- the gated feed-forward block ----------------------------------------------------------------------
+class GatedFFN:
+    """out = (act(X Wg) * (X Wu)) Wd on contiguous bf16 CUDA tensors: X, out [..., dim], Wg, Wu [dim][hidden], Wd [hidden][dim]
+    (y = x W).  The leading dimensions of X are its tokens."""
+
+    def __init__(self, cfg: FFNConfig, device: str = "cuda:0"):
+        import torch
+        self.cfg = cfg
+        self._torch = torch
+        self.handle = C.c_void_p()
+        self._c = c = ff_ffn_config_t(cfg.dim, cfg.hidden, {"silu": 0, "gelu_tanh": 1, "gelu": 2}.get(cfg.activation, -1))
+        _check(library().ff_ffn_validate(C.byref(c)))
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        with torch.cuda.device(self.device):
+            _check(library().ff_ffn_create(C.byref(c), C.byref(self.handle)))
+        self._raw_stream = _stream_getter(torch)
+
+    def destroy(self):
+        if self.handle:
+            library().ff_ffn_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def _status(self, status: int):
+        if status != FF_OK:
+            raise FFError(status, library().ff_ffn_last_error(self.handle).decode())
+
+    def _tokens(self, X, Wg, Wu, Wd) -> int:
+        D, F = self.cfg.dim, self.cfg.hidden
+        if X.dim() < 1 or X.shape[-1] != D:
+            raise FFError(1, f"expected X of shape [...][{D}]")
+        self._tensors((D, F), Wg, Wu)
+        self._tensors((F, D), Wd)
+        return X.numel() // D
+
+    def _tensors(self, shape, *tensors):
+        """They are bf16, contiguous, of that shape and here (None: not given)."""
+        bf16, device = self._torch.bfloat16, self.device
+        for t in tensors:
+            if t is not None and (t.shape != shape or t.dtype != bf16 or t.device != device or not t.is_contiguous()):
+                raise FFError(1, f"expected a contiguous bf16 tensor of shape {tuple(shape)} on {device}")
+
+    def _call(self, fn, training, tokens, *pointers):
+        torch, dev = self._torch, self.device
+        # (a workspace per call: calls on different streams and captured graphs share none)
+        n = (3 if training else 1) * ((tokens * self.cfg.hidden * 2 + 255) // 256 * 256)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        if torch.cuda.current_device() == dev.index:
+            return self._status(fn(self.handle, tokens, *pointers, ws.data_ptr(), n, self._raw_stream(dev.index)))
+        with torch.cuda.device(dev):
+            return self._status(fn(self.handle, tokens, *pointers, ws.data_ptr(), n, self._raw_stream(dev.index)))
+
+    def forward(self, X, Wg, Wu, Wd, out, gate=None, up=None):
+        """gate, up [..., hidden]: X Wg and X Wu are written there, for backward."""
+        M = self._tokens(X, Wg, Wu, Wd)
+        self._tensors(X.shape, X, out)
+        self._tensors(X.shape[:-1] + (self.cfg.hidden,), gate, up)
+        p = [None if t is None else t.data_ptr() for t in (X, Wg, Wu, Wd, gate, up, out)]
+        self._call(library().ff_ffn_forward, False, M, *p)
+        return out
+
+    def backward(self, X, Wg, Wu, Wd, gate, up, dout, dX=None, dWg=None, dWu=None, dWd=None):
+        """Gradients of X and the weights, where given, from that of out (dWg and dWu together)."""
+        M = self._tokens(X, Wg, Wu, Wd)
+        self._tensors(X.shape, X, dout, dX)
+        self._tensors(X.shape[:-1] + (self.cfg.hidden,), gate, up)
+        self._tensors(Wg.shape, dWg, dWu)
+        self._tensors(Wd.shape, dWd)
+        p = [None if t is None else t.data_ptr() for t in (X, Wg, Wu, Wd, gate, up, dout, dX, dWg, dWu, dWd)]
+        self._call(library().ff_ffn_backward, True, M, *p)
+        return dX, dWg, dWu, dWd
+
+    def device_status(self) -> int:
+        return library().ff_ffn_device_status(self.handle, self._raw_stream(self.device.index))
 
 
 # Same names as the C entry points, for callers that prefer the flat API.

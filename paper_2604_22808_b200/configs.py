@@ -75,6 +75,14 @@ class RotaryConfig:
     grid: Tuple[int, int, int] = (0, 0, 0)          # T, H, W of calls without positions
 
 
+@dataclass(frozen=True)
+class FFNConfig:
+    """The gated feed-forward block (include/freqformer.h, ff_ffn_config_t)."""
+    dim: int
+    hidden: int
+    activation: str = "silu"                        # "silu", "gelu_tanh" or "gelu"
+
+
 def _cuts(grid, c_low_num, c_low_den):
     """L_a = n_a * c_low, M_a = n_a * (c_low + 1/2), both exact integers here."""
     low = tuple(n * c_low_num // c_low_den for n in grid)

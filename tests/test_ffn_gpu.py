@@ -1,0 +1,293 @@
+"""The gated feed-forward block against its formulas in 64 bits.
+
+Tolerances, element by element.  A result, and every operand kept between two products, is rounded to bf16 once: 2^-8 relative.
+A sum of K products in fp32 is below K 2^-22 off, relative to the sum of the products' sizes (2^-23 for every addition, whichever way the
+tensor core cuts).  The activation and its derivative are below 1e-5 (1 + |g|) off absolutely (exponential and reciprocal, 2^-21
+relative, its argument's rounding |g| 2^-23 in front), and their slopes below 1.2 and 2.  What goes into a product reaches its result
+through the other operand's sizes."""
+import math
+
+import pytest
+import torch
+
+from paper_2604_22808_b200 import binding as B
+from paper_2604_22808_b200.configs import FFNConfig
+
+pytestmark = pytest.mark.gpu
+STEP = 2.0 ** -8
+
+
+def summed(K):
+    return K * 2.0 ** -22
+
+
+def act(name, g):
+    if name == "silu":
+        return g * torch.sigmoid(g)
+    if name == "gelu_tanh":
+        return 0.5 * g * (1 + torch.tanh(math.sqrt(2 / math.pi) * (g + 0.044715 * g ** 3)))
+    return 0.5 * g * (1 + torch.erf(g / math.sqrt(2)))
+
+
+def act_and_slope(name, g):
+    g = g.detach().clone().requires_grad_()
+    a = act(name, g)
+    return a.detach(), torch.autograd.grad(a.sum(), g)[0]
+
+
+def within(got, want, bound, what):
+    over = (got.double() - want).abs() - bound
+    assert not torch.isnan(over).any(), what
+    assert over.max().item() <= 0, f"{what}: {over.max().item():.3g} beyond the bound at {int(over.argmax())}"
+
+
+def inputs(M, D, F, seed=0, scale=1.0):
+    gen = torch.Generator("cuda").manual_seed(seed)
+
+    def normal(*shape, s=1.0):
+        return (s * torch.randn(*shape, generator=gen, device="cuda")).to(torch.bfloat16)
+    return normal(M, D, s=scale), normal(D, F, s=D ** -0.5), normal(D, F, s=D ** -0.5), normal(F, D, s=F ** -0.5), normal(M, D)
+
+
+def nan_like(*shape):
+    """A bf16 tensor of that shape, all NaN, in front of rows that must stay NaN (the second result says so)."""
+    n = math.prod(shape)
+    store = torch.full((n + 4096,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    return store[:n].view(shape), lambda: bool(store[n:].isnan().all())
+
+
+def forward_bounds(activation, X, Wg, Wu, Wd):
+    X, Wg, Wu, Wd = (t.double() for t in (X, Wg, Wu, Wd))
+    D, F = Wg.shape
+    g, u = X @ Wg, X @ Wu
+    eg, eu = summed(D) * (X.abs() @ Wg.abs()), summed(D) * (X.abs() @ Wu.abs())
+    a = act(activation, g)
+    h = a * u
+    ea = 1.2 * eg + 1e-5 * (1 + g.abs())
+    eh = STEP * h.abs() + (1 + STEP) * (ea * u.abs() + a.abs() * eu + ea * eu)
+    out = h @ Wd
+    eo = eh @ Wd.abs() + summed(F) * ((h.abs() + eh) @ Wd.abs())
+    return (out, STEP * out.abs() + (1 + STEP) * eo), (g, STEP * g.abs() + 2 * eg), (u, STEP * u.abs() + 2 * eu)
+
+
+def check_forward(M, D, F, activation, keep, scale=1.0):
+    X, Wg, Wu, Wd, _ = inputs(M, D, F, scale=scale)
+    ffn = B.GatedFFN(FFNConfig(D, F, activation))
+    out, clean = nan_like(M, D)
+    gate, gate_clean = nan_like(M, F)
+    up, up_clean = nan_like(M, F)
+    ffn.forward(X, Wg, Wu, Wd, out, *((gate, up) if keep else ()))
+    assert ffn.device_status() == 0
+    want = forward_bounds(activation, X, Wg, Wu, Wd)
+    within(out, *want[0], "out")
+    if keep:
+        within(gate, *want[1], "gate")
+        within(up, *want[2], "up")
+    assert clean() and gate_clean() and up_clean()
+
+
+def check_backward(M, D, F, activation, seed=0):
+    X, Wg, Wu, Wd, dout = inputs(M, D, F, seed)
+    gate, up = X @ Wg, X @ Wu
+    ffn = B.GatedFFN(FFNConfig(D, F, activation))
+    (dX, c0), (dWg, c1), (dWu, c2), (dWd, c3) = nan_like(M, D), nan_like(D, F), nan_like(D, F), nan_like(F, D)
+    ffn.backward(X, Wg, Wu, Wd, gate, up, dout, dX, dWg, dWu, dWd)
+    assert ffn.device_status() == 0
+    x, wg, wu, wd, g, u, do = (t.double() for t in (X, Wg, Wu, Wd, gate, up, dout))
+    a, slope = act_and_slope(activation, g)
+    ea = 1e-5 * (1 + g.abs())
+    dh = do @ wd.T
+    edh = summed(D) * (do.abs() @ wd.abs().T)
+    dg, du, h = dh * u * slope, dh * a, a * u
+    edg = STEP * dg.abs() + (1 + STEP) * u.abs() * (edh * (slope.abs() + ea) + dh.abs() * ea)
+    edu = STEP * du.abs() + (1 + STEP) * (edh * (a.abs() + ea) + dh.abs() * ea)
+    eh = STEP * h.abs() + (1 + STEP) * ea * u.abs()
+
+    def product(pairs, K):
+        """sum of A B over the pairs ((A, error of A), B), and its bound"""
+        y = sum(A @ Bm for (A, _), Bm in pairs)
+        e = sum(E @ Bm.abs() + summed(K) * ((A.abs() + E) @ Bm.abs()) for (A, E), Bm in pairs)
+        return y, STEP * y.abs() + (1 + STEP) * e
+    within(dX, *product([((dg, edg), wg.T), ((du, edu), wu.T)], 2 * F), "dX")
+    for got, (v, e), name in ((dWg, (dg, edg), "dWg"), (dWu, (du, edu), "dWu")):
+        y, e = product([((v.T, e.T), x)], M)
+        within(got, y.T, e.T, name)
+    within(dWd, *product([((h.T, eh.T), do)], M), "dWd")
+    assert c0() and c1() and c2() and c3()
+
+
+SIZES = [(1, 8, 8), (1, 256, 520), (2, 64, 64), (9, 72, 136), (16, 512, 128), (17, 1024, 264), (33, 200, 1000), (64, 128, 384), (65, 264, 512),
+         (100, 2048, 72), (128, 256, 256), (129, 136, 200), (200, 768, 2056), (256, 64, 1024), (300, 520, 648), (513, 256, 136), (1000, 384, 512)]
+
+
+@pytest.mark.parametrize("M,D,F", SIZES)
+def test_forward(M, D, F):
+    check_forward(M, D, F, ("silu", "gelu_tanh", "gelu")[M % 3], False)
+
+
+@pytest.mark.parametrize("M,D,F", SIZES[::2])
+def test_training_forward(M, D, F):
+    check_forward(M, D, F, ("silu", "gelu_tanh", "gelu")[(M + 1) % 3], True, scale=3.0)
+
+
+@pytest.mark.parametrize("M,D,F", SIZES)
+def test_backward(M, D, F):
+    check_backward(M, D, F, ("silu", "gelu_tanh", "gelu")[M % 3])
+
+
+def test_many_tiles():
+    """Several tiles for every block of the persistent launches, in each product."""
+    check_forward(5000, 72, 2600, "silu", True)
+    check_backward(5000, 1032, 1544, "gelu_tanh")
+    check_forward(100, 1032, 40000, "silu", False)
+
+
+def test_shapes_and_empty():
+    X, Wg, Wu, Wd, dout = inputs(24, 64, 128)
+    ffn = B.GatedFFN(FFNConfig(64, 128))
+    flat, deep = torch.empty_like(X), torch.empty_like(X)
+    ffn.forward(X, Wg, Wu, Wd, flat)
+    ffn.forward(X.view(2, 3, 4, 64), Wg, Wu, Wd, deep.view(2, 3, 4, 64))
+    assert torch.equal(flat, deep)
+    none = X[:0]
+    ffn.forward(none, Wg, Wu, Wd, none)
+    h = torch.empty(0, 128, dtype=torch.bfloat16, device="cuda")
+    grads = [torch.full_like(w, 7.0) for w in (Wg, Wu, Wd)]
+    ffn.backward(none, Wg, Wu, Wd, h, h, none, none, *grads)
+    assert not any(g.any() for g in grads)
+
+
+def test_chosen_gradients():
+    """Any subset of the gradients gives the bits of all of them, and the same call the same bits."""
+    M, D, F = 300, 136, 264
+    X, Wg, Wu, Wd, dout = inputs(M, D, F)
+    gate, up = X @ Wg, X @ Wu
+    ffn = B.GatedFFN(FFNConfig(D, F))
+    like = (X, Wg, Wu, Wd)
+    want = [torch.empty_like(t) for t in like]
+    ffn.backward(X, Wg, Wu, Wd, gate, up, dout, *want)
+    for chosen in ((0,), (1, 2), (3,), (0, 3), (0, 1, 2, 3), ()):
+        got = [torch.empty_like(t) if i in chosen else None for i, t in enumerate(like)]
+        ffn.backward(X, Wg, Wu, Wd, gate, up, dout, *got)
+        assert all(torch.equal(got[i], want[i]) for i in chosen)
+
+
+@pytest.mark.parametrize("M", (5, 300))
+def test_special_values(M):
+    """A token's infinities and NaN stay its own; gates far out saturate."""
+    D, F = 64, 192
+    X, Wg, Wu, Wd, _ = inputs(M, D, F)
+    ffn = B.GatedFFN(FFNConfig(D, F))
+    a, b = torch.empty_like(X), torch.empty_like(X)
+    ffn.forward(X, Wg, Wu, Wd, a)
+    bad = X.clone()
+    bad[1, 3], bad[M - 1, 5] = math.nan, math.inf
+    ffn.forward(bad, Wg, Wu, Wd, b)
+    rows = torch.ones(M, dtype=torch.bool, device="cuda")
+    rows[1] = rows[M - 1] = False
+    assert torch.equal(a[rows], b[rows]) and b[1].isnan().all() and not b[M - 1].isfinite().any()
+    for activation in ("silu", "gelu_tanh", "gelu"):         # |gate| up to about 1e5: the activation is 0 or the gate
+        one = B.GatedFFN(FFNConfig(D, F, activation))
+        far = (X.float() * 1e4).to(torch.bfloat16)
+        one.forward(far, Wg, Wu, Wd, b)
+        want = forward_bounds(activation, far, Wg, Wu, Wd)[0]
+        within(b, *want, activation)
+        gate, up = far @ Wg, far @ Wu
+        grads = [torch.empty_like(t) for t in (X, Wg, Wu, Wd)]
+        one.backward(far, Wg, Wu, Wd, gate, up, X, *grads)
+        assert all(g.isfinite().all() for g in grads)
+
+
+def test_gradient_against_differences():
+    """The four gradients against central differences of the formula in 64 bits along random directions: the difference of the
+    formula is exact to h^2, and a gradient's own error along a direction is below its bound of test_backward; 2 % of the
+    directional derivative's scale covers both at these sizes (2^-8 from each of two roundings, of terms with random signs)."""
+    M, D, F = 40, 64, 96
+    X, Wg, Wu, Wd, dout = inputs(M, D, F, seed=4)
+    for activation in ("silu", "gelu_tanh", "gelu"):
+        ffn = B.GatedFFN(FFNConfig(D, F, activation))
+        out, gate, up = torch.empty_like(X), *(torch.empty(M, F, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        ffn.forward(X, Wg, Wu, Wd, out, gate, up)
+        grads = [torch.empty_like(t) for t in (X, Wg, Wu, Wd)]
+        ffn.backward(X, Wg, Wu, Wd, gate, up, dout, *grads)
+        args = [t.double() for t in (X, Wg, Wu, Wd)]
+
+        def loss(x, wg, wu, wd):
+            return ((act(activation, x @ wg) * (x @ wu)) @ wd * dout.double()).sum().item()
+        gen = torch.Generator("cuda").manual_seed(6)
+        for i, g in enumerate(grads):
+            v = torch.randn(args[i].shape, generator=gen, device="cuda", dtype=torch.float64)
+            v *= args[i].abs().mean()
+            e = 1e-5
+            plus, minus = ([a + s * e * v if j == i else a for j, a in enumerate(args)] for s in (1, -1))
+            slope = (loss(*plus) - loss(*minus)) / (2 * e)
+            scale = (g.double().norm() * v.norm()).item() / math.sqrt(v.numel())
+            assert abs(slope - (g.double() * v).sum().item()) <= 0.02 * scale, (activation, i)
+
+
+@pytest.mark.parametrize("M", (3, 700))
+def test_streams_and_graphs(M):
+    """Calls on two streams at once and two captured graphs give what a call alone gives; a graph takes new inputs."""
+    D, F = 256, 520
+    ffn = B.GatedFFN(FFNConfig(D, F))
+    sets = []
+    for seed in range(2):
+        X, Wg, Wu, Wd, dout = inputs(M, D, F, seed)
+        hid = [torch.empty(M, F, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        sets.append((X, Wg, Wu, Wd, dout, hid, [torch.empty_like(t) for t in (X, X, Wg, Wu, Wd)]))
+
+    def call(s):
+        X, Wg, Wu, Wd, dout, hid, r = s
+        ffn.forward(X, Wg, Wu, Wd, r[0], *hid)
+        ffn.backward(X, Wg, Wu, Wd, *hid, dout, *r[1:])
+
+    def same(s, want):
+        return all(torch.equal(a, b) for a, b in zip(s[6], want))
+    want = []
+    for s in sets:
+        call(s)
+        want.append([t.clone() for t in s[6]])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(5):
+        for s, st in zip(sets, streams):
+            with torch.cuda.stream(st):
+                call(s)
+    torch.cuda.synchronize()
+    assert all(same(s, w) for s, w in zip(sets, want))
+    graphs = []
+    for s in sets:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(s)
+        graphs.append(graph)
+    for s in sets:
+        for t in s[6]:
+            t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for graph, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(same(s, w) for s, w in zip(sets, want))
+    for a, b in zip(sets[0][:5], sets[1][:5]):
+        a.copy_(b)
+    graphs[0].replay()
+    torch.cuda.synchronize()
+    assert same(sets[0], want[1]) and ffn.device_status() == 0
+
+
+def test_binding_refusals():
+    X, Wg, Wu, Wd, dout = inputs(4, 64, 128)
+    ffn = B.GatedFFN(FFNConfig(64, 128))
+    h = torch.empty(4, 128, dtype=torch.bfloat16, device="cuda")
+    y = torch.empty_like(X)
+    for call in (lambda: ffn.forward(X.float(), Wg, Wu, Wd, y), lambda: ffn.forward(X, Wg.t(), Wu, Wd, y), lambda: ffn.forward(X, Wg, Wu, Wg, y),
+                 lambda: ffn.forward(X, Wg, Wu, Wd, y[:3]), lambda: ffn.forward(X, Wg, Wu, Wd, y, gate=h), lambda: ffn.forward(X.cpu(), Wg, Wu, Wd, y),
+                 lambda: ffn.forward(X[:, :32], Wg, Wu, Wd, y), lambda: ffn.forward(X, Wg, Wu, Wd.t().contiguous().t(), y),
+                 lambda: ffn.forward(X.flatten()[1:193].view(3, 64), Wg, Wu, Wd, y[:3]),
+                 lambda: ffn.backward(X, Wg, Wu, Wd, h, h, dout, dWg=torch.empty_like(Wg)), lambda: ffn.backward(X, Wg, Wu, Wd, h, h[:2], dout),
+                 lambda: B.GatedFFN(FFNConfig(60, 128)), lambda: B.GatedFFN(FFNConfig(64, 128, "relu"))):
+        with pytest.raises(B.FFError):
+            call()
