@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 from typing import Optional, Sequence
 
 import numpy as np
@@ -106,7 +107,7 @@ def library() -> C.CDLL:
         lib.ff_plan_stage_times.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_int64)]
         lib.ff_high_attention_noalloc.argtypes = [C.c_void_p] * 4 + [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p]
         lib.ff_plan_selftest_bounded_wait.argtypes = [C.c_void_p, C.c_int64, C.POINTER(C.c_int32), C.c_void_p]
-        heads, place = C.POINTER(ff_heads_t), [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64]
+        heads, place = C.c_void_p, [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64]
         lib.ff_rotary_create.argtypes = [C.POINTER(ff_rotary_config_t), C.POINTER(C.c_void_p)]
         lib.ff_rotary_destroy.argtypes = [C.c_void_p]
         lib.ff_rotary_frequencies.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double)]
@@ -442,19 +443,33 @@ class Rotary:
         if status != FF_OK:
             raise FFError(status, library().ff_rotary_last_error(self.handle).decode())
 
-    def _heads(self, t, shape, device):
-        """The ff_heads_t of a tensor of that shape on that device."""
-        if t.shape != shape or t.dtype != self._dtype or t.device != device or not t.is_cuda:
-            raise FFError(1, f"expected a {self._dtype} tensor of shape {tuple(shape)} on {device}")
-        s = t.stride()
-        if s[3] != 1:
-            raise FFError(1, "the channels of a head must be contiguous")
-        return C.byref(ff_heads_t(t.data_ptr(), s[0], s[1], s[2], shape[1]))
+    def _heads(self, device, *tensors):
+        """Addresses of the tensors' ff_heads_t (None for None), and the array that holds them; the tensors are q- and k-like in
+        turns, those of a kind alike in shape."""
+        dtype, rows, at = self._dtype, [], []
+        shapes = tensors[0].shape, None if tensors[1] is None else tensors[1].shape
+        for i, t in enumerate(tensors):
+            shape = shapes[i & 1]
+            if t is None or shape is None:
+                if t is not None or shape is not None:
+                    raise FFError(1, "k comes with its outputs and gradients, or none of them is given")
+                at.append(None)
+                continue
+            if t.shape != shape or t.dtype != dtype or t.device != device:
+                raise FFError(1, f"expected a {dtype} tensor of shape {tuple(shape)} on {device}")
+            sb, sh, st, sc = t.stride()
+            if sc != 1:
+                raise FFError(1, "the channels of a head must be contiguous")
+            at.append(8 * len(rows))
+            rows += (t.data_ptr(), sb, sh, st, shape[1])         # (the layout of ff_heads_t, heads in its low half word)
+        rows = array("q", rows)
+        base = rows.buffer_info()[0]
+        return [None if o is None else base + o for o in at], rows
 
     def _place(self, q, k, positions):
-        """(batch, tokens, positions, stride between the samples' positions) and the shape of k, all checked."""
-        if q.dim() != 4 or q.shape[3] != self.cfg.head_dim:
-            raise FFError(1, f"expected q of shape [batch][heads][tokens][{self.cfg.head_dim}]")
+        """(batch, tokens, positions, stride between the samples' positions), checked."""
+        if q.dim() != 4 or q.shape[3] != self.cfg.head_dim or not q.is_cuda:
+            raise FFError(1, f"expected q on a GPU, of shape [batch][heads][tokens][{self.cfg.head_dim}]")
         B, _, N, d = q.shape
         if k is not None and (k.dim() != 4 or k.shape[0] != B or k.shape[2] != N or k.shape[3] != d):
             raise FFError(1, f"expected k of shape [{B}][heads][{N}][{d}]")
@@ -482,41 +497,26 @@ class Rotary:
 
     def apply(self, q, q_out, k=None, k_out=None, positions=None, inverse: bool = False):
         """The rotation of q and k; inverse: its transpose, the backward pass."""
-        B, N, pos, ps = self._place(q, k, positions)
-        dev = q.device
-        if (k is None) != (k_out is None):
-            raise FFError(1, "k comes with its output, or neither does")
-        ks = None if k is None else k.shape
-        self._call(dev, library().ff_rotary_apply, B, N, pos, ps, self._heads(q, q.shape, dev), None if ks is None else self._heads(k, ks, dev),
-                   int(inverse), self._heads(q_out, q.shape, dev), None if ks is None else self._heads(k_out, ks, dev))
+        place, dev = self._place(q, k, positions), q.device
+        (hq, hk, hqo, hko), keep = self._heads(dev, q, k, q_out, k_out)
+        self._call(dev, library().ff_rotary_apply, *place, hq, hk, int(inverse), hqo, hko)
         return q_out, k_out
 
     def qk_norm(self, q, k, wq, wk, q_out, k_out, eps: float = 1e-6, positions=None):
         """Norm of every row, times wq / wk (fp32 [head_dim], None: ones), then the rotation."""
-        B, N, pos, ps = self._place(q, k, positions)
-        dev = q.device
-        if (k is None) != (k_out is None):
-            raise FFError(1, "k comes with its output, or neither does")
-        ks = None if k is None else k.shape
-        self._call(dev, library().ff_qk_norm, B, N, pos, ps, self._heads(q, q.shape, dev), None if ks is None else self._heads(k, ks, dev),
-                   self._weight(wq, dev), self._weight(wk, dev), eps, self._heads(q_out, q.shape, dev),
-                   None if ks is None else self._heads(k_out, ks, dev))
+        place, dev = self._place(q, k, positions), q.device
+        (hq, hk, hqo, hko), keep = self._heads(dev, q, k, q_out, k_out)
+        self._call(dev, library().ff_qk_norm, *place, hq, hk, self._weight(wq, dev), self._weight(wk, dev), eps, hqo, hko)
         return q_out, k_out
 
     def qk_norm_backward(self, q, k, wq, wk, dq_out, dk_out, dq, dk, dwq=None, dwk=None, eps: float = 1e-6, positions=None):
         """Gradients of q, k (and of the weights, fp32 [head_dim], where given) from those of qk_norm's outputs."""
-        B, N, pos, ps = self._place(q, k, positions)
-        dev = q.device
-        if (k is None) != (dk_out is None) or (k is None) != (dk is None):
-            raise FFError(1, "k comes with its gradients, or neither does")
-        ks = None if k is None else k.shape
+        place, dev = self._place(q, k, positions), q.device
+        (hq, hk, hgq, hgk, hdq, hdk), keep = self._heads(dev, q, k, dq_out, dk_out, dq, dk)
         # (a workspace per call: calls on different streams and captured graphs share none)
         ws = self._torch.empty(self.workspace_bytes, dtype=self._torch.uint8, device=dev)
-        self._call(dev, library().ff_qk_norm_backward, B, N, pos, ps, self._heads(q, q.shape, dev), None if ks is None else self._heads(k, ks, dev),
-                   self._weight(wq, dev), self._weight(wk, dev), eps, self._heads(dq_out, q.shape, dev),
-                   None if ks is None else self._heads(dk_out, ks, dev), self._heads(dq, q.shape, dev),
-                   None if ks is None else self._heads(dk, ks, dev), self._weight(dwq, dev), self._weight(dwk, dev),
-                   ws.data_ptr(), self.workspace_bytes)
+        self._call(dev, library().ff_qk_norm_backward, *place, hq, hk, self._weight(wq, dev), self._weight(wk, dev), eps, hgq, hgk, hdq, hdk,
+                   self._weight(dwq, dev), self._weight(dwk, dev), ws.data_ptr(), self.workspace_bytes)
         return dq, dk
 
 
@@ -537,6 +537,7 @@ class GatedFFN:
             self.device = torch.device("cuda", torch.cuda.current_device())
         with torch.cuda.device(self.device):
             _check(library().ff_ffn_create(C.byref(c), C.byref(self.handle)))
+        self._sized, self._bytes = None, 0                       # the workspace's size for the last number of tokens
         self._raw_stream = _stream_getter(torch)
 
     def destroy(self):
@@ -572,7 +573,11 @@ class GatedFFN:
     def _call(self, fn, training, tokens, *pointers):
         torch, dev = self._torch, self.device
         # (a workspace per call: calls on different streams and captured graphs share none)
-        n = (3 if training else 1) * ((tokens * self.cfg.hidden * 2 + 255) // 256 * 256)
+        if self._sized != (tokens, training):
+            size = C.c_size_t()
+            _check(library().ff_ffn_workspace_bytes(C.byref(self._c), tokens, training, C.byref(size)))
+            self._sized, self._bytes = (tokens, training), size.value
+        n = self._bytes
         ws = torch.empty(n, dtype=torch.uint8, device=dev)
         if torch.cuda.current_device() == dev.index:
             return self._status(fn(self.handle, tokens, *pointers, ws.data_ptr(), n, self._raw_stream(dev.index)))

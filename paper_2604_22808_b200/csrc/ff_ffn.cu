@@ -13,9 +13,12 @@
 //   dX            K runs over the columns of dG, then those of dU
 //   dWg, dWu      one launch, the matrices side by side along N; K runs over the tokens
 // H, dG and dU are rounded to bf16 between the products: they are operands of the next one.
+// Products with few tiles are cut along K (split_of); with few tokens the weights are the rows (ffn_few_kernel).
 //
 //   warp 0      TMA producer          warp 1      tcgen05.mma issuer of the pair (even CTA), owns the tensor memory
-//   warps 2..9  epilogue: a thread owns one row of the tile and half its columns
+//   warps 2..9  epilogue: a thread owns one row of the tile and half its columns, which reach memory by TMA from a staging area of
+//               the warp (stored from registers, every thread a row of its own, dH took 343 us instead of 266, G and U kept 141
+//               instead of 111)
 #include <cuda.h>
 #include <stdio.h>
 
@@ -30,7 +33,9 @@ using namespace sm100;
 struct ff_ffn {
   ff_ffn_config_t cfg;
   int device, sm_count;
+  int room[2][2][9];       // few-token kernel: blocks that run at the same time, [matrices - 1][tiles of 128 tokens][blocks of a cluster]
   int* status;             // device status word (plan-like: raised by an expired wait)
+  mutable FFMapCache maps; // tensor maps by matrix and box; every use puts in its address
   char err[512];
 };
 
@@ -40,91 +45,134 @@ constexpr int TM = 256, TN = 256, TK = 64;
 constexpr int PIECE = 64 * 128;                  // 64 rows of 128 bytes
 constexpr int OPERAND = 2 * PIECE;               // one CTA's 128 rows (or columns) of a K chunk
 constexpr int STAGE = 2 * OPERAND;
-constexpr int NSTAGE = 6;
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 
-enum { STORE = 0, GATE = 1, DGATE = 2 };         // epilogues
+enum { STORE = 0, GATE = 1, DGATE = 2, PARTIAL = 3 };           // epilogues
+// Stages of the ring, and staging areas of an epilogue warp: 32 rows of 64 columns each, on their way to or from memory by TMA
+constexpr int AREA = 32 * 128;
+__host__ __device__ constexpr int ring_stages(int epi) { return epi == DGATE ? 5 : 6; }
+__host__ __device__ constexpr int areas(int epi) { return epi == DGATE ? 2 : 1; }
 
 struct GemmParams {
   long long rows;                  // output rows
   int cols;                        // output columns of one matrix
   int m_tiles, n_tiles, mats;      // tiles; matrices side by side
   int kchunks, sources;            // K chunks of one source, sources one after the other
-  int act;
-  __nv_bfloat16* out[3];           // STORE: one per matrix;  GATE: H, G or NULL, U;  DGATE: dG, dU, H
-  const __nv_bfloat16* gate;       // DGATE
-  const __nv_bfloat16* up;
+  int split;                       // PARTIAL: parts of K, each with its own sums
+  int act, keep;                   // GATE: G and U are written too
   int* status;
 };
+// Operands by source (K) or matrix (N), and what the epilogue moves: STORE: the outputs by matrix;  GATE: H, G, U;
+// DGATE: G, U (read), dG, dU, H;  PARTIAL: fp32 sums [matrix][part][rows][cols]
+struct GemmMaps { CUtensorMap a[2], b[2], e[5]; };
 
 struct Shared {
-  uint64_t full[NSTAGE], empty[NSTAGE], acc_full[2], acc_empty[2];
+  uint64_t full[6], empty[6], acc_full[2], acc_empty[2], in_full[EPI_WARPS];
   uint32_t tmem_base;
   int abort_flag;
 };
-constexpr size_t SMEM = (size_t)NSTAGE * STAGE + sizeof(Shared) + 1024;
+inline int chunks(long long k) { return (int)((k + TK - 1) / TK); }
+__host__ __device__ constexpr size_t smem_bytes(int epi) { return (size_t)ring_stages(epi) * STAGE + (size_t)EPI_WARPS * areas(epi) * AREA + sizeof(Shared) + 1024; }
+static_assert(smem_bytes(STORE) <= 232448 && smem_bytes(GATE) <= 232448 && smem_bytes(DGATE) <= 232448, "227 KB a block");
 
 // act(g) and, with SLOPE, its derivative.  The cubic inside gelu_tanh saturates long before |g| = 16.
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
-template <bool SLOPE>
-__device__ __forceinline__ float activation(int act, float g, float* slope) {
-  if (act == FF_ACT_SILU) {
+__device__ __forceinline__ float exponential(float v) { return ex2(1.4426950408889634f * v); }
+__device__ __forceinline__ float sigmoid(float v) { return rcp(1.f + exponential(-v)); }
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float activation(float g, float* slope) {
+  if constexpr (ACT == FF_ACT_SILU) {
     const float s = sigmoid(g);
     if (SLOPE) *slope = s * (1.f + g * (1.f - s));
     return g * s;
   }
-  if (act == FF_ACT_GELU_TANH) {
+  else if constexpr (ACT == FF_ACT_GELU_TANH) {
     const float c = 1.5957691216057308f;         // 2 sqrt(2 / pi)
     const float t = fminf(fmaxf(g, -16.f), 16.f), t2 = t * t;
     const float s = sigmoid(c * t * (1.f + 0.044715f * t2));
     if (SLOPE) *slope = s + t * s * (1.f - s) * c * (1.f + 0.134145f * t2);
     return g * s;
   }
-  const float p = 0.5f * erfcf(-0.70710678118654752f * g);
-  if (SLOPE) {
-    const float t = fminf(fmaxf(g, -32.f), 32.f);
-    *slope = p + t * 0.3989422804014327f * __expf(-0.5f * t * t);
+  else {
+    const float p = 0.5f * erfcf(-0.70710678118654752f * g);
+    if (SLOPE) {
+      const float t = fminf(fmaxf(g, -32.f), 32.f);
+      *slope = p + t * 0.3989422804014327f * exponential(-0.5f * t * t);
+    }
+    return g * p;
   }
-  return g * p;
+}
+// body(constant) with the configuration's activation as a compile-time constant: chosen once for many elements, whose
+// instructions then overlap (chosen for each of them, the launch of dH took 266 us instead of 221: 9999 tokens, dim 2048, hidden 5632)
+template <int ACT> struct Act { static constexpr int value = ACT; };
+template <class Body>
+__device__ __forceinline__ void with_activation(int act, Body body) {
+  if (act == FF_ACT_SILU) body(Act<FF_ACT_SILU>());
+  else if (act == FF_ACT_GELU_TANH) body(Act<FF_ACT_GELU_TANH>());
+  else body(Act<FF_ACT_GELU>());
 }
 
-__device__ __forceinline__ void store32(__nv_bfloat16* dst, const float (&v)[32], int left) {
+template <int N>
+__device__ __forceinline__ void pack(const float (&v)[N], uint32_t* w) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) w[i] = bf16_pair(__float_as_uint(v[2 * i]), __float_as_uint(v[2 * i + 1]));
+}
+// A lane's row of a staging area: pieces of 16 bytes in the order of the 128-byte swizzle.  `half` selects 32 of the 64 columns.
+__device__ __forceinline__ void stage32(uint8_t* area, int lane, int half, const uint32_t* w) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (j * 8 < left) {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = bf16_pair(__float_as_uint(v[j * 8 + 2 * i]), __float_as_uint(v[j * 8 + 2 * i + 1]));
-      *(uint4*)(dst + j * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    *(uint4*)(area + lane * 128 + (((half * 4 + j) ^ (lane & 7)) * 16)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
 }
-__device__ __forceinline__ void load32(const __nv_bfloat16* src, uint4 (&v)[4], int left) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = j * 8 < left ? __ldcs((const uint4*)(src + j * 8)) : make_uint4(0, 0, 0, 0);
+__device__ __forceinline__ void stage32(uint8_t* area, int lane, int half, const float (&v)[32]) {
+  uint32_t w[16];
+  pack(v, w);
+  stage32(area, lane, half, w);
 }
-__device__ __forceinline__ float element(const uint4 (&v)[4], int i) {
+template <int N>
+__device__ __forceinline__ float element(const uint4 (&v)[N], int i) {
   const uint32_t w = ((const uint32_t*)v)[i >> 1];
   return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
 }
 
+// Work item t: a tile and its part of K.  The tiles of up to eight rows of tiles follow one another column by column, so that
+// what runs at the same time reads few rows of A and few columns of B (row by row, dWg and dWu of dim 2048, hidden 5632, 9999
+// tokens read dG and dU from memory in each of five waves: 420 us in a row of calls, 372 column by column).
+struct Item { int m, n, mat, part; };
+__device__ __forceinline__ Item item_of(const GemmParams& P, int t) {
+  const int cols = P.n_tiles * P.mats, tiles = P.m_tiles * cols;
+  Item w;
+  w.part = P.split > 1 ? t / tiles : 0;
+  t -= w.part * tiles;
+  const int band = t / (8 * cols), height = min(8, P.m_tiles - band * 8);
+  const int r = t - band * 8 * cols, c = r / height;
+  w.m = band * 8 + r - c * height;
+  w.mat = P.mats > 1 && c >= P.n_tiles;
+  w.n = c - w.mat * P.n_tiles;
+  return w;
+}
+// K chunks of a part
+__device__ __forceinline__ void part_of_k(const GemmParams& P, int part, int& begin, int& end) {
+  const int k = P.kchunks * P.sources, q = k / P.split, r = k - q * P.split;         // (the first r parts have one more)
+  begin = part * q + min(part, r);
+  end = begin + q + (part < r);
+}
+
 template <bool A_MN, bool B_MN, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
-ffn_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_a1,
-                const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1, const GemmParams P) {
+ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
+  constexpr int NSTAGE = ring_stages(EPI), AREAS = areas(EPI);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  Shared& sh = *(Shared*)(smem + NSTAGE * STAGE);
+  Shared& sh = *(Shared*)(smem + NSTAGE * STAGE + EPI_WARPS * AREAS * AREA);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const int per_row = P.n_tiles * P.mats;                       // tiles of a row of tiles
-  const long long tiles = (long long)P.m_tiles * per_row;
-  const int kchunks = P.kchunks * P.sources;
+  const int tiles = P.m_tiles * P.n_tiles * P.mats, items = tiles * P.split;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < NSTAGE; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.acc_full[i], 1); mbar_init(&sh.acc_empty[i], 2 * EPI_WARPS); }
+    for (int i = 0; i < EPI_WARPS; ++i) mbar_init(&sh.in_full[i], 1);
     sh.abort_flag = 0;
     fence_mbar_init();
   }
@@ -141,17 +189,19 @@ ffn_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constan
     if (lane == 0) {
       unsigned n = 0;
       bool ok = true;
-      for (long long t = pair; t < tiles && ok; t += pairs) {
-        const int mt = (int)(t / per_row), j = (int)(t % per_row), mat = j / P.n_tiles, nt = j % P.n_tiles;
-        const int m0 = mt * TM + (int)rank * 128;
-        const int n0 = EPI == GATE ? nt * 128 : nt * TN + (int)rank * 128;
-        for (int kc = 0; kc < kchunks && ok; ++kc, ++n) {
+      for (int t = pair; t < items && ok; t += pairs) {
+        const Item w = item_of(P, t);
+        const int m0 = w.m * TM + (int)rank * 128;
+        const int n0 = EPI == GATE ? w.n * 128 : w.n * TN + (int)rank * 128;
+        int k_begin, k_end;
+        part_of_k(P, w.part, k_begin, k_end);
+        for (int kc = k_begin; kc < k_end && ok; ++kc, ++n) {
           const int slot = n % NSTAGE;
           if (n >= (unsigned)NSTAGE) ok = mbar_wait(&sh.empty[slot], ((n / NSTAGE) - 1) & 1, abort_flag);
           if (!ok) break;
           const int second = kc >= P.kchunks, k0 = (kc - (second ? P.kchunks : 0)) * TK;
-          const CUtensorMap* ma = second ? &map_a1 : &map_a0;
-          const CUtensorMap* mb = (EPI == GATE ? (int)rank : second | mat) ? &map_b1 : &map_b0;
+          const CUtensorMap* ma = &maps.a[second];
+          const CUtensorMap* mb = &maps.b[EPI == GATE ? (int)rank : second | w.mat];
           uint8_t* dst = smem + slot * STAGE;
           const uint32_t bar = map_shared(&sh.full[slot], 0);
           if (rank == 0) mbar_arrive_expect_tx(&sh.full[slot], 2 * STAGE);
@@ -178,12 +228,14 @@ ffn_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constan
       constexpr uint64_t A_STEP = A_MN ? 128 : 2, B_STEP = B_MN ? 128 : 2;      // 16 K elements on, in units of 16 bytes
       unsigned n = 0, nt = 0;
       bool ok = true;
-      for (long long t = pair; t < tiles && ok; t += pairs, ++nt) {
+      for (int t = pair; t < items && ok; t += pairs, ++nt) {
         const int ab = nt & 1;
+        int k_begin, k_end;
+        part_of_k(P, P.split > 1 ? t / tiles : 0, k_begin, k_end);
         if (nt >= 2) ok = mbar_wait_warp(&sh.acc_empty[ab], ((nt >> 1) - 1) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        for (int kc = 0; kc < kchunks && ok; ++kc, ++n) {
+        for (int kc = k_begin; kc < k_end && ok; ++kc, ++n) {
           const int slot = n % NSTAGE;
           ok = mbar_wait_warp(&sh.full[slot], (n / NSTAGE) & 1, abort_flag);
           if (!ok) break;
@@ -191,7 +243,7 @@ ffn_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constan
           const uint64_t at = (uint64_t)(slot * (STAGE >> 4));
 #pragma unroll
           for (int ks = 0; ks < TK / 16; ++ks)
-            umma_ss_pair(tm + ab * TN, a0 + at + ks * A_STEP, b0 + at + ks * B_STEP, idesc, ks > 0 ? 1u : (kc > 0 ? 1u : 0u));
+            umma_ss_pair(tm + ab * TN, a0 + at + ks * A_STEP, b0 + at + ks * B_STEP, idesc, ks > 0 ? 1u : (kc > k_begin ? 1u : 0u));
           umma_commit_pair(&sh.empty[slot]);
         }
         umma_commit_pair(&sh.acc_full[ab]);
@@ -200,76 +252,157 @@ ffn_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constan
   } else {
     const int quarter = warp & 3, half = (warp - 2) >> 2;
     const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
-    unsigned nt = 0;
+    uint8_t* area = smem + NSTAGE * STAGE + (warp - 2) * AREAS * AREA;
+    uint64_t* in_full = &sh.in_full[warp - 2];
+    unsigned nt = 0, loads = 0;
     bool ok = true;
-    for (long long t = pair; t < tiles && ok; t += pairs, ++nt) {
+    // The warp's rows of one output, 64 columns of them, from `values` by way of a staging area.
+    auto put = [&](const CUtensorMap* map, uint8_t* to, int col, int row, auto values, auto read) {
+      if (lane == 0) bulk_wait_read0();                         // (the area's last store has read it)
+      __syncwarp();
+#pragma unroll 1
+      for (int q = 0; q < 2; ++q) {
+        float v[32];
+        values(q, v);
+        if (q) read();
+        stage32(to, lane, q, v);
+      }
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) { tma_store_3d(to, map, col, row, 0); bulk_commit(); }
+    };
+    for (int t = pair; t < items && ok; t += pairs, ++nt) {
+      const Item w = item_of(P, t);
       const int ab = nt & 1;
-      const int j = (int)(t % per_row), mat = j / P.n_tiles;
-      const long long row = (t / per_row) * TM + rank * 128 + quarter * 32 + lane;
-      const bool live = row < P.rows;
-      const size_t line = (size_t)row * P.cols;
+      const int row = w.m * TM + (int)rank * 128 + quarter * 32;
       const uint32_t acc = tm + lane_addr + ab * TN;
       constexpr int WIDTH = EPI == GATE ? 64 : 128;             // columns of the warp
-      const int c0 = (j % P.n_tiles) * (2 * WIDTH) + half * WIDTH;
-      uint4 g[4], u[4];
-      if (EPI == DGATE) {                                       // (on their way before the accumulator is complete)
-        load32(P.gate + line + c0, g, live ? P.cols - c0 : 0);
-        load32(P.up + line + c0, u, live ? P.cols - c0 : 0);
+      const int c0 = w.n * (2 * WIDTH) + half * WIDTH;
+      const bool rows = row < P.rows;
+      auto get = [&](int col) {                                 // DGATE: G and U of 64 columns into the first two areas
+        if (lane == 0) {
+          bulk_wait_read0();
+          mbar_arrive_expect_tx(in_full, 2 * AREA);
+          tma_load_3d(area, &maps.e[0], in_full, col, row, 0);
+          tma_load_3d(area + AREA, &maps.e[1], in_full, col, row, 0);
+        }
+      };
+      if (EPI == DGATE && rows && c0 < P.cols) {                // (on their way before the accumulator is complete)
+        get(c0);
+        if (lane == 0 && c0 + 64 < P.cols) {
+          tma_prefetch_3d(&maps.e[0], c0 + 64, row, 0);
+          tma_prefetch_3d(&maps.e[1], c0 + 64, row, 0);
+        }
       }
       ok = __all_sync(0xffffffffu, mbar_wait(&sh.acc_full[ab], (nt >> 1) & 1, abort_flag));
       if (!ok) break;
       tc_fence_after();
+      auto release = [&] {                                      // the warp has read its part of the accumulator
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_shared(&sh.acc_empty[ab], 0));
+      };
+      const int parts = rows ? min(WIDTH, (P.cols - c0 + 63) / 64 * 64) : 0;
+      if (parts <= 0) release();
 #pragma unroll 1
-      for (int q = 0; q < WIDTH / 32; ++q) {
-        const int col = c0 + q * 32, left = live ? P.cols - col : 0;
-        uint32_t r[32];
-        tmem_ld32(acc + half * WIDTH + q * 32, r);
-        float v[32];
-        if (EPI == STORE) {
-          tmem_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-          store32((mat ? P.out[1] : P.out[0]) + line + col, v, left);
-        } else if (EPI == GATE) {
-          uint32_t s[32];
-          tmem_ld32(acc + 128 + half * WIDTH + q * 32, s);
-          tmem_wait_ld();
-          if (P.out[1]) {                                       // kept for the backward pass
+      for (int s = 0; s < parts; s += 64) {
+        const int col = c0 + s;
+        const uint32_t at = acc + half * WIDTH + s;
+        const bool last = s + 64 >= parts;
+        auto done = [&] { if (last) release(); };
+        auto more = [] {};
+        auto sums = [&](uint32_t from) {
+          return [=](int q, float (&v)[32]) {
+            uint32_t r[32];
+            tmem_ld32(from + q * 32, r);
+            tmem_wait_ld();
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-            store32(P.out[1] + line + col, v, left);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(s[i]);
-            store32(P.out[2] + line + col, v, left);
+          };
+        };
+        if (EPI == STORE) {
+          put(&maps.e[w.mat], area, col, row, sums(at), done);
+        } else if (EPI == PARTIAL) {
+#pragma unroll 1
+          for (int q = 0; q < 2; ++q) {                         // 32 columns of fp32 fill a row of the area
+            uint32_t r[32];
+            tmem_ld32(at + q * 32, r);
+            tmem_wait_ld();
+            if (q) done();
+            if (lane == 0) bulk_wait_read0();
+            __syncwarp();
+            stage32(area, lane, 0, r);
+            stage32(area, lane, 1, r + 16);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0 && col + q * 32 < P.cols) { tma_store_3d(area, &maps.e[0], col + q * 32, row, w.mat * P.split + w.part); bulk_commit(); }
           }
+        } else if (EPI == GATE) {
+          if (P.keep) {                                         // for the backward pass
+            put(&maps.e[1], area, col, row, sums(at), more);
+            put(&maps.e[2], area, col, row, sums(at + 128), more);
+          }
+          put(&maps.e[0], area, col, row, [&](int q, float (&v)[32]) {
+            uint32_t g[32], u[32];
+            tmem_ld32(at + q * 32, g);
+            tmem_ld32(at + 128 + q * 32, u);
+            tmem_wait_ld();
+            with_activation(P.act, [&](auto act) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = activation<false>(P.act, __uint_as_float(r[i]), nullptr) * __uint_as_float(s[i]);
-          store32(P.out[0] + line + col, v, left);
+              for (int i = 0; i < 32; ++i) v[i] = activation<act.value, false>(__uint_as_float(g[i]), nullptr) * __uint_as_float(u[i]);
+            });
+          }, done);
         } else {
-          uint4 g2[4], u2[4];
-          const bool more = q + 1 < WIDTH / 32;
-          load32(P.gate + line + col + 32, g2, more ? left - 32 : 0);
-          load32(P.up + line + col + 32, u2, more ? left - 32 : 0);
-          tmem_wait_ld();
-          float dg[32], h[32];
+          if (s) get(col);
+          ok = __all_sync(0xffffffffu, mbar_wait(in_full, loads++ & 1, abort_flag));
+          if (!ok) break;
+          // The gradients take the places of what they are made from, H that of dG once it has left.
+          uint32_t hid[32];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float d = __uint_as_float(r[i]), up = element(u, i);
-            float slope;
-            const float a = activation<true>(P.act, element(g, i), &slope);
-            dg[i] = d * up * slope; v[i] = d * a; h[i] = a * up;
+          for (int q = 0; q < 4; ++q) {                         // 16 columns: two pieces of a row
+            uint32_t d[16];
+            tmem_ld16(at + q * 16, d);
+            uint4* const p[2] = {(uint4*)(area + lane * 128 + (((2 * q) ^ (lane & 7)) * 16)), (uint4*)(area + lane * 128 + (((2 * q + 1) ^ (lane & 7)) * 16))};
+            const uint4 g[2] = {*p[0], *p[1]}, u[2] = {p[0][AREA / 16], p[1][AREA / 16]};
+            tmem_wait_ld();
+            if (q == 3 && last) release();
+            float dg[16], du[16], h[16];
+            with_activation(P.act, [&](auto act) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float dh = __uint_as_float(d[i]), up = element(u, i);
+                float slope;
+                const float a = activation<act.value, true>(element(g, i), &slope);
+                dg[i] = dh * up * slope; du[i] = dh * a; h[i] = a * up;
+              }
+            });
+            uint32_t w0[8], w1[8];
+            pack(dg, w0); pack(du, w1); pack(h, hid + 8 * q);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              *p[j] = make_uint4(w0[4 * j], w0[4 * j + 1], w0[4 * j + 2], w0[4 * j + 3]);
+              p[j][AREA / 16] = make_uint4(w1[4 * j], w1[4 * j + 1], w1[4 * j + 2], w1[4 * j + 3]);
+            }
           }
-          store32(P.out[0] + line + col, dg, left);
-          store32(P.out[1] + line + col, v, left);
-          store32(P.out[2] + line + col, h, left);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) { g[i] = g2[i]; u[i] = u2[i]; }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_3d(area, &maps.e[2], col, row, 0);
+            bulk_commit();
+            tma_store_3d(area + AREA, &maps.e[3], col, row, 0);
+            bulk_commit();
+            bulk_wait_read1();                                  // (the first of the two has read its area)
+          }
+          __syncwarp();
+          stage32(area, lane, 0, hid);
+          stage32(area, lane, 1, hid + 16);
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) { tma_store_3d(area, &maps.e[4], col, row, 0); bulk_commit(); }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_shared(&sh.acc_empty[ab], 0));
     }
+    if (lane == 0) bulk_wait0();
   }
 
   tc_fence_before();
@@ -287,34 +420,336 @@ ffn_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constan
   }
 }
 
-// [rows][cols] bf16 with a box of box_rows rows x 64 columns, 128-byte swizzle.
-bool matrix_map(CUtensorMap* map, const void* base, long long rows, long long cols, int box_rows) {
-  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 1};
-  cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)rows * cols * 2};
-  cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
-  return ff_encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B,
-                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+// The parts of K added up, in their order, and rounded: out[m] = sum over s of sums[m][s].  A thread has eight values.
+__global__ void __launch_bounds__(256) ffn_join_kernel(const float* sums, int split, long long values, __nv_bfloat16* out0, __nv_bfloat16* out1) {
+  ff_pdl_wait();
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= values) return;
+  const float* p = sums + (long long)blockIdx.y * split * values + i;
+  float v[8] = {};
+#pragma unroll 4
+  for (int s = 0; s < split; ++s) {
+    const float4 a = *(const float4*)(p + s * values), b = *(const float4*)(p + s * values + 4);
+    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+  }
+  uint32_t w[4];
+  pack(v, w);
+  *(uint4*)((blockIdx.y ? out1 : out0) + i) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The matrix of an operand: [rows][cols] as it lies in memory.  K-major: a row is one M or N index; MN-major: one K index.
-struct Operand { const void* p; long long rows, cols; };
+// ---- few tokens -----------------------------------------------------------------------------------------------------------
+// With few tokens the products are as long as their weights take to arrive, and tiles of 256 tokens leave most of the device
+// idle (one token, dim 2048: eight tiles for the product with Wd).  Here the weights are the A operand, read as they lie
+// (MN-major): 128 features are the rows of the accumulator, and the tokens (16 .. 128 of them) its columns.  K is split over a
+// cluster of up to eight CTAs, so that about every SM streams its own part of the weights; the partial sums meet in shared memory,
+// where every CTA of the cluster adds up a part of the tile, in the order of the ranks: the same bits in every call.
+//   GATE   128 features of Wg and the same of Wu beside each other, two accumulators
+//   STORE  (the product with Wd) starts while the launch before it, of the same call, still runs: that one writes nothing of
+//          Wd, and had itself waited for everything before it; so the first stages of weights are requested ahead of the wait
+constexpr size_t FEW_SMEM = 193 * 1024;
+constexpr int FEW_THREADS = 64 + 32 * EPI_WARPS;
+struct FewParams {
+  int tokens, cols, kchunks;       // tokens; features in all; K chunks
+  int nt, stages, stage_bytes;     // tokens of a tile; ring
+  int act;
+  __nv_bfloat16* out[3];           // STORE: out;  GATE: H, G or NULL, U
+  int* status;
+};
+struct FewShared {
+  uint64_t full[8], empty[8], done;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add4(float (&v)[4], const float4& a) { v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; }
+__device__ __forceinline__ void store4(__nv_bfloat16* dst, const float (&v)[4]) {
+  *(uint2*)dst = make_uint2(bf16_pair(__float_as_uint(v[0]), __float_as_uint(v[1])), bf16_pair(__float_as_uint(v[2]), __float_as_uint(v[3])));
+}
 
+template <int EPI>
+__global__ void __launch_bounds__(FEW_THREADS, 1)
+ffn_few_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1,
+               const __grid_constant__ CUtensorMap map_x, const FewParams P) {
+  constexpr int MATS = EPI == GATE ? 2 : 1;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  __shared__ FewShared sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_rank(), split = (int)cluster_size();
+  const int f0 = (int)(blockIdx.x / split) * 128, t0 = (int)blockIdx.y * P.nt;
+  const int k_begin = (int)((long long)P.kchunks * rank / split), k_end = (int)((long long)P.kchunks * (rank + 1) / split);
+  const uint32_t columns = MATS * P.nt < 32 ? 32 : MATS * P.nt;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < P.stages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+    mbar_init(&sh.done, 1);
+    sh.abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) { tmem_alloc(&sh.tmem_base, columns); tmem_relinquish(); }
+  if (EPI == GATE) ff_pdl_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (EPI == STORE && warp != 0) ff_pdl_wait();                 // (warp 0: below)
+  const uint32_t tm = sh.tmem_base;
+  volatile int* abort_flag = &sh.abort_flag;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      auto weights = [&](int kc, int slot) {
+        uint8_t* dst = smem + slot * P.stage_bytes;
+        mbar_arrive_expect_tx(&sh.full[slot], P.stage_bytes);
+#pragma unroll
+        for (int m = 0; m < MATS; ++m)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            tma_load_3d(dst + (2 * m + c) * PIECE, m ? &map_w1 : &map_w0, &sh.full[slot], f0 + 64 * c, kc * TK, 0);
+      };
+      int ahead = 0;
+      if (EPI == STORE) {
+        for (; ahead < P.stages && k_begin + ahead < k_end; ++ahead) weights(k_begin + ahead, ahead);
+        ff_pdl_wait();
+      }
+      bool ok = true;
+      int slot = 0;
+      unsigned phase = 1;                                       // (a slot's first use waits for nothing)
+      for (int kc = k_begin, n = 0; kc < k_end && ok; ++kc, ++n) {
+        if (n >= P.stages) ok = mbar_wait(&sh.empty[slot], phase, abort_flag);
+        if (!ok) break;
+        if (n >= ahead) weights(kc, slot);
+        tma_load_3d(smem + slot * P.stage_bytes + 2 * MATS * PIECE, &map_x, &sh.full[slot], kc * TK, t0, 0);
+        if (++slot == P.stages) { slot = 0; phase ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    const uint32_t idesc = idesc_bf16_f32(128, P.nt, true, false);
+    const uint64_t a0 = smem_desc_sw128(smem_u32(smem), PIECE, 1024), b0 = smem_desc_sw128(smem_u32(smem) + 2 * MATS * PIECE, 16, 1024);
+    bool ok = true;
+    int slot = 0;
+    unsigned phase = 0;
+    for (int kc = k_begin; kc < k_end && ok; ++kc) {
+      ok = mbar_wait_warp(&sh.full[slot], phase, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      const uint64_t at = (uint64_t)(slot * (P.stage_bytes >> 4));
+#pragma unroll
+      for (int ks = 0; ks < TK / 16; ++ks)
+#pragma unroll
+        for (int m = 0; m < MATS; ++m)
+          umma_ss(tm + m * P.nt, a0 + at + (uint64_t)(m * (2 * PIECE >> 4) + ks * 128), b0 + at + (uint64_t)(ks * 2), idesc, ks > 0 ? 1u : (kc > k_begin ? 1u : 0u));
+      umma_commit(&sh.empty[slot]);
+      if (++slot == P.stages) { slot = 0; phase ^= 1; }
+    }
+    umma_commit(&sh.done);
+  }
+
+  // partial sums [MATS][token][128 features] over the ring, whose last stage the tensor core has read
+  float* part = (float*)smem;
+  const int live = min(P.nt, P.tokens - t0);
+  if (warp >= 2) {
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(&sh.done, 0, abort_flag));
+    if (ok) {
+      tc_fence_after();
+#pragma unroll 1
+      for (int m = 0; m < MATS; ++m)
+#pragma unroll 1
+        for (int c = 16 * half; c < live; c += 32) {
+          uint32_t r[16];
+          tmem_ld16(tm + ((uint32_t)(quarter * 32) << 16) + m * P.nt + c, r);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) part[(m * P.nt + c + i) * 128 + quarter * 32 + lane] = __uint_as_float(r[i]);
+        }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  if (!sh.abort_flag) {
+    // a warp's share: 128 features of one token, four a lane; the CTAs of the cluster take the tokens in turns
+    for (int i = (warp * split + rank) * 32 + lane; i < live * 32; i += split * FEW_THREADS) {
+      const int token = i >> 5, fg = (i & 31) * 4;
+      if (f0 + fg >= P.cols) continue;
+      float g[4] = {}, u[4] = {};
+      for (int r0 = 0; r0 < split; r0 += 4) {                   // four CTAs' values are on their way together
+        float4 a[4][MATS];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (r0 + r < split) {
+            const uint32_t at = map_shared(part + token * 128 + fg, r0 + r);
+#pragma unroll
+            for (int m = 0; m < MATS; ++m) a[r][m] = load_cluster(at + (uint32_t)(m * P.nt * 512));
+          }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (r0 + r < split) {
+            add4(g, a[r][0]);
+            if constexpr (EPI == GATE) add4(u, a[r][1]);
+          }
+      }
+      const size_t to = (size_t)(t0 + token) * P.cols + f0 + fg;
+      if (EPI == GATE) {
+        if (P.out[1]) { store4(P.out[1] + to, g); store4(P.out[2] + to, u); }
+        with_activation(P.act, [&](auto act) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) g[j] = activation<act.value, false>(g[j], nullptr) * u[j];
+        });
+      }
+      store4(P.out[0] + to, g);
+    }
+  } else {
+    if (threadIdx.x == 0) atomicExch(P.status, FF_ERR_TIMEOUT | 0xb00);   // low byte: status, next byte: which kernel
+    const long long start = clock64();
+    while (clock64() - start < 2000000) { }
+  }
+  __syncthreads();
+  cluster_sync();                                               // no CTA leaves while another reads its sums
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tm, columns);
+  }
+}
+
+// [rows][cols] bf16 with a box of box_rows rows x 64 columns, 128-byte swizzle.
+bool matrix_map(const ff_ffn* h, CUtensorMap* map, const void* base, long long rows, long long cols, int box_rows) {
+  // (of the two extents one is dim or hidden: those two, the other extent and the box name the map)
+  const int code = (int)(cols == h->cfg.dim ? 0 : 1) * 1024 + box_rows;
+  return h->maps.get(map, base, code, (int)rows, [&] {
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, 1};
+    cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)rows * cols * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+    return ff_encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+  });
+}
+
+// fp32 sums [parts][rows][cols] with a box of 32 x 32.
+bool sums_map(const ff_ffn*, CUtensorMap* map, const void* base, long long rows, long long cols, int parts) {
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+  cuuint64_t strides[2] = {(cuuint64_t)cols * 4, (cuuint64_t)rows * cols * 4};
+  cuuint32_t box[3] = {32, 32, 1};
+  return ff_encode_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+}
+
+// A matrix [rows][cols] as it lies in memory.  An operand's rows are one M or N index each (K-major) or one K index (MN-major).
+struct Matrix { const void* p; long long rows, cols; };
+
+// Parts of K for a product with `tiles` tiles of `k` chunks each and an output of `values` values: the number whose estimated time is
+// least.  A pair takes 0.28 us for a chunk; with several parts, their sums are written and read in fp32 (4 TB/s) by a second
+// launch (2.5 us), and at most two waves of pairs have one each, which bounds the workspace at 148 tiles.
+int split_of(long long tiles, int k, double values, double* us = nullptr) {
+  constexpr int pairs = FF_B200_SMS / 2;
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= 16 && s <= k && (s == 1 || tiles * s <= 2 * pairs); ++s) {
+    const double t = 0.28 * (double)((tiles * s + pairs - 1) / pairs) * ((k + s - 1) / s) + (s > 1 ? 2.5 + values * 4 * 2 * s / 4e6 : 0);
+    if (s == 1 || t < least) { best = s; least = t; }
+  }
+  if (us) *us = least;
+  return best;
+}
+struct Product { long long rows; int cols, mats, k; };          // extents of an output, matrices, K chunks in all
+int split_of(const Product& p, double* us = nullptr) {
+  return split_of(((p.rows + TM - 1) / TM) * ((p.cols + TN - 1) / TN) * p.mats, p.k, (double)p.rows * p.cols * p.mats, us);
+}
+size_t sums_bytes(const Product& p) {
+  const int s = split_of(p);
+  return s > 1 ? (size_t)p.rows * p.cols * p.mats * s * 4 : 0;
+}
+
+// `e`: the matrices of the epilogue in the order of GemmMaps; all have the extents of the outputs.
 template <bool A_MN, bool B_MN, int EPI>
-cudaError_t gemm(const ff_ffn* h, const Operand (&a)[2], const Operand (&b)[2], GemmParams P, cudaStream_t st) {
-  CUtensorMap m[4];
+cudaError_t gemm(const ff_ffn* h, const Matrix (&a)[2], const Matrix (&b)[2], std::initializer_list<const void*> e, GemmParams P, cudaStream_t st) {
+  GemmMaps m;
   for (int i = 0; i < 2; ++i)
-    if (!matrix_map(&m[i], a[i].p, a[i].rows, a[i].cols, A_MN ? 64 : 128) || !matrix_map(&m[2 + i], b[i].p, b[i].rows, b[i].cols, B_MN ? 64 : 128))
+    if (!matrix_map(h, &m.a[i], a[i].p, a[i].rows, a[i].cols, A_MN ? 64 : 128) || !matrix_map(h, &m.b[i], b[i].p, b[i].rows, b[i].cols, B_MN ? 64 : 128))
       return cudaErrorInvalidValue;
+  int n = 0;
+  for (const void* p : e)
+    if (!(EPI == PARTIAL ? sums_map(h, &m.e[n++], p, P.rows, P.cols, P.mats * P.split) : matrix_map(h, &m.e[n++], p, P.rows, P.cols, 32)))
+      return cudaErrorInvalidValue;
+  for (; n < 5; ++n) m.e[n] = m.e[0];
   const int width = EPI == GATE ? 128 : TN;
   P.m_tiles = (int)((P.rows + TM - 1) / TM);
   P.n_tiles = (P.cols + width - 1) / width;
   P.act = h->cfg.activation;
   P.status = h->status;
-  const long long tiles = (long long)P.m_tiles * P.n_tiles * P.mats;
+  const int tiles = P.m_tiles * P.n_tiles * P.mats, items = tiles * P.split;
   const int pairs = h->sm_count / 2;
-  return ff_launch(ffn_gemm_kernel<A_MN, B_MN, EPI>, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(THREADS), SMEM, st, m[0], m[1], m[2], m[3], P);
+  return ff_launch(ffn_gemm_kernel<A_MN, B_MN, EPI>, dim3(2 * (unsigned)(items < pairs ? items : pairs)), dim3(THREADS), smem_bytes(EPI), st, m, P);
 }
-inline int chunks(long long k) { return (int)((k + TK - 1) / TK); }
+// A product without more to do: out[i] = A B[i], or (two sources) out[0] = A[0] B[0] + A[1] B[1].
+template <bool A_MN, bool B_MN>
+cudaError_t product(const ff_ffn* h, const Matrix (&a)[2], const Matrix (&b)[2], const Product& p, int sources, void* out0, void* out1, void* sums,
+                    cudaStream_t st) {
+  GemmParams P{};
+  P.rows = p.rows; P.cols = p.cols; P.mats = p.mats;
+  P.sources = sources; P.kchunks = p.k / sources;
+  P.split = split_of(p);
+  if (P.split == 1) return p.mats == 2 ? gemm<A_MN, B_MN, STORE>(h, a, b, {out0, out1}, P, st) : gemm<A_MN, B_MN, STORE>(h, a, b, {out0}, P, st);
+  const cudaError_t e = gemm<A_MN, B_MN, PARTIAL>(h, a, b, {sums}, P, st);
+  if (e != cudaSuccess) return e;
+  const long long values = p.rows * p.cols;
+  return ff_launch(ffn_join_kernel, dim3((unsigned)((values / 8 + 255) / 256), (unsigned)p.mats), dim3(256), 0, st, (const float*)sums, P.split, values,
+                   (__nv_bfloat16*)out0, (__nv_bfloat16*)out1);
+}
+
+// How the few-token kernel would run a product (tokens of a tile, CTAs of a cluster), and the estimated time of that: a chunk of
+// K takes a CTA 0.35 us (0.5 with two matrices: more to load), the exchange of the partial sums 0.02 us for a token and matrix
+// (what a CTA reads from others' shared memory, at 25 B/ns), start and end 1 us.  Clusters of three and more do not fill all SMs.
+struct FewShape { int nt, split, f_tiles, t_tiles; double us; };
+int few_stages(int nt, int mats) {
+  // Up to 64 tokens the rings leave room for a CTA of either product on an SM, so that the second one's weights are on their way
+  // while the first one ends.
+  return nt <= 64 ? (mats == 2 ? 3 : nt <= 16 ? 6 : nt <= 32 ? 5 : 4) : 192 * 1024 / (mats * OPERAND + nt * 128);
+}
+size_t few_smem(int nt, int mats) {
+  const size_t ring = (size_t)few_stages(nt, mats) * (mats * OPERAND + nt * 128), sums = (size_t)mats * nt * 512;
+  return (ring > sums ? ring : sums) + 1024;
+}
+FewShape few_shape(const ff_ffn* h, long long tokens, int features, int kchunks, int mats) {
+  FewShape s;
+  s.nt = tokens <= 16 ? 16 : tokens <= 32 ? 32 : tokens <= 64 ? 64 : 128;
+  s.f_tiles = (features + 127) / 128;
+  s.t_tiles = (int)((tokens + s.nt - 1) / s.nt);
+  const long long tiles = (long long)s.f_tiles * s.t_tiles;
+  s.us = 0;
+  for (int split = 1; split <= 8 && split <= kchunks; ++split) {
+    const int room = h->room[mats - 1][s.nt == 128][split];
+    if (room < split) continue;
+    const double us = 1 + (double)((tiles * split + room - 1) / room) * ((kchunks + split - 1) / split) * (mats == 2 ? 0.5 : 0.35) +
+                      (split > 1 ? 0.02 * mats * (double)(tokens < s.nt ? tokens : s.nt) : 0);
+    if (split == 1 || us < s.us) { s.split = split; s.us = us; }
+  }
+  return s;
+}
+
+template <int EPI>
+cudaError_t few(const ff_ffn* h, const FewShape& s, const void* w0, const void* w1, const void* x, long long tokens, int features, int k,
+                void* const (&out)[3], cudaStream_t st) {
+  CUtensorMap m[3];
+  if (!matrix_map(h, &m[0], w0, k, features, 64) || !matrix_map(h, &m[1], w1, k, features, 64) || !matrix_map(h, &m[2], x, tokens, k, s.nt))
+    return cudaErrorInvalidValue;
+  FewParams P{};
+  P.tokens = (int)tokens; P.cols = features; P.kchunks = chunks(k);
+  P.nt = s.nt;
+  const int mats = EPI == GATE ? 2 : 1;
+  P.stage_bytes = mats * OPERAND + s.nt * 128;
+  P.stages = few_stages(s.nt, mats);
+  P.act = h->cfg.activation;
+  for (int i = 0; i < 3; ++i) P.out[i] = (__nv_bfloat16*)out[i];
+  P.status = h->status;
+  return ff_launch_cluster(ffn_few_kernel<EPI>, dim3((unsigned)(s.f_tiles * s.split), (unsigned)s.t_tiles), dim3(FEW_THREADS), s.split,
+                           few_smem(s.nt, mats), st, m[0], m[1], m[2], P);
+}
+
 
 ff_status_t fail(ff_ffn* h, ff_status_t code, const char* msg) {
   if (h) snprintf(h->err, sizeof h->err, "%s", msg);
@@ -339,7 +774,8 @@ bool misaligned(std::initializer_list<const void*> ps) {
 }
 ff_status_t check_call(ff_ffn* h, int64_t tokens, void* ws, size_t ws_bytes, int training) {
   if (tokens < 0) return fail(h, FF_ERR_INVALID_ARG, "tokens must not be negative");
-  if (tokens > 0x7fffff00) return fail(h, FF_ERR_UNSUPPORTED, "tokens must be below 2^31 - 256");
+  const int64_t widest = h->cfg.dim > h->cfg.hidden ? h->cfg.dim : h->cfg.hidden;
+  if (tokens > 0x7fffff00 || tokens * widest > (1ll << 38)) return fail(h, FF_ERR_UNSUPPORTED, "tokens must be below 2^31 - 256, and tokens * hidden at most 2^38");
   int device = -1;
   if (cudaGetDevice(&device) != cudaSuccess || device != h->device) return fail(h, FF_ERR_INVALID_ARG, "the handle belongs to another device than the current one");
   size_t need = 0;
@@ -348,6 +784,11 @@ ff_status_t check_call(ff_ffn* h, int64_t tokens, void* ws, size_t ws_bytes, int
   if (need && (((uintptr_t)ws) & 255)) return fail(h, FF_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
   return FF_OK;
 }
+// The products of a call: out;  dX;  dWg and dWu;  dWd
+Product down_product(const ff_ffn_config_t& c, int64_t tokens) { return {tokens, c.dim, 1, chunks(c.hidden)}; }
+Product dx_product(const ff_ffn_config_t& c, int64_t tokens) { return {tokens, c.dim, 1, 2 * chunks(c.hidden)}; }
+Product dw_product(const ff_ffn_config_t& c, int64_t tokens) { return {c.dim, c.hidden, 2, chunks(tokens)}; }
+Product dwd_product(const ff_ffn_config_t& c, int64_t tokens) { return {c.hidden, c.dim, 1, chunks(tokens)}; }
 size_t hidden_bytes(const ff_ffn_config_t& c, int64_t tokens) { return ((size_t)tokens * c.hidden * 2 + 255) / 256 * 256; }
 
 }  // namespace
@@ -365,7 +806,15 @@ extern "C" ff_status_t ff_ffn_workspace_bytes(const ff_ffn_config_t* c, int64_t 
   const ff_status_t s = ff_ffn_validate(c);
   if (s != FF_OK) return s;
   if (!bytes || tokens < 0) return fail(nullptr, FF_ERR_INVALID_ARG, "bytes is NULL or tokens negative");
-  *bytes = (training ? 3 : 1) * hidden_bytes(*c, tokens);      // H;  backward: dG, dU, H
+  // H;  backward: dG, dU, H;  behind them the sums of the product that needs most (one at a time)
+  *bytes = (training ? 3 : 1) * hidden_bytes(*c, tokens);
+  if (tokens > 0) {
+    size_t sums = 0;
+    auto need = [&](const Product& p) { const size_t b = sums_bytes(p); if (b > sums) sums = b; };
+    if (training) { need(dx_product(*c, tokens)); need(dw_product(*c, tokens)); need(dwd_product(*c, tokens)); }
+    else need(down_product(*c, tokens));
+    *bytes += (sums + 255) / 256 * 256;
+  }
   return FF_OK;
 }
 
@@ -379,11 +828,25 @@ extern "C" ff_status_t ff_ffn_create(const ff_ffn_config_t* cfg, ff_ffn_t** out)
   h->cfg = *cfg;
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device);
-  const void* kernels[] = {(const void*)ffn_gemm_kernel<false, true, GATE>, (const void*)ffn_gemm_kernel<false, true, STORE>,
-                           (const void*)ffn_gemm_kernel<false, false, DGATE>, (const void*)ffn_gemm_kernel<false, false, STORE>,
-                           (const void*)ffn_gemm_kernel<true, true, STORE>};
-  for (const void* k : kernels)
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM);
+  const struct { const void* kernel; size_t smem; } kernels[] = {
+      {(const void*)ffn_gemm_kernel<false, true, GATE>, smem_bytes(GATE)}, {(const void*)ffn_gemm_kernel<false, true, STORE>, smem_bytes(STORE)},
+      {(const void*)ffn_gemm_kernel<false, false, DGATE>, smem_bytes(DGATE)}, {(const void*)ffn_gemm_kernel<false, false, STORE>, smem_bytes(STORE)},
+      {(const void*)ffn_gemm_kernel<true, true, STORE>, smem_bytes(STORE)}, {(const void*)ffn_gemm_kernel<false, true, PARTIAL>, smem_bytes(PARTIAL)},
+      {(const void*)ffn_gemm_kernel<false, false, PARTIAL>, smem_bytes(PARTIAL)}, {(const void*)ffn_gemm_kernel<true, true, PARTIAL>, smem_bytes(PARTIAL)},
+      {(const void*)ffn_few_kernel<GATE>, FEW_SMEM},
+      {(const void*)ffn_few_kernel<STORE>, FEW_SMEM}};
+  for (const auto& k : kernels)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.smem);
+  for (int mats = 1; mats <= 2; ++mats)
+    for (int wide = 0; wide < 2; ++wide)
+      for (int split = 1; split <= 8 && e == cudaSuccess; ++split) {
+        int clusters = 0;
+        const size_t smem = few_smem(wide ? 128 : 64, mats);
+        e = mats == 2 ? ff_max_clusters(&clusters, ffn_few_kernel<GATE>, dim3(FEW_THREADS), split, smem)
+                      : ff_max_clusters(&clusters, ffn_few_kernel<STORE>, dim3(FEW_THREADS), split, smem);
+        // (asked for kernels that use tensor memory, the runtime counts one block an SM; two run where shared memory has room for them)
+        h->room[mats - 1][wide][split] = clusters * split * (int)(233472 / (smem + 1024));
+      }
   if (e == cudaSuccess) e = cudaMalloc((void**)&h->status, 256);
   if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);
   if (e != cudaSuccess) {
@@ -428,15 +891,26 @@ extern "C" ff_status_t ff_ffn_forward(ff_ffn_t* h, int64_t tokens, const void* X
   if (misaligned({X, Wg, Wu, Wd, gate, up, out})) return fail(h, FF_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
   const int D = h->cfg.dim, F = h->cfg.hidden;
   cudaStream_t st = (cudaStream_t)stream;
-  GemmParams P{};
-  P.rows = tokens; P.mats = 1; P.sources = 1;
-  P.cols = F; P.kchunks = chunks(D);
-  P.out[0] = (__nv_bfloat16*)ws; P.out[1] = (__nv_bfloat16*)gate; P.out[2] = (__nv_bfloat16*)up;
-  const Operand x{X, tokens, D}, hid{ws, tokens, F}, wd{Wd, F, D};
-  FFN_CUDA(h, (gemm<false, true, GATE>(h, {x, x}, {Operand{Wg, D, F}, Operand{Wu, D, F}}, P, st)));
-  P.cols = D; P.kchunks = chunks(F);
-  P.out[0] = (__nv_bfloat16*)out;
-  FFN_CUDA(h, (gemm<false, true, STORE>(h, {hid, hid}, {wd, wd}, P, st)));
+  const Matrix x{X, tokens, D}, hid{ws, tokens, F}, wg{Wg, D, F}, wu{Wu, D, F}, wd{Wd, F, D};
+  // Either product runs on the kernel whose estimate is lower.  Measured, dim 2048, hidden 5632, both products on tiles of 256
+  // tokens / on the few-token kernel, us: 1 token 34.0 / 21.1, 64 tokens 31.6 / 25.2, 128 32.7 / 35.9, 512 46.5 / 64.3; dim 1024, hidden
+  // 2816, product with Wd: 400 tokens 25.9 / 21.5, 768 27.8 / 32.4.
+  const FewShape up_few = few_shape(h, tokens, F, chunks(D), 2), down_few = few_shape(h, tokens, D, chunks(F), 1);
+  const Product down = down_product(h->cfg, tokens);
+  const long long up_tiles = ((tokens + TM - 1) / TM) * ((F + 127) / 128);
+  double down_us;
+  split_of(down, &down_us);
+  const double up_us = 0.28 * chunks(D) * (double)((up_tiles + FF_B200_SMS / 2 - 1) / (FF_B200_SMS / 2));
+  if (up_few.us < up_us) {
+    FFN_CUDA(h, few<GATE>(h, up_few, Wg, Wu, X, tokens, F, D, {ws, gate, up}, st));
+  } else {
+    GemmParams P{};
+    P.rows = tokens; P.cols = F; P.mats = P.sources = P.split = 1;
+    P.kchunks = chunks(D); P.keep = gate != nullptr;
+    FFN_CUDA(h, (gemm<false, true, GATE>(h, {x, x}, {wg, wu}, {ws, gate ? gate : ws, up ? up : ws}, P, st)));
+  }
+  if (down_few.us < down_us) FFN_CUDA(h, few<STORE>(h, down_few, Wd, Wd, ws, tokens, D, F, {out, nullptr, nullptr}, st));
+  else FFN_CUDA(h, (product<false, true>(h, {hid, hid}, {wd, wd}, down, 1, out, nullptr, (char*)ws + hidden_bytes(h->cfg, tokens), st)));
   return FF_OK;
 }
 
@@ -460,28 +934,15 @@ extern "C" ff_status_t ff_ffn_backward(ff_ffn_t* h, int64_t tokens, const void* 
   if (!dX && !dWg && !dWd) return FF_OK;
   char* base = (char*)ws;
   void *dG = base, *dU = base + hidden_bytes(h->cfg, tokens), *H = base + 2 * hidden_bytes(h->cfg, tokens);
-  const Operand x{X, tokens, D}, g{dout, tokens, D}, wd{Wd, F, D}, dg{dG, tokens, F}, du{dU, tokens, F}, hid{H, tokens, F};
+  const Matrix x{X, tokens, D}, g{dout, tokens, D}, wg{Wg, D, F}, wu{Wu, D, F}, wd{Wd, F, D};
+  const Matrix dg{dG, tokens, F}, du{dU, tokens, F}, hid{H, tokens, F};
   GemmParams P{};
-  P.mats = 1; P.sources = 1;
-  P.rows = tokens; P.cols = F; P.kchunks = chunks(D);
-  P.gate = (const __nv_bfloat16*)gate; P.up = (const __nv_bfloat16*)up;
-  P.out[0] = (__nv_bfloat16*)dG; P.out[1] = (__nv_bfloat16*)dU; P.out[2] = (__nv_bfloat16*)H;
-  FFN_CUDA(h, (gemm<false, false, DGATE>(h, {g, g}, {wd, wd}, P, st)));
-  if (dX) {
-    P.cols = D; P.kchunks = chunks(F); P.sources = 2;
-    P.out[0] = (__nv_bfloat16*)dX;
-    FFN_CUDA(h, (gemm<false, false, STORE>(h, {dg, du}, {Operand{Wg, D, F}, Operand{Wu, D, F}}, P, st)));
-  }
-  P.sources = 1; P.kchunks = chunks(tokens);
-  if (dWg) {
-    P.rows = D; P.cols = F; P.mats = 2;
-    P.out[0] = (__nv_bfloat16*)dWg; P.out[1] = (__nv_bfloat16*)dWu;
-    FFN_CUDA(h, (gemm<true, true, STORE>(h, {x, x}, {dg, du}, P, st)));
-  }
-  if (dWd) {
-    P.rows = F; P.cols = D; P.mats = 1;
-    P.out[0] = (__nv_bfloat16*)dWd;
-    FFN_CUDA(h, (gemm<true, true, STORE>(h, {hid, hid}, {g, g}, P, st)));
-  }
+  P.rows = tokens; P.cols = F; P.mats = P.sources = P.split = 1;
+  P.kchunks = chunks(D);
+  FFN_CUDA(h, (gemm<false, false, DGATE>(h, {g, g}, {wd, wd}, {gate, up, dG, dU, H}, P, st)));
+  void* sums = base + 3 * hidden_bytes(h->cfg, tokens);
+  if (dX) FFN_CUDA(h, (product<false, false>(h, {dg, du}, {wg, wu}, dx_product(h->cfg, tokens), 2, dX, nullptr, sums, st)));
+  if (dWg) FFN_CUDA(h, (product<true, true>(h, {x, x}, {dg, du}, dw_product(h->cfg, tokens), 1, dWg, dWu, sums, st)));
+  if (dWd) FFN_CUDA(h, (product<true, true>(h, {hid, hid}, {g, g}, dwd_product(h->cfg, tokens), 1, dWd, nullptr, sums, st)));
   return FF_OK;
 }
