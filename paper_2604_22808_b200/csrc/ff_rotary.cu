@@ -54,7 +54,8 @@ struct HeadsParams {
   long long pos_stride;            // elements between the samples' positions
   int rows;                        // batch * tokens
   FFFastDiv tokens, gw, gh;        // tokens per sample; the grid's W and H
-  int heads[2], chunk, nchunk0;    // heads of q and k, heads a block walks over, blocks in y that belong to q
+  int heads[2], groups;            // heads of q and k; groups of tokens
+  int chunk, nblocks0;             // forward: heads a block walks over, blocks in y that belong to q;  backward: blocks that belong to q
   int d, rot, np, lanes_log2;      // channels, turned channels, chunk pairs of a row, log2 of the lanes of a row
   int axis_end0, axis_end1, axes;
   int inverse;
@@ -69,86 +70,147 @@ template <> struct Word<4> { using type = unsigned; };
 template <> struct Word<2> { using type = unsigned short; };
 template <class T, int CH> using Chunk = typename Word<sizeof(T) * CH>::type;
 
+// Two fp32 values in one 64-bit register: the arithmetic below takes an instruction for both.
+using F2 = unsigned long long;
+__device__ __forceinline__ F2 two(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float low(F2 v) { return __uint_as_float((unsigned)v); }
+__device__ __forceinline__ float high(F2 v) { return __uint_as_float((unsigned)(v >> 32)); }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// A chunk as pairs of neighbouring channels (CH = 1: one value and a zero).
+__host__ __device__ constexpr int pairs_of(int ch) { return (ch + 1) / 2; }
 template <class T, int CH>
-__device__ __forceinline__ void unpack(const Chunk<T, CH>& c, float (&v)[CH]) {
+__device__ __forceinline__ void unpack(const Chunk<T, CH>& c, F2 (&v)[pairs_of(CH)]) {
   if constexpr (sizeof(T) == 4) {
     const float* f = reinterpret_cast<const float*>(&c);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) v[i] = f[i];
+    for (int i = 0; i < pairs_of(CH); ++i) v[i] = two(f[2 * i], CH > 1 ? f[2 * i + 1] : 0.f);
+  } else if constexpr (CH == 1) {
+    v[0] = two(__uint_as_float((unsigned)c << 16), 0.f);
   } else {
-    const unsigned short* h = reinterpret_cast<const unsigned short*>(&c);
+    const unsigned* h = reinterpret_cast<const unsigned*>(&c);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) v[i] = __uint_as_float((unsigned)h[i] << 16);
+    for (int i = 0; i < CH / 2; ++i) v[i] = two(__uint_as_float(h[i] << 16), __uint_as_float(h[i] & 0xffff0000u));
   }
 }
 // (the one rounding of the operators with bf16 tensors)
 template <class T, int CH>
-__device__ __forceinline__ Chunk<T, CH> pack(const float (&v)[CH]) {
+__device__ __forceinline__ Chunk<T, CH> pack(const F2 (&v)[pairs_of(CH)]) {
   Chunk<T, CH> c;
-  T* t = reinterpret_cast<T*>(&c);
+  if constexpr (sizeof(T) == 4) {
+    float* f = reinterpret_cast<float*>(&c);
 #pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    if constexpr (sizeof(T) == 4) t[i] = v[i];
-    else t[i] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < CH; ++i) f[i] = i & 1 ? high(v[i / 2]) : low(v[i / 2]);
+  } else if constexpr (CH == 1) {
+    const __nv_bfloat16 h = __float2bfloat16_rn(low(v[0]));
+    c = *reinterpret_cast<const unsigned short*>(&h);
+  } else {
+    unsigned* h = reinterpret_cast<unsigned*>(&c);
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+      const __nv_bfloat162 w = __floats2bfloat162_rn(low(v[i]), high(v[i]));
+      h[i] = *reinterpret_cast<const unsigned*>(&w);
+    }
   }
   return c;
 }
 
-// The pairs of two chunks turned by (c, s).  Interleaved: the first half of c, s belongs to `a`.
+// What turns two chunks a, b of a row, with the norm's weights in it (NORM).  Half layout: a' = a p + b q, b' = a r + b t;  interleaved:
+// every pair (x, y) of a goes to (x, x) p + (y, y) q, those of b to (x, x) r + (y, y) t.  Chunks that are not turned are multiplied by
+// p (a) and t (b) alone: what stands beside them does not touch them, infinite or not.
+template <int CH> struct Turn { F2 p[pairs_of(CH)], q[pairs_of(CH)], r[pairs_of(CH)], t[pairs_of(CH)]; };
+
 template <int CH, bool INTER>
-__device__ __forceinline__ void turn(float (&a)[CH], float (&b)[CH], const float (&c)[CH], const float (&s)[CH], bool turned_a, bool turned_b) {
+__device__ __forceinline__ void turn(F2 (&a)[pairs_of(CH)], F2 (&b)[pairs_of(CH)], const Turn<CH>& k, bool turned_a, bool turned_b, bool scaled) {
+  constexpr int N = pairs_of(CH);
   if constexpr (INTER) {
+    if (turned_a) {
 #pragma unroll
-    for (int i = 0; i < CH / 2; ++i) {
-      const float a0 = a[2 * i], a1 = a[2 * i + 1], b0 = b[2 * i], b1 = b[2 * i + 1];
-      if (turned_a) { a[2 * i] = a0 * c[i] - a1 * s[i]; a[2 * i + 1] = a0 * s[i] + a1 * c[i]; }
-      if (turned_b) { b[2 * i] = b0 * c[CH / 2 + i] - b1 * s[CH / 2 + i]; b[2 * i + 1] = b0 * s[CH / 2 + i] + b1 * c[CH / 2 + i]; }
+      for (int i = 0; i < N; ++i) a[i] = fma(two(low(a[i]), low(a[i])), k.p[i], mul(two(high(a[i]), high(a[i])), k.q[i]));
+    } else if (scaled) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) a[i] = mul(a[i], k.p[i]);
+    }
+    if (turned_b) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) b[i] = fma(two(low(b[i]), low(b[i])), k.r[i], mul(two(high(b[i]), high(b[i])), k.t[i]));
+    } else if (scaled) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) b[i] = mul(b[i], k.t[i]);
     }
   } else if (turned_a) {            // (both chunks of a half-layout pair are turned or neither is)
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const float x = a[i], y = b[i];
-      a[i] = x * c[i] - y * s[i];
-      b[i] = x * s[i] + y * c[i];
+    for (int i = 0; i < N; ++i) {
+      const F2 x = a[i];
+      a[i] = fma(x, k.p[i], mul(b[i], k.q[i]));
+      b[i] = fma(x, k.r[i], mul(b[i], k.t[i]));
     }
+  } else if (scaled) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) { a[i] = mul(a[i], k.p[i]); b[i] = mul(b[i], k.t[i]); }
   }
 }
 
-// 1 / sqrt(mean of squares + eps) of a row whose values the lanes of a group hold.  Rows whose squares leave fp32 are summed
-// again scaled by 2^-70 (eps is far below their mean).
-template <int CH, int PER>
-__device__ __forceinline__ float row_rms(const float (&a)[PER][CH], const float (&b)[PER][CH], int lanes, float inv_d, float eps) {
-  float ss = 0.f;
+template <int N, int PER>
+__device__ __forceinline__ float dot(const F2 (&x)[PER][N], const F2 (&y)[PER][N], const F2 (&u)[PER][N], const F2 (&v)[PER][N]) {
+  F2 s = 0, t = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i)
 #pragma unroll
-    for (int c = 0; c < CH; ++c) ss += a[i][c] * a[i][c] + b[i][c] * b[i][c];
-  for (int m = 1; m < lanes; m <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+    for (int c = 0; c < N; ++c) { s = fma(x[i][c], y[i][c], s); t = fma(u[i][c], v[i][c], t); }
+  return (low(s) + high(s)) + (low(t) + high(t));
+}
+__device__ __forceinline__ float row_sum(float v, int lanes) {
+  for (int m = 1; m < lanes; m <<= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+  return v;
+}
+// 1 / sqrt(mean of squares + eps) of a row whose values the lanes of a group hold.  Rows whose squares leave fp32 are summed
+// again scaled by 2^-70 (eps is far below their mean).
+template <int N, int PER>
+__device__ __forceinline__ float row_rms(const F2 (&a)[PER][N], const F2 (&b)[PER][N], int lanes, float inv_d, float eps) {
+  const float ss = row_sum(dot<N, PER>(a, a, b, b), lanes);
   const bool big = !(ss < 3.0e38f);
   if (!__any_sync(0xffffffffu, big)) return rsqrtf(ss * inv_d + eps);
   const float down = 8.4703294725430034e-22f;   // 2^-70
-  float sc = 0.f;
+  F2 sa[PER][N], sb[PER][N];
 #pragma unroll
   for (int i = 0; i < PER; ++i)
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const float u = a[i][c] * down, v = b[i][c] * down;
-      sc += u * u + v * v;
-    }
-  for (int m = 1; m < lanes; m <<= 1) sc += __shfl_xor_sync(0xffffffffu, sc, m);
+    for (int c = 0; c < N; ++c) { sa[i][c] = mul(a[i][c], two(down, down)); sb[i][c] = mul(b[i][c], two(down, down)); }
+  const float sc = row_sum(dot<N, PER>(sa, sa, sb, sb), lanes);
   return big ? rsqrtf(sc * inv_d) * down : rsqrtf(ss * inv_d + eps);
 }
 
 template <class T, int CH, int PER, bool INTER, int MODE>
 __global__ void __launch_bounds__(H_THREADS, 2) heads_kernel(const __grid_constant__ HeadsParams P) {
   constexpr int U = MODE == NORM_BACKWARD ? 2 : 4;            // heads whose rows are in flight together
+  constexpr int N = pairs_of(CH);
   using C = Chunk<T, CH>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int lanes = 1 << P.lanes_log2, lig = lane & (lanes - 1);
   const int per_warp = 32 >> P.lanes_log2;                    // tokens of a warp
-  const int t = blockIdx.y >= (unsigned)P.nchunk0;            // 0: q, 1: k
-  const int h0 = ((int)blockIdx.y - (t ? P.nchunk0 : 0)) * P.chunk;
-  const int h1 = min(h0 + P.chunk, P.heads[t]);
+  // A block's work.  Forward: one group of 32 / lanes x 8 tokens, blockIdx.x, and one chunk of heads of q or k, blockIdx.y.  Backward, one
+  // wave of blocks divided between q and k by their heads: a run of equal length of the units (group, head), head by head.
+  const int t = (MODE == NORM_BACKWARD ? blockIdx.x : blockIdx.y) >= (unsigned)P.nblocks0;            // 0: q, 1: k
+  long long unit = 0, end = 1;
+  if (MODE == NORM_BACKWARD) {
+    const long long units = (long long)P.groups * P.heads[t];
+    const int blocks = t ? (int)gridDim.x - P.nblocks0 : P.nblocks0, at = (int)blockIdx.x - (t ? P.nblocks0 : 0);
+    unit = units * at / blocks; end = units * (at + 1) / blocks;
+  }
   const float inv_d = 1.f / (float)P.d;
 
   // the thread's chunks
@@ -170,40 +232,45 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_kernel(const __grid_consta
   }
   ff_pdl_wait();
 
-  float wa[PER][CH], wb[PER][CH];
-  if constexpr (MODE != ROTATE) {
-    const float* w = P.w[t];
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        wa[i][c] = have[i] ? (w ? w[oa[i] + c] : 1.f) : 0.f;
-        wb[i][c] = have[i] ? (w ? w[ob[i] + c] : 1.f) : 0.f;
-      }
-  }
-  float da[PER][CH], db[PER][CH];                             // backward: the thread's share of dw
+  const float* weights = MODE == ROTATE ? nullptr : P.w[t];
+  auto weight = [&](int i, int at, int c) { return weights && have[i] && (CH > 1 || c == 0) ? weights[at + c] : 1.f; };
+  F2 wa[PER][N], wb[PER][N];                                  // backward: the weights
+  F2 da[PER][N], db[PER][N];                                  // backward: the thread's share of dw
   if constexpr (MODE == NORM_BACKWARD) {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
 #pragma unroll
-      for (int c = 0; c < CH; ++c) da[i][c] = db[i][c] = 0.f;
+      for (int c = 0; c < N; ++c) {
+        wa[i][c] = two(weight(i, oa[i], 2 * c), weight(i, oa[i], 2 * c + 1));
+        wb[i][c] = two(weight(i, ob[i], 2 * c), weight(i, ob[i], 2 * c + 1));
+        da[i][c] = db[i][c] = 0;
+      }
   }
 
-  const long long step = (long long)gridDim.x * H_WARPS * per_warp;
-  for (long long r0 = ((long long)blockIdx.x * H_WARPS + warp) * per_warp; r0 < P.rows; r0 += step) {
-    const long long row = r0 + (lane >> P.lanes_log2);
+  while (unit < end) {
+    int group, h0, h1;
+    if (MODE == NORM_BACKWARD) {
+      group = (int)(unit / P.heads[t]);
+      h0 = (int)(unit - (long long)group * P.heads[t]);
+      h1 = (int)min((long long)P.heads[t], h0 + (end - unit));
+    } else {
+      group = blockIdx.x;
+      h0 = ((int)blockIdx.y - (t ? P.nblocks0 : 0)) * P.chunk;
+      h1 = min(h0 + P.chunk, P.heads[t]);
+    }
+    unit += h1 - h0;
+    const long long row = ((long long)group * H_WARPS + warp) * per_warp + (lane >> P.lanes_log2);
     const bool live = row < P.rows;
-    const unsigned ru = live ? (unsigned)row : 0u;
+    const unsigned ru = live ? (unsigned)row : (unsigned)(P.rows - 1);    // (lanes behind the last row read it once more and write nothing)
     const unsigned b = ff_div(ru, P.tokens), n = ru - b * P.tokens.d;
-    // angles of the token
-    float cs[PER][CH], sn[PER][CH];
+    Turn<CH> k[PER];
     {
       int pos[3];
       if (P.positions) {
         const int* at = P.positions + b * P.pos_stride + (long long)n * P.axes;
-        pos[0] = live ? at[0] : 0;
-        pos[1] = live && P.axes == 3 ? at[1] : 0;
-        pos[2] = live && P.axes == 3 ? at[2] : 0;
+        pos[0] = at[0];
+        pos[1] = P.axes == 3 ? at[1] : 0;
+        pos[2] = P.axes == 3 ? at[2] : 0;
       } else if (P.axes == 3) {
         const unsigned line = ff_div(n, P.gw);
         pos[2] = (int)(n - line * P.gw.d);
@@ -212,89 +279,109 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_kernel(const __grid_consta
       } else {
         pos[0] = (int)n; pos[1] = pos[2] = 0;
       }
+      auto angle = [&](int p, float& c, float& s) {
+        const int at = p < P.axis_end0 ? pos[0] : (p < P.axis_end1 ? pos[1] : pos[2]);
+        const unsigned long long turns = (unsigned long long)(long long)at * P.phase[p];
+        sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &s, &c);          // 2^-31: half turns
+        c *= P.magnitude;
+        s *= P.inverse ? -P.magnitude : P.magnitude;
+      };
 #pragma unroll
       for (int i = 0; i < PER; ++i)
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const int p = INTER ? (c < CH / 2 ? oa[i] / 2 + c : ob[i] / 2 + c - CH / 2) : oa[i] + c;
-          const bool on = INTER && c >= CH / 2 ? tb[i] : ta[i];
-          cs[i][c] = sn[i][c] = 0.f;
-          if (on) {
-            const int at = p < P.axis_end0 ? pos[0] : (p < P.axis_end1 ? pos[1] : pos[2]);
-            const unsigned long long turns = (unsigned long long)(long long)at * P.phase[p];
-            float s, co;
-            sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &s, &co);     // 2^-31: half turns
-            cs[i][c] = co * P.magnitude;
-            sn[i][c] = (P.inverse ? -s : s) * P.magnitude;
+        for (int c = 0; c < N; ++c) {
+          float w0 = 1.f, w1 = 1.f, w2 = 1.f, w3 = 1.f;
+          if constexpr (MODE == NORM) {
+            w0 = weight(i, oa[i], 2 * c); w1 = weight(i, oa[i], 2 * c + 1);
+            w2 = weight(i, ob[i], 2 * c); w3 = weight(i, ob[i], 2 * c + 1);
+          }
+          k[i].p[c] = two(w0, w1); k[i].q[c] = k[i].r[c] = 0; k[i].t[c] = two(w2, w3);
+          float c0, s0, c1 = 0.f, s1 = 0.f;
+          if constexpr (INTER) {
+            if (ta[i]) {
+              angle(oa[i] / 2 + c, c0, s0);
+              k[i].p[c] = two(c0 * w0, s0 * w0); k[i].q[c] = two(-s0 * w1, c0 * w1);
+            }
+            if (tb[i]) {
+              angle(ob[i] / 2 + c, c1, s1);
+              k[i].r[c] = two(c1 * w2, s1 * w2); k[i].t[c] = two(-s1 * w3, c1 * w3);
+            }
+          } else if (ta[i]) {
+            angle(oa[i] + 2 * c, c0, s0);
+            if (CH > 1) angle(oa[i] + 2 * c + 1, c1, s1);
+            k[i].p[c] = two(c0 * w0, c1 * w1); k[i].q[c] = two(-s0 * w2, -s1 * w3);
+            k[i].r[c] = two(s0 * w0, s1 * w1); k[i].t[c] = two(c0 * w2, c1 * w3);
           }
         }
     }
-    const char* xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st;
-    char* yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st;
-    const char* gp = MODE == NORM_BACKWARD ? P.g[t].p + b * P.g[t].sb + n * P.g[t].st : nullptr;
+    const char* xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st + h0 * P.x[t].sh;
+    char* yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st + h0 * P.y[t].sh;
+    const char* gp = MODE == NORM_BACKWARD ? P.g[t].p + b * P.g[t].sb + n * P.g[t].st + h0 * P.g[t].sh : nullptr;
 #pragma unroll 1
     for (int h = h0; h < h1; h += U) {
       C xa[U][PER], xb[U][PER], ga[U][PER], gb[U][PER];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        const bool on = u == 0 || h + u < h1;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          const bool on = live && have[i] && h + u < h1;
-          const char* src = xp + (long long)(h + u) * P.x[t].sh;
-          xa[u][i] = on ? __ldcs((const C*)(src + oa[i] * sizeof(T))) : C{};
-          xb[u][i] = on ? __ldcs((const C*)(src + ob[i] * sizeof(T))) : C{};
+          xa[u][i] = on && have[i] ? __ldcs((const C*)(xp + oa[i] * sizeof(T))) : C{};
+          xb[u][i] = on && have[i] ? __ldcs((const C*)(xp + ob[i] * sizeof(T))) : C{};
           if constexpr (MODE == NORM_BACKWARD) {
-            const char* gs = gp + (long long)(h + u) * P.g[t].sh;
-            ga[u][i] = on ? __ldcs((const C*)(gs + oa[i] * sizeof(T))) : C{};
-            gb[u][i] = on ? __ldcs((const C*)(gs + ob[i] * sizeof(T))) : C{};
+            ga[u][i] = on && have[i] ? __ldcs((const C*)(gp + oa[i] * sizeof(T))) : C{};
+            gb[u][i] = on && have[i] ? __ldcs((const C*)(gp + ob[i] * sizeof(T))) : C{};
           }
         }
+        xp += P.x[t].sh;
+        if constexpr (MODE == NORM_BACKWARD) gp += P.g[t].sh;
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        float a[PER][CH], c[PER][CH];                         // the two chunks
+        F2 a[PER][N], c[PER][N];                              // the two chunks
 #pragma unroll
         for (int i = 0; i < PER; ++i) { unpack<T, CH>(xa[u][i], a[i]); unpack<T, CH>(xb[u][i], c[i]); }
-        if constexpr (MODE == NORM) {
-          const float r = row_rms<CH, PER>(a, c, lanes, inv_d, P.eps);
-#pragma unroll
-          for (int i = 0; i < PER; ++i)
-#pragma unroll
-            for (int k = 0; k < CH; ++k) { a[i][k] = a[i][k] * r * wa[i][k]; c[i][k] = c[i][k] * r * wb[i][k]; }
-        }
         if constexpr (MODE != NORM_BACKWARD) {
+          if constexpr (MODE == NORM) {
+            const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
 #pragma unroll
-          for (int i = 0; i < PER; ++i) turn<CH, INTER>(a[i], c[i], cs[i], sn[i], ta[i], tb[i]);
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+              for (int j = 0; j < N; ++j) { a[i][j] = mul(a[i][j], two(r, r)); c[i][j] = mul(c[i][j], two(r, r)); }
+          }
+#pragma unroll
+          for (int i = 0; i < PER; ++i) turn<CH, INTER>(a[i], c[i], k[i], ta[i], tb[i], MODE == NORM);
         } else {
-          const float r = row_rms<CH, PER>(a, c, lanes, inv_d, P.eps);
-          float g0[PER][CH], g1[PER][CH], dot = 0.f;
+          const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
+          F2 g0[PER][N], g1[PER][N];
 #pragma unroll
           for (int i = 0; i < PER; ++i) {
             unpack<T, CH>(ga[u][i], g0[i]); unpack<T, CH>(gb[u][i], g1[i]);
-            turn<CH, INTER>(g0[i], g1[i], cs[i], sn[i], ta[i], tb[i]);
+            turn<CH, INTER>(g0[i], g1[i], k[i], ta[i], tb[i], false);
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-              a[i][k] *= r; c[i][k] *= r;                     // n
-              da[i][k] += g0[i][k] * a[i][k]; db[i][k] += g1[i][k] * c[i][k];
-              g0[i][k] *= wa[i][k]; g1[i][k] *= wb[i][k];     // g
-              dot += g0[i][k] * a[i][k] + g1[i][k] * c[i][k];
+            for (int j = 0; j < N; ++j) {
+              a[i][j] = mul(a[i][j], two(r, r)); c[i][j] = mul(c[i][j], two(r, r));              // n
+              if (live) { da[i][j] = fma(g0[i][j], a[i][j], da[i][j]); db[i][j] = fma(g1[i][j], c[i][j], db[i][j]); }
+              g0[i][j] = mul(g0[i][j], wa[i][j]); g1[i][j] = mul(g1[i][j], wb[i][j]);            // g
             }
           }
-          for (int m = 1; m < lanes; m <<= 1) dot += __shfl_xor_sync(0xffffffffu, dot, m);
-          dot *= inv_d;
+          const float m = -row_sum(dot<N, PER>(g0, a, g1, c), lanes) * inv_d;
 #pragma unroll
           for (int i = 0; i < PER; ++i)
 #pragma unroll
-            for (int k = 0; k < CH; ++k) { a[i][k] = r * (g0[i][k] - a[i][k] * dot); c[i][k] = r * (g1[i][k] - c[i][k] * dot); }
+            for (int j = 0; j < N; ++j) {
+              a[i][j] = mul(fma(a[i][j], two(m, m), g0[i][j]), two(r, r));
+              c[i][j] = mul(fma(c[i][j], two(m, m), g1[i][j]), two(r, r));
+            }
         }
-        if (live && h + u < h1) {
-          char* dst = yp + (long long)(h + u) * P.y[t].sh;
+        if (live && (u == 0 || h + u < h1)) {
 #pragma unroll
           for (int i = 0; i < PER; ++i)
             if (have[i]) {
-              *(C*)(dst + oa[i] * sizeof(T)) = pack<T, CH>(a[i]);
-              *(C*)(dst + ob[i] * sizeof(T)) = pack<T, CH>(c[i]);
+              *(C*)(yp + oa[i] * sizeof(T)) = pack<T, CH>(a[i]);
+              *(C*)(yp + ob[i] * sizeof(T)) = pack<T, CH>(c[i]);
             }
         }
+        yp += P.y[t].sh;
       }
     }
   }
@@ -305,19 +392,20 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_kernel(const __grid_consta
 #pragma unroll
     for (int i = 0; i < PER; ++i)
 #pragma unroll
-      for (int k = 0; k < CH; ++k) {
+      for (int c = 0; c < CH; ++c) {
+        float va = c & 1 ? high(da[i][c / 2]) : low(da[i][c / 2]), vb = c & 1 ? high(db[i][c / 2]) : low(db[i][c / 2]);
         for (int m = lanes; m < 32; m <<= 1) {
-          da[i][k] += __shfl_xor_sync(0xffffffffu, da[i][k], m);
-          db[i][k] += __shfl_xor_sync(0xffffffffu, db[i][k], m);
+          va += __shfl_xor_sync(0xffffffffu, va, m);
+          vb += __shfl_xor_sync(0xffffffffu, vb, m);
         }
-        if (lane < lanes && have[i]) { sum[warp][oa[i] + k] = da[i][k]; sum[warp][ob[i] + k] = db[i][k]; }
+        if (lane < lanes && have[i]) { sum[warp][oa[i] + c] = va; sum[warp][ob[i] + c] = vb; }
       }
     __syncthreads();
     for (int c = threadIdx.x; c < P.d; c += H_THREADS) {
       float s = 0.f;
 #pragma unroll
       for (int w = 0; w < H_WARPS; ++w) s += sum[w][c];
-      P.partial[((long long)blockIdx.y * gridDim.x + blockIdx.x) * P.d + c] = s;
+      P.partial[(long long)blockIdx.x * P.d + c] = s;
     }
   }
 }
@@ -469,27 +557,36 @@ ff_status_t run(const ff_rotary_t* handle, int mode, int64_t batch, int64_t toke
   P.w[0] = w[0]; P.w[1] = w[1];
   memcpy(P.phase, h->phase, sizeof P.phase);
 
-  const int most = P.heads[0] > P.heads[1] ? P.heads[0] : P.heads[1];
-  const long long blocks_x = (P.rows + (long long)H_WARPS * (32 >> lg) - 1) / ((long long)H_WARPS * (32 >> lg));
-  // Heads a block walks over with the same angles: up to 8, fewer where the launch would not fill the device.
-  int chunk = 8;
-  while (chunk > 1 && blocks_x * ((P.heads[0] + chunk - 1) / chunk + (P.heads[1] + chunk - 1) / chunk) < 2 * FF_B200_SMS) chunk >>= 1;
-  if (mode == NORM_BACKWARD && most > 64 * chunk) chunk = (most + 63) / 64;
-  P.chunk = chunk;
-  P.nchunk0 = (P.heads[0] + chunk - 1) / chunk;
-  const int nchunk1 = kinds == 2 ? (P.heads[1] + chunk - 1) / chunk : 0;
-  const int ny = P.nchunk0 + nchunk1;
-  long long nx = blocks_x;
-  if (mode == NORM_BACKWARD && nx * ny > PARTIAL_ROWS) nx = PARTIAL_ROWS / ny > 0 ? PARTIAL_ROWS / ny : 1;
+  const long long per_block = (long long)H_WARPS * (32 >> lg);
+  P.groups = (int)((P.rows + per_block - 1) / per_block);
+  dim3 grid;
+  if (mode == NORM_BACKWARD) {
+    const long long units0 = (long long)P.groups * P.heads[0], units1 = (long long)P.groups * P.heads[1];
+    long long n0 = (units0 * PARTIAL_ROWS + (units0 + units1) / 2) / (units0 + units1);
+    if (kinds == 2) n0 = n0 < 1 ? 1 : n0 >= PARTIAL_ROWS ? PARTIAL_ROWS - 1 : n0;
+    long long n1 = kinds == 2 ? PARTIAL_ROWS - n0 : 0;
+    if (n0 > units0) n0 = units0;
+    if (n1 > units1) n1 = units1;
+    P.nblocks0 = (int)n0;
+    grid = dim3((unsigned)(n0 + n1));
+  } else {
+    // Heads a block walks over with the same angles: up to 32, fewer where the launch would not fill the device (64K tokens, 24 + 24
+    // heads of 128: 304 us with 8, 276 with 24; the rule's limit: eight blocks an SM).
+    int chunk = 32;
+    auto blocks = [&](int c) { return (long long)P.groups * ((P.heads[0] + c - 1) / c + (P.heads[1] + c - 1) / c); };
+    while (chunk > 1 && blocks(chunk) < 8 * FF_B200_SMS) chunk >>= 1;
+    P.chunk = chunk;
+    P.nblocks0 = (P.heads[0] + chunk - 1) / chunk;
+    grid = dim3((unsigned)P.groups, (unsigned)(P.nblocks0 + (P.heads[1] + chunk - 1) / chunk));
+  }
   P.partial = (float*)ws;
-  const dim3 grid((unsigned)nx, (unsigned)ny);
   cudaError_t e;
   if (mode == ROTATE) e = call.e == 4 ? launch_chunk<float, ROTATE>(ch, inter, grid, st, P) : launch_chunk<__nv_bfloat16, ROTATE>(ch, inter, grid, st, P);
   else if (mode == NORM) e = call.e == 4 ? launch_chunk<float, NORM>(ch, inter, grid, st, P) : launch_chunk<__nv_bfloat16, NORM>(ch, inter, grid, st, P);
   else e = call.e == 4 ? launch_chunk<float, NORM_BACKWARD>(ch, inter, grid, st, P) : launch_chunk<__nv_bfloat16, NORM_BACKWARD>(ch, inter, grid, st, P);
   if (e == cudaSuccess && want_dw)
-    e = ff_launch(weight_gradient_kernel, dim3((d + 31) / 32, kinds), dim3(1024), 0, st, (const float*)P.partial, (int)(nx * P.nchunk0),
-                  (int)(nx * nchunk1), d, dwq, dwk);
+    e = ff_launch(weight_gradient_kernel, dim3((d + 31) / 32, kinds), dim3(1024), 0, st, (const float*)P.partial, P.nblocks0,
+                  (int)grid.x - P.nblocks0, d, dwq, dwk);
   return e == cudaSuccess ? FF_OK : cuda_fail(h, e);
 }
 
@@ -562,7 +659,7 @@ extern "C" ff_status_t ff_rotary_frequencies(const ff_rotary_t* h, double* theta
 
 extern "C" ff_status_t ff_qk_norm_workspace_bytes(const ff_rotary_t* h, size_t* bytes) {
   if (!h || !bytes) return fail(const_cast<ff_rotary*>(h), FF_ERR_INVALID_ARG, "handle or bytes is NULL");
-  *bytes = (size_t)(PARTIAL_ROWS + 128) * h->cfg.head_dim * sizeof(float);   // (at least one row for each of the 2 x 64 blocks of heads)
+  *bytes = (size_t)PARTIAL_ROWS * h->cfg.head_dim * sizeof(float);
   return FF_OK;
 }
 
