@@ -417,6 +417,7 @@ class Rotary:
         _check(library().ff_rotary_create(C.byref(c), C.byref(self.handle)))
         self._dtype = torch.float32 if cfg.dtype == "fp32" else torch.bfloat16
         self._axes = 3 if any(cfg.axis_pairs) else 1
+        self._int32, self._float32, self._channels, self._lib = torch.int32, torch.float32, torch.Size((cfg.head_dim,)), library()
         self._raw_stream = _stream_getter(torch)
         n = C.c_size_t()
         _check(library().ff_qk_norm_workspace_bytes(self.handle, C.byref(n)))
@@ -443,47 +444,59 @@ class Rotary:
         if status != FF_OK:
             raise FFError(status, library().ff_rotary_last_error(self.handle).decode())
 
-    def _heads(self, device, *tensors):
-        """Addresses of the tensors' ff_heads_t (None for None), and the array that holds them; the tensors are q- and k-like in
-        turns, those of a kind alike in shape."""
-        dtype, rows, at = self._dtype, [], []
-        shapes = tensors[0].shape, None if tensors[1] is None else tensors[1].shape
-        for i, t in enumerate(tensors):
-            shape = shapes[i & 1]
+    def _arguments(self, positions, q, k, *others):
+        """Checks the tensors of a call, `others` q- and k-like in turns: the arguments (batch, tokens, positions, stride between the
+        samples' positions), the addresses of the tensors' ff_heads_t (None for None), and the array that holds those."""
+        dtype, device, qs = self._dtype, q.device, q.shape
+        if len(qs) != 4 or qs[3] != self.cfg.head_dim or not q.is_cuda or q.dtype != dtype:
+            raise FFError(1, f"expected q a {dtype} tensor [batch][heads][tokens][{self.cfg.head_dim}] on a GPU")
+        B, Hq, N, d = qs
+        sb, sh, st, sc = q.stride()
+        rows, at, contiguous = [q.data_ptr(), sb, sh, st, Hq], [0], sc == 1      # (the layout of ff_heads_t, heads in its low half word)
+        if k is None:
+            ks, Hk = None, 0
+            at.append(None)
+        else:
+            ks = k.shape
+            if len(ks) != 4 or ks[0] != B or ks[2] != N or ks[3] != d or k.dtype != dtype or k.device != device:
+                raise FFError(1, f"expected k a {dtype} tensor [{B}][heads][{N}][{d}] on {device}")
+            Hk = ks[1]
+            sb, sh, st, sc = k.stride()
+            at.append(40)
+            rows += (k.data_ptr(), sb, sh, st, Hk)
+            contiguous &= sc == 1
+        like_k = False
+        for t in others:
+            shape, heads = (ks, Hk) if like_k else (qs, Hq)
+            like_k = not like_k
             if t is None or shape is None:
-                if t is not None or shape is not None:
+                if t is not shape:
                     raise FFError(1, "k comes with its outputs and gradients, or none of them is given")
                 at.append(None)
                 continue
             if t.shape != shape or t.dtype != dtype or t.device != device:
                 raise FFError(1, f"expected a {dtype} tensor of shape {tuple(shape)} on {device}")
             sb, sh, st, sc = t.stride()
-            if sc != 1:
-                raise FFError(1, "the channels of a head must be contiguous")
             at.append(8 * len(rows))
-            rows += (t.data_ptr(), sb, sh, st, shape[1])         # (the layout of ff_heads_t, heads in its low half word)
+            rows += (t.data_ptr(), sb, sh, st, heads)
+            contiguous &= sc == 1
+        if not contiguous:
+            raise FFError(1, "the channels of a head must be contiguous")
         rows = array("q", rows)
         base = rows.buffer_info()[0]
-        return [None if o is None else base + o for o in at], rows
-
-    def _place(self, q, k, positions):
-        """(batch, tokens, positions, stride between the samples' positions), checked."""
-        if q.dim() != 4 or q.shape[3] != self.cfg.head_dim or not q.is_cuda:
-            raise FFError(1, f"expected q on a GPU, of shape [batch][heads][tokens][{self.cfg.head_dim}]")
-        B, _, N, d = q.shape
-        if k is not None and (k.dim() != 4 or k.shape[0] != B or k.shape[2] != N or k.shape[3] != d):
-            raise FFError(1, f"expected k of shape [{B}][heads][{N}][{d}]")
+        at = [None if o is None else base + o for o in at]
         if positions is None:
-            return B, N, None, 0
+            return (B, N, None, 0), at, rows
         p, tail = positions, (N,) if self._axes == 1 else (N, 3)
-        if p.dtype != self._torch.int32 or p.device != q.device or not p.is_contiguous() or (p.shape != tail and p.shape != (B,) + tail):
-            raise FFError(1, f"expected contiguous int32 positions of shape {tail} or {(B,) + tail} on {q.device}")
-        return B, N, p.data_ptr(), N * self._axes if p.dim() > len(tail) else 0
+        ps = p.shape
+        if p.dtype != self._int32 or p.device != device or not p.is_contiguous() or (ps != tail and ps != (B,) + tail):
+            raise FFError(1, f"expected contiguous int32 positions of shape {tail} or {(B,) + tail} on {device}")
+        return (B, N, p.data_ptr(), N * self._axes if len(ps) > len(tail) else 0), at, rows
 
     def _weight(self, w, device):
         if w is None:
             return None
-        if w.dtype != self._torch.float32 or w.shape != (self.cfg.head_dim,) or not w.is_contiguous() or w.device != device:
+        if w.dtype != self._float32 or w.shape != self._channels or not w.is_contiguous() or w.device != device:
             raise FFError(1, f"expected contiguous fp32 weights of shape [{self.cfg.head_dim}] on {device}")
         return w.data_ptr()
 
@@ -497,25 +510,24 @@ class Rotary:
 
     def apply(self, q, q_out, k=None, k_out=None, positions=None, inverse: bool = False):
         """The rotation of q and k; inverse: its transpose, the backward pass."""
-        place, dev = self._place(q, k, positions), q.device
-        (hq, hk, hqo, hko), keep = self._heads(dev, q, k, q_out, k_out)
-        self._call(dev, library().ff_rotary_apply, *place, hq, hk, int(inverse), hqo, hko)
+        place, (hq, hk, hqo, hko), keep = self._arguments(positions, q, k, q_out, k_out)
+        self._call(q.device, self._lib.ff_rotary_apply, *place, hq, hk, int(inverse), hqo, hko)
         return q_out, k_out
 
     def qk_norm(self, q, k, wq, wk, q_out, k_out, eps: float = 1e-6, positions=None):
         """Norm of every row, times wq / wk (fp32 [head_dim], None: ones), then the rotation."""
-        place, dev = self._place(q, k, positions), q.device
-        (hq, hk, hqo, hko), keep = self._heads(dev, q, k, q_out, k_out)
-        self._call(dev, library().ff_qk_norm, *place, hq, hk, self._weight(wq, dev), self._weight(wk, dev), eps, hqo, hko)
+        place, (hq, hk, hqo, hko), keep = self._arguments(positions, q, k, q_out, k_out)
+        dev = q.device
+        self._call(dev, self._lib.ff_qk_norm, *place, hq, hk, self._weight(wq, dev), self._weight(wk, dev), eps, hqo, hko)
         return q_out, k_out
 
     def qk_norm_backward(self, q, k, wq, wk, dq_out, dk_out, dq, dk, dwq=None, dwk=None, eps: float = 1e-6, positions=None):
         """Gradients of q, k (and of the weights, fp32 [head_dim], where given) from those of qk_norm's outputs."""
-        place, dev = self._place(q, k, positions), q.device
-        (hq, hk, hgq, hgk, hdq, hdk), keep = self._heads(dev, q, k, dq_out, dk_out, dq, dk)
+        place, (hq, hk, hgq, hgk, hdq, hdk), keep = self._arguments(positions, q, k, dq_out, dk_out, dq, dk)
+        dev = q.device
         # (a workspace per call: calls on different streams and captured graphs share none)
         ws = self._torch.empty(self.workspace_bytes, dtype=self._torch.uint8, device=dev)
-        self._call(dev, library().ff_qk_norm_backward, *place, hq, hk, self._weight(wq, dev), self._weight(wk, dev), eps, hgq, hgk, hdq, hdk,
+        self._call(dev, self._lib.ff_qk_norm_backward, *place, hq, hk, self._weight(wq, dev), self._weight(wk, dev), eps, hgq, hgk, hdq, hdk,
                    self._weight(dwq, dev), self._weight(dwk, dev), ws.data_ptr(), self.workspace_bytes)
         return dq, dk
 

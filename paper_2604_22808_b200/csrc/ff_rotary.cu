@@ -194,219 +194,317 @@ __device__ __forceinline__ float row_rms(const F2 (&a)[PER][N], const F2 (&b)[PE
   return big ? rsqrtf(sc * inv_d) * down : rsqrtf(ss * inv_d + eps);
 }
 
+// The chunks that lane `lig` of a row has: channels, whether there are any, whether they are turned.
+template <int CH, int PER, bool INTER>
+struct Own {
+  int oa[PER], ob[PER];
+  bool have[PER], ta[PER], tb[PER];
+  __device__ __forceinline__ Own(const HeadsParams& P, int lig, int lanes) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int j = lig + i * lanes;
+      have[i] = j < P.np;
+      if (INTER) {
+        oa[i] = j * CH; ob[i] = (j + P.np) * CH;
+        ta[i] = have[i] && oa[i] < P.rot; tb[i] = have[i] && ob[i] < P.rot;
+      } else {
+        const int turned = P.rot / (2 * CH);
+        ta[i] = tb[i] = have[i] && j < turned;
+        oa[i] = j < turned ? j * CH : P.rot + 2 * (j - turned) * CH;
+        ob[i] = j < turned ? P.rot / 2 + j * CH : oa[i] + CH;
+      }
+    }
+  }
+  // Two neighbouring weights of a chunk, or ones.
+  __device__ __forceinline__ F2 weights(const float* w, int i, int at, int c) const {
+    if (!w || !have[i]) return two(1.f, 1.f);
+    return two(w[at + 2 * c], CH > 1 ? w[at + 2 * c + 1] : 1.f);
+  }
+};
+
+// The rotation of token n of sample b for a lane's chunks, times the weights (NULL: ones).
+template <int CH, int PER, bool INTER>
+__device__ __forceinline__ void turn_of_token(const HeadsParams& P, const Own<CH, PER, INTER>& own, unsigned b, unsigned n, const float* weights,
+                                              Turn<CH> (&k)[PER]) {
+  int pos[3];
+  if (P.positions) {
+    const int* at = P.positions + b * P.pos_stride + (long long)n * P.axes;
+    pos[0] = at[0];
+    pos[1] = P.axes == 3 ? at[1] : 0;
+    pos[2] = P.axes == 3 ? at[2] : 0;
+  } else if (P.axes == 3) {
+    const unsigned line = ff_div(n, P.gw);
+    pos[2] = (int)(n - line * P.gw.d);
+    pos[0] = (int)ff_div(line, P.gh);
+    pos[1] = (int)(line - pos[0] * P.gh.d);
+  } else {
+    pos[0] = (int)n; pos[1] = pos[2] = 0;
+  }
+  auto angle = [&](int p, float& c, float& s) {
+    const int at = p < P.axis_end0 ? pos[0] : (p < P.axis_end1 ? pos[1] : pos[2]);
+    const unsigned long long turns = (unsigned long long)(long long)at * P.phase[p];
+    sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &s, &c);          // 2^-31: half turns
+    c *= P.magnitude;
+    s *= P.inverse ? -P.magnitude : P.magnitude;
+  };
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+#pragma unroll
+    for (int c = 0; c < pairs_of(CH); ++c) {
+      const F2 wa = own.weights(weights, i, own.oa[i], c), wb = own.weights(weights, i, own.ob[i], c);
+      k[i].p[c] = wa; k[i].q[c] = k[i].r[c] = 0; k[i].t[c] = wb;
+      float c0, s0, c1 = 0.f, s1 = 0.f;
+      if constexpr (INTER) {
+        if (own.ta[i]) {
+          angle(own.oa[i] / 2 + c, c0, s0);
+          k[i].p[c] = two(c0 * low(wa), s0 * low(wa)); k[i].q[c] = two(-s0 * high(wa), c0 * high(wa));
+        }
+        if (own.tb[i]) {
+          angle(own.ob[i] / 2 + c, c1, s1);
+          k[i].r[c] = two(c1 * low(wb), s1 * low(wb)); k[i].t[c] = two(-s1 * high(wb), c1 * high(wb));
+        }
+      } else if (own.ta[i]) {
+        angle(own.oa[i] + 2 * c, c0, s0);
+        if (CH > 1) angle(own.oa[i] + 2 * c + 1, c1, s1);
+        k[i].p[c] = mul(wa, two(c0, c1)); k[i].q[c] = mul(wb, two(-s0, -s1));
+        k[i].r[c] = mul(wa, two(s0, s1)); k[i].t[c] = mul(wb, two(c0, c1));
+      }
+    }
+}
+
+// Forward.  A block: one group of 32 / lanes x 8 tokens, blockIdx.x, and one chunk of heads of q or k, blockIdx.y.
 template <class T, int CH, int PER, bool INTER, int MODE>
 __global__ void __launch_bounds__(H_THREADS, 2) heads_kernel(const __grid_constant__ HeadsParams P) {
-  constexpr int U = MODE == NORM_BACKWARD ? 2 : 4;            // heads whose rows are in flight together
+  constexpr int U = 4;                                        // heads whose rows are in flight together
   constexpr int N = pairs_of(CH);
   using C = Chunk<T, CH>;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int lanes = 1 << P.lanes_log2, lig = lane & (lanes - 1);
-  const int per_warp = 32 >> P.lanes_log2;                    // tokens of a warp
-  // A block's work.  Forward: one group of 32 / lanes x 8 tokens, blockIdx.x, and one chunk of heads of q or k, blockIdx.y.  Backward, one
-  // wave of blocks divided between q and k by their heads: a run of equal length of the units (group, head), head by head.
-  const int t = (MODE == NORM_BACKWARD ? blockIdx.x : blockIdx.y) >= (unsigned)P.nblocks0;            // 0: q, 1: k
-  long long unit = 0, end = 1;
-  if (MODE == NORM_BACKWARD) {
-    const long long units = (long long)P.groups * P.heads[t];
-    const int blocks = t ? (int)gridDim.x - P.nblocks0 : P.nblocks0, at = (int)blockIdx.x - (t ? P.nblocks0 : 0);
-    unit = units * at / blocks; end = units * (at + 1) / blocks;
-  }
+  const int lanes = 1 << P.lanes_log2;
+  const int t = blockIdx.y >= (unsigned)P.nblocks0;           // 0: q, 1: k
+  const int h0 = ((int)blockIdx.y - (t ? P.nblocks0 : 0)) * P.chunk;
+  const int h1 = min(h0 + P.chunk, P.heads[t]);
   const float inv_d = 1.f / (float)P.d;
-
-  // the thread's chunks
-  int oa[PER], ob[PER];
-  bool have[PER], ta[PER], tb[PER];
+  const Own<CH, PER, INTER> own(P, lane & (lanes - 1), lanes);
+  const long long row = ((long long)blockIdx.x * H_WARPS + warp) * (32 >> P.lanes_log2) + (lane >> P.lanes_log2);
+  const bool live = row < P.rows;
+  const unsigned ru = live ? (unsigned)row : (unsigned)(P.rows - 1);      // (lanes behind the last row read it once more and write nothing)
+  const unsigned b = ff_div(ru, P.tokens), n = ru - b * P.tokens.d;
+  ff_pdl_wait();
+  Turn<CH> k[PER];
+  turn_of_token<CH, PER, INTER>(P, own, b, n, MODE == NORM ? P.w[t] : nullptr, k);
+  const char* xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st + h0 * P.x[t].sh;
+  char* yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st + h0 * P.y[t].sh;
+#pragma unroll 1
+  for (int h = h0; h < h1; h += U) {
+    C xa[U][PER], xb[U][PER];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int j = lig + i * lanes;
-    have[i] = j < P.np;
-    if (INTER) {
-      oa[i] = j * CH; ob[i] = (j + P.np) * CH;
-      ta[i] = have[i] && oa[i] < P.rot; tb[i] = have[i] && ob[i] < P.rot;
-    } else {
-      const int turned = P.rot / (2 * CH);
-      ta[i] = tb[i] = have[i] && j < turned;
-      oa[i] = j < turned ? j * CH : P.rot + 2 * (j - turned) * CH;
-      ob[i] = j < turned ? P.rot / 2 + j * CH : oa[i] + CH;
+    for (int u = 0; u < U; ++u) {
+      const bool on = u == 0 || h + u < h1;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        xa[u][i] = on && own.have[i] ? __ldcs((const C*)(xp + own.oa[i] * sizeof(T))) : C{};
+        xb[u][i] = on && own.have[i] ? __ldcs((const C*)(xp + own.ob[i] * sizeof(T))) : C{};
+      }
+      xp += P.x[t].sh;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      F2 a[PER][N], c[PER][N];                                // the two chunks
+#pragma unroll
+      for (int i = 0; i < PER; ++i) { unpack<T, CH>(xa[u][i], a[i]); unpack<T, CH>(xb[u][i], c[i]); }
+      if constexpr (MODE == NORM) {
+        const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+          for (int j = 0; j < N; ++j) { a[i][j] = mul(a[i][j], two(r, r)); c[i][j] = mul(c[i][j], two(r, r)); }
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) turn<CH, INTER>(a[i], c[i], k[i], own.ta[i], own.tb[i], MODE == NORM);
+      if (live && (u == 0 || h + u < h1)) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (own.have[i]) {
+            *(C*)(yp + own.oa[i] * sizeof(T)) = pack<T, CH>(a[i]);
+            *(C*)(yp + own.ob[i] * sizeof(T)) = pack<T, CH>(c[i]);
+          }
+      }
+      yp += P.y[t].sh;
     }
   }
-  ff_pdl_wait();
+}
 
-  const float* weights = MODE == ROTATE ? nullptr : P.w[t];
-  auto weight = [&](int i, int at, int c) { return weights && have[i] && (CH > 1 || c == 0) ? weights[at + c] : 1.f; };
-  F2 wa[PER][N], wb[PER][N];                                  // backward: the weights
-  F2 da[PER][N], db[PER][N];                                  // backward: the thread's share of dw
-  if constexpr (MODE == NORM_BACKWARD) {
+// A thread's own piece of memory into its own place in shared memory, asynchronously (`on` false: zeros).
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from, bool on) {
+  const unsigned at = (unsigned)__cvta_generic_to_shared(to), n = on ? BYTES : 0;
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(n) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(at), "l"(from), "r"(n), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// Backward.  One wave of blocks, divided between q and k by their heads; a block has a run of the units (group of tokens, head), head by
+// head, all runs of a tensor equally long.  Weights, their gradients and the rotation fill the registers, so the rows on their way wait
+// in shared memory, each thread's pieces in places of its own: two units ahead, from one group into the next.  (Rows of two-byte pieces,
+// which cannot be copied that way, are loaded when they are needed.)
+template <class T, int CH, int PER, bool INTER>
+__global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __grid_constant__ HeadsParams P) {
+  constexpr int N = pairs_of(CH);
+  constexpr bool RING = sizeof(T) * CH >= 4;
+  constexpr int STAGES = 3;
+  using C = Chunk<T, CH>;
+  constexpr int RING_BYTES = RING ? STAGES * 4 * PER * H_THREADS * (int)sizeof(C) : 0, SUM_BYTES = H_WARPS * 256 * 4;
+  __shared__ __align__(16) unsigned char smem[RING_BYTES > SUM_BYTES ? RING_BYTES : SUM_BYTES];
+  C* ring = (C*)smem + threadIdx.x;                           // [stage][x a, x b, g a, g b][piece][thread]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int lanes = 1 << P.lanes_log2;
+  const int t = blockIdx.x >= (unsigned)P.nblocks0;           // 0: q, 1: k
+  const int heads = P.heads[t];
+  const long long units = (long long)P.groups * heads;
+  const int blocks = t ? (int)gridDim.x - P.nblocks0 : P.nblocks0, at = (int)blockIdx.x - (t ? P.nblocks0 : 0);
+  const long long first = units * at / blocks;
+  const int count = (int)(units * (at + 1) / blocks - first);
+  const float inv_d = 1.f / (float)P.d;
+  const Own<CH, PER, INTER> own(P, lane & (lanes - 1), lanes);
+  auto token = [&](int group, unsigned& b, unsigned& n) {     // the lane's token of a group; false: behind the last
+    const long long row = ((long long)group * H_WARPS + warp) * (32 >> P.lanes_log2) + (lane >> P.lanes_log2);
+    const unsigned ru = row < P.rows ? (unsigned)row : (unsigned)(P.rows - 1);
+    b = ff_div(ru, P.tokens); n = ru - b * P.tokens.d;
+    return row < P.rows;
+  };
+  ff_pdl_wait();
+  F2 wa[PER][N], wb[PER][N], da[PER][N], db[PER][N];          // weights, the thread's share of dw
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      wa[i][c] = own.weights(P.w[t], i, own.oa[i], c);
+      wb[i][c] = own.weights(P.w[t], i, own.ob[i], c);
+      da[i][c] = db[i][c] = 0;
+    }
+
+  // what is requested next: its group, head and addresses
+  int ngroup = (int)(first / heads), nhead = (int)(first - (long long)ngroup * heads), asked = 0;
+  const char *xp, *gp;
+  auto go_to = [&](int group, int head) {
+    unsigned b, n;
+    token(group, b, n);
+    xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st + head * P.x[t].sh;
+    gp = P.g[t].p + b * P.g[t].sb + n * P.g[t].st + head * P.g[t].sh;
+  };
+  go_to(ngroup, nhead);
+  auto ask = [&](int stage) {
+    if (asked < count) {
+      C* to = ring + stage * 4 * PER * H_THREADS;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        copy_async<sizeof(C)>(to + (0 * PER + i) * H_THREADS, xp + own.oa[i] * sizeof(T), own.have[i]);
+        copy_async<sizeof(C)>(to + (1 * PER + i) * H_THREADS, xp + own.ob[i] * sizeof(T), own.have[i]);
+        copy_async<sizeof(C)>(to + (2 * PER + i) * H_THREADS, gp + own.oa[i] * sizeof(T), own.have[i]);
+        copy_async<sizeof(C)>(to + (3 * PER + i) * H_THREADS, gp + own.ob[i] * sizeof(T), own.have[i]);
+      }
+      ++asked;
+      xp += P.x[t].sh; gp += P.g[t].sh;
+      if (++nhead == heads) { nhead = 0; if (asked < count) go_to(++ngroup, 0); }
+    }
+    copy_commit();
+  };
+  if constexpr (RING) {
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) ask(s);
+  }
+
+  int group = ngroup, head = nhead, stage = 0;
+  if (RING) { group = (int)(first / heads); head = (int)(first - (long long)group * heads); }
+  bool fresh = true, live = false;
+  Turn<CH> k[PER];
+  char* yp = nullptr;
+#pragma unroll 1
+  for (int u = 0; u < count; ++u) {
+    if (fresh) {                                              // a new group: its tokens' rotation
+      unsigned b, n;
+      live = token(group, b, n);
+      turn_of_token<CH, PER, INTER>(P, own, b, n, nullptr, k);
+      yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st + head * P.y[t].sh;
+    }
+    F2 a[PER][N], c[PER][N], g0[PER][N], g1[PER][N];
+    if constexpr (RING) {
+      ask(stage == 0 ? STAGES - 1 : stage - 1);               // (the stage read last)
+      copy_wait<STAGES - 1>();
+      const C* from = ring + stage * 4 * PER * H_THREADS;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        unpack<T, CH>(from[(0 * PER + i) * H_THREADS], a[i]); unpack<T, CH>(from[(1 * PER + i) * H_THREADS], c[i]);
+        unpack<T, CH>(from[(2 * PER + i) * H_THREADS], g0[i]); unpack<T, CH>(from[(3 * PER + i) * H_THREADS], g1[i]);
+      }
+      if (++stage == STAGES) stage = 0;
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const C none{};
+        unpack<T, CH>(own.have[i] ? *(const C*)(xp + own.oa[i] * sizeof(T)) : none, a[i]);
+        unpack<T, CH>(own.have[i] ? *(const C*)(xp + own.ob[i] * sizeof(T)) : none, c[i]);
+        unpack<T, CH>(own.have[i] ? *(const C*)(gp + own.oa[i] * sizeof(T)) : none, g0[i]);
+        unpack<T, CH>(own.have[i] ? *(const C*)(gp + own.ob[i] * sizeof(T)) : none, g1[i]);
+      }
+    }
+    const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      turn<CH, INTER>(g0[i], g1[i], k[i], own.ta[i], own.tb[i], false);                          // dz
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        a[i][j] = mul(a[i][j], two(r, r)); c[i][j] = mul(c[i][j], two(r, r));                    // n
+        if (live) { da[i][j] = fma(g0[i][j], a[i][j], da[i][j]); db[i][j] = fma(g1[i][j], c[i][j], db[i][j]); }
+        g0[i][j] = mul(g0[i][j], wa[i][j]); g1[i][j] = mul(g1[i][j], wb[i][j]);                  // g
+      }
+    }
+    const float m = -row_sum(dot<N, PER>(g0, a, g1, c), lanes) * inv_d;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
 #pragma unroll
-      for (int c = 0; c < N; ++c) {
-        wa[i][c] = two(weight(i, oa[i], 2 * c), weight(i, oa[i], 2 * c + 1));
-        wb[i][c] = two(weight(i, ob[i], 2 * c), weight(i, ob[i], 2 * c + 1));
-        da[i][c] = db[i][c] = 0;
+      for (int j = 0; j < N; ++j) {
+        a[i][j] = mul(fma(a[i][j], two(m, m), g0[i][j]), two(r, r));
+        c[i][j] = mul(fma(c[i][j], two(m, m), g1[i][j]), two(r, r));
       }
-  }
-
-  while (unit < end) {
-    int group, h0, h1;
-    if (MODE == NORM_BACKWARD) {
-      group = (int)(unit / P.heads[t]);
-      h0 = (int)(unit - (long long)group * P.heads[t]);
-      h1 = (int)min((long long)P.heads[t], h0 + (end - unit));
-    } else {
-      group = blockIdx.x;
-      h0 = ((int)blockIdx.y - (t ? P.nblocks0 : 0)) * P.chunk;
-      h1 = min(h0 + P.chunk, P.heads[t]);
-    }
-    unit += h1 - h0;
-    const long long row = ((long long)group * H_WARPS + warp) * per_warp + (lane >> P.lanes_log2);
-    const bool live = row < P.rows;
-    const unsigned ru = live ? (unsigned)row : (unsigned)(P.rows - 1);    // (lanes behind the last row read it once more and write nothing)
-    const unsigned b = ff_div(ru, P.tokens), n = ru - b * P.tokens.d;
-    Turn<CH> k[PER];
-    {
-      int pos[3];
-      if (P.positions) {
-        const int* at = P.positions + b * P.pos_stride + (long long)n * P.axes;
-        pos[0] = at[0];
-        pos[1] = P.axes == 3 ? at[1] : 0;
-        pos[2] = P.axes == 3 ? at[2] : 0;
-      } else if (P.axes == 3) {
-        const unsigned line = ff_div(n, P.gw);
-        pos[2] = (int)(n - line * P.gw.d);
-        pos[0] = (int)ff_div(line, P.gh);
-        pos[1] = (int)(line - pos[0] * P.gh.d);
-      } else {
-        pos[0] = (int)n; pos[1] = pos[2] = 0;
-      }
-      auto angle = [&](int p, float& c, float& s) {
-        const int at = p < P.axis_end0 ? pos[0] : (p < P.axis_end1 ? pos[1] : pos[2]);
-        const unsigned long long turns = (unsigned long long)(long long)at * P.phase[p];
-        sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &s, &c);          // 2^-31: half turns
-        c *= P.magnitude;
-        s *= P.inverse ? -P.magnitude : P.magnitude;
-      };
+    if (live) {
 #pragma unroll
       for (int i = 0; i < PER; ++i)
-#pragma unroll
-        for (int c = 0; c < N; ++c) {
-          float w0 = 1.f, w1 = 1.f, w2 = 1.f, w3 = 1.f;
-          if constexpr (MODE == NORM) {
-            w0 = weight(i, oa[i], 2 * c); w1 = weight(i, oa[i], 2 * c + 1);
-            w2 = weight(i, ob[i], 2 * c); w3 = weight(i, ob[i], 2 * c + 1);
-          }
-          k[i].p[c] = two(w0, w1); k[i].q[c] = k[i].r[c] = 0; k[i].t[c] = two(w2, w3);
-          float c0, s0, c1 = 0.f, s1 = 0.f;
-          if constexpr (INTER) {
-            if (ta[i]) {
-              angle(oa[i] / 2 + c, c0, s0);
-              k[i].p[c] = two(c0 * w0, s0 * w0); k[i].q[c] = two(-s0 * w1, c0 * w1);
-            }
-            if (tb[i]) {
-              angle(ob[i] / 2 + c, c1, s1);
-              k[i].r[c] = two(c1 * w2, s1 * w2); k[i].t[c] = two(-s1 * w3, c1 * w3);
-            }
-          } else if (ta[i]) {
-            angle(oa[i] + 2 * c, c0, s0);
-            if (CH > 1) angle(oa[i] + 2 * c + 1, c1, s1);
-            k[i].p[c] = two(c0 * w0, c1 * w1); k[i].q[c] = two(-s0 * w2, -s1 * w3);
-            k[i].r[c] = two(s0 * w0, s1 * w1); k[i].t[c] = two(c0 * w2, c1 * w3);
-          }
+        if (own.have[i]) {
+          *(C*)(yp + own.oa[i] * sizeof(T)) = pack<T, CH>(a[i]);
+          *(C*)(yp + own.ob[i] * sizeof(T)) = pack<T, CH>(c[i]);
         }
     }
-    const char* xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st + h0 * P.x[t].sh;
-    char* yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st + h0 * P.y[t].sh;
-    const char* gp = MODE == NORM_BACKWARD ? P.g[t].p + b * P.g[t].sb + n * P.g[t].st + h0 * P.g[t].sh : nullptr;
-#pragma unroll 1
-    for (int h = h0; h < h1; h += U) {
-      C xa[U][PER], xb[U][PER], ga[U][PER], gb[U][PER];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const bool on = u == 0 || h + u < h1;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          xa[u][i] = on && have[i] ? __ldcs((const C*)(xp + oa[i] * sizeof(T))) : C{};
-          xb[u][i] = on && have[i] ? __ldcs((const C*)(xp + ob[i] * sizeof(T))) : C{};
-          if constexpr (MODE == NORM_BACKWARD) {
-            ga[u][i] = on && have[i] ? __ldcs((const C*)(gp + oa[i] * sizeof(T))) : C{};
-            gb[u][i] = on && have[i] ? __ldcs((const C*)(gp + ob[i] * sizeof(T))) : C{};
-          }
-        }
-        xp += P.x[t].sh;
-        if constexpr (MODE == NORM_BACKWARD) gp += P.g[t].sh;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        F2 a[PER][N], c[PER][N];                              // the two chunks
-#pragma unroll
-        for (int i = 0; i < PER; ++i) { unpack<T, CH>(xa[u][i], a[i]); unpack<T, CH>(xb[u][i], c[i]); }
-        if constexpr (MODE != NORM_BACKWARD) {
-          if constexpr (MODE == NORM) {
-            const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-#pragma unroll
-              for (int j = 0; j < N; ++j) { a[i][j] = mul(a[i][j], two(r, r)); c[i][j] = mul(c[i][j], two(r, r)); }
-          }
-#pragma unroll
-          for (int i = 0; i < PER; ++i) turn<CH, INTER>(a[i], c[i], k[i], ta[i], tb[i], MODE == NORM);
-        } else {
-          const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
-          F2 g0[PER][N], g1[PER][N];
-#pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            unpack<T, CH>(ga[u][i], g0[i]); unpack<T, CH>(gb[u][i], g1[i]);
-            turn<CH, INTER>(g0[i], g1[i], k[i], ta[i], tb[i], false);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-              a[i][j] = mul(a[i][j], two(r, r)); c[i][j] = mul(c[i][j], two(r, r));              // n
-              if (live) { da[i][j] = fma(g0[i][j], a[i][j], da[i][j]); db[i][j] = fma(g1[i][j], c[i][j], db[i][j]); }
-              g0[i][j] = mul(g0[i][j], wa[i][j]); g1[i][j] = mul(g1[i][j], wb[i][j]);            // g
-            }
-          }
-          const float m = -row_sum(dot<N, PER>(g0, a, g1, c), lanes) * inv_d;
-#pragma unroll
-          for (int i = 0; i < PER; ++i)
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-              a[i][j] = mul(fma(a[i][j], two(m, m), g0[i][j]), two(r, r));
-              c[i][j] = mul(fma(c[i][j], two(m, m), g1[i][j]), two(r, r));
-            }
-        }
-        if (live && (u == 0 || h + u < h1)) {
-#pragma unroll
-          for (int i = 0; i < PER; ++i)
-            if (have[i]) {
-              *(C*)(yp + oa[i] * sizeof(T)) = pack<T, CH>(a[i]);
-              *(C*)(yp + ob[i] * sizeof(T)) = pack<T, CH>(c[i]);
-            }
-        }
-        yp += P.y[t].sh;
-      }
+    yp += P.y[t].sh;
+    fresh = ++head == heads;
+    if (fresh) { head = 0; ++group; }
+    if constexpr (!RING) {
+      if (fresh) { if (u + 1 < count) go_to(group, 0); }
+      else { xp += P.x[t].sh; gp += P.g[t].sh; }
     }
   }
 
-  if constexpr (MODE == NORM_BACKWARD) {
-    // the block's rows of dw: lanes that own the same channels, then the warps, in a fixed order
-    __shared__ float sum[H_WARPS][256];
+  // the block's rows of dw: lanes that own the same channels, then the warps, in a fixed order
+  if constexpr (RING) { copy_wait<0>(); __syncthreads(); }
+  float (*sum)[256] = (float (*)[256])smem;
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+  for (int i = 0; i < PER; ++i)
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        float va = c & 1 ? high(da[i][c / 2]) : low(da[i][c / 2]), vb = c & 1 ? high(db[i][c / 2]) : low(db[i][c / 2]);
-        for (int m = lanes; m < 32; m <<= 1) {
-          va += __shfl_xor_sync(0xffffffffu, va, m);
-          vb += __shfl_xor_sync(0xffffffffu, vb, m);
-        }
-        if (lane < lanes && have[i]) { sum[warp][oa[i] + c] = va; sum[warp][ob[i] + c] = vb; }
+    for (int c = 0; c < CH; ++c) {
+      float va = c & 1 ? high(da[i][c / 2]) : low(da[i][c / 2]), vb = c & 1 ? high(db[i][c / 2]) : low(db[i][c / 2]);
+      for (int m = lanes; m < 32; m <<= 1) {
+        va += __shfl_xor_sync(0xffffffffu, va, m);
+        vb += __shfl_xor_sync(0xffffffffu, vb, m);
       }
-    __syncthreads();
-    for (int c = threadIdx.x; c < P.d; c += H_THREADS) {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < H_WARPS; ++w) s += sum[w][c];
-      P.partial[(long long)blockIdx.x * P.d + c] = s;
+      if (lane < lanes && own.have[i]) { sum[warp][own.oa[i] + c] = va; sum[warp][own.ob[i] + c] = vb; }
     }
+  __syncthreads();
+  for (int c = threadIdx.x; c < P.d; c += H_THREADS) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < H_WARPS; ++w) s += sum[w][c];
+    P.partial[(long long)blockIdx.x * P.d + c] = s;
   }
 }
 
@@ -418,9 +516,12 @@ __global__ void __launch_bounds__(1024) weight_gradient_kernel(const float* part
   const float* p = partial + (t ? (long long)rows_q * d : 0);
   const int rows = t ? rows_k : rows_q;
   float s = 0.f;
-  if (c < d)
-#pragma unroll 4
-    for (int r = ty; r < rows; r += 32) s += p[(long long)r * d + c];
+  constexpr int EACH = (PARTIAL_ROWS + 31) / 32;              // (all on their way together)
+  float v[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) v[i] = c < d && ty + 32 * i < rows ? p[(long long)(ty + 32 * i) * d + c] : 0.f;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) s += v[i];
   sum[ty][threadIdx.x & 31] = s;
   __syncthreads();
   if (ty == 0) {
@@ -470,9 +571,15 @@ HeadsView view(const ff_heads_t* v, int e) {
 
 template <class T, int CH, int PER, int MODE>
 cudaError_t launch_layout(bool inter, dim3 grid, cudaStream_t st, const HeadsParams& P) {
-  if constexpr (CH > 1)
-    if (inter) return ff_launch(heads_kernel<T, CH, PER, true, MODE>, grid, dim3(H_THREADS), 0, st, P);
-  return ff_launch(heads_kernel<T, CH, PER, false, MODE>, grid, dim3(H_THREADS), 0, st, P);
+  if constexpr (MODE == NORM_BACKWARD) {
+    if constexpr (CH > 1)
+      if (inter) return ff_launch(heads_backward_kernel<T, CH, PER, true>, grid, dim3(H_THREADS), 0, st, P);
+    return ff_launch(heads_backward_kernel<T, CH, PER, false>, grid, dim3(H_THREADS), 0, st, P);
+  } else {
+    if constexpr (CH > 1)
+      if (inter) return ff_launch(heads_kernel<T, CH, PER, true, MODE>, grid, dim3(H_THREADS), 0, st, P);
+    return ff_launch(heads_kernel<T, CH, PER, false, MODE>, grid, dim3(H_THREADS), 0, st, P);
+  }
 }
 template <class T, int MODE>
 cudaError_t launch_chunk(int ch, bool inter, dim3 grid, cudaStream_t st, const HeadsParams& P) {
