@@ -707,8 +707,9 @@ cudaError_t product(const ff_ffn* h, const Matrix (&a)[2], const Matrix (&b)[2],
 struct FewShape { int nt, split, f_tiles, t_tiles; double us; };
 int few_stages(int nt, int mats) {
   // Up to 64 tokens the rings leave room for a CTA of either product on an SM, so that the second one's weights are on their way
-  // while the first one ends.
-  return nt <= 64 ? (mats == 2 ? 3 : nt <= 16 ? 6 : nt <= 32 ? 5 : 4) : 192 * 1024 / (mats * OPERAND + nt * 128);
+  // while the first one ends (one token, dim 2048, hidden 5632: four stages each 18.4 us, three and six 18.8; the rest of Wd asked
+  // into L2 ahead of the wait as well: 20.1).
+  return nt <= 64 ? (mats == 2 ? (nt <= 16 ? 4 : 3) : nt == 32 ? 5 : 4) : 192 * 1024 / (mats * OPERAND + nt * 128);
 }
 size_t few_smem(int nt, int mats) {
   const size_t ring = (size_t)few_stages(nt, mats) * (mats * OPERAND + nt * 128), sums = (size_t)mats * nt * 512;
