@@ -11,7 +11,8 @@
 // keeps them in registers while it walks over the heads.
 //
 // Angles: theta_p / 2 pi is kept as a 64-bit fraction of a turn.  position * fraction modulo 2^64 is then the angle modulo a
-// whole turn, exact to 2^-33 turns for any 32-bit position, and its high word is what sincospi is asked for: no floating-point
+// whole turn, exact to 2^-33 turns for any 32-bit position: its high word gives the quadrant and a remainder of at most an eighth of a
+// turn, whose sine and cosine are short Taylor polynomials (two values an instruction: the pair of them), and no floating-point
 // product of a far position ever has to be reduced.
 //
 // Threads: a row is cut in chunks of CH channels (16 bytes where strides, rot_dim and head_dim allow, else 8, 4 or 2), and a
@@ -42,6 +43,8 @@ namespace {
 
 enum { ROTATE = 0, NORM = 1, NORM_BACKWARD = 2 };
 constexpr int H_THREADS = 256, H_WARPS = H_THREADS / 32;
+constexpr int FORWARD_WAVES = 8;
+constexpr int FORWARD_BLOCKS = 2;                 // blocks of a forward launch on an SM
 constexpr int PARTIAL_ROWS = 2 * FF_B200_SMS;     // rows of partial weight gradients at most: one wave of two blocks per SM
 
 struct HeadsView { char* p; long long sb, sh, st; };   // strides in bytes
@@ -55,7 +58,7 @@ struct HeadsParams {
   int rows;                        // batch * tokens
   FFFastDiv tokens, gw, gh;        // tokens per sample; the grid's W and H
   int heads[2], groups;            // heads of q and k; groups of tokens
-  int chunk, nblocks0;             // forward: heads a block walks over, blocks in y that belong to q;  backward: blocks that belong to q
+  int nblocks0;                    // backward: blocks that belong to q
   int d, rot, np, lanes_log2;      // channels, turned channels, chunk pairs of a row, log2 of the lanes of a row
   int axis_end0, axis_end1, axes;
   int inverse;
@@ -128,28 +131,22 @@ __device__ __forceinline__ Chunk<T, CH> pack(const F2 (&v)[pairs_of(CH)]) {
   return c;
 }
 
-// What turns two chunks a, b of a row, with the norm's weights in it (NORM).  Half layout: a' = a p + b q, b' = a r + b t;  interleaved:
-// every pair (x, y) of a goes to (x, x) p + (y, y) q, those of b to (x, x) r + (y, y) t.  Chunks that are not turned are multiplied by
-// p (a) and t (b) alone: what stands beside them does not touch them, infinite or not.
+// What turns two chunks a, b of a row.  Half layout: a' = a p + b q, b' = a r + b t;  interleaved: every pair (x, y) of a goes to
+// (x, x) p + (y, y) q, those of b to (x, x) r + (y, y) t.  Chunks that are not turned are left alone: what stands beside them does not
+// touch them, infinite or not.
 template <int CH> struct Turn { F2 p[pairs_of(CH)], q[pairs_of(CH)], r[pairs_of(CH)], t[pairs_of(CH)]; };
 
 template <int CH, bool INTER>
-__device__ __forceinline__ void turn(F2 (&a)[pairs_of(CH)], F2 (&b)[pairs_of(CH)], const Turn<CH>& k, bool turned_a, bool turned_b, bool scaled) {
+__device__ __forceinline__ void turn(F2 (&a)[pairs_of(CH)], F2 (&b)[pairs_of(CH)], const Turn<CH>& k, bool turned_a, bool turned_b) {
   constexpr int N = pairs_of(CH);
   if constexpr (INTER) {
     if (turned_a) {
 #pragma unroll
       for (int i = 0; i < N; ++i) a[i] = fma(two(low(a[i]), low(a[i])), k.p[i], mul(two(high(a[i]), high(a[i])), k.q[i]));
-    } else if (scaled) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) a[i] = mul(a[i], k.p[i]);
     }
     if (turned_b) {
 #pragma unroll
       for (int i = 0; i < N; ++i) b[i] = fma(two(low(b[i]), low(b[i])), k.r[i], mul(two(high(b[i]), high(b[i])), k.t[i]));
-    } else if (scaled) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) b[i] = mul(b[i], k.t[i]);
     }
   } else if (turned_a) {            // (both chunks of a half-layout pair are turned or neither is)
 #pragma unroll
@@ -158,9 +155,6 @@ __device__ __forceinline__ void turn(F2 (&a)[pairs_of(CH)], F2 (&b)[pairs_of(CH)
       a[i] = fma(x, k.p[i], mul(b[i], k.q[i]));
       b[i] = fma(x, k.r[i], mul(b[i], k.t[i]));
     }
-  } else if (scaled) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) { a[i] = mul(a[i], k.p[i]); b[i] = mul(b[i], k.t[i]); }
   }
 }
 
@@ -222,10 +216,24 @@ struct Own {
   }
 };
 
-// The rotation of token n of sample b for a lane's chunks, times the weights (NULL: ones).
+// Sine and cosine of an angle in 2^-32 turns.  |x| <= pi / 4: the first terms left out are x^11 / 11! < 2e-9 and x^12 / 12! < 2e-10.
+__device__ __forceinline__ void sine_and_cosine(unsigned turns, float& sine, float& cosine) {
+  const unsigned quadrant = (turns + 0x20000000u) >> 30;
+  const float x = (float)(int)(turns - (quadrant << 30)) * 1.4629180792671596e-9f;          // 2 pi / 2^32
+  const F2 x2 = two(x * x, x * x);
+  F2 v = two(2.7557319224e-6f, fmaf(x * x, -2.7557319224e-7f, 2.4801587302e-5f));             // sin(x) / x: 1/9!;  cos(x): 1/8!, -1/10!
+  v = fma(x2, v, two(-1.9841269841e-4f, -1.3888888889e-3f));
+  v = fma(x2, v, two(8.3333333333e-3f, 4.1666666667e-2f));
+  v = fma(x2, v, two(-1.6666666667e-1f, -0.5f));
+  v = fma(x2, v, two(1.f, 1.f));
+  const float s = x * low(v), c = high(v);
+  sine = __uint_as_float(__float_as_uint(quadrant & 1 ? c : s) ^ ((quadrant & 2) << 30));
+  cosine = __uint_as_float(__float_as_uint(quadrant & 1 ? s : c) ^ (((quadrant + 1) & 2) << 30));
+}
+
+// The rotation of token n of sample b for a lane's chunks.
 template <int CH, int PER, bool INTER>
-__device__ __forceinline__ void turn_of_token(const HeadsParams& P, const Own<CH, PER, INTER>& own, unsigned b, unsigned n, const float* weights,
-                                              Turn<CH> (&k)[PER]) {
+__device__ __forceinline__ void turn_of_token(const HeadsParams& P, const Own<CH, PER, INTER>& own, unsigned b, unsigned n, Turn<CH> (&k)[PER]) {
   int pos[3];
   if (P.positions) {
     const int* at = P.positions + b * P.pos_stride + (long long)n * P.axes;
@@ -233,17 +241,14 @@ __device__ __forceinline__ void turn_of_token(const HeadsParams& P, const Own<CH
     pos[1] = P.axes == 3 ? at[1] : 0;
     pos[2] = P.axes == 3 ? at[2] : 0;
   } else if (P.axes == 3) {
-    const unsigned line = ff_div(n, P.gw);
-    pos[2] = (int)(n - line * P.gw.d);
-    pos[0] = (int)ff_div(line, P.gh);
-    pos[1] = (int)(line - pos[0] * P.gh.d);
+    const unsigned line = ff_div(n, P.gw), plane = ff_div(line, P.gh);
+    pos[0] = (int)plane; pos[1] = (int)(line - plane * P.gh.d); pos[2] = (int)(n - line * P.gw.d);
   } else {
     pos[0] = (int)n; pos[1] = pos[2] = 0;
   }
-  auto angle = [&](int p, float& c, float& s) {
+  auto angle = [&](int p, float& c, float& s) {               // times the magnitude
     const int at = p < P.axis_end0 ? pos[0] : (p < P.axis_end1 ? pos[1] : pos[2]);
-    const unsigned long long turns = (unsigned long long)(long long)at * P.phase[p];
-    sincospif((float)(int)(turns >> 32) * 4.656612873077393e-10f, &s, &c);          // 2^-31: half turns
+    sine_and_cosine((unsigned)(((unsigned long long)(long long)at * P.phase[p]) >> 32), s, c);
     c *= P.magnitude;
     s *= P.inverse ? -P.magnitude : P.magnitude;
   };
@@ -251,87 +256,37 @@ __device__ __forceinline__ void turn_of_token(const HeadsParams& P, const Own<CH
   for (int i = 0; i < PER; ++i)
 #pragma unroll
     for (int c = 0; c < pairs_of(CH); ++c) {
-      const F2 wa = own.weights(weights, i, own.oa[i], c), wb = own.weights(weights, i, own.ob[i], c);
-      k[i].p[c] = wa; k[i].q[c] = k[i].r[c] = 0; k[i].t[c] = wb;
+      k[i].p[c] = k[i].q[c] = k[i].r[c] = k[i].t[c] = 0;
       float c0, s0, c1 = 0.f, s1 = 0.f;
       if constexpr (INTER) {
         if (own.ta[i]) {
           angle(own.oa[i] / 2 + c, c0, s0);
-          k[i].p[c] = two(c0 * low(wa), s0 * low(wa)); k[i].q[c] = two(-s0 * high(wa), c0 * high(wa));
+          k[i].p[c] = two(c0, s0); k[i].q[c] = two(-s0, c0);
         }
         if (own.tb[i]) {
           angle(own.ob[i] / 2 + c, c1, s1);
-          k[i].r[c] = two(c1 * low(wb), s1 * low(wb)); k[i].t[c] = two(-s1 * high(wb), c1 * high(wb));
+          k[i].r[c] = two(c1, s1); k[i].t[c] = two(-s1, c1);
         }
       } else if (own.ta[i]) {
         angle(own.oa[i] + 2 * c, c0, s0);
         if (CH > 1) angle(own.oa[i] + 2 * c + 1, c1, s1);
-        k[i].p[c] = mul(wa, two(c0, c1)); k[i].q[c] = mul(wb, two(-s0, -s1));
-        k[i].r[c] = mul(wa, two(s0, s1)); k[i].t[c] = mul(wb, two(c0, c1));
+        k[i].p[c] = k[i].t[c] = two(c0, c1);
+        k[i].q[c] = two(-s0, -s1); k[i].r[c] = two(s0, s1);
       }
     }
 }
 
-// Forward.  A block: one group of 32 / lanes x 8 tokens, blockIdx.x, and one chunk of heads of q or k, blockIdx.y.
-template <class T, int CH, int PER, bool INTER, int MODE>
-__global__ void __launch_bounds__(H_THREADS, 2) heads_kernel(const __grid_constant__ HeadsParams P) {
-  constexpr int U = 4;                                        // heads whose rows are in flight together
-  constexpr int N = pairs_of(CH);
-  using C = Chunk<T, CH>;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int lanes = 1 << P.lanes_log2;
-  const int t = blockIdx.y >= (unsigned)P.nblocks0;           // 0: q, 1: k
-  const int h0 = ((int)blockIdx.y - (t ? P.nblocks0 : 0)) * P.chunk;
-  const int h1 = min(h0 + P.chunk, P.heads[t]);
-  const float inv_d = 1.f / (float)P.d;
-  const Own<CH, PER, INTER> own(P, lane & (lanes - 1), lanes);
-  const long long row = ((long long)blockIdx.x * H_WARPS + warp) * (32 >> P.lanes_log2) + (lane >> P.lanes_log2);
-  const bool live = row < P.rows;
-  const unsigned ru = live ? (unsigned)row : (unsigned)(P.rows - 1);      // (lanes behind the last row read it once more and write nothing)
-  const unsigned b = ff_div(ru, P.tokens), n = ru - b * P.tokens.d;
-  ff_pdl_wait();
-  Turn<CH> k[PER];
-  turn_of_token<CH, PER, INTER>(P, own, b, n, MODE == NORM ? P.w[t] : nullptr, k);
-  const char* xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st + h0 * P.x[t].sh;
-  char* yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st + h0 * P.y[t].sh;
-#pragma unroll 1
-  for (int h = h0; h < h1; h += U) {
-    C xa[U][PER], xb[U][PER];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool on = u == 0 || h + u < h1;
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        xa[u][i] = on && own.have[i] ? __ldcs((const C*)(xp + own.oa[i] * sizeof(T))) : C{};
-        xb[u][i] = on && own.have[i] ? __ldcs((const C*)(xp + own.ob[i] * sizeof(T))) : C{};
-      }
-      xp += P.x[t].sh;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      F2 a[PER][N], c[PER][N];                                // the two chunks
-#pragma unroll
-      for (int i = 0; i < PER; ++i) { unpack<T, CH>(xa[u][i], a[i]); unpack<T, CH>(xb[u][i], c[i]); }
-      if constexpr (MODE == NORM) {
-        const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-#pragma unroll
-          for (int j = 0; j < N; ++j) { a[i][j] = mul(a[i][j], two(r, r)); c[i][j] = mul(c[i][j], two(r, r)); }
-      }
-#pragma unroll
-      for (int i = 0; i < PER; ++i) turn<CH, INTER>(a[i], c[i], k[i], own.ta[i], own.tb[i], MODE == NORM);
-      if (live && (u == 0 || h + u < h1)) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (own.have[i]) {
-            *(C*)(yp + own.oa[i] * sizeof(T)) = pack<T, CH>(a[i]);
-            *(C*)(yp + own.ob[i] * sizeof(T)) = pack<T, CH>(c[i]);
-          }
-      }
-      yp += P.y[t].sh;
-    }
-  }
+// The positions of a token that will be turned soon, on their way into L1.
+__device__ __forceinline__ void prefetch_position(const HeadsParams& P, unsigned b, unsigned n) {
+  if (P.positions) asm volatile("prefetch.global.L1 [%0];" ::"l"(P.positions + b * P.pos_stride + (long long)n * P.axes) : "memory");
+}
+
+// The lane's token of a group; false: behind the last row (it then reads that one once more and writes nothing).
+__device__ __forceinline__ bool token_of(const HeadsParams& P, int group, int warp, int lane, unsigned& b, unsigned& n) {
+  const long long row = ((long long)group * H_WARPS + warp) * (32 >> P.lanes_log2) + (lane >> P.lanes_log2);
+  const unsigned r = (unsigned)min(row, (long long)P.rows - 1);
+  b = ff_div(r, P.tokens); n = r - b * P.tokens.d;
+  return row < P.rows;
 }
 
 // A thread's own piece of memory into its own place in shared memory, asynchronously (`on` false: zeros).
@@ -344,8 +299,159 @@ __device__ __forceinline__ void copy_async(void* to, const void* from, bool on) 
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// Backward.  One wave of blocks, divided between q and k by their heads; a block has a run of the units (group of tokens, head), head by
-// head, all runs of a tensor equally long.  Weights, their gradients and the rotation fill the registers, so the rows on their way wait
+// A block's way through the units (group of 8 x 32 / lanes tokens, head or two): a run of them, those of a group following one another, all
+// blocks' runs equally long.  (Whole groups in turns over all blocks and shares of what is left measured no better.)
+struct Walk {
+  int group, head, heads, count;
+  __device__ __forceinline__ Walk(int groups, int heads_, int blocks, int block) : heads(heads_) {
+    const long long units = (long long)groups * heads, first = units * block / blocks;
+    count = (int)(units * (block + 1) / blocks - first);
+    group = (int)(first / heads); head = (int)(first - (long long)group * heads);
+  }
+  __device__ __forceinline__ bool next() {                    // to the next unit; true: another group
+    if (++head < heads) return false;
+    head = 0; ++group;
+    return true;
+  }
+};
+
+// Forward.  One wave of blocks; a unit is two heads of q, or of k behind them: the rotation of a thread's pairs of one token stays in
+// its registers for all heads.  The rows on their way wait in shared memory, each thread's pieces in places of its own, two units ahead,
+// from one group into the next.  (Rows of two-byte pieces, which cannot be copied that way, are loaded when they are needed.)
+template <class T, int CH, int PER, bool INTER, int MODE>
+__global__ void __launch_bounds__(H_THREADS, FORWARD_BLOCKS) heads_kernel(const __grid_constant__ HeadsParams P) {
+  constexpr int N = pairs_of(CH), U = 2;
+  using C = Chunk<T, CH>;
+  constexpr bool RING = sizeof(C) >= 4;
+  constexpr int STAGES = RING ? 3 : 1;
+  __shared__ __align__(16) C ring_store[STAGES * U * 2 * PER * H_THREADS];       // [stage][head][a, b][piece][thread]
+  C* ring = ring_store + threadIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int lanes = 1 << P.lanes_log2;
+  const int in_q = (P.heads[0] + U - 1) / U, in_k = (P.heads[1] + U - 1) / U;
+  const float inv_d = 1.f / (float)P.d;
+  const Own<CH, PER, INTER> own(P, lane & (lanes - 1), lanes);
+  ff_pdl_wait();
+
+  Walk now(P.groups, in_q + in_k, gridDim.x, blockIdx.x), ahead = now;           // what is computed, what is requested next
+  const int count = now.count;
+  int asked = 0;
+  unsigned nb, nn;
+  const char* xp;
+  auto go_to = [&](bool other) {                              // to the rows of `ahead`, of another group or not
+    if (other) { token_of(P, ahead.group, warp, lane, nb, nn); prefetch_position(P, nb, nn); }
+    const int t = ahead.head >= in_q;
+    xp = P.x[t].p + nb * P.x[t].sb + nn * P.x[t].st + (long long)(ahead.head - (t ? in_q : 0)) * U * P.x[t].sh;
+  };
+  go_to(true);
+  auto advance = [&] {
+    const bool other = ahead.next();
+    if (other || ahead.head == in_q) go_to(other);
+    else xp += U * P.x[ahead.head > in_q].sh;
+  };
+  auto heads_of = [&](const Walk& w) {                        // of the unit's heads, those there are
+    const int t = w.head >= in_q;
+    return min(U, P.heads[t] - (w.head - (t ? in_q : 0)) * U);
+  };
+  auto ask = [&](int stage) {
+    if (asked < count) {
+      C* to = ring + stage * U * 2 * PER * H_THREADS;
+      const int there = heads_of(ahead);
+      const long long sh = P.x[ahead.head >= in_q].sh;
+#pragma unroll
+      for (int h = 0; h < U; ++h)
+        if (h < there)
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            copy_async<sizeof(C)>(to + (h * 2 * PER + i) * H_THREADS, xp + h * sh + own.oa[i] * sizeof(T), own.have[i]);
+            copy_async<sizeof(C)>(to + (h * 2 * PER + PER + i) * H_THREADS, xp + h * sh + own.ob[i] * sizeof(T), own.have[i]);
+          }
+      if (++asked < count) advance();
+    }
+    copy_commit();
+  };
+  if constexpr (RING) {
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) ask(s);
+  }
+
+  int stage = 0;
+  bool live = false, other = true;
+  Turn<CH> k[PER];
+  F2 wa[PER][N], wb[PER][N];
+  char* yp = nullptr;
+  unsigned b, n;
+#pragma unroll 1
+  for (int u = 0; u < count; ++u) {
+    const int t = now.head >= in_q, there = heads_of(now);
+    if (other) {                                              // another group: its tokens' rotation
+      live = token_of(P, now.group, warp, lane, b, n);
+      turn_of_token<CH, PER, INTER>(P, own, b, n, k);
+    }
+    if (other || now.head == in_q) {
+      yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st + (long long)(now.head - (t ? in_q : 0)) * U * P.y[t].sh;
+      if constexpr (MODE == NORM) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+          for (int c = 0; c < N; ++c) { wa[i][c] = own.weights(P.w[t], i, own.oa[i], c); wb[i][c] = own.weights(P.w[t], i, own.ob[i], c); }
+      }
+    }
+    C xa[U][PER], xb[U][PER];
+    if constexpr (RING) {
+      ask(stage == 0 ? STAGES - 1 : stage - 1);               // (the stage read last)
+      copy_wait<STAGES - 1>();
+      const C* from = ring + stage * U * 2 * PER * H_THREADS;
+#pragma unroll
+      for (int h = 0; h < U; ++h)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          xa[h][i] = from[(h * 2 * PER + i) * H_THREADS];
+          xb[h][i] = from[(h * 2 * PER + PER + i) * H_THREADS];
+        }
+      if (++stage == STAGES) stage = 0;
+    } else {
+#pragma unroll
+      for (int h = 0; h < U; ++h)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const char* from = xp + h * P.x[t].sh;
+          xa[h][i] = own.have[i] && h < there ? *(const C*)(from + own.oa[i] * sizeof(T)) : C{};
+          xb[h][i] = own.have[i] && h < there ? *(const C*)(from + own.ob[i] * sizeof(T)) : C{};
+        }
+      if (u + 1 < count) advance();
+    }
+#pragma unroll
+    for (int h = 0; h < U; ++h) {
+      if (h && h >= there) break;                             // (the whole block)
+      F2 a[PER][N], c[PER][N];                                // the two chunks
+#pragma unroll
+      for (int i = 0; i < PER; ++i) { unpack<T, CH>(xa[h][i], a[i]); unpack<T, CH>(xb[h][i], c[i]); }
+      if constexpr (MODE == NORM) {
+        const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+          for (int j = 0; j < N; ++j) { a[i][j] = mul(mul(a[i][j], two(r, r)), wa[i][j]); c[i][j] = mul(mul(c[i][j], two(r, r)), wb[i][j]); }
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) turn<CH, INTER>(a[i], c[i], k[i], own.ta[i], own.tb[i]);
+      if (live) {
+        char* to = yp + h * P.y[t].sh;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (own.have[i]) {
+            *(C*)(to + own.oa[i] * sizeof(T)) = pack<T, CH>(a[i]);
+            *(C*)(to + own.ob[i] * sizeof(T)) = pack<T, CH>(c[i]);
+          }
+      }
+    }
+    yp += U * P.y[t].sh;
+    other = now.next();
+  }
+}
+
+// Backward.  One wave of blocks, divided between q and k by their heads.  Weights, their gradients and the rotation fill the registers, so the rows on their way wait
 // in shared memory, each thread's pieces in places of its own: two units ahead, from one group into the next.  (Rows of two-byte pieces,
 // which cannot be copied that way, are loaded when they are needed.)
 template <class T, int CH, int PER, bool INTER>
@@ -361,18 +467,10 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __gr
   const int lanes = 1 << P.lanes_log2;
   const int t = blockIdx.x >= (unsigned)P.nblocks0;           // 0: q, 1: k
   const int heads = P.heads[t];
-  const long long units = (long long)P.groups * heads;
-  const int blocks = t ? (int)gridDim.x - P.nblocks0 : P.nblocks0, at = (int)blockIdx.x - (t ? P.nblocks0 : 0);
-  const long long first = units * at / blocks;
-  const int count = (int)(units * (at + 1) / blocks - first);
+  Walk now(P.groups, heads, t ? (int)gridDim.x - P.nblocks0 : P.nblocks0, (int)blockIdx.x - (t ? P.nblocks0 : 0)), ahead = now;
+  const int count = now.count;                                // (`now`: what is computed, `ahead`: what is requested next)
   const float inv_d = 1.f / (float)P.d;
   const Own<CH, PER, INTER> own(P, lane & (lanes - 1), lanes);
-  auto token = [&](int group, unsigned& b, unsigned& n) {     // the lane's token of a group; false: behind the last
-    const long long row = ((long long)group * H_WARPS + warp) * (32 >> P.lanes_log2) + (lane >> P.lanes_log2);
-    const unsigned ru = row < P.rows ? (unsigned)row : (unsigned)(P.rows - 1);
-    b = ff_div(ru, P.tokens); n = ru - b * P.tokens.d;
-    return row < P.rows;
-  };
   ff_pdl_wait();
   F2 wa[PER][N], wb[PER][N], da[PER][N], db[PER][N];          // weights, the thread's share of dw
 #pragma unroll
@@ -384,16 +482,20 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __gr
       da[i][c] = db[i][c] = 0;
     }
 
-  // what is requested next: its group, head and addresses
-  int ngroup = (int)(first / heads), nhead = (int)(first - (long long)ngroup * heads), asked = 0;
+  int asked = 0;
   const char *xp, *gp;
-  auto go_to = [&](int group, int head) {
+  auto go_to = [&] {
     unsigned b, n;
-    token(group, b, n);
-    xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st + head * P.x[t].sh;
-    gp = P.g[t].p + b * P.g[t].sb + n * P.g[t].st + head * P.g[t].sh;
+    token_of(P, ahead.group, warp, lane, b, n);
+    prefetch_position(P, b, n);
+    xp = P.x[t].p + b * P.x[t].sb + n * P.x[t].st + ahead.head * P.x[t].sh;
+    gp = P.g[t].p + b * P.g[t].sb + n * P.g[t].st + ahead.head * P.g[t].sh;
   };
-  go_to(ngroup, nhead);
+  go_to();
+  auto advance = [&] {
+    if (ahead.next()) go_to();
+    else { xp += P.x[t].sh; gp += P.g[t].sh; }
+  };
   auto ask = [&](int stage) {
     if (asked < count) {
       C* to = ring + stage * 4 * PER * H_THREADS;
@@ -404,9 +506,7 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __gr
         copy_async<sizeof(C)>(to + (2 * PER + i) * H_THREADS, gp + own.oa[i] * sizeof(T), own.have[i]);
         copy_async<sizeof(C)>(to + (3 * PER + i) * H_THREADS, gp + own.ob[i] * sizeof(T), own.have[i]);
       }
-      ++asked;
-      xp += P.x[t].sh; gp += P.g[t].sh;
-      if (++nhead == heads) { nhead = 0; if (asked < count) go_to(++ngroup, 0); }
+      if (++asked < count) advance();
     }
     copy_commit();
   };
@@ -415,18 +515,17 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __gr
     for (int s = 0; s < STAGES - 1; ++s) ask(s);
   }
 
-  int group = ngroup, head = nhead, stage = 0;
-  if (RING) { group = (int)(first / heads); head = (int)(first - (long long)group * heads); }
-  bool fresh = true, live = false;
+  int stage = 0;
+  bool other = true, live = false;
   Turn<CH> k[PER];
   char* yp = nullptr;
 #pragma unroll 1
   for (int u = 0; u < count; ++u) {
-    if (fresh) {                                              // a new group: its tokens' rotation
+    if (other) {                                              // another group: its tokens' rotation
       unsigned b, n;
-      live = token(group, b, n);
-      turn_of_token<CH, PER, INTER>(P, own, b, n, nullptr, k);
-      yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st + head * P.y[t].sh;
+      live = token_of(P, now.group, warp, lane, b, n);
+      turn_of_token<CH, PER, INTER>(P, own, b, n, k);
+      yp = P.y[t].p + b * P.y[t].sb + n * P.y[t].st + now.head * P.y[t].sh;
     }
     F2 a[PER][N], c[PER][N], g0[PER][N], g1[PER][N];
     if constexpr (RING) {
@@ -452,7 +551,7 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __gr
     const float r = row_rms<N, PER>(a, c, lanes, inv_d, P.eps);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      turn<CH, INTER>(g0[i], g1[i], k[i], own.ta[i], own.tb[i], false);                          // dz
+      turn<CH, INTER>(g0[i], g1[i], k[i], own.ta[i], own.tb[i]);                          // dz
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         a[i][j] = mul(a[i][j], two(r, r)); c[i][j] = mul(c[i][j], two(r, r));                    // n
@@ -477,12 +576,8 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __gr
         }
     }
     yp += P.y[t].sh;
-    fresh = ++head == heads;
-    if (fresh) { head = 0; ++group; }
-    if constexpr (!RING) {
-      if (fresh) { if (u + 1 < count) go_to(group, 0); }
-      else { xp += P.x[t].sh; gp += P.g[t].sh; }
-    }
+    other = now.next();
+    if constexpr (!RING) { if (u + 1 < count) advance(); }
   }
 
   // the block's rows of dw: lanes that own the same channels, then the warps, in a fixed order
@@ -677,14 +772,12 @@ ff_status_t run(const ff_rotary_t* handle, int mode, int64_t batch, int64_t toke
     P.nblocks0 = (int)n0;
     grid = dim3((unsigned)(n0 + n1));
   } else {
-    // Heads a block walks over with the same angles: up to 32, fewer where the launch would not fill the device (64K tokens, 24 + 24
-    // heads of 128: 304 us with 8, 276 with 24; the rule's limit: eight blocks an SM).
-    int chunk = 32;
-    auto blocks = [&](int c) { return (long long)P.groups * ((P.heads[0] + c - 1) / c + (P.heads[1] + c - 1) / c); };
-    while (chunk > 1 && blocks(chunk) < 8 * FF_B200_SMS) chunk >>= 1;
-    P.chunk = chunk;
-    P.nblocks0 = (P.heads[0] + chunk - 1) / chunk;
-    grid = dim3((unsigned)P.groups, (unsigned)(P.nblocks0 + (P.heads[1] + chunk - 1) / chunk));
+    const long long units = (long long)P.groups * ((P.heads[0] + 1) / 2 + (P.heads[1] + 1) / 2);
+    const long long wave = FORWARD_BLOCKS * FF_B200_SMS;
+    long long each = units / (FORWARD_WAVES * wave);
+    each = each < 8 ? 8 : each > 16 ? 16 : each;
+    const long long blocks = units < wave ? units : units / each > wave ? units / each : wave;
+    grid = dim3((unsigned)blocks);
   }
   P.partial = (float*)ws;
   cudaError_t e;
