@@ -345,6 +345,14 @@ ff_status_t ff_qk_norm_backward(const ff_rotary_t *rotary, int64_t batch, int64_
                                 size_t workspace_bytes, void *cuda_stream);
 ff_status_t ff_qk_norm_workspace_bytes(const ff_rotary_t *rotary, size_t *bytes);
 
+/* ff_forward_projected with the rotation of Q and K between the projections and the attention, and, with eps > 0,
+ * their norm in the same pass (eps = 0: none; wq and wk NULL then).  The handle is for bf16 and the plan's
+ * head_dim; without positions its grid is the plan's, or it turns the tokens by their index. */
+ff_status_t ff_forward_projected_rotary(ff_plan_t *plan, const void *X, const void *Wqkv, const void *Wo,
+                                        const ff_rotary_t *rotary, const int32_t *positions, int64_t position_stride,
+                                        const float *wq, const float *wk, float eps, const uint8_t *alloc_dev,
+                                        const float *timestep, void *out, void *cuda_stream);
+
 /* ---- the gated feed-forward block ---------------------------------------------------------------------
  *
  * The other half of a transformer layer, behind ff_forward_projected (no counterpart in the paper):

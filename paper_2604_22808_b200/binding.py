@@ -34,7 +34,7 @@ EXPORTS = ("ff_config_validate", "ff_band_sizes", "ff_band_rank", "ff_workspace_
            "ff_route", "ff_forward", "ff_forward_host", "ff_forward_projected", "ff_plan_device_status", "ff_plan_last_launches", "ff_plan_kernel_info",
            "ff_get_tap", "ff_plan_set_attention_impl", "ff_plan_set_profiling", "ff_plan_stage_times", "ff_high_attention_noalloc",
            "ff_plan_selftest_bounded_wait", "ff_rotary_create", "ff_rotary_destroy", "ff_rotary_last_error", "ff_rotary_frequencies",
-           "ff_rotary_apply", "ff_qk_norm", "ff_qk_norm_backward", "ff_qk_norm_workspace_bytes", "ff_ffn_validate",
+           "ff_rotary_apply", "ff_qk_norm", "ff_qk_norm_backward", "ff_qk_norm_workspace_bytes", "ff_forward_projected_rotary", "ff_ffn_validate",
            "ff_ffn_workspace_bytes", "ff_ffn_create", "ff_ffn_destroy", "ff_ffn_last_error", "ff_ffn_forward", "ff_ffn_backward",
            "ff_ffn_device_status")
 STAGES = ("transform", "router", "attention", "summary", "inverse")
@@ -115,6 +115,7 @@ def library() -> C.CDLL:
         lib.ff_qk_norm.argtypes = place + [heads, heads, C.c_void_p, C.c_void_p, C.c_float, heads, heads, C.c_void_p]
         lib.ff_qk_norm_backward.argtypes = (place + [heads, heads, C.c_void_p, C.c_void_p, C.c_float] + [heads] * 4
                                             + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p])
+        lib.ff_forward_projected_rotary.argtypes = ([C.c_void_p] * 6 + [C.c_int64, C.c_void_p, C.c_void_p, C.c_float] + [C.c_void_p] * 4)
         lib.ff_qk_norm_workspace_bytes.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
         lib.ff_ffn_validate.argtypes = [C.POINTER(ff_ffn_config_t)]
         lib.ff_ffn_workspace_bytes.argtypes = [C.POINTER(ff_ffn_config_t), C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
@@ -319,9 +320,12 @@ class Plan:
                                          out_h.data_ptr(), self._stream()), self.handle)
         return out_h
 
-    def forward_projected(self, X, Wqkv, Wo, out, alloc=None, timesteps: Optional[Sequence[float]] = None):
+    def forward_projected(self, X, Wqkv, Wo, out, alloc=None, timesteps: Optional[Sequence[float]] = None,
+                          rotary: Optional["Rotary"] = None, wq=None, wk=None, eps: float = 0.0, positions=None):
         """X, out: bf16 CUDA tensors [batch][T*H*W][heads*head_dim]; Wqkv [3][D][D], Wo [D][D] (y = x W).
-        The plan must have been created with host_staging=True (Q, K, V and the attention output live there)."""
+        The plan must have been created with host_staging=True (Q, K, V and the attention output live there).
+        rotary: Q and K are turned before the attention, and with eps > 0 normed first (times wq, wk: fp32 [head_dim] or None);
+        positions as for Rotary, None: the plan's grid, or the token's index."""
         torch = self._torch
         cfg = self.cfg
         D = cfg.heads * cfg.head_dim
@@ -330,6 +334,13 @@ class Plan:
                     or t.device != self.device):
                 raise FFError(1, f"expected a contiguous bf16 tensor of shape {shape} on {self.device}")
         ts = _floats(timesteps, self.cfg.batch)
+        if rotary is not None:
+            w, (pos, stride) = [rotary._weight(t, self.device) for t in (wq, wk)], rotary._positions(positions, cfg.batch, cfg.N, self.device)
+            _check(library().ff_forward_projected_rotary(self.handle, X.data_ptr(), Wqkv.data_ptr(), Wo.data_ptr(), rotary.handle, pos, stride,
+                                                         *w, eps, self._check_masks(alloc), ts, out.data_ptr(), self._stream()), self.handle)
+            return out
+        if wq is not None or wk is not None or eps or positions is not None:
+            raise FFError(1, "norm weights, eps and positions belong to a rotary handle")
         _check(library().ff_forward_projected(self.handle, X.data_ptr(), Wqkv.data_ptr(), Wo.data_ptr(),
                                               self._check_masks(alloc), ts, out.data_ptr(), self._stream()), self.handle)
         return out
@@ -485,13 +496,17 @@ class Rotary:
         rows = array("q", rows)
         base = rows.buffer_info()[0]
         at = [None if o is None else base + o for o in at]
-        if positions is None:
-            return (B, N, None, 0), at, rows
-        p, tail = positions, (N,) if self._axes == 1 else (N, 3)
-        ps = p.shape
+        pos, stride = self._positions(positions, B, N, device)
+        return (B, N, pos, stride), at, rows
+
+    def _positions(self, p, B, N, device):
+        """Address of the positions and the elements between the samples' (None: none given), checked."""
+        if p is None:
+            return None, 0
+        ps, tail = p.shape, (N,) if self._axes == 1 else (N, 3)
         if p.dtype != self._int32 or p.device != device or not p.is_contiguous() or (ps != tail and ps != (B,) + tail):
             raise FFError(1, f"expected contiguous int32 positions of shape {tail} or {(B,) + tail} on {device}")
-        return (B, N, p.data_ptr(), N * self._axes if len(ps) > len(tail) else 0), at, rows
+        return p.data_ptr(), N * self._axes if len(ps) > len(tail) else 0
 
     def _weight(self, w, device):
         if w is None:
@@ -639,6 +654,39 @@ def ff_forward_host(plan: Plan, Qh, Kh, Vh, out_h, alloc_host=None, timesteps=No
 
 def ff_forward_projected(plan: Plan, X, Wqkv, Wo, out, alloc=None, timesteps=None):
     return plan.forward_projected(X, Wqkv, Wo, out, alloc, timesteps)
+
+
+def ff_forward_projected_rotary(plan: Plan, X, Wqkv, Wo, out, rotary: Rotary, wq=None, wk=None, eps=0.0, positions=None, alloc=None,
+                                timesteps=None):
+    return plan.forward_projected(X, Wqkv, Wo, out, alloc, timesteps, rotary, wq, wk, eps, positions)
+
+
+def ff_rotary_create(cfg: RotaryConfig) -> Rotary:
+    return Rotary(cfg)
+
+
+def ff_rotary_apply(rotary: Rotary, q, q_out, k=None, k_out=None, positions=None, inverse=False):
+    return rotary.apply(q, q_out, k, k_out, positions, inverse)
+
+
+def ff_qk_norm(rotary: Rotary, q, k, wq, wk, q_out, k_out, eps=1e-6, positions=None):
+    return rotary.qk_norm(q, k, wq, wk, q_out, k_out, eps, positions)
+
+
+def ff_qk_norm_backward(rotary: Rotary, q, k, wq, wk, dq_out, dk_out, dq, dk, dwq=None, dwk=None, eps=1e-6, positions=None):
+    return rotary.qk_norm_backward(q, k, wq, wk, dq_out, dk_out, dq, dk, dwq, dwk, eps, positions)
+
+
+def ff_ffn_create(cfg: FFNConfig, device="cuda:0") -> GatedFFN:
+    return GatedFFN(cfg, device)
+
+
+def ff_ffn_forward(ffn: GatedFFN, X, Wg, Wu, Wd, out, gate=None, up=None):
+    return ffn.forward(X, Wg, Wu, Wd, out, gate, up)
+
+
+def ff_ffn_backward(ffn: GatedFFN, X, Wg, Wu, Wd, gate, up, dout, dX=None, dWg=None, dWu=None, dWd=None):
+    return ffn.backward(X, Wg, Wu, Wd, gate, up, dout, dX, dWg, dWu, dWd)
 
 
 def ff_high_attention_noalloc(q, k, v, y, radius: int, sync: bool = True):

@@ -485,8 +485,17 @@ extern "C" ff_status_t ff_forward(ff_plan_t* p, const void* Q, const void* K, co
   return FF_OK;
 }
 
-extern "C" ff_status_t ff_forward_projected(ff_plan_t* p, const void* X, const void* Wqkv, const void* Wo,
-                                            const uint8_t* alloc_dev, const float* timestep, void* out, void* stream) {
+// What stands between the projections and the attention of a call.
+struct QKRotary {
+  const ff_rotary_t* rotary;
+  const int32_t* positions;
+  int64_t position_stride;
+  const float *wq, *wk;
+  float eps;               // 0: no norm
+};
+
+static ff_status_t forward_projected(ff_plan_t* p, const void* X, const void* Wqkv, const void* Wo, const QKRotary* qk,
+                                     const uint8_t* alloc_dev, const float* timestep, void* out, void* stream) {
   if (!p) return fail(nullptr, FF_ERR_INVALID_ARG, "plan is NULL%s");
   if (!X || !Wqkv || !Wo || !out) return fail(p, FF_ERR_INVALID_ARG, "X, Wqkv, Wo or out is NULL%s");
   if ((((uintptr_t)X) | ((uintptr_t)Wqkv) | ((uintptr_t)Wo) | ((uintptr_t)out)) & 15)
@@ -496,13 +505,44 @@ extern "C" ff_status_t ff_forward_projected(ff_plan_t* p, const void* X, const v
   if (!ffk_proj_supported(p->dm))
     return fail(p, FF_ERR_UNSUPPORTED, "projections need bf16, head_dim 64 or 128, tokens %% 128 == 0 and heads * head_dim %% 256 == 0%s");
   if (!alloc_dev && !timestep) return fail(p, FF_ERR_NOT_ROUTED, "neither an allocation nor a timestep was given%s");
+  const FFDims& dm = p->dm;
+  const bool norm = qk && qk->eps != 0.f;
+  if (qk) {
+    if (!qk->rotary) return fail(p, FF_ERR_INVALID_ARG, "rotary is NULL%s");
+    const ff_rotary_config_t& c = *ffk_rotary_config(qk->rotary);
+    if (c.head_dim != dm.d || c.dtype != FF_BF16) return fail(p, FF_ERR_INVALID_ARG, "the rotary handle is for another head_dim or type%s");
+    const bool axes = c.axis_pairs[0] || c.axis_pairs[1] || c.axis_pairs[2];
+    if (!qk->positions && axes && (c.grid[0] != dm.T || c.grid[1] != dm.H || c.grid[2] != dm.W))
+      return fail(p, FF_ERR_INVALID_ARG, "without positions the rotary handle's grid must be the plan's%s");
+    if (!norm && (qk->wq || qk->wk)) return fail(p, FF_ERR_INVALID_ARG, "norm weights need an eps above 0%s");
+    if (norm && !(qk->eps > 0.f && qk->eps < 3.0e38f)) return fail(p, FF_ERR_INVALID_ARG, "eps must be positive and finite, or 0 for no norm%s");
+  }
   cudaStream_t st = (cudaStream_t)stream;
   FF_CUDA(p, ffk_project_qkv(p, X, Wqkv, p->buf.stage_q, p->buf.stage_k, p->buf.stage_v, st));
+  if (qk) {
+    const int64_t row = dm.d, head = row * dm.N;
+    const ff_heads_t q = {p->buf.stage_q, head * dm.heads, head, row, dm.heads}, k = {p->buf.stage_k, head * dm.heads, head, row, dm.heads};
+    const ff_status_t s = norm ? ff_qk_norm(qk->rotary, dm.B, dm.N, qk->positions, qk->position_stride, &q, &k, qk->wq, qk->wk, qk->eps, &q, &k, st)
+                               : ff_rotary_apply(qk->rotary, dm.B, dm.N, qk->positions, qk->position_stride, &q, &k, 0, &q, &k, st);
+    if (s != FF_OK) return fail(p, s, "%s", ff_rotary_last_error(qk->rotary));
+  }
   ff_status_t s = ff_forward(p, p->buf.stage_q, p->buf.stage_k, p->buf.stage_v, alloc_dev, timestep, p->buf.stage_out, st);
   if (s != FF_OK) return s;
   FF_CUDA(p, ffk_project_out(p, p->buf.stage_out, Wo, out, st));
-  p->launches += 1;                                 // (ff_forward restarted the count: add the first projection)
+  p->launches += qk ? 2 : 1;                        // (ff_forward restarted the count: add what stands in front of it)
   return FF_OK;
+}
+
+extern "C" ff_status_t ff_forward_projected(ff_plan_t* p, const void* X, const void* Wqkv, const void* Wo,
+                                            const uint8_t* alloc_dev, const float* timestep, void* out, void* stream) {
+  return forward_projected(p, X, Wqkv, Wo, nullptr, alloc_dev, timestep, out, stream);
+}
+
+extern "C" ff_status_t ff_forward_projected_rotary(ff_plan_t* p, const void* X, const void* Wqkv, const void* Wo, const ff_rotary_t* rotary,
+                                                   const int32_t* positions, int64_t position_stride, const float* wq, const float* wk,
+                                                   float eps, const uint8_t* alloc_dev, const float* timestep, void* out, void* stream) {
+  const QKRotary qk = {rotary, positions, position_stride, wq, wk, eps};
+  return forward_projected(p, X, Wqkv, Wo, &qk, alloc_dev, timestep, out, stream);
 }
 
 extern "C" ff_status_t ff_forward_host(ff_plan_t* p, const void* Qh, const void* Kh, const void* Vh,

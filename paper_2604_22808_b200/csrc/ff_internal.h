@@ -318,6 +318,8 @@ cudaError_t ffk_dct_t16_inverse(ff_plan* p, const void* in_hi, const void* in_lo
 bool ffk_proj_supported(const FFDims& dm);
 cudaError_t ffk_project_qkv(ff_plan* p, const void* X, const void* Wqkv, void* Q, void* K, void* V, cudaStream_t st);
 cudaError_t ffk_project_out(ff_plan* p, const void* O, const void* Wo, void* out, cudaStream_t st);
+// ---- queries and keys between the projections and the attention (ff_rotary.cu) ----------------------------
+const ff_rotary_config_t* ffk_rotary_config(const ff_rotary_t* rotary);
 // ---- summary tokens and the low band's part of the exchange (ff_summary.cu) ----------------------------
 int ffk_summary_pieces(const FFDims& dm);
 bool ffk_low_in_summary(const ff_plan* p);     // the summary launch computes the (short) pooled low band's attention too

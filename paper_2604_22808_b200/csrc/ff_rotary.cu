@@ -74,24 +74,12 @@ template <> struct Word<2> { using type = unsigned short; };
 template <class T, int CH> using Chunk = typename Word<sizeof(T) * CH>::type;
 
 // Two fp32 values in one 64-bit register: the arithmetic below takes an instruction for both.
-using F2 = unsigned long long;
-__device__ __forceinline__ F2 two(float lo, float hi) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ float low(F2 v) { return __uint_as_float((unsigned)v); }
-__device__ __forceinline__ float high(F2 v) { return __uint_as_float((unsigned)(v >> 32)); }
-__device__ __forceinline__ F2 mul(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
+using F2 = float2;
+__device__ __forceinline__ F2 two(float lo, float hi) { return make_float2(lo, hi); }
+__device__ __forceinline__ float low(F2 v) { return v.x; }
+__device__ __forceinline__ float high(F2 v) { return v.y; }
+__device__ __forceinline__ F2 mul(F2 a, F2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) { return __ffma2_rn(a, b, c); }
 
 // A chunk as pairs of neighbouring channels (CH = 1: one value and a zero).
 __host__ __device__ constexpr int pairs_of(int ch) { return (ch + 1) / 2; }
@@ -160,7 +148,7 @@ __device__ __forceinline__ void turn(F2 (&a)[pairs_of(CH)], F2 (&b)[pairs_of(CH)
 
 template <int N, int PER>
 __device__ __forceinline__ float dot(const F2 (&x)[PER][N], const F2 (&y)[PER][N], const F2 (&u)[PER][N], const F2 (&v)[PER][N]) {
-  F2 s = 0, t = 0;
+  F2 s = two(0.f, 0.f), t = s;
 #pragma unroll
   for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -256,7 +244,7 @@ __device__ __forceinline__ void turn_of_token(const HeadsParams& P, const Own<CH
   for (int i = 0; i < PER; ++i)
 #pragma unroll
     for (int c = 0; c < pairs_of(CH); ++c) {
-      k[i].p[c] = k[i].q[c] = k[i].r[c] = k[i].t[c] = 0;
+      k[i].p[c] = k[i].q[c] = k[i].r[c] = k[i].t[c] = two(0.f, 0.f);
       float c0, s0, c1 = 0.f, s1 = 0.f;
       if constexpr (INTER) {
         if (own.ta[i]) {
@@ -479,7 +467,7 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __gr
     for (int c = 0; c < N; ++c) {
       wa[i][c] = own.weights(P.w[t], i, own.oa[i], c);
       wb[i][c] = own.weights(P.w[t], i, own.ob[i], c);
-      da[i][c] = db[i][c] = 0;
+      da[i][c] = db[i][c] = two(0.f, 0.f);
     }
 
   int asked = 0;
@@ -791,6 +779,8 @@ ff_status_t run(const ff_rotary_t* handle, int mode, int64_t batch, int64_t toke
 }
 
 }  // namespace
+
+const ff_rotary_config_t* ffk_rotary_config(const ff_rotary_t* rotary) { return &rotary->cfg; }
 
 extern "C" ff_status_t ff_rotary_create(const ff_rotary_config_t* cfg, ff_rotary_t** out) {
   if (!cfg || !out) return fail(nullptr, FF_ERR_INVALID_ARG, "cfg or out is NULL");
