@@ -365,8 +365,9 @@ ff_status_t ff_forward_projected_rotary(ff_plan_t *plan, const void *X, const vo
  * The hidden activations (and, backward, the gradients of gate and up) are rounded to bf16 between the products; the
  * accumulators and the activation are fp32.  Any number of tokens, one and zero included.
  *
- * A handle belongs to the device that was current at ff_ffn_create and holds a status word there; calls are
- * asynchronous on the given stream, which has to be one of that device, the current one.  The caller owns the workspace
+ * A handle belongs to the device that was current at ff_ffn_create and holds a status word there; like a plan it is
+ * not thread-safe, and it has to outlive the graphs its calls are captured into.  Calls are asynchronous on the
+ * given stream, which has to be one of that device, the current one.  The caller owns the workspace
  * (device, 256-byte aligned); calls that may run at the same time need one each. */
 typedef struct ff_ffn ff_ffn_t; /* opaque */
 

@@ -565,6 +565,8 @@ class GatedFFN:
         with torch.cuda.device(self.device):
             _check(library().ff_ffn_create(C.byref(c), C.byref(self.handle)))
         self._sized, self._bytes = None, 0                       # the workspace's size for the last number of tokens
+        self._lib, self._bf16, self._uint8 = library(), torch.bfloat16, torch.uint8
+        self._into, self._back = torch.Size((cfg.dim, cfg.hidden)), torch.Size((cfg.hidden, cfg.dim))
         self._raw_stream = _stream_getter(torch)
 
     def destroy(self):
@@ -582,30 +584,34 @@ class GatedFFN:
         if status != FF_OK:
             raise FFError(status, library().ff_ffn_last_error(self.handle).decode())
 
-    def _tokens(self, X, Wg, Wu, Wd) -> int:
-        D, F = self.cfg.dim, self.cfg.hidden
-        if X.dim() < 1 or X.shape[-1] != D:
-            raise FFError(1, f"expected X of shape [...][{D}]")
-        self._tensors((D, F), Wg, Wu)
-        self._tensors((F, D), Wd)
-        return X.numel() // D
-
-    def _tensors(self, shape, *tensors):
-        """They are bf16, contiguous, of that shape and here (None: not given)."""
-        bf16, device = self._torch.bfloat16, self.device
-        for t in tensors:
-            if t is not None and (t.shape != shape or t.dtype != bf16 or t.device != device or not t.is_contiguous()):
+    def _pointers(self, *tensors):
+        """Addresses of (tensor or None, shape) in turns: bf16, contiguous, of that shape and here."""
+        bf16, device, at = self._bf16, self.device, []
+        for t, shape in zip(tensors[::2], tensors[1::2]):
+            if t is None:
+                at.append(None)
+                continue
+            if t.shape != shape or t.dtype != bf16 or t.device != device or not t.is_contiguous():
                 raise FFError(1, f"expected a contiguous bf16 tensor of shape {tuple(shape)} on {device}")
+            at.append(t.data_ptr())
+        return at
 
-    def _call(self, fn, training, tokens, *pointers):
+    def _shapes(self, X):
+        """Number of tokens, shape of X and of the hidden activations."""
+        xs = X.shape
+        if not xs or xs[-1] != self.cfg.dim:
+            raise FFError(1, f"expected X of shape [...][{self.cfg.dim}]")
+        return X.numel() // self.cfg.dim, xs, xs[:-1] + (self.cfg.hidden,)
+
+    def _call(self, fn, training, tokens, pointers):
         torch, dev = self._torch, self.device
-        # (a workspace per call: calls on different streams and captured graphs share none)
         if self._sized != (tokens, training):
             size = C.c_size_t()
             _check(library().ff_ffn_workspace_bytes(C.byref(self._c), tokens, training, C.byref(size)))
             self._sized, self._bytes = (tokens, training), size.value
         n = self._bytes
-        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        # (a workspace per call: calls on different streams and captured graphs share none)
+        ws = torch.empty(n, dtype=self._uint8, device=dev)
         if torch.cuda.current_device() == dev.index:
             return self._status(fn(self.handle, tokens, *pointers, ws.data_ptr(), n, self._raw_stream(dev.index)))
         with torch.cuda.device(dev):
@@ -613,22 +619,17 @@ class GatedFFN:
 
     def forward(self, X, Wg, Wu, Wd, out, gate=None, up=None):
         """gate, up [..., hidden]: X Wg and X Wu are written there, for backward."""
-        M = self._tokens(X, Wg, Wu, Wd)
-        self._tensors(X.shape, X, out)
-        self._tensors(X.shape[:-1] + (self.cfg.hidden,), gate, up)
-        p = [None if t is None else t.data_ptr() for t in (X, Wg, Wu, Wd, gate, up, out)]
-        self._call(library().ff_ffn_forward, False, M, *p)
+        M, xs, hs = self._shapes(X)
+        into, back = self._into, self._back
+        self._call(self._lib.ff_ffn_forward, False, M, self._pointers(X, xs, Wg, into, Wu, into, Wd, back, gate, hs, up, hs, out, xs))
         return out
 
     def backward(self, X, Wg, Wu, Wd, gate, up, dout, dX=None, dWg=None, dWu=None, dWd=None):
         """Gradients of X and the weights, where given, from that of out (dWg and dWu together)."""
-        M = self._tokens(X, Wg, Wu, Wd)
-        self._tensors(X.shape, X, dout, dX)
-        self._tensors(X.shape[:-1] + (self.cfg.hidden,), gate, up)
-        self._tensors(Wg.shape, dWg, dWu)
-        self._tensors(Wd.shape, dWd)
-        p = [None if t is None else t.data_ptr() for t in (X, Wg, Wu, Wd, gate, up, dout, dX, dWg, dWu, dWd)]
-        self._call(library().ff_ffn_backward, True, M, *p)
+        M, xs, hs = self._shapes(X)
+        into, back = self._into, self._back
+        self._call(self._lib.ff_ffn_backward, True, M, self._pointers(X, xs, Wg, into, Wu, into, Wd, back, gate, hs, up, hs, dout, xs, dX, xs,
+                                                                      dWg, into, dWu, into, dWd, back))
         return dX, dWg, dWu, dWd
 
     def device_status(self) -> int:

@@ -94,11 +94,13 @@ __device__ __forceinline__ float activation(float g, float* slope) {
     return g * s;
   }
   else {
-    const float p = 0.5f * erfcf(-0.70710678118654752f * g);
-    if (SLOPE) {
-      const float t = fminf(fmaxf(g, -32.f), 32.f);
-      *slope = p + t * 0.3989422804014327f * exponential(-0.5f * t * t);
-    }
+    // 1 - Phi(|g|) = e^(-x^2) (a1 t + .. + a5 t^5) / 2, x = |g| / sqrt 2, t = 1 / (1 + 0.3275911 x), to 0.75e-7: Abramowitz and
+    // Stegun, "Handbook of Mathematical Functions", 7.1.26.  Its exponential is the one of the derivative.  (With erfcf the launches
+    // of dH and dWd took 276 us instead of 249: 16384 tokens, dim and hidden 2048.)
+    const float x = 0.70710678118654752f * fabsf(g), t = rcp(fmaf(0.3275911f, x, 1.f)), e = exponential(-x * x);
+    const float h = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float p = g < 0.f ? h : 1.f - h;
+    if (SLOPE) *slope = p + fminf(fmaxf(g, -32.f), 32.f) * 0.3989422804014327f * e;
     return g * p;
   }
 }
@@ -169,6 +171,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const int tiles = P.m_tiles * P.n_tiles * P.mats, items = tiles * P.split;
 
+  if (threadIdx.x < 4) tma_prefetch_desc(threadIdx.x < 2 ? &maps.a[threadIdx.x] : &maps.b[threadIdx.x - 2]);
   if (threadIdx.x == 0) {
     for (int i = 0; i < NSTAGE; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.acc_full[i], 1); mbar_init(&sh.acc_empty[i], 2 * EPI_WARPS); }
@@ -485,6 +488,10 @@ ffn_few_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
   const int k_begin = (int)((long long)P.kchunks * rank / split), k_end = (int)((long long)P.kchunks * (rank + 1) / split);
   const uint32_t columns = MATS * P.nt < 32 ? 32 : MATS * P.nt;
 
+  if (threadIdx.x == 32) {
+    tma_prefetch_desc(&map_w0); tma_prefetch_desc(&map_x);
+    if (EPI == GATE) tma_prefetch_desc(&map_w1);
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < P.stages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
     mbar_init(&sh.done, 1);
@@ -668,9 +675,12 @@ size_t sums_bytes(const Product& p) {
 template <bool A_MN, bool B_MN, int EPI>
 cudaError_t gemm(const ff_ffn* h, const Matrix (&a)[2], const Matrix (&b)[2], std::initializer_list<const void*> e, GemmParams P, cudaStream_t st) {
   GemmMaps m;
-  for (int i = 0; i < 2; ++i)
-    if (!matrix_map(h, &m.a[i], a[i].p, a[i].rows, a[i].cols, A_MN ? 64 : 128) || !matrix_map(h, &m.b[i], b[i].p, b[i].rows, b[i].cols, B_MN ? 64 : 128))
-      return cudaErrorInvalidValue;
+  for (int i = 0; i < 2; ++i) {
+    if (i && a[1].p == a[0].p) m.a[1] = m.a[0];
+    else if (!matrix_map(h, &m.a[i], a[i].p, a[i].rows, a[i].cols, A_MN ? 64 : 128)) return cudaErrorInvalidValue;
+    if (i && b[1].p == b[0].p) m.b[1] = m.b[0];
+    else if (!matrix_map(h, &m.b[i], b[i].p, b[i].rows, b[i].cols, B_MN ? 64 : 128)) return cudaErrorInvalidValue;
+  }
   int n = 0;
   for (const void* p : e)
     if (!(EPI == PARTIAL ? sums_map(h, &m.e[n++], p, P.rows, P.cols, P.mats * P.split) : matrix_map(h, &m.e[n++], p, P.rows, P.cols, 32)))
@@ -721,13 +731,15 @@ FewShape few_shape(const ff_ffn* h, long long tokens, int features, int kchunks,
   s.f_tiles = (features + 127) / 128;
   s.t_tiles = (int)((tokens + s.nt - 1) / s.nt);
   const long long tiles = (long long)s.f_tiles * s.t_tiles;
-  s.us = 0;
+  s.us = 1e30;
+  s.split = 1;
+  if (s.t_tiles > 65535) return s;                              // (more than a grid has)
   for (int split = 1; split <= 8 && split <= kchunks; ++split) {
     const int room = h->room[mats - 1][s.nt == 128][split];
     if (room < split) continue;
     const double us = 1 + (double)((tiles * split + room - 1) / room) * ((kchunks + split - 1) / split) * (mats == 2 ? 0.5 : 0.35) +
                       (split > 1 ? 0.02 * mats * (double)(tokens < s.nt ? tokens : s.nt) : 0);
-    if (split == 1 || us < s.us) { s.split = split; s.us = us; }
+    if (us < s.us) { s.split = split; s.us = us; }
   }
   return s;
 }
@@ -736,8 +748,9 @@ template <int EPI>
 cudaError_t few(const ff_ffn* h, const FewShape& s, const void* w0, const void* w1, const void* x, long long tokens, int features, int k,
                 void* const (&out)[3], cudaStream_t st) {
   CUtensorMap m[3];
-  if (!matrix_map(h, &m[0], w0, k, features, 64) || !matrix_map(h, &m[1], w1, k, features, 64) || !matrix_map(h, &m[2], x, tokens, k, s.nt))
-    return cudaErrorInvalidValue;
+  if (!matrix_map(h, &m[0], w0, k, features, 64) || !matrix_map(h, &m[2], x, tokens, k, s.nt)) return cudaErrorInvalidValue;
+  if (EPI != GATE) m[1] = m[0];
+  else if (!matrix_map(h, &m[1], w1, k, features, 64)) return cudaErrorInvalidValue;
   FewParams P{};
   P.tokens = (int)tokens; P.cols = features; P.kchunks = chunks(k);
   P.nt = s.nt;
@@ -893,7 +906,7 @@ extern "C" ff_status_t ff_ffn_forward(ff_ffn_t* h, int64_t tokens, const void* X
   const int D = h->cfg.dim, F = h->cfg.hidden;
   cudaStream_t st = (cudaStream_t)stream;
   const Matrix x{X, tokens, D}, hid{ws, tokens, F}, wg{Wg, D, F}, wu{Wu, D, F}, wd{Wd, F, D};
-  // Either product runs on the kernel whose estimate is lower.  Measured, dim 2048, hidden 5632, both products on tiles of 256
+  // Either product runs on the kernel whose estimate is lower (2 us more for start and end of the larger one).  Measured, dim 2048, hidden 5632, both products on tiles of 256
   // tokens / on the few-token kernel, us: 1 token 34.0 / 21.1, 64 tokens 31.6 / 25.2, 128 32.7 / 35.9, 512 46.5 / 64.3; dim 1024, hidden
   // 2816, product with Wd: 400 tokens 25.9 / 21.5, 768 27.8 / 32.4.
   const FewShape up_few = few_shape(h, tokens, F, chunks(D), 2), down_few = few_shape(h, tokens, D, chunks(F), 1);
@@ -901,7 +914,8 @@ extern "C" ff_status_t ff_ffn_forward(ff_ffn_t* h, int64_t tokens, const void* X
   const long long up_tiles = ((tokens + TM - 1) / TM) * ((F + 127) / 128);
   double down_us;
   split_of(down, &down_us);
-  const double up_us = 0.28 * chunks(D) * (double)((up_tiles + FF_B200_SMS / 2 - 1) / (FF_B200_SMS / 2));
+  down_us += 2;
+  const double up_us = 2 + 0.28 * chunks(D) * (double)((up_tiles + FF_B200_SMS / 2 - 1) / (FF_B200_SMS / 2));
   if (up_few.us < up_us) {
     FFN_CUDA(h, few<GATE>(h, up_few, Wg, Wu, X, tokens, F, D, {ws, gate, up}, st));
   } else {

@@ -142,6 +142,33 @@ def test_many_tiles():
     check_forward(100, 1032, 40000, "silu", False)
 
 
+@pytest.mark.parametrize("M,D,F", [(4100, 64, 72), (700, 136, 2056), (2500, 264, 520), (520, 64, 8200)])
+def test_parts_of_k(M, D, F):
+    """Few tiles and a long K: the sums of its parts, joined in a second launch, in each product that has such a K."""
+    check_forward(M, D, F, "silu", False)
+    check_backward(M, D, F, "gelu")
+
+
+def test_far_rows():
+    """Hidden activations beyond 2^31 elements: the last tokens against the formula, and a batch of them alone."""
+    M, D, F = 70000, 8, 31000
+    X, Wg, Wu, Wd, dout = inputs(M, D, F)
+    ffn = B.GatedFFN(FFNConfig(D, F))
+    out, dX = torch.empty_like(X), torch.empty_like(X)
+    gate, up = (torch.empty(M, F, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ffn.forward(X, Wg, Wu, Wd, out, gate, up)
+    last = slice(M - 300, M)
+    want = forward_bounds("silu", X[last], Wg, Wu, Wd)
+    within(out[last], *want[0], "out")
+    within(gate[last], *want[1], "gate")
+    within(up[last], *want[2], "up")
+    ffn.backward(X, Wg, Wu, Wd, gate, up, dout, dX)
+    few, g, u = torch.empty_like(X[last]), gate[last].clone(), up[last].clone()
+    ffn.backward(X[last], Wg, Wu, Wd, g, u, dout[last], few)
+    # (the same sums in parts of K or in one: fp32 sums of 2 F products each, rounded to bf16)
+    within(dX[last], few.double(), 2 * STEP * few.double().abs() + 1e-2, "dX")
+
+
 def test_shapes_and_empty():
     X, Wg, Wu, Wd, dout = inputs(24, 64, 128)
     ffn = B.GatedFFN(FFNConfig(64, 128))
