@@ -18,7 +18,8 @@
 // Threads: a row is cut in chunks of CH channels (16 bytes where strides, rot_dim and head_dim allow, else 8, 4 or 2), and a
 // thread owns two chunks of it so that both channels of a pair are its own: no exchange between threads for the rotation.
 //   half layout          chunk j of the first half of the turned channels and chunk j of the second; the channels that are not
-//                        turned follow in neighbouring chunks
+//                        turned follow in the same manner, so that neighbouring lanes have neighbouring chunks (two chunks of
+//                        a lane side by side, every lane half a sector: 11000 tokens, 12 + 4 fp32 heads of 80, 28 us instead of 25)
 //   interleaved layout   chunk j of the first half of the row and chunk j of the second: pairs lie inside a chunk
 // A row takes L = 2^k lanes (8 for 128 bf16 channels), a warp 32 / L tokens at a time.
 #include <math.h>
@@ -43,7 +44,7 @@ namespace {
 
 enum { ROTATE = 0, NORM = 1, NORM_BACKWARD = 2 };
 constexpr int H_THREADS = 256, H_WARPS = H_THREADS / 32;
-constexpr int FORWARD_WAVES = 8;
+constexpr int FORWARD_WAVES = 8;                  // waves of blocks that a large forward launch is cut in
 constexpr int FORWARD_BLOCKS = 2;                 // blocks of a forward launch on an SM
 constexpr int PARTIAL_ROWS = 2 * FF_B200_SMS;     // rows of partial weight gradients at most: one wave of two blocks per SM
 
@@ -192,8 +193,8 @@ struct Own {
       } else {
         const int turned = P.rot / (2 * CH);
         ta[i] = tb[i] = have[i] && j < turned;
-        oa[i] = j < turned ? j * CH : P.rot + 2 * (j - turned) * CH;
-        ob[i] = j < turned ? P.rot / 2 + j * CH : oa[i] + CH;
+        oa[i] = j < turned ? j * CH : P.rot + (j - turned) * CH;
+        ob[i] = j < turned ? P.rot / 2 + j * CH : oa[i] + (P.d - P.rot) / 2;
       }
     }
   }
@@ -303,9 +304,12 @@ struct Walk {
   }
 };
 
-// Forward.  One wave of blocks; a unit is two heads of q, or of k behind them: the rotation of a thread's pairs of one token stays in
+// Forward.  A unit is two heads of q, or of k behind them: the rotation of a thread's pairs of one token stays in
 // its registers for all heads.  The rows on their way wait in shared memory, each thread's pieces in places of its own, two units ahead,
 // from one group into the next.  (Rows of two-byte pieces, which cannot be copied that way, are loaded when they are needed.)
+// Bound by memory: 64K tokens, 16 + 16 heads of 64 turned in 82 us = 6.5 TB/s, 24 + 24 heads of 128 normed in 258 = 6.2 TB/s.  (Loaded
+// into registers, four heads at a time, by blocks of 32 tokens and up to 24 heads: 87 and 262, but 16.7 us instead of 6.6 for 6855 tokens of
+// 4 + 2 heads of 128, where such blocks are few or each compute the angles again.)
 template <class T, int CH, int PER, bool INTER, int MODE>
 __global__ void __launch_bounds__(H_THREADS, FORWARD_BLOCKS) heads_kernel(const __grid_constant__ HeadsParams P) {
   constexpr int N = pairs_of(CH), U = 2;
@@ -441,7 +445,8 @@ __global__ void __launch_bounds__(H_THREADS, FORWARD_BLOCKS) heads_kernel(const 
 
 // Backward.  One wave of blocks, divided between q and k by their heads.  Weights, their gradients and the rotation fill the registers, so the rows on their way wait
 // in shared memory, each thread's pieces in places of its own: two units ahead, from one group into the next.  (Rows of two-byte pieces,
-// which cannot be copied that way, are loaded when they are needed.)
+// which cannot be copied that way, are loaded when they are needed.)  Instructions and memory together bound it: 2 x 8191 tokens, 32 + 8 heads
+// of 128, 89 us = 5.7 TB/s at 60 % of the issue slots; with the rows of two heads at a time in registers 105.
 template <class T, int CH, int PER, bool INTER>
 __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __grid_constant__ HeadsParams P) {
   constexpr int N = pairs_of(CH);
@@ -761,6 +766,10 @@ ff_status_t run(const ff_rotary_t* handle, int mode, int64_t batch, int64_t toke
     grid = dim3((unsigned)(n0 + n1));
   } else {
     const long long units = (long long)P.groups * ((P.heads[0] + 1) / 2 + (P.heads[1] + 1) / 2);
+    // Runs of 16 units where there are eight waves of blocks of that many, shorter ones down to 8 units where there are not, and one wave
+    // of equal runs where those would be fewer.  The SMs are not served by memory equally fast, so one wave of equal runs waits for the
+    // last (64K tokens, 24 + 24 heads of 128 normed: 297 us in one wave, 258 in runs of 16; 16 + 16 heads of 64 turned: 95 and 82); a run has
+    // to pay for its first token's angles and first loads (18228 tokens, 8 + 8 heads of 80 turned: 19.8 us in runs of 8, 23 of 4, 30 of 2).
     const long long wave = FORWARD_BLOCKS * FF_B200_SMS;
     long long each = units / (FORWARD_WAVES * wave);
     each = each < 8 ? 8 : each > 16 ? 16 : each;
