@@ -85,15 +85,13 @@ __device__ __forceinline__ float activation(float g, float* slope) {
     const float s = sigmoid(g);
     if (SLOPE) *slope = s * (1.f + g * (1.f - s));
     return g * s;
-  }
-  else if constexpr (ACT == FF_ACT_GELU_TANH) {
+  } else if constexpr (ACT == FF_ACT_GELU_TANH) {
     const float c = 1.5957691216057308f;         // 2 sqrt(2 / pi)
-    const float t = fminf(fmaxf(g, -16.f), 16.f), t2 = t * t;
+    const float t = g != g ? g : fminf(fmaxf(g, -16.f), 16.f), t2 = t * t;
     const float s = sigmoid(c * t * (1.f + 0.044715f * t2));
     if (SLOPE) *slope = s + t * s * (1.f - s) * c * (1.f + 0.134145f * t2);
     return g * s;
-  }
-  else {
+  } else {
     // 1 - Phi(|g|) = e^(-x^2) (a1 t + .. + a5 t^5) / 2, x = |g| / sqrt 2, t = 1 / (1 + 0.3275911 x), to 0.75e-7: Abramowitz and
     // Stegun, "Handbook of Mathematical Functions", 7.1.26.  Its exponential is the one of the derivative.  (With erfcf the launches
     // of dH and dWd took 276 us instead of 249: 16384 tokens, dim and hidden 2048.)

@@ -225,6 +225,25 @@ def test_special_values(M):
         assert all(g.isfinite().all() for g in grads)
 
 
+@pytest.mark.parametrize("activation", ("silu", "gelu_tanh", "gelu"))
+def test_nan_in_the_hidden_activations(activation):
+    """A NaN among the kept activations reaches its token's dX and its hidden unit's weights, and nothing else."""
+    M, D, F = 140, 72, 200
+    X, Wg, Wu, Wd, dout = inputs(M, D, F)
+    gate, up = X @ Wg, X @ Wu
+    ffn = B.GatedFFN(FFNConfig(D, F, activation))
+    clean, got = ([torch.empty_like(t) for t in (X, Wg, Wu, Wd)] for _ in range(2))
+    ffn.backward(X, Wg, Wu, Wd, gate, up, dout, *clean)
+    gate[131, 77] = math.nan
+    ffn.backward(X, Wg, Wu, Wd, gate, up, dout, *got)
+    for a, b, (axis, at) in zip(clean, got, ((0, 131), (1, 77), (1, 77), (0, 77))):
+        assert b.select(axis, at).isnan().all()
+        keep = torch.ones(b.shape[axis], dtype=torch.bool, device="cuda")
+        keep[at] = False
+        keep = keep.nonzero().flatten()
+        assert torch.equal(a.index_select(axis, keep), b.index_select(axis, keep))
+
+
 def test_gradient_against_differences():
     """The four gradients against central differences of the formula in 64 bits along random directions: the difference of the
     formula is exact to h^2, and a gradient's own error along a direction is below its bound of test_backward; 2 % of the
