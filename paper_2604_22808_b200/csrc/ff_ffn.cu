@@ -41,10 +41,10 @@ struct ff_ffn {
 
 namespace {
 
-constexpr int TM = 256, TN = 256, TK = 64;
+constexpr int TM = 256, TN = 256, TK = 64;     // (a narrow tile: 128 columns)
 constexpr int PIECE = 64 * 128;                  // 64 rows of 128 bytes
 constexpr int OPERAND = 2 * PIECE;               // one CTA's 128 rows (or columns) of a K chunk
-constexpr int STAGE = 2 * OPERAND;
+__host__ __device__ constexpr int stage_bytes(int nt) { return OPERAND + nt / 2 * 128; }
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 
@@ -73,7 +73,7 @@ struct Shared {
   int abort_flag;
 };
 inline int chunks(long long k) { return (int)((k + TK - 1) / TK); }
-__host__ __device__ constexpr size_t smem_bytes(int epi) { return (size_t)ring_stages(epi) * STAGE + (size_t)EPI_WARPS * areas(epi) * AREA + sizeof(Shared) + 1024; }
+__host__ __device__ constexpr size_t smem_bytes(int epi, int nt = TN) { return (size_t)ring_stages(epi) * stage_bytes(nt) + (size_t)EPI_WARPS * areas(epi) * AREA + sizeof(Shared) + 1024; }
 static_assert(smem_bytes(STORE) <= 232448 && smem_bytes(GATE) <= 232448 && smem_bytes(DGATE) <= 232448, "227 KB a block");
 
 // act(g) and, with SLOPE, its derivative.  The cubic inside gelu_tanh saturates long before |g| = 16.
@@ -157,10 +157,10 @@ __device__ __forceinline__ void part_of_k(const GemmParams& P, int part, int& be
   end = begin + q + (part < r);
 }
 
-template <bool A_MN, bool B_MN, int EPI>
+template <bool A_MN, bool B_MN, int EPI, int NT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
-  constexpr int NSTAGE = ring_stages(EPI), AREAS = areas(EPI);
+  constexpr int NSTAGE = ring_stages(EPI), AREAS = areas(EPI), STAGE = stage_bytes(NT);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   Shared& sh = *(Shared*)(smem + NSTAGE * STAGE + EPI_WARPS * AREAS * AREA);
@@ -177,7 +177,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
     sh.abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 1) { tmem_alloc_pair(&sh.tmem_base, 512); tmem_relinquish_pair(); }
+  if (warp == 1) { tmem_alloc_pair(&sh.tmem_base, 2 * NT); tmem_relinquish_pair(); }
   tc_fence_before();
   __syncthreads();
   cluster_sync();                                               // the other CTA's barriers are there
@@ -193,7 +193,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
       for (int t = pair; t < items && ok; t += pairs) {
         const Item w = item_of(P, t);
         const int m0 = w.m * TM + (int)rank * 128;
-        const int n0 = EPI == GATE ? w.n * 128 : w.n * TN + (int)rank * 128;
+        const int n0 = EPI == GATE ? w.n * (NT / 2) : w.n * NT + (int)rank * (NT / 2);
         int k_begin, k_end;
         part_of_k(P, w.part, k_begin, k_end);
         for (int kc = k_begin; kc < k_end && ok; ++kc, ++n) {
@@ -214,7 +214,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
           }
           if (B_MN) {
             tma_load_3d_pair(dst + OPERAND, mb, bar, n0, k0, 0);
-            tma_load_3d_pair(dst + OPERAND + PIECE, mb, bar, n0 + 64, k0, 0);
+            if (NT == 256) tma_load_3d_pair(dst + OPERAND + PIECE, mb, bar, n0 + 64, k0, 0);
           } else {
             tma_load_3d_pair(dst + OPERAND, mb, bar, k0, n0, 0);
           }
@@ -223,7 +223,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
     }
   } else if (warp == 1) {
     if (rank == 0) {
-      const uint32_t idesc = idesc_bf16_f32(TM, TN, A_MN, B_MN);
+      const uint32_t idesc = idesc_bf16_f32(TM, NT, A_MN, B_MN);
       const uint64_t a0 = smem_desc_sw128(smem_u32(smem), A_MN ? PIECE : 16, 1024);
       const uint64_t b0 = smem_desc_sw128(smem_u32(smem) + OPERAND, B_MN ? PIECE : 16, 1024);
       constexpr uint64_t A_STEP = A_MN ? 128 : 2, B_STEP = B_MN ? 128 : 2;      // 16 K elements on, in units of 16 bytes
@@ -244,7 +244,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
           const uint64_t at = (uint64_t)(slot * (STAGE >> 4));
 #pragma unroll
           for (int ks = 0; ks < TK / 16; ++ks)
-            umma_ss_pair(tm + ab * TN, a0 + at + ks * A_STEP, b0 + at + ks * B_STEP, idesc, ks > 0 ? 1u : (kc > k_begin ? 1u : 0u));
+            umma_ss_pair(tm + ab * NT, a0 + at + ks * A_STEP, b0 + at + ks * B_STEP, idesc, ks > 0 ? 1u : (kc > k_begin ? 1u : 0u));
           umma_commit_pair(&sh.empty[slot]);
         }
         umma_commit_pair(&sh.acc_full[ab]);
@@ -276,9 +276,11 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
       const Item w = item_of(P, t);
       const int ab = nt & 1;
       const int row = w.m * TM + (int)rank * 128 + quarter * 32;
-      const uint32_t acc = tm + lane_addr + ab * TN;
-      constexpr int WIDTH = EPI == GATE ? 64 : 128;             // columns of the warp
-      const int c0 = w.n * (2 * WIDTH) + half * WIDTH;
+      const uint32_t acc = tm + lane_addr + ab * NT;
+      // Columns of the warp.  Of a narrow tile's 64 hidden columns H is the first half's warps', G and U the second's.
+      constexpr bool SHARED = EPI == GATE && NT == 128;
+      constexpr int WIDTH = EPI == GATE ? 64 : NT / 2;
+      const int at0 = SHARED ? 0 : half * WIDTH, c0 = SHARED ? w.n * WIDTH : w.n * (2 * WIDTH) + at0;
       const bool rows = row < P.rows;
       auto get = [&](int col) {                                 // DGATE: G and U of 64 columns into the first two areas
         if (lane == 0) {
@@ -290,7 +292,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
       };
       if (EPI == DGATE && rows && c0 < P.cols) {                // (on their way before the accumulator is complete)
         get(c0);
-        if (lane == 0 && c0 + 64 < P.cols) {
+        if (WIDTH > 64 && lane == 0 && c0 + 64 < P.cols) {
           tma_prefetch_3d(&maps.e[0], c0 + 64, row, 0);
           tma_prefetch_3d(&maps.e[1], c0 + 64, row, 0);
         }
@@ -303,12 +305,12 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(map_shared(&sh.acc_empty[ab], 0));
       };
-      const int parts = rows ? min(WIDTH, (P.cols - c0 + 63) / 64 * 64) : 0;
+      const int parts = rows && !(SHARED && half && !P.keep) ? min(WIDTH, (P.cols - c0 + 63) / 64 * 64) : 0;
       if (parts <= 0) release();
 #pragma unroll 1
       for (int s = 0; s < parts; s += 64) {
         const int col = c0 + s;
-        const uint32_t at = acc + half * WIDTH + s;
+        const uint32_t at = acc + at0 + s;
         const bool last = s + 64 >= parts;
         auto done = [&] { if (last) release(); };
         auto more = [] {};
@@ -339,14 +341,16 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
             if (lane == 0 && col + q * 32 < P.cols) { tma_store_3d(area, &maps.e[0], col + q * 32, row, w.mat * P.split + w.part); bulk_commit(); }
           }
         } else if (EPI == GATE) {
-          if (P.keep) {                                         // for the backward pass
+          if (P.keep && (!SHARED || half)) {                    // for the backward pass
             put(&maps.e[1], area, col, row, sums(at), more);
-            put(&maps.e[2], area, col, row, sums(at + 128), more);
+            if (SHARED) put(&maps.e[2], area, col, row, sums(at + NT / 2), done);
+            else put(&maps.e[2], area, col, row, sums(at + NT / 2), more);
           }
+          if (SHARED && half) break;
           put(&maps.e[0], area, col, row, [&](int q, float (&v)[32]) {
             uint32_t g[32], u[32];
             tmem_ld32(at + q * 32, g);
-            tmem_ld32(at + 128 + q * 32, u);
+            tmem_ld32(at + NT / 2 + q * 32, u);
             tmem_wait_ld();
             with_activation(P.act, [&](auto act) {
 #pragma unroll
@@ -417,7 +421,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
   cluster_sync();                                               // neither CTA leaves while the other still reads or signals it
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc_pair(tm, 512);
+    tmem_dealloc_pair(tm, 2 * NT);
   }
 }
 
@@ -660,6 +664,21 @@ int split_of(long long tiles, int k, double values, double* us = nullptr) {
   if (us) *us = least;
   return best;
 }
+// The same for a product with an epilogue, whose K stays whole: tiles of 256 columns or narrow ones, of which there are twice as many.
+// A chunk of a narrow tile takes 0.22 us (three quarters of the bytes for half the products), the epilogue of a tile, which overlaps the
+// next tile's products, `epilogue` us or half of that.  Measured, wide / narrow, us: backward of 200 tokens, dim 1264, hidden 2464 44.7 / 38.1,
+// of 4000 165 / 175; forward of 128 tokens, dim 512, hidden 1408 13.5 / 12.0, of 1000 tokens, dim 1024, hidden 2816 28.6 / 30.2.
+struct Tiling { bool narrow; double us; };
+Tiling tiling_of(long long rows, int cols, int width, int k, double epilogue) {
+  constexpr int pairs = FF_B200_SMS / 2;
+  auto time = [&](int w, double chunk, double epi) {
+    const long long tiles = ((rows + TM - 1) / TM) * ((cols + w - 1) / w);
+    return (double)((tiles + pairs - 1) / pairs) * (k * chunk > epi ? k * chunk : epi) + epi;
+  };
+  const double wide = time(width, 0.28, epilogue), narrow = time(width / 2, 0.22, epilogue / 2);
+  return {narrow < wide, narrow < wide ? narrow : wide};
+}
+constexpr double GATE_EPILOGUE = 2, DGATE_EPILOGUE = 8;
 struct Product { long long rows; int cols, mats, k; };          // extents of an output, matrices, K chunks in all
 int split_of(const Product& p, double* us = nullptr) {
   return split_of(((p.rows + TM - 1) / TM) * ((p.cols + TN - 1) / TN) * p.mats, p.k, (double)p.rows * p.cols * p.mats, us);
@@ -670,28 +689,28 @@ size_t sums_bytes(const Product& p) {
 }
 
 // `e`: the matrices of the epilogue in the order of GemmMaps; all have the extents of the outputs.
-template <bool A_MN, bool B_MN, int EPI>
+template <bool A_MN, bool B_MN, int EPI, int NT = TN>
 cudaError_t gemm(const ff_ffn* h, const Matrix (&a)[2], const Matrix (&b)[2], std::initializer_list<const void*> e, GemmParams P, cudaStream_t st) {
   GemmMaps m;
   for (int i = 0; i < 2; ++i) {
     if (i && a[1].p == a[0].p) m.a[1] = m.a[0];
     else if (!matrix_map(h, &m.a[i], a[i].p, a[i].rows, a[i].cols, A_MN ? 64 : 128)) return cudaErrorInvalidValue;
     if (i && b[1].p == b[0].p) m.b[1] = m.b[0];
-    else if (!matrix_map(h, &m.b[i], b[i].p, b[i].rows, b[i].cols, B_MN ? 64 : 128)) return cudaErrorInvalidValue;
+    else if (!matrix_map(h, &m.b[i], b[i].p, b[i].rows, b[i].cols, B_MN ? 64 : NT / 2)) return cudaErrorInvalidValue;
   }
   int n = 0;
   for (const void* p : e)
     if (!(EPI == PARTIAL ? sums_map(h, &m.e[n++], p, P.rows, P.cols, P.mats * P.split) : matrix_map(h, &m.e[n++], p, P.rows, P.cols, 32)))
       return cudaErrorInvalidValue;
   for (; n < 5; ++n) m.e[n] = m.e[0];
-  const int width = EPI == GATE ? 128 : TN;
+  const int width = EPI == GATE ? NT / 2 : NT;
   P.m_tiles = (int)((P.rows + TM - 1) / TM);
   P.n_tiles = (P.cols + width - 1) / width;
   P.act = h->cfg.activation;
   P.status = h->status;
   const int tiles = P.m_tiles * P.n_tiles * P.mats, items = tiles * P.split;
   const int pairs = h->sm_count / 2;
-  return ff_launch(ffn_gemm_kernel<A_MN, B_MN, EPI>, dim3(2 * (unsigned)(items < pairs ? items : pairs)), dim3(THREADS), smem_bytes(EPI), st, m, P);
+  return ff_launch(ffn_gemm_kernel<A_MN, B_MN, EPI, NT>, dim3(2 * (unsigned)(items < pairs ? items : pairs)), dim3(THREADS), smem_bytes(EPI, NT), st, m, P);
 }
 // A product without more to do: out[i] = A B[i], or (two sources) out[0] = A[0] B[0] + A[1] B[1].
 template <bool A_MN, bool B_MN>
@@ -841,11 +860,12 @@ extern "C" ff_status_t ff_ffn_create(const ff_ffn_config_t* cfg, ff_ffn_t** out)
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device);
   const struct { const void* kernel; size_t smem; } kernels[] = {
-      {(const void*)ffn_gemm_kernel<false, true, GATE>, smem_bytes(GATE)}, {(const void*)ffn_gemm_kernel<false, true, STORE>, smem_bytes(STORE)},
-      {(const void*)ffn_gemm_kernel<false, false, DGATE>, smem_bytes(DGATE)}, {(const void*)ffn_gemm_kernel<false, false, STORE>, smem_bytes(STORE)},
-      {(const void*)ffn_gemm_kernel<true, true, STORE>, smem_bytes(STORE)}, {(const void*)ffn_gemm_kernel<false, true, PARTIAL>, smem_bytes(PARTIAL)},
-      {(const void*)ffn_gemm_kernel<false, false, PARTIAL>, smem_bytes(PARTIAL)}, {(const void*)ffn_gemm_kernel<true, true, PARTIAL>, smem_bytes(PARTIAL)},
-      {(const void*)ffn_few_kernel<GATE>, FEW_SMEM},
+      {(const void*)ffn_gemm_kernel<false, true, GATE, TN>, smem_bytes(GATE)}, {(const void*)ffn_gemm_kernel<false, true, STORE, TN>, smem_bytes(STORE)},
+      {(const void*)ffn_gemm_kernel<false, false, DGATE, TN>, smem_bytes(DGATE)}, {(const void*)ffn_gemm_kernel<false, false, STORE, TN>, smem_bytes(STORE)},
+      {(const void*)ffn_gemm_kernel<true, true, STORE, TN>, smem_bytes(STORE)}, {(const void*)ffn_gemm_kernel<false, true, PARTIAL, TN>, smem_bytes(PARTIAL)},
+      {(const void*)ffn_gemm_kernel<false, false, PARTIAL, TN>, smem_bytes(PARTIAL)}, {(const void*)ffn_gemm_kernel<true, true, PARTIAL, TN>, smem_bytes(PARTIAL)},
+      {(const void*)ffn_gemm_kernel<false, true, GATE, 128>, smem_bytes(GATE, 128)},
+      {(const void*)ffn_gemm_kernel<false, false, DGATE, 128>, smem_bytes(DGATE, 128)}, {(const void*)ffn_few_kernel<GATE>, FEW_SMEM},
       {(const void*)ffn_few_kernel<STORE>, FEW_SMEM}};
   for (const auto& k : kernels)
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.smem);
@@ -909,18 +929,19 @@ extern "C" ff_status_t ff_ffn_forward(ff_ffn_t* h, int64_t tokens, const void* X
   // 2816, product with Wd: 400 tokens 25.9 / 21.5, 768 27.8 / 32.4.
   const FewShape up_few = few_shape(h, tokens, F, chunks(D), 2), down_few = few_shape(h, tokens, D, chunks(F), 1);
   const Product down = down_product(h->cfg, tokens);
-  const long long up_tiles = ((tokens + TM - 1) / TM) * ((F + 127) / 128);
   double down_us;
   split_of(down, &down_us);
   down_us += 2;
-  const double up_us = 2 + 0.28 * chunks(D) * (double)((up_tiles + FF_B200_SMS / 2 - 1) / (FF_B200_SMS / 2));
+  const Tiling up_tiling = tiling_of(tokens, F, 128, chunks(D), GATE_EPILOGUE);
+  const double up_us = up_tiling.us;
   if (up_few.us < up_us) {
     FFN_CUDA(h, few<GATE>(h, up_few, Wg, Wu, X, tokens, F, D, {ws, gate, up}, st));
   } else {
     GemmParams P{};
     P.rows = tokens; P.cols = F; P.mats = P.sources = P.split = 1;
     P.kchunks = chunks(D); P.keep = gate != nullptr;
-    FFN_CUDA(h, (gemm<false, true, GATE>(h, {x, x}, {wg, wu}, {ws, gate ? gate : ws, up ? up : ws}, P, st)));
+    if (up_tiling.narrow) FFN_CUDA(h, (gemm<false, true, GATE, 128>(h, {x, x}, {wg, wu}, {ws, gate ? gate : ws, up ? up : ws}, P, st)));
+    else FFN_CUDA(h, (gemm<false, true, GATE>(h, {x, x}, {wg, wu}, {ws, gate ? gate : ws, up ? up : ws}, P, st)));
   }
   if (down_few.us < down_us) FFN_CUDA(h, few<STORE>(h, down_few, Wd, Wd, ws, tokens, D, F, {out, nullptr, nullptr}, st));
   else FFN_CUDA(h, (product<false, true>(h, {hid, hid}, {wd, wd}, down, 1, out, nullptr, (char*)ws + hidden_bytes(h->cfg, tokens), st)));
@@ -952,7 +973,8 @@ extern "C" ff_status_t ff_ffn_backward(ff_ffn_t* h, int64_t tokens, const void* 
   GemmParams P{};
   P.rows = tokens; P.cols = F; P.mats = P.sources = P.split = 1;
   P.kchunks = chunks(D);
-  FFN_CUDA(h, (gemm<false, false, DGATE>(h, {g, g}, {wd, wd}, {gate, up, dG, dU, H}, P, st)));
+  if (tiling_of(tokens, F, TN, chunks(D), DGATE_EPILOGUE).narrow) FFN_CUDA(h, (gemm<false, false, DGATE, 128>(h, {g, g}, {wd, wd}, {gate, up, dG, dU, H}, P, st)));
+  else FFN_CUDA(h, (gemm<false, false, DGATE>(h, {g, g}, {wd, wd}, {gate, up, dG, dU, H}, P, st)));
   void* sums = base + 3 * hidden_bytes(h->cfg, tokens);
   if (dX) FFN_CUDA(h, (product<false, false>(h, {dg, du}, {wg, wu}, dx_product(h->cfg, tokens), 2, dX, nullptr, sums, st)));
   if (dWg) FFN_CUDA(h, (product<true, true>(h, {x, x}, {dg, du}, dw_product(h->cfg, tokens), 1, dWg, dWu, sums, st)));
