@@ -3,17 +3,18 @@
 //   dH = dout Wd^T, dG = dH U act'(G), dU = dH act(G), dX = dG Wg^T + dU Wu^T,
 //   dWg = X^T dG, dWu = X^T dU, dWd = H^T dout
 //
-// Every product is one launch of one kernel: a persistent GEMM on CTA pairs (tcgen05, cta_group::2) with tiles of 256 x 256
-// (128 rows of A and 128 columns of B in either CTA's shared memory), K in chunks of 64, a ring of six stages filled by TMA, and
-// two accumulators of 256 tensor-memory columns, so that the epilogue of a tile overlaps the main loop of the next.  Operands
-// are read as they lie in memory, K-major or MN-major, so nothing is transposed: the products differ in majorness and epilogue.
+// Three launches of one kernel: gate and up (then out), dH (then all gradients together).  It is a persistent GEMM on CTA pairs (tcgen05,
+// cta_group::2) with tiles of 256 x 256 (128 rows of A and 128 columns of B in either CTA's shared memory), K in chunks of 64, a ring of
+// six stages filled by TMA, and two accumulators of 256 tensor-memory columns, so that the epilogue of a tile overlaps the main loop of
+// the next.  Operands are read as they lie in memory, K-major or MN-major, so nothing is transposed.
 //   gate and up   one tile is 128 columns of G (the even CTA's half of B) beside the same 128 columns of U (the odd CTA's), so
 //                 that both values of an element lie in one lane of tensor memory and H leaves without G and U reaching memory
 //   dH            its epilogue reads G and U and writes dG, dU and H (needed for dWd; made again rather than kept)
-//   dX            K runs over the columns of dG, then those of dU
-//   dWg, dWu      one launch, the matrices side by side along N; K runs over the tokens
+//   gradients     dX, dWg and dWu, dWd in one launch, whose items go to the pairs one after another (in a launch each: 4000 tokens, dim
+//                 1024, hidden 2816 150 us instead of 124, 64 tokens 35 instead of 24); dX: K runs over the columns of dG, then those of
+//                 dU;  dWg, dWu: the matrices side by side along N, K runs over the tokens
 // H, dG and dU are rounded to bf16 between the products: they are operands of the next one.
-// Products with few tiles are cut along K (split_of); with few tokens the weights are the rows (ffn_few_kernel).
+// Products with few tiles are cut along K (split_of, splits_of); with few tokens the weights are the rows (ffn_few_kernel).
 //
 //   warp 0      TMA producer          warp 1      tcgen05.mma issuer of the pair (even CTA), owns the tensor memory
 //   warps 2..9  epilogue: a thread owns one row of the tile and half its columns, which reach memory by TMA from a staging area of
@@ -48,24 +49,31 @@ __host__ __device__ constexpr int stage_bytes(int nt) { return OPERAND + nt / 2 
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 
-enum { STORE = 0, GATE = 1, DGATE = 2, PARTIAL = 3 };           // epilogues
+enum { PRODUCTS = 0, GATE = 1, DGATE = 2 };      // what a launch makes
 // Stages of the ring, and staging areas of an epilogue warp: 32 rows of 64 columns each, on their way to or from memory by TMA
 constexpr int AREA = 32 * 128;
 __host__ __device__ constexpr int ring_stages(int epi) { return epi == DGATE ? 5 : 6; }
 __host__ __device__ constexpr int areas(int epi) { return epi == DGATE ? 2 : 1; }
 
-struct GemmParams {
+// One product of a launch.
+struct Sub {
   long long rows;                  // output rows
   int cols;                        // output columns of one matrix
   int m_tiles, n_tiles, mats;      // tiles; matrices side by side
   int kchunks, sources;            // K chunks of one source, sources one after the other
-  int split;                       // PARTIAL: parts of K, each with its own sums
-  int act, keep;                   // GATE: G and U are written too
+  int split;                       // parts of K; more than one: each with its own fp32 sums
+  int items;                       // tiles times parts
+  int a_mn, b_mn;                  // operands MN-major
+  int a, b, e;                     // its first maps
+};
+struct GemmParams {
+  Sub sub[3];
+  int items, act, keep;            // keep: GATE writes G and U too
   int* status;
 };
-// Operands by source (K) or matrix (N), and what the epilogue moves: STORE: the outputs by matrix;  GATE: H, G, U;
-// DGATE: G, U (read), dG, dU, H;  PARTIAL: fp32 sums [matrix][part][rows][cols]
-struct GemmMaps { CUtensorMap a[2], b[2], e[5]; };
+// Operands by source (K) or matrix (N), and what the epilogue moves: PRODUCTS: the outputs by matrix, or the sums [matrix][part][rows][cols];
+// GATE: H, G, U;  DGATE: G, U (read), dG, dU, H
+struct GemmMaps { CUtensorMap a[4], b[5], e[5]; };
 
 struct Shared {
   uint64_t full[6], empty[6], acc_full[2], acc_empty[2], in_full[EPI_WARPS];
@@ -74,7 +82,7 @@ struct Shared {
 };
 inline int chunks(long long k) { return (int)((k + TK - 1) / TK); }
 __host__ __device__ constexpr size_t smem_bytes(int epi, int nt = TN) { return (size_t)ring_stages(epi) * stage_bytes(nt) + (size_t)EPI_WARPS * areas(epi) * AREA + sizeof(Shared) + 1024; }
-static_assert(smem_bytes(STORE) <= 232448 && smem_bytes(GATE) <= 232448 && smem_bytes(DGATE) <= 232448, "227 KB a block");
+static_assert(smem_bytes(PRODUCTS) <= 232448 && smem_bytes(GATE) <= 232448 && smem_bytes(DGATE) <= 232448, "227 KB a block");
 
 // act(g) and, with SLOPE, its derivative.  The cubic inside gelu_tanh saturates long before |g| = 16.
 __device__ __forceinline__ float exponential(float v) { return ex2(1.4426950408889634f * v); }
@@ -138,7 +146,7 @@ __device__ __forceinline__ float element(const uint4 (&v)[N], int i) {
 // what runs at the same time reads few rows of A and few columns of B (row by row, dWg and dWu of dim 2048, hidden 5632, 9999
 // tokens read dG and dU from memory in each of five waves: 420 us in a row of calls, 372 column by column).
 struct Item { int m, n, mat, part; };
-__device__ __forceinline__ Item item_of(const GemmParams& P, int t) {
+__device__ __forceinline__ Item item_of(const Sub& P, int t) {
   const int cols = P.n_tiles * P.mats, tiles = P.m_tiles * cols;
   Item w;
   w.part = P.split > 1 ? t / tiles : 0;
@@ -150,13 +158,24 @@ __device__ __forceinline__ Item item_of(const GemmParams& P, int t) {
   w.n = c - w.mat * P.n_tiles;
   return w;
 }
+// The product of item t of the launch; t becomes the item of the product.
+template <int EPI>
+__device__ __forceinline__ const Sub& sub_of(const GemmParams& P, int& t) {
+  const Sub* s = P.sub;
+  if (EPI == PRODUCTS)
+    for (; t >= s->items; ++s) t -= s->items;
+  return *s;
+}
 // K chunks of a part
-__device__ __forceinline__ void part_of_k(const GemmParams& P, int part, int& begin, int& end) {
+__device__ __forceinline__ void part_of_k(const Sub& P, int part, int& begin, int& end) {
   const int k = P.kchunks * P.sources, q = k / P.split, r = k - q * P.split;         // (the first r parts have one more)
   begin = part * q + min(part, r);
   end = begin + q + (part < r);
 }
 
+template <bool V> struct Const { static constexpr bool value = V; };
+// A_MN, B_MN: the operands' majorness; of PRODUCTS each product says its own: both MN-major, B alone, or neither, the
+// one case with two sources.
 template <bool A_MN, bool B_MN, int EPI, int NT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
@@ -167,9 +186,8 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const int tiles = P.m_tiles * P.n_tiles * P.mats, items = tiles * P.split;
 
-  if (threadIdx.x < 4) tma_prefetch_desc(threadIdx.x < 2 ? &maps.a[threadIdx.x] : &maps.b[threadIdx.x - 2]);
+  if (threadIdx.x < 14) tma_prefetch_desc(&maps.a[0] + threadIdx.x);
   if (threadIdx.x == 0) {
     for (int i = 0; i < NSTAGE; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.acc_full[i], 1); mbar_init(&sh.acc_empty[i], 2 * EPI_WARPS); }
@@ -190,63 +208,85 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
     if (lane == 0) {
       unsigned n = 0;
       bool ok = true;
-      for (int t = pair; t < items && ok; t += pairs) {
-        const Item w = item_of(P, t);
+      for (int i = pair; i < P.items && ok; i += pairs) {
+        int t = i;
+        const Sub sub = sub_of<EPI>(P, t);                      // (a copy: read once an item, not once a chunk)
+        const Item w = item_of(sub, t);
         const int m0 = w.m * TM + (int)rank * 128;
         const int n0 = EPI == GATE ? w.n * (NT / 2) : w.n * NT + (int)rank * (NT / 2);
         int k_begin, k_end;
-        part_of_k(P, w.part, k_begin, k_end);
-        for (int kc = k_begin; kc < k_end && ok; ++kc, ++n) {
-          const int slot = n % NSTAGE;
-          if (n >= (unsigned)NSTAGE) ok = mbar_wait(&sh.empty[slot], ((n / NSTAGE) - 1) & 1, abort_flag);
-          if (!ok) break;
-          const int second = kc >= P.kchunks, k0 = (kc - (second ? P.kchunks : 0)) * TK;
-          const CUtensorMap* ma = &maps.a[second];
-          const CUtensorMap* mb = &maps.b[EPI == GATE ? (int)rank : second | w.mat];
-          uint8_t* dst = smem + slot * STAGE;
-          const uint32_t bar = map_shared(&sh.full[slot], 0);
-          if (rank == 0) mbar_arrive_expect_tx(&sh.full[slot], 2 * STAGE);
-          if (A_MN) {
-            tma_load_3d_pair(dst, ma, bar, m0, k0, 0);
-            tma_load_3d_pair(dst + PIECE, ma, bar, m0 + 64, k0, 0);
-          } else {
-            tma_load_3d_pair(dst, ma, bar, k0, m0, 0);
+        part_of_k(sub, w.part, k_begin, k_end);
+        // (a loop for each majorness, here and at the products: with it as a variable the product with Wd took 15 % more)
+        auto load = [&](auto a_mn, auto b_mn, const CUtensorMap* ma, const CUtensorMap* mb, int from, int to, int first) {
+          for (int kc = from; kc < to && ok; ++kc, ++n) {
+            const int slot = n % NSTAGE, k0 = (kc - first) * TK;
+            if (n >= (unsigned)NSTAGE) ok = mbar_wait(&sh.empty[slot], ((n / NSTAGE) - 1) & 1, abort_flag);
+            if (!ok) break;
+            uint8_t* dst = smem + slot * STAGE;
+            const uint32_t bar = map_shared(&sh.full[slot], 0);
+            if (rank == 0) mbar_arrive_expect_tx(&sh.full[slot], 2 * STAGE);
+            if constexpr (decltype(a_mn)::value) {
+              tma_load_3d_pair(dst, ma, bar, m0, k0, 0);
+              tma_load_3d_pair(dst + PIECE, ma, bar, m0 + 64, k0, 0);
+            } else {
+              tma_load_3d_pair(dst, ma, bar, k0, m0, 0);
+            }
+            if constexpr (decltype(b_mn)::value) {
+              tma_load_3d_pair(dst + OPERAND, mb, bar, n0, k0, 0);
+              if (NT == 256) tma_load_3d_pair(dst + OPERAND + PIECE, mb, bar, n0 + 64, k0, 0);
+            } else {
+              tma_load_3d_pair(dst + OPERAND, mb, bar, k0, n0, 0);
+            }
           }
-          if (B_MN) {
-            tma_load_3d_pair(dst + OPERAND, mb, bar, n0, k0, 0);
-            if (NT == 256) tma_load_3d_pair(dst + OPERAND + PIECE, mb, bar, n0 + 64, k0, 0);
-          } else {
-            tma_load_3d_pair(dst + OPERAND, mb, bar, k0, n0, 0);
-          }
+        };
+        const CUtensorMap *ma = &maps.a[sub.a], *mb = &maps.b[EPI == GATE ? (int)rank : sub.b + w.mat];
+        if constexpr (EPI != PRODUCTS) {
+          load(Const<A_MN>(), Const<B_MN>(), ma, mb, k_begin, k_end, 0);
+        } else if (sub.a_mn) {
+          load(Const<true>(), Const<true>(), ma, mb, k_begin, k_end, 0);
+        } else if (sub.b_mn) {
+          load(Const<false>(), Const<true>(), ma, mb, k_begin, k_end, 0);
+        } else {                                                // the one with two sources
+          load(Const<false>(), Const<false>(), ma, mb, k_begin, min(k_end, sub.kchunks), 0);
+          load(Const<false>(), Const<false>(), ma + 1, mb + 1, max(k_begin, sub.kchunks), k_end, sub.kchunks);
         }
       }
     }
   } else if (warp == 1) {
     if (rank == 0) {
-      const uint32_t idesc = idesc_bf16_f32(TM, NT, A_MN, B_MN);
-      const uint64_t a0 = smem_desc_sw128(smem_u32(smem), A_MN ? PIECE : 16, 1024);
-      const uint64_t b0 = smem_desc_sw128(smem_u32(smem) + OPERAND, B_MN ? PIECE : 16, 1024);
-      constexpr uint64_t A_STEP = A_MN ? 128 : 2, B_STEP = B_MN ? 128 : 2;      // 16 K elements on, in units of 16 bytes
       unsigned n = 0, nt = 0;
       bool ok = true;
-      for (int t = pair; t < items && ok; t += pairs, ++nt) {
+      for (int i = pair; i < P.items && ok; i += pairs, ++nt) {
         const int ab = nt & 1;
-        int k_begin, k_end;
-        part_of_k(P, P.split > 1 ? t / tiles : 0, k_begin, k_end);
+        int t = i, k_begin, k_end;
+        const Sub sub = sub_of<EPI>(P, t);                      // (a copy: read once an item, not once a chunk)
+        part_of_k(sub, sub.split > 1 ? t / (sub.m_tiles * sub.n_tiles * sub.mats) : 0, k_begin, k_end);
         if (nt >= 2) ok = mbar_wait_warp(&sh.acc_empty[ab], ((nt >> 1) - 1) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        for (int kc = k_begin; kc < k_end && ok; ++kc, ++n) {
-          const int slot = n % NSTAGE;
-          ok = mbar_wait_warp(&sh.full[slot], (n / NSTAGE) & 1, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t at = (uint64_t)(slot * (STAGE >> 4));
+        auto multiply = [&](auto a_mn, auto b_mn) {
+          constexpr bool AM = decltype(a_mn)::value, BM = decltype(b_mn)::value;
+          constexpr uint32_t idesc = idesc_bf16_f32(TM, NT, AM, BM);
+          constexpr uint64_t A_STEP = AM ? 128 : 2, B_STEP = BM ? 128 : 2;      // 16 K elements on, in units of 16 bytes
+          const uint64_t a0 = smem_desc_sw128(smem_u32(smem), AM ? PIECE : 16, 1024);
+          const uint64_t b0 = smem_desc_sw128(smem_u32(smem) + OPERAND, BM ? PIECE : 16, 1024);
+          for (int kc = k_begin; kc < k_end && ok; ++kc, ++n) {
+            const int slot = n % NSTAGE;
+            ok = mbar_wait_warp(&sh.full[slot], (n / NSTAGE) & 1, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t at = (uint64_t)(slot * (STAGE >> 4));
 #pragma unroll
-          for (int ks = 0; ks < TK / 16; ++ks)
-            umma_ss_pair(tm + ab * NT, a0 + at + ks * A_STEP, b0 + at + ks * B_STEP, idesc, ks > 0 ? 1u : (kc > k_begin ? 1u : 0u));
-          umma_commit_pair(&sh.empty[slot]);
-        }
+            for (int ks = 0; ks < TK / 16; ++ks)
+              umma_ss_pair(tm + ab * NT, a0 + at + ks * A_STEP, b0 + at + ks * B_STEP, idesc, ks > 0 ? 1u : (kc > k_begin ? 1u : 0u));
+            umma_commit_pair(&sh.empty[slot]);
+          }
+        };
+        if constexpr (EPI != PRODUCTS) multiply(Const<A_MN>(), Const<B_MN>());
+        else if (sub.a_mn) multiply(Const<true>(), Const<true>());
+        else if (sub.b_mn) multiply(Const<false>(), Const<true>());
+        else multiply(Const<false>(), Const<false>());
+        if (!ok) break;
         umma_commit_pair(&sh.acc_full[ab]);
       }
     }
@@ -272,8 +312,10 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
       __syncwarp();
       if (lane == 0) { tma_store_3d(to, map, col, row, 0); bulk_commit(); }
     };
-    for (int t = pair; t < items && ok; t += pairs, ++nt) {
-      const Item w = item_of(P, t);
+    for (int i = pair; i < P.items && ok; i += pairs, ++nt) {
+      int t = i;
+      const Sub sub = sub_of<EPI>(P, t);                      // (a copy: read once an item, not once a chunk)
+      const Item w = item_of(sub, t);
       const int ab = nt & 1;
       const int row = w.m * TM + (int)rank * 128 + quarter * 32;
       const uint32_t acc = tm + lane_addr + ab * NT;
@@ -281,7 +323,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
       constexpr bool SHARED = EPI == GATE && NT == 128;
       constexpr int WIDTH = EPI == GATE ? 64 : NT / 2;
       const int at0 = SHARED ? 0 : half * WIDTH, c0 = SHARED ? w.n * WIDTH : w.n * (2 * WIDTH) + at0;
-      const bool rows = row < P.rows;
+      const bool rows = row < sub.rows;
       auto get = [&](int col) {                                 // DGATE: G and U of 64 columns into the first two areas
         if (lane == 0) {
           bulk_wait_read0();
@@ -290,9 +332,9 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
           tma_load_3d(area + AREA, &maps.e[1], in_full, col, row, 0);
         }
       };
-      if (EPI == DGATE && rows && c0 < P.cols) {                // (on their way before the accumulator is complete)
+      if (EPI == DGATE && rows && c0 < sub.cols) {                // (on their way before the accumulator is complete)
         get(c0);
-        if (WIDTH > 64 && lane == 0 && c0 + 64 < P.cols) {
+        if (WIDTH > 64 && lane == 0 && c0 + 64 < sub.cols) {
           tma_prefetch_3d(&maps.e[0], c0 + 64, row, 0);
           tma_prefetch_3d(&maps.e[1], c0 + 64, row, 0);
         }
@@ -305,7 +347,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(map_shared(&sh.acc_empty[ab], 0));
       };
-      const int parts = rows && !(SHARED && half && !P.keep) ? min(WIDTH, (P.cols - c0 + 63) / 64 * 64) : 0;
+      const int parts = rows && !(SHARED && half && !P.keep) ? min(WIDTH, (sub.cols - c0 + 63) / 64 * 64) : 0;
       if (parts <= 0) release();
 #pragma unroll 1
       for (int s = 0; s < parts; s += 64) {
@@ -323,9 +365,9 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
             for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
           };
         };
-        if (EPI == STORE) {
-          put(&maps.e[w.mat], area, col, row, sums(at), done);
-        } else if (EPI == PARTIAL) {
+        if (EPI == PRODUCTS && sub.split == 1) {
+          put(&maps.e[sub.e + w.mat], area, col, row, sums(at), done);
+        } else if (EPI == PRODUCTS) {
 #pragma unroll 1
           for (int q = 0; q < 2; ++q) {                         // 32 columns of fp32 fill a row of the area
             uint32_t r[32];
@@ -338,7 +380,7 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
             stage32(area, lane, 1, r + 16);
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0 && col + q * 32 < P.cols) { tma_store_3d(area, &maps.e[0], col + q * 32, row, w.mat * P.split + w.part); bulk_commit(); }
+            if (lane == 0 && col + q * 32 < sub.cols) { tma_store_3d(area, &maps.e[sub.e], col + q * 32, row, w.mat * sub.split + w.part); bulk_commit(); }
           }
         } else if (EPI == GATE) {
           if (P.keep && (!SHARED || half)) {                    // for the backward pass
@@ -425,22 +467,27 @@ ffn_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams P) {
   }
 }
 
-// The parts of K added up, in their order, and rounded: out[m] = sum over s of sums[m][s].  A thread has eight values.
-__global__ void __launch_bounds__(256) ffn_join_kernel(const float* sums, int split, long long values, __nv_bfloat16* out0, __nv_bfloat16* out1) {
+// The parts of K added up, in their order, and rounded.  A block has 2048 values of one output, a thread eight.
+struct Joined { const float* sums; __nv_bfloat16* out; long long values; int split, first; };     // first: its first block
+struct JoinParams { Joined j[4]; int count; };
+__global__ void __launch_bounds__(256) ffn_join_kernel(const JoinParams P) {
+  int n = 0;
+  while (n + 1 < P.count && (int)blockIdx.x >= P.j[n + 1].first) ++n;
+  const Joined& j = P.j[n];
   ff_pdl_wait();
-  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8;
-  if (i >= values) return;
-  const float* p = sums + (long long)blockIdx.y * split * values + i;
+  const long long i = ((long long)((int)blockIdx.x - j.first) * 256 + threadIdx.x) * 8;
+  if (i >= j.values) return;
+  const float* p = j.sums + i;
   float v[8] = {};
 #pragma unroll 4
-  for (int s = 0; s < split; ++s) {
-    const float4 a = *(const float4*)(p + s * values), b = *(const float4*)(p + s * values + 4);
+  for (int s = 0; s < j.split; ++s) {
+    const float4 a = *(const float4*)(p + s * j.values), b = *(const float4*)(p + s * j.values + 4);
     v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
     v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
   }
   uint32_t w[4];
   pack(v, w);
-  *(uint4*)((blockIdx.y ? out1 : out0) + i) = make_uint4(w[0], w[1], w[2], w[3]);
+  *(uint4*)(j.out + i) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------------
@@ -505,7 +552,7 @@ ffn_few_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (EPI == STORE && warp != 0) ff_pdl_wait();                 // (warp 0: below)
+  if (EPI == PRODUCTS && warp != 0) ff_pdl_wait();                 // (warp 0: below)
   const uint32_t tm = sh.tmem_base;
   volatile int* abort_flag = &sh.abort_flag;
 
@@ -521,7 +568,7 @@ ffn_few_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant
             tma_load_3d(dst + (2 * m + c) * PIECE, m ? &map_w1 : &map_w0, &sh.full[slot], f0 + 64 * c, kc * TK, 0);
       };
       int ahead = 0;
-      if (EPI == STORE) {
+      if (EPI == PRODUCTS) {
         for (; ahead < P.stages && k_begin + ahead < k_end; ++ahead) weights(k_begin + ahead, ahead);
         ff_pdl_wait();
       }
@@ -640,7 +687,7 @@ bool matrix_map(const ff_ffn* h, CUtensorMap* map, const void* base, long long r
 }
 
 // fp32 sums [parts][rows][cols] with a box of 32 x 32.
-bool sums_map(const ff_ffn*, CUtensorMap* map, const void* base, long long rows, long long cols, int parts) {
+bool sums_map(CUtensorMap* map, const void* base, long long rows, long long cols, int parts) {
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
   cuuint64_t strides[2] = {(cuuint64_t)cols * 4, (cuuint64_t)rows * cols * 4};
   cuuint32_t box[3] = {32, 32, 1};
@@ -679,53 +726,119 @@ Tiling tiling_of(long long rows, int cols, int width, int k, double epilogue) {
   return {narrow < wide, narrow < wide ? narrow : wide};
 }
 constexpr double GATE_EPILOGUE = 2, DGATE_EPILOGUE = 8;
-struct Product { long long rows; int cols, mats, k; };          // extents of an output, matrices, K chunks in all
-int split_of(const Product& p, double* us = nullptr) {
-  return split_of(((p.rows + TM - 1) / TM) * ((p.cols + TN - 1) / TN) * p.mats, p.k, (double)p.rows * p.cols * p.mats, us);
-}
-size_t sums_bytes(const Product& p) {
-  const int s = split_of(p);
-  return s > 1 ? (size_t)p.rows * p.cols * p.mats * s * 4 : 0;
+struct Product {
+  long long rows;                  // extents of an output
+  int cols, mats, k;               // matrices, K chunks in all
+  long long tiles() const { return ((rows + TM - 1) / TM) * ((cols + TN - 1) / TN) * mats; }
+  long long values() const { return rows * cols * mats; }
+};
+int split_of(const Product& p, double* us = nullptr) { return split_of(p.tiles(), p.k, (double)p.values(), us); }
+size_t sums_bytes(const Product& p, int split) { return split > 1 ? ((size_t)p.values() * split * 4 + 255) / 256 * 256 : 0; }
+// The same for several products in one launch, whose items go to the pairs as they come: K of each is cut into parts of at most one
+// length, that of the least estimated time (the work evenly divided and half an item more, or the longest item).
+void splits_of(const Product* p, int count, int* split) {
+  constexpr int pairs = FF_B200_SMS / 2;
+  int longest = 0;
+  for (int i = 0; i < count; ++i) longest = p[i].k > longest ? p[i].k : longest;
+  double least = 0;
+  for (int s = 1; s <= 16 && s <= longest; ++s) {
+    const int most = (longest + s - 1) / s;
+    double work = 0, item = 0, moved = 0;
+    long long tiles = 0;
+    int cut[3];
+    for (int i = 0; i < count; ++i) {
+      cut[i] = (p[i].k + most - 1) / most;
+      work += (double)p[i].tiles() * p[i].k;
+      const double length = (p[i].k + cut[i] - 1) / cut[i];
+      item = length > item ? length : item;
+      if (cut[i] > 1) { tiles += p[i].tiles() * cut[i]; moved += (double)p[i].values() * 8 * cut[i]; }
+    }
+    if (tiles > 4 * pairs) continue;                             // (bounds the sums at 296 tiles)
+    const double even = work / pairs + item / 2, us = 0.28 * (even > item ? even : item) + (tiles ? 2.5 + moved / 4e6 : 0);
+    if (s == 1 || us < least) {
+      least = us;
+      for (int i = 0; i < count; ++i) split[i] = cut[i];
+    }
+  }
 }
 
-// `e`: the matrices of the epilogue in the order of GemmMaps; all have the extents of the outputs.
-template <bool A_MN, bool B_MN, int EPI, int NT = TN>
-cudaError_t gemm(const ff_ffn* h, const Matrix (&a)[2], const Matrix (&b)[2], std::initializer_list<const void*> e, GemmParams P, cudaStream_t st) {
-  GemmMaps m;
-  for (int i = 0; i < 2; ++i) {
-    if (i && a[1].p == a[0].p) m.a[1] = m.a[0];
-    else if (!matrix_map(h, &m.a[i], a[i].p, a[i].rows, a[i].cols, A_MN ? 64 : 128)) return cudaErrorInvalidValue;
-    if (i && b[1].p == b[0].p) m.b[1] = m.b[0];
-    else if (!matrix_map(h, &m.b[i], b[i].p, b[i].rows, b[i].cols, B_MN ? 64 : NT / 2)) return cudaErrorInvalidValue;
-  }
-  int n = 0;
-  for (const void* p : e)
-    if (!(EPI == PARTIAL ? sums_map(h, &m.e[n++], p, P.rows, P.cols, P.mats * P.split) : matrix_map(h, &m.e[n++], p, P.rows, P.cols, 32)))
-      return cudaErrorInvalidValue;
-  for (; n < 5; ++n) m.e[n] = m.e[0];
-  const int width = EPI == GATE ? NT / 2 : NT;
-  P.m_tiles = (int)((P.rows + TM - 1) / TM);
-  P.n_tiles = (P.cols + width - 1) / width;
+// (na, nb, ne: the maps there are; the others, which no product names, are copies)
+template <int EPI, int NT>
+cudaError_t launch_gemm(const ff_ffn* h, void (*kernel)(GemmMaps, GemmParams), GemmMaps& m, int na, int nb, int ne, GemmParams& P, cudaStream_t st) {
+  for (int i = na; i < 4; ++i) m.a[i] = m.a[0];
+  for (int i = nb; i < 5; ++i) m.b[i] = m.b[0];
+  for (int i = ne; i < 5; ++i) m.e[i] = m.e[0];
   P.act = h->cfg.activation;
   P.status = h->status;
-  const int tiles = P.m_tiles * P.n_tiles * P.mats, items = tiles * P.split;
   const int pairs = h->sm_count / 2;
-  return ff_launch(ffn_gemm_kernel<A_MN, B_MN, EPI, NT>, dim3(2 * (unsigned)(items < pairs ? items : pairs)), dim3(THREADS), smem_bytes(EPI, NT), st, m, P);
+  return ff_launch(kernel, dim3(2 * (unsigned)(P.items < pairs ? P.items : pairs)), dim3(THREADS), smem_bytes(EPI, NT), st, m, P);
 }
-// A product without more to do: out[i] = A B[i], or (two sources) out[0] = A[0] B[0] + A[1] B[1].
-template <bool A_MN, bool B_MN>
-cudaError_t product(const ff_ffn* h, const Matrix (&a)[2], const Matrix (&b)[2], const Product& p, int sources, void* out0, void* out1, void* sums,
-                    cudaStream_t st) {
-  GemmParams P{};
-  P.rows = p.rows; P.cols = p.cols; P.mats = p.mats;
-  P.sources = sources; P.kchunks = p.k / sources;
-  P.split = split_of(p);
-  if (P.split == 1) return p.mats == 2 ? gemm<A_MN, B_MN, STORE>(h, a, b, {out0, out1}, P, st) : gemm<A_MN, B_MN, STORE>(h, a, b, {out0}, P, st);
-  const cudaError_t e = gemm<A_MN, B_MN, PARTIAL>(h, a, b, {sums}, P, st);
-  if (e != cudaSuccess) return e;
-  const long long values = p.rows * p.cols;
-  return ff_launch(ffn_join_kernel, dim3((unsigned)((values / 8 + 255) / 256), (unsigned)p.mats), dim3(256), 0, st, (const float*)sums, P.split, values,
-                   (__nv_bfloat16*)out0, (__nv_bfloat16*)out1);
+// GATE or DGATE: `e` are the matrices of the epilogue in the order of GemmMaps, all with the extents of the output.
+template <bool A_MN, bool B_MN, int EPI, int NT>
+cudaError_t gemm(const ff_ffn* h, const Matrix& a, const Matrix& b0, const Matrix& b1, long long rows, int cols, int k, std::initializer_list<const void*> e,
+                 int keep, cudaStream_t st) {
+  GemmMaps m = {};
+  if (!matrix_map(h, &m.a[0], a.p, a.rows, a.cols, A_MN ? 64 : 128) || !matrix_map(h, &m.b[0], b0.p, b0.rows, b0.cols, B_MN ? 64 : NT / 2) ||
+      !matrix_map(h, &m.b[1], b1.p, b1.rows, b1.cols, B_MN ? 64 : NT / 2))
+    return cudaErrorInvalidValue;
+  int n = 0;
+  for (const void* p : e)
+    if (!matrix_map(h, &m.e[n++], p, rows, cols, 32)) return cudaErrorInvalidValue;
+  GemmParams P = {};
+  Sub& s = P.sub[0];
+  const int width = EPI == GATE ? NT / 2 : NT;
+  s.rows = rows; s.cols = cols;
+  s.m_tiles = (int)((rows + TM - 1) / TM);
+  s.n_tiles = (cols + width - 1) / width;
+  s.mats = s.sources = s.split = 1;
+  s.kchunks = k;
+  P.items = s.items = s.m_tiles * s.n_tiles;
+  P.keep = keep;
+  return launch_gemm<EPI, NT>(h, ffn_gemm_kernel<A_MN, B_MN, EPI, NT>, m, 1, 2, n, P, st);
+}
+// Up to three products without more to do, in one launch, and the join of those cut along K: out[i] = A[0] B[i], or with two sources
+// out[0] = A[0] B[0] + A[1] B[1].
+struct Wanted { Product p; int split, sources; bool a_mn, b_mn; Matrix a[2], b[2]; void* out[2]; };
+cudaError_t products(const ff_ffn* h, const Wanted* w, int count, char* sums, cudaStream_t st) {
+  GemmMaps m = {};
+  GemmParams P = {};
+  JoinParams J = {};
+  int na = 0, nb = 0, ne = 0, order[3] = {0, 1, 2}, blocks = 0;
+  for (int i = 1; i < count; ++i)                                // the longest items first
+    for (int j = i; j && w[order[j]].p.k / w[order[j]].split > w[order[j - 1]].p.k / w[order[j - 1]].split; --j) {
+      const int t = order[j]; order[j] = order[j - 1]; order[j - 1] = t;
+    }
+  for (int i = 0; i < count; ++i) {
+    const Wanted& x = w[order[i]];
+    Sub& s = P.sub[i];
+    s.rows = x.p.rows; s.cols = x.p.cols; s.mats = x.p.mats;
+    s.m_tiles = (int)((s.rows + TM - 1) / TM);
+    s.n_tiles = (s.cols + TN - 1) / TN;
+    s.sources = x.sources; s.kchunks = x.p.k / x.sources;
+    s.split = x.split;
+    s.items = s.m_tiles * s.n_tiles * s.mats * s.split;
+    s.a_mn = x.a_mn; s.b_mn = x.b_mn;
+    s.a = na; s.b = nb; s.e = ne;
+    P.items += s.items;
+    for (int j = 0; j < x.sources; ++j)
+      if (!matrix_map(h, &m.a[na++], x.a[j].p, x.a[j].rows, x.a[j].cols, x.a_mn ? 64 : 128)) return cudaErrorInvalidValue;
+    for (int j = 0; j < (x.sources > s.mats ? x.sources : s.mats); ++j)
+      if (!matrix_map(h, &m.b[nb++], x.b[j].p, x.b[j].rows, x.b[j].cols, x.b_mn ? 64 : 128)) return cudaErrorInvalidValue;
+    if (s.split == 1) {
+      for (int j = 0; j < s.mats; ++j)
+        if (!matrix_map(h, &m.e[ne++], x.out[j], s.rows, s.cols, 32)) return cudaErrorInvalidValue;
+      continue;
+    }
+    if (!sums_map(&m.e[ne++], sums, s.rows, s.cols, s.mats * s.split)) return cudaErrorInvalidValue;
+    const long long values = s.rows * s.cols;
+    for (int j = 0; j < s.mats; ++j) {
+      J.j[J.count++] = Joined{(const float*)sums + j * s.split * values, (__nv_bfloat16*)x.out[j], values, s.split, blocks};
+      blocks += (int)((values + 2047) / 2048);
+    }
+    sums += sums_bytes(x.p, s.split);
+  }
+  const cudaError_t e = launch_gemm<PRODUCTS, TN>(h, ffn_gemm_kernel<false, false, PRODUCTS, TN>, m, na, nb, ne, P, st);
+  return e != cudaSuccess || !J.count ? e : ff_launch(ffn_join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, J);
 }
 
 // How the few-token kernel would run a product (tokens of a tile, CTAs of a cluster), and the estimated time of that: a chunk of
@@ -815,11 +928,14 @@ ff_status_t check_call(ff_ffn* h, int64_t tokens, void* ws, size_t ws_bytes, int
   if (need && (((uintptr_t)ws) & 255)) return fail(h, FF_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
   return FF_OK;
 }
-// The products of a call: out;  dX;  dWg and dWu;  dWd
 Product down_product(const ff_ffn_config_t& c, int64_t tokens) { return {tokens, c.dim, 1, chunks(c.hidden)}; }
-Product dx_product(const ff_ffn_config_t& c, int64_t tokens) { return {tokens, c.dim, 1, 2 * chunks(c.hidden)}; }
-Product dw_product(const ff_ffn_config_t& c, int64_t tokens) { return {c.dim, c.hidden, 2, chunks(tokens)}; }
-Product dwd_product(const ff_ffn_config_t& c, int64_t tokens) { return {c.hidden, c.dim, 1, chunks(tokens)}; }
+// dX;  dWg and dWu;  dWd, with their parts, the same whichever of them a call wants
+struct Gradients { Product p[3]; int split[3]; };
+Gradients gradients_of(const ff_ffn_config_t& c, int64_t tokens) {
+  Gradients g = {{{tokens, c.dim, 1, 2 * chunks(c.hidden)}, {c.dim, c.hidden, 2, chunks(tokens)}, {c.hidden, c.dim, 1, chunks(tokens)}}, {1, 1, 1}};
+  splits_of(g.p, 3, g.split);
+  return g;
+}
 size_t hidden_bytes(const ff_ffn_config_t& c, int64_t tokens) { return ((size_t)tokens * c.hidden * 2 + 255) / 256 * 256; }
 
 }  // namespace
@@ -837,14 +953,14 @@ extern "C" ff_status_t ff_ffn_workspace_bytes(const ff_ffn_config_t* c, int64_t 
   const ff_status_t s = ff_ffn_validate(c);
   if (s != FF_OK) return s;
   if (!bytes || tokens < 0) return fail(nullptr, FF_ERR_INVALID_ARG, "bytes is NULL or tokens negative");
-  // H;  backward: dG, dU, H;  behind them the sums of the product that needs most (one at a time)
+  // H;  backward: dG, dU, H;  behind them the sums of products whose K is cut
   *bytes = (training ? 3 : 1) * hidden_bytes(*c, tokens);
-  if (tokens > 0) {
-    size_t sums = 0;
-    auto need = [&](const Product& p) { const size_t b = sums_bytes(p); if (b > sums) sums = b; };
-    if (training) { need(dx_product(*c, tokens)); need(dw_product(*c, tokens)); need(dwd_product(*c, tokens)); }
-    else need(down_product(*c, tokens));
-    *bytes += (sums + 255) / 256 * 256;
+  if (tokens > 0 && training) {
+    const Gradients g = gradients_of(*c, tokens);
+    for (int i = 0; i < 3; ++i) *bytes += sums_bytes(g.p[i], g.split[i]);
+  } else if (tokens > 0) {
+    const Product down = down_product(*c, tokens);
+    *bytes += sums_bytes(down, split_of(down));
   }
   return FF_OK;
 }
@@ -860,13 +976,10 @@ extern "C" ff_status_t ff_ffn_create(const ff_ffn_config_t* cfg, ff_ffn_t** out)
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device);
   const struct { const void* kernel; size_t smem; } kernels[] = {
-      {(const void*)ffn_gemm_kernel<false, true, GATE, TN>, smem_bytes(GATE)}, {(const void*)ffn_gemm_kernel<false, true, STORE, TN>, smem_bytes(STORE)},
-      {(const void*)ffn_gemm_kernel<false, false, DGATE, TN>, smem_bytes(DGATE)}, {(const void*)ffn_gemm_kernel<false, false, STORE, TN>, smem_bytes(STORE)},
-      {(const void*)ffn_gemm_kernel<true, true, STORE, TN>, smem_bytes(STORE)}, {(const void*)ffn_gemm_kernel<false, true, PARTIAL, TN>, smem_bytes(PARTIAL)},
-      {(const void*)ffn_gemm_kernel<false, false, PARTIAL, TN>, smem_bytes(PARTIAL)}, {(const void*)ffn_gemm_kernel<true, true, PARTIAL, TN>, smem_bytes(PARTIAL)},
-      {(const void*)ffn_gemm_kernel<false, true, GATE, 128>, smem_bytes(GATE, 128)},
-      {(const void*)ffn_gemm_kernel<false, false, DGATE, 128>, smem_bytes(DGATE, 128)}, {(const void*)ffn_few_kernel<GATE>, FEW_SMEM},
-      {(const void*)ffn_few_kernel<STORE>, FEW_SMEM}};
+      {(const void*)ffn_gemm_kernel<false, true, GATE, TN>, smem_bytes(GATE)}, {(const void*)ffn_gemm_kernel<false, true, GATE, 128>, smem_bytes(GATE, 128)},
+      {(const void*)ffn_gemm_kernel<false, false, DGATE, TN>, smem_bytes(DGATE)}, {(const void*)ffn_gemm_kernel<false, false, DGATE, 128>, smem_bytes(DGATE, 128)},
+      {(const void*)ffn_gemm_kernel<false, false, PRODUCTS, TN>, smem_bytes(PRODUCTS)}, {(const void*)ffn_few_kernel<GATE>, FEW_SMEM},
+      {(const void*)ffn_few_kernel<PRODUCTS>, FEW_SMEM}};
   for (const auto& k : kernels)
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.smem);
   for (int mats = 1; mats <= 2; ++mats)
@@ -875,7 +988,7 @@ extern "C" ff_status_t ff_ffn_create(const ff_ffn_config_t* cfg, ff_ffn_t** out)
         int clusters = 0;
         const size_t smem = few_smem(wide ? 128 : 64, mats);
         e = mats == 2 ? ff_max_clusters(&clusters, ffn_few_kernel<GATE>, dim3(FEW_THREADS), split, smem)
-                      : ff_max_clusters(&clusters, ffn_few_kernel<STORE>, dim3(FEW_THREADS), split, smem);
+                      : ff_max_clusters(&clusters, ffn_few_kernel<PRODUCTS>, dim3(FEW_THREADS), split, smem);
         // (asked for kernels that use tensor memory, the runtime counts one block an SM; two run where shared memory has room for them)
         h->room[mats - 1][wide][split] = clusters * split * (int)(233472 / (smem + 1024));
       }
@@ -930,21 +1043,21 @@ extern "C" ff_status_t ff_ffn_forward(ff_ffn_t* h, int64_t tokens, const void* X
   const FewShape up_few = few_shape(h, tokens, F, chunks(D), 2), down_few = few_shape(h, tokens, D, chunks(F), 1);
   const Product down = down_product(h->cfg, tokens);
   double down_us;
-  split_of(down, &down_us);
+  const int down_split = split_of(down, &down_us);
   down_us += 2;
   const Tiling up_tiling = tiling_of(tokens, F, 128, chunks(D), GATE_EPILOGUE);
-  const double up_us = up_tiling.us;
-  if (up_few.us < up_us) {
+  if (up_few.us < up_tiling.us) {
     FFN_CUDA(h, few<GATE>(h, up_few, Wg, Wu, X, tokens, F, D, {ws, gate, up}, st));
   } else {
-    GemmParams P{};
-    P.rows = tokens; P.cols = F; P.mats = P.sources = P.split = 1;
-    P.kchunks = chunks(D); P.keep = gate != nullptr;
-    if (up_tiling.narrow) FFN_CUDA(h, (gemm<false, true, GATE, 128>(h, {x, x}, {wg, wu}, {ws, gate ? gate : ws, up ? up : ws}, P, st)));
-    else FFN_CUDA(h, (gemm<false, true, GATE>(h, {x, x}, {wg, wu}, {ws, gate ? gate : ws, up ? up : ws}, P, st)));
+    const auto run = up_tiling.narrow ? gemm<false, true, GATE, 128> : gemm<false, true, GATE, TN>;
+    FFN_CUDA(h, run(h, x, wg, wu, tokens, F, chunks(D), {ws, gate ? gate : ws, up ? up : ws}, gate != nullptr, st));
   }
-  if (down_few.us < down_us) FFN_CUDA(h, few<STORE>(h, down_few, Wd, Wd, ws, tokens, D, F, {out, nullptr, nullptr}, st));
-  else FFN_CUDA(h, (product<false, true>(h, {hid, hid}, {wd, wd}, down, 1, out, nullptr, (char*)ws + hidden_bytes(h->cfg, tokens), st)));
+  if (down_few.us < down_us) {
+    FFN_CUDA(h, few<PRODUCTS>(h, down_few, Wd, Wd, ws, tokens, D, F, {out, nullptr, nullptr}, st));
+  } else {
+    const Wanted w = {down, down_split, 1, false, true, {hid}, {wd}, {out}};
+    FFN_CUDA(h, products(h, &w, 1, (char*)ws + hidden_bytes(h->cfg, tokens), st));
+  }
   return FF_OK;
 }
 
@@ -970,14 +1083,14 @@ extern "C" ff_status_t ff_ffn_backward(ff_ffn_t* h, int64_t tokens, const void* 
   void *dG = base, *dU = base + hidden_bytes(h->cfg, tokens), *H = base + 2 * hidden_bytes(h->cfg, tokens);
   const Matrix x{X, tokens, D}, g{dout, tokens, D}, wg{Wg, D, F}, wu{Wu, D, F}, wd{Wd, F, D};
   const Matrix dg{dG, tokens, F}, du{dU, tokens, F}, hid{H, tokens, F};
-  GemmParams P{};
-  P.rows = tokens; P.cols = F; P.mats = P.sources = P.split = 1;
-  P.kchunks = chunks(D);
-  if (tiling_of(tokens, F, TN, chunks(D), DGATE_EPILOGUE).narrow) FFN_CUDA(h, (gemm<false, false, DGATE, 128>(h, {g, g}, {wd, wd}, {gate, up, dG, dU, H}, P, st)));
-  else FFN_CUDA(h, (gemm<false, false, DGATE>(h, {g, g}, {wd, wd}, {gate, up, dG, dU, H}, P, st)));
-  void* sums = base + 3 * hidden_bytes(h->cfg, tokens);
-  if (dX) FFN_CUDA(h, (product<false, false>(h, {dg, du}, {wg, wu}, dx_product(h->cfg, tokens), 2, dX, nullptr, sums, st)));
-  if (dWg) FFN_CUDA(h, (product<true, true>(h, {x, x}, {dg, du}, dw_product(h->cfg, tokens), 1, dWg, dWu, sums, st)));
-  if (dWd) FFN_CUDA(h, (product<true, true>(h, {hid, hid}, {g, g}, dwd_product(h->cfg, tokens), 1, dWd, nullptr, sums, st)));
+  const auto run = tiling_of(tokens, F, TN, chunks(D), DGATE_EPILOGUE).narrow ? gemm<false, false, DGATE, 128> : gemm<false, false, DGATE, TN>;
+  FFN_CUDA(h, run(h, g, wd, wd, tokens, F, chunks(D), {gate, up, dG, dU, H}, 0, st));
+  const Gradients made = gradients_of(h->cfg, tokens);
+  Wanted w[3];
+  int count = 0;
+  if (dX) w[count++] = Wanted{made.p[0], made.split[0], 2, false, false, {dg, du}, {wg, wu}, {dX}};
+  if (dWg) w[count++] = Wanted{made.p[1], made.split[1], 1, true, true, {x}, {dg, du}, {dWg, dWu}};
+  if (dWd) w[count++] = Wanted{made.p[2], made.split[2], 1, true, true, {hid}, {g}, {dWd}};
+  FFN_CUDA(h, products(h, w, count, base + 3 * hidden_bytes(h->cfg, tokens), st));
   return FF_OK;
 }
