@@ -713,19 +713,19 @@ int split_of(long long tiles, int k, double values, double* us = nullptr) {
 }
 // The same for a product with an epilogue, whose K stays whole: tiles of 256 columns or narrow ones, of which there are twice as many.
 // A chunk of a narrow tile takes 0.22 us (three quarters of the bytes for half the products), the epilogue of a tile, which overlaps the
-// next tile's products, `epilogue` us or half of that.  Measured, wide / narrow, us: backward of 200 tokens, dim 1264, hidden 2464 44.7 / 38.1,
+// next tile's products, `epilogue` us of a wide one and of a narrow one.  Measured, wide / narrow, us: backward of 200 tokens, dim 1264, hidden 2464 44.7 / 38.1,
 // of 4000 165 / 175; forward of 128 tokens, dim 512, hidden 1408 13.5 / 12.0, of 1000 tokens, dim 1024, hidden 2816 28.6 / 30.2.
 struct Tiling { bool narrow; double us; };
-Tiling tiling_of(long long rows, int cols, int width, int k, double epilogue) {
+Tiling tiling_of(long long rows, int cols, int width, int k, const double (&epilogue)[2]) {
   constexpr int pairs = FF_B200_SMS / 2;
   auto time = [&](int w, double chunk, double epi) {
     const long long tiles = ((rows + TM - 1) / TM) * ((cols + w - 1) / w);
     return (double)((tiles + pairs - 1) / pairs) * (k * chunk > epi ? k * chunk : epi) + epi;
   };
-  const double wide = time(width, 0.28, epilogue), narrow = time(width / 2, 0.22, epilogue / 2);
+  const double wide = time(width, 0.28, epilogue[0]), narrow = time(width / 2, 0.22, epilogue[1]);
   return {narrow < wide, narrow < wide ? narrow : wide};
 }
-constexpr double GATE_EPILOGUE = 2, DGATE_EPILOGUE = 8;
+constexpr double GATE_EPILOGUE[2] = {2, 1.8}, DGATE_EPILOGUE[2] = {8, 4};       // (of a narrow gated tile half the warps make H)
 struct Product {
   long long rows;                  // extents of an output
   int cols, mats, k;               // matrices, K chunks in all
@@ -843,7 +843,7 @@ cudaError_t products(const ff_ffn* h, const Wanted* w, int count, char* sums, cu
 
 // How the few-token kernel would run a product (tokens of a tile, CTAs of a cluster), and the estimated time of that: a chunk of
 // K takes a CTA 0.35 us (0.5 with two matrices: more to load), the exchange of the partial sums 0.02 us for a token and matrix
-// (what a CTA reads from others' shared memory, at 25 B/ns), start and end 1 us.  Clusters of three and more do not fill all SMs.
+// (what a CTA reads from others' shared memory, at 25 B/ns; 0.012 from its own), start and end 1 us.  Clusters of three and more do not fill all SMs.
 struct FewShape { int nt, split, f_tiles, t_tiles; double us; };
 int few_stages(int nt, int mats) {
   // Up to 64 tokens the rings leave room for a CTA of either product on an SM, so that the second one's weights are on their way
@@ -867,8 +867,8 @@ FewShape few_shape(const ff_ffn* h, long long tokens, int features, int kchunks,
   for (int split = 1; split <= 8 && split <= kchunks; ++split) {
     const int room = h->room[mats - 1][s.nt == 128][split];
     if (room < split) continue;
-    const double us = 1 + (double)((tiles * split + room - 1) / room) * ((kchunks + split - 1) / split) * (mats == 2 ? 0.5 : 0.35) +
-                      (split > 1 ? 0.02 * mats * (double)(tokens < s.nt ? tokens : s.nt) : 0);
+    const double exchange = (split > 1 ? 0.02 : 0.012) * mats * (double)(tokens < s.nt ? tokens : s.nt);
+    const double us = 1 + (double)((tiles * split + room - 1) / room) * (((kchunks + split - 1) / split) * (mats == 2 ? 0.5 : 0.35) + exchange);
     if (us < s.us) { s.split = split; s.us = us; }
   }
   return s;
