@@ -109,3 +109,25 @@ def test_refusals():
     assert lib.ff_forward_projected_rotary(plan.handle, *[x.data_ptr()] * 3, None, None, 0, None, None, 0.0, None, None, x.data_ptr(), None) != 0
     assert lib.ff_forward_projected_rotary(None, *[None] * 5, 0, None, None, 0.0, None, None, None, None) == 1
     plan.destroy()
+
+
+def test_positions_of_each_sample():
+    # samples do not enter each other's sums: each must be what the same call gives it with its positions for both
+    cfg = CFG.scaled("layer_pair", batch=2)
+    rotary = B.Rotary(RotaryConfig(cfg.head_dim, 48))
+    weights = I.router_weights(cfg)
+    plan = B.Plan(cfg, weights, host_staging=True)
+    X, (Wqkv, Wo) = I.layer_input(cfg), I.projection_weights(cfg)
+    x, wqkv, wo = (torch.from_numpy(a).to("cuda", torch.bfloat16) for a in (X, Wqkv, Wo))
+    masks = torch.tensor([1, 2, 4, 7] * 2, dtype=torch.uint8, device="cuda")
+    one = torch.arange(cfg.N, dtype=torch.int32, device="cuda")
+    two = one.flip(0).contiguous()
+
+    def call(positions):
+        return plan.forward_projected(x, wqkv, wo, torch.empty_like(x), alloc=masks, rotary=rotary, eps=EPS, positions=positions).clone()
+    first, second, both = call(one), call(two), call(torch.stack((one, two)))
+    assert plan.device_status() == 0
+    assert not torch.equal(first[1], second[1])
+    assert torch.equal(both[0], first[0]) and torch.equal(both[1], second[1])
+    assert torch.equal(call(None), first)
+    plan.destroy()
