@@ -335,7 +335,8 @@ ff_status_t ff_qk_norm(const ff_rotary_t *rotary, int64_t batch, int64_t tokens,
 
 /* Its backward pass: from the inputs q, k and the gradients of the outputs, the gradients of the inputs (dq may
  * be dq_out, or q) and of the weights (device, float [head_dim]; NULL: not wanted).  The weights' sums run over
- * all rows in an order that depends on the sizes alone: the same call gives the same bits.
+ * all rows in an order that depends on the sizes alone: the same call gives the same bits.  Sums over no rows are
+ * zeros: of a call with no tokens, and dwk of one without k (whose wk is not read).
  *   workspace  device, 16-byte aligned, ff_qk_norm_workspace_bytes; calls that may run at the same time need
  *              one each */
 ff_status_t ff_qk_norm_backward(const ff_rotary_t *rotary, int64_t batch, int64_t tokens, const int32_t *positions,

@@ -537,7 +537,7 @@ class Rotary:
         return q_out, k_out
 
     def qk_norm_backward(self, q, k, wq, wk, dq_out, dk_out, dq, dk, dwq=None, dwk=None, eps: float = 1e-6, positions=None):
-        """Gradients of q, k (and of the weights, fp32 [head_dim], where given) from those of qk_norm's outputs."""
+        """Gradients of q, k (and of the weights, fp32 [head_dim], where given) from those of qk_norm's outputs; dwk without k: zeros."""
         place, (hq, hk, hgq, hgk, hdq, hdk), keep = self._arguments(positions, q, k, dq_out, dk_out, dq, dk)
         dev = q.device
         # (a workspace per call: calls on different streams and captured graphs share none)

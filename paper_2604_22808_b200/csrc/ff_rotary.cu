@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(H_THREADS, 2) heads_backward_kernel(const __gr
   }
 }
 
-// dw[t][c] = sum of the partial rows of q (t = 0) or k, in a fixed order.  One block: 32 columns of one of them.
+// dw[t][c] = sum of the partial rows of q (t = 0) or k, in a fixed order (no rows: zeros).  One block: 32 columns of one of them.
 __global__ void __launch_bounds__(1024) weight_gradient_kernel(const float* partial, int rows_q, int rows_k, int d, float* dwq, float* dwk) {
   __shared__ float sum[32][33];
   ff_pdl_wait();
@@ -724,7 +724,7 @@ ff_status_t run(const ff_rotary_t* handle, int mode, int64_t batch, int64_t toke
   if (batch * tokens == 0) {        // nothing to turn; sums over no rows are zero
     cudaError_t e = cudaSuccess;
     if (mode == NORM_BACKWARD && dwq) e = cudaMemsetAsync(dwq, 0, sizeof(float) * c.head_dim, st);
-    if (e == cudaSuccess && mode == NORM_BACKWARD && dwk && kinds == 2) e = cudaMemsetAsync(dwk, 0, sizeof(float) * c.head_dim, st);
+    if (e == cudaSuccess && mode == NORM_BACKWARD && dwk) e = cudaMemsetAsync(dwk, 0, sizeof(float) * c.head_dim, st);
     return e == cudaSuccess ? FF_OK : cuda_fail(h, e);
   }
 
@@ -782,7 +782,7 @@ ff_status_t run(const ff_rotary_t* handle, int mode, int64_t batch, int64_t toke
   else if (mode == NORM) e = call.e == 4 ? launch_chunk<float, NORM>(ch, inter, grid, st, P) : launch_chunk<__nv_bfloat16, NORM>(ch, inter, grid, st, P);
   else e = call.e == 4 ? launch_chunk<float, NORM_BACKWARD>(ch, inter, grid, st, P) : launch_chunk<__nv_bfloat16, NORM_BACKWARD>(ch, inter, grid, st, P);
   if (e == cudaSuccess && want_dw)
-    e = ff_launch(weight_gradient_kernel, dim3((d + 31) / 32, kinds), dim3(1024), 0, st, (const float*)P.partial, P.nblocks0,
+    e = ff_launch(weight_gradient_kernel, dim3((d + 31) / 32, dwk ? 2 : 1), dim3(1024), 0, st, (const float*)P.partial, P.nblocks0,
                   (int)grid.x - P.nblocks0, d, dwq, dwk);
   return e == cudaSuccess ? FF_OK : cuda_fail(h, e);
 }

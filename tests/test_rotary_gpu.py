@@ -364,3 +364,19 @@ def test_binding_refusals():
                  lambda: h.qk_norm_backward(x, x, None, None, x, None, x, x)):
         with pytest.raises(B.FFError):
             call()
+
+
+@pytest.mark.parametrize("tokens", (0, 1, 700))
+def test_weight_gradient_without_keys(tokens):
+    """dwk of a call without keys is a sum over no rows: zeros, and dwq as without it."""
+    h = B.Rotary(RotaryConfig(64, 64))
+    gen = torch.Generator("cuda").manual_seed(11)
+    x, g = (torch.randn(1, 2, tokens, 64, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    w = torch.rand(64, generator=gen, device="cuda") + 0.5
+    dq, dwq, alone, dwk = torch.empty_like(x), *(torch.full((64,), 7.0, device="cuda") for _ in range(3))
+    h.qk_norm_backward(x, None, w, None, g, None, dq, None, alone)
+    h.qk_norm_backward(x, None, w, w, g, None, dq, None, dwq, dwk)
+    assert not dwk.any() and torch.equal(dwq, alone)
+    dwk.fill_(7.0)
+    h.qk_norm_backward(x, None, w, None, g, None, dq, None, None, dwk)
+    assert not dwk.any()
