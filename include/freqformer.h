@@ -388,12 +388,15 @@ ff_status_t ff_ffn_create(const ff_ffn_config_t *cfg, ff_ffn_t **out);
 ff_status_t ff_ffn_destroy(ff_ffn_t *ffn);            /* NULL is allowed */
 const char *ff_ffn_last_error(const ff_ffn_t *ffn);   /* as ff_last_error */
 
-/* gate, up: both, to keep them for ff_ffn_backward, or both NULL. */
+/* gate, up: both, to keep them for ff_ffn_backward, or both NULL.  They and the workspace overlap no other tensor; out may lie
+ * over X (as over Wg and Wu), which has been read by then, but not over Wd. */
 ff_status_t ff_ffn_forward(ff_ffn_t *ffn, int64_t tokens, const void *X, const void *Wg, const void *Wu, const void *Wd,
                            void *gate, void *up, void *out, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* The gradients of X and of the weights from that of out; dX, dWd, or dWg and dWu together may be NULL.  They
- * overwrite what was there and are the same bits in every call with the same inputs. */
+ * overwrite what was there and are the same bits in every call with the same inputs.  A gradient overlaps neither another
+ * one nor what its launch reads: X where dWg and dWu are wanted, dout where dWd is, Wg and Wu where dX is.  So, unlike dq of
+ * the norm, dX may not be dout in a call for all gradients.  The workspace overlaps no tensor.  Other calls are refused. */
 ff_status_t ff_ffn_backward(ff_ffn_t *ffn, int64_t tokens, const void *X, const void *Wg, const void *Wu, const void *Wd,
                             const void *gate, const void *up, const void *dout, void *dX, void *dWg, void *dWu,
                             void *dWd, void *workspace, size_t workspace_bytes, void *cuda_stream);

@@ -618,14 +618,15 @@ class GatedFFN:
             return self._status(fn(self.handle, tokens, *pointers, ws.data_ptr(), n, self._raw_stream(dev.index)))
 
     def forward(self, X, Wg, Wu, Wd, out, gate=None, up=None):
-        """gate, up [..., hidden]: X Wg and X Wu are written there, for backward."""
+        """gate, up [..., hidden]: X Wg and X Wu are written there, for backward; they overlap nothing.  out may be X."""
         M, xs, hs = self._shapes(X)
         into, back = self._into, self._back
         self._call(self._lib.ff_ffn_forward, False, M, self._pointers(X, xs, Wg, into, Wu, into, Wd, back, gate, hs, up, hs, out, xs))
         return out
 
     def backward(self, X, Wg, Wu, Wd, gate, up, dout, dX=None, dWg=None, dWu=None, dWd=None):
-        """Gradients of X and the weights, where given, from that of out (dWg and dWu together)."""
+        """Gradients of X and the weights, where given, from that of out (dWg and dWu together).  dX may be neither X (where dWg is
+        given) nor dout (where dWd is): other gradients are made from those in the same launch."""
         M, xs, hs = self._shapes(X)
         into, back = self._into, self._back
         self._call(self._lib.ff_ffn_backward, True, M, self._pointers(X, xs, Wg, into, Wu, into, Wd, back, gate, hs, up, hs, dout, xs, dX, xs,

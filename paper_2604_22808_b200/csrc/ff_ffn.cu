@@ -916,16 +916,32 @@ bool misaligned(std::initializer_list<const void*> ps) {
   for (const void* p : ps) all |= (uintptr_t)p;
   return all & 15;
 }
-ff_status_t check_call(ff_ffn* h, int64_t tokens, void* ws, size_t ws_bytes, int training) {
+// A tensor of a call that a launch reads or writes; NULL: not given, or not read by then.
+struct Span { const void* p; size_t bytes; };
+bool meet(const Span& a, const Span& b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+}
+// Does one of `written` overlap another of them or one of `read`?
+bool overlap(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span* w = written.begin(); w != written.end(); ++w) {
+    for (const Span* v = written.begin(); v != w; ++v)
+      if (meet(*w, *v)) return true;
+    for (const Span& r : read)
+      if (meet(*w, r)) return true;
+  }
+  return false;
+}
+ff_status_t check_call(ff_ffn* h, int64_t tokens, void* ws, size_t ws_bytes, int training, size_t* need) {
   if (tokens < 0) return fail(h, FF_ERR_INVALID_ARG, "tokens must not be negative");
   const int64_t widest = h->cfg.dim > h->cfg.hidden ? h->cfg.dim : h->cfg.hidden;
   if (tokens > 0x7fffff00 || tokens * widest > (1ll << 38)) return fail(h, FF_ERR_UNSUPPORTED, "tokens must be below 2^31 - 256, and tokens * hidden at most 2^38");
   int device = -1;
   if (cudaGetDevice(&device) != cudaSuccess || device != h->device) return fail(h, FF_ERR_INVALID_ARG, "the handle belongs to another device than the current one");
-  size_t need = 0;
-  ff_ffn_workspace_bytes(&h->cfg, tokens, training, &need);
-  if (need && (!ws || ws_bytes < need)) return fail(h, FF_ERR_WORKSPACE, "the workspace is missing or smaller than ff_ffn_workspace_bytes");
-  if (need && (((uintptr_t)ws) & 255)) return fail(h, FF_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
+  *need = 0;
+  ff_ffn_workspace_bytes(&h->cfg, tokens, training, need);
+  if (*need && (!ws || ws_bytes < *need)) return fail(h, FF_ERR_WORKSPACE, "the workspace is missing or smaller than ff_ffn_workspace_bytes");
+  if (*need && (((uintptr_t)ws) & 255)) return fail(h, FF_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
   return FF_OK;
 }
 Product down_product(const ff_ffn_config_t& c, int64_t tokens) { return {tokens, c.dim, 1, chunks(c.hidden)}; }
@@ -1028,13 +1044,18 @@ extern "C" ff_status_t ff_ffn_device_status(ff_ffn_t* h, void* stream) {
 extern "C" ff_status_t ff_ffn_forward(ff_ffn_t* h, int64_t tokens, const void* X, const void* Wg, const void* Wu, const void* Wd, void* gate,
                                       void* up, void* out, void* ws, size_t ws_bytes, void* stream) {
   if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "the handle is NULL");
-  ff_status_t s = check_call(h, tokens, ws, ws_bytes, 0);
+  size_t need;
+  ff_status_t s = check_call(h, tokens, ws, ws_bytes, 0, &need);
   if (s != FF_OK) return s;
   if (!gate != !up) return fail(h, FF_ERR_INVALID_ARG, "gate and up are kept together, or neither is");
   if (tokens == 0) return FF_OK;
   if (!X || !Wg || !Wu || !Wd || !out) return fail(h, FF_ERR_INVALID_ARG, "X, Wg, Wu, Wd or out is NULL");
   if (misaligned({X, Wg, Wu, Wd, gate, up, out})) return fail(h, FF_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
   const int D = h->cfg.dim, F = h->cfg.hidden;
+  // (out is written when X, Wg and Wu have been read)
+  const size_t row = (size_t)tokens * D * 2, hidden = (size_t)tokens * F * 2, weight = (size_t)D * F * 2;
+  if (overlap({{gate, hidden}, {up, hidden}, {ws, need}}, {{X, row}, {Wg, weight}, {Wu, weight}, {Wd, weight}, {out, row}}) || meet({out, row}, {Wd, weight}))
+    return fail(h, FF_ERR_INVALID_ARG, "gate, up or the workspace overlaps another tensor, or out overlaps Wd");
   cudaStream_t st = (cudaStream_t)stream;
   const Matrix x{X, tokens, D}, hid{ws, tokens, F}, wg{Wg, D, F}, wu{Wu, D, F}, wd{Wd, F, D};
   // Either product runs on the kernel whose estimate is lower (2 us more for start and end of the larger one).  Measured, dim 2048, hidden 5632, both products on tiles of 256
@@ -1065,7 +1086,8 @@ extern "C" ff_status_t ff_ffn_backward(ff_ffn_t* h, int64_t tokens, const void* 
                                        const void* up, const void* dout, void* dX, void* dWg, void* dWu, void* dWd, void* ws, size_t ws_bytes,
                                        void* stream) {
   if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "the handle is NULL");
-  ff_status_t s = check_call(h, tokens, ws, ws_bytes, 1);
+  size_t need;
+  ff_status_t s = check_call(h, tokens, ws, ws_bytes, 1, &need);
   if (s != FF_OK) return s;
   if (!dWg != !dWu) return fail(h, FF_ERR_INVALID_ARG, "dWg and dWu are made together, or neither is");
   if (misaligned({X, Wg, Wu, Wd, gate, up, dout, dX, dWg, dWu, dWd})) return fail(h, FF_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
@@ -1079,6 +1101,13 @@ extern "C" ff_status_t ff_ffn_backward(ff_ffn_t* h, int64_t tokens, const void* 
   }
   if (!X || !Wg || !Wu || !Wd || !gate || !up || !dout) return fail(h, FF_ERR_INVALID_ARG, "X, Wg, Wu, Wd, gate, up or dout is NULL");
   if (!dX && !dWg && !dWd) return FF_OK;
+  // (the launch that writes the gradients reads X for dWg and dWu, dout for dWd, Wg and Wu for dX; gate, up and Wd have been read by then)
+  const size_t row = (size_t)tokens * D * 2, hidden = (size_t)tokens * F * 2, weight = (size_t)D * F * 2;
+  const Span all{ws, need};
+  if (overlap({{dX, row}, {dWg, weight}, {dWu, weight}, {dWd, weight}, all},
+              {{dWg ? X : nullptr, row}, {dWd ? dout : nullptr, row}, {dX ? Wg : nullptr, weight}, {dX ? Wu : nullptr, weight}}) ||
+      overlap({all}, {{X, row}, {Wg, weight}, {Wu, weight}, {Wd, weight}, {gate, hidden}, {up, hidden}, {dout, row}}))
+    return fail(h, FF_ERR_INVALID_ARG, "a gradient overlaps another one or what it is made from, or the workspace overlaps a tensor");
   char* base = (char*)ws;
   void *dG = base, *dU = base + hidden_bytes(h->cfg, tokens), *H = base + 2 * hidden_bytes(h->cfg, tokens);
   const Matrix x{X, tokens, D}, g{dout, tokens, D}, wg{Wg, D, F}, wu{Wu, D, F}, wd{Wd, F, D};

@@ -5,6 +5,7 @@ A sum of K products in fp32 is below K 2^-22 off, relative to the sum of the pro
 tensor core cuts).  The activation and its derivative are below 1e-5 (1 + |g|) off absolutely (exponential and reciprocal, 2^-21
 relative, its argument's rounding |g| 2^-23 in front), and their slopes below 1.2 and 2.  What goes into a product reaches its result
 through the other operand's sizes."""
+import ctypes as C
 import math
 
 import pytest
@@ -337,3 +338,52 @@ def test_binding_refusals():
                  lambda: B.GatedFFN(FFNConfig(60, 128)), lambda: B.GatedFFN(FFNConfig(64, 128, "relu"))):
         with pytest.raises(B.FFError):
             call()
+
+
+def test_overlap():
+    """What a launch would read while it is written is refused; what has been read by then may be written over."""
+    M, D, F = 40, 128, 128                       # (one size for all: any tensor may be laid over any other)
+    X, Wg, Wu, Wd, dout = inputs(M, D, F)
+    gate, up = X @ Wg, X @ Wu
+    ffn = B.GatedFFN(FFNConfig(D, F))
+    out, dX, y = (torch.empty_like(X) for _ in range(3))
+    grads = [torch.empty_like(t) for t in (Wg, Wu, Wd)]
+    ffn.forward(X, Wg, Wu, Wd, out)
+    ffn.backward(X, Wg, Wu, Wd, gate, up, dout, dX, *grads)
+
+    def refused(call):
+        with pytest.raises(B.FFError) as e:
+            call()
+        assert e.value.status == 1 and "overlap" in str(e.value)
+    both = torch.cat([X, X])                     # rows 0 .. M-1 and 1 .. M of it overlap
+    part, shifted = both[:M], both[1:M + 1]
+    refused(lambda: ffn.forward(X, Wg, Wu, Wd, y, X, up))
+    refused(lambda: ffn.forward(X, Wg, Wu, Wd, y, gate, gate))
+    refused(lambda: ffn.forward(X, Wg, Wu, Wd, gate, gate, up))
+    refused(lambda: ffn.forward(X, Wg, Wu, Wd, y, Wd[:M], up))
+    refused(lambda: ffn.forward(X, Wg, Wu, Wd, Wd[:M]))
+    refused(lambda: ffn.forward(part, Wg, Wu, Wd, y, shifted, up))
+    for bad in (X, dout, Wg[:M], Wu[:M], grads[2][:M]):
+        refused(lambda: ffn.backward(X, Wg, Wu, Wd, gate, up, dout, bad, *grads))
+    refused(lambda: ffn.backward(part, Wg, Wu, Wd, gate, up, dout, shifted, *grads))
+    refused(lambda: ffn.backward(X, Wg, Wu, Wd, gate, up, dout, None, grads[0], grads[0]))
+    refused(lambda: ffn.backward(X, Wg, Wu, Wd, gate, up, dout, dX, Wg, grads[1]))
+    lib, need = B.library(), C.c_size_t()
+    args = [t.data_ptr() for t in (X, Wg, Wu, Wd)]
+    B._check(lib.ff_ffn_workspace_bytes(C.byref(ffn._c), M, False, C.byref(need)))
+    store = torch.empty(need.value + 2 * X.numel(), dtype=torch.uint8, device="cuda")
+    over = store[need.value - 256:].data_ptr()   # its first 256 bytes are the workspace's last
+    assert lib.ff_ffn_forward(ffn.handle, M, *args, None, None, over, store.data_ptr(), need.value, None) == 1
+    # what has been read: out over X, dX over gate, dWd over Wd, dX over dout without dWd, over X without dWg
+    z = X.clone()
+    ffn.forward(z, Wg, Wu, Wd, z)
+    assert torch.equal(z, out)
+    g, w, u = gate.clone(), Wd.clone(), up.clone()
+    ffn.backward(X, Wg, Wu, w, g, u, dout, g, grads[0], u.new_empty(D, F), w)
+    assert torch.equal(g, dX) and torch.equal(w, grads[2])
+    z = dout.clone()
+    ffn.backward(X, Wg, Wu, Wd, gate, up, z, z)
+    assert torch.equal(z, dX)
+    z = X.clone()
+    ffn.backward(z, Wg, Wu, Wd, gate, up, dout, z, dWd=grads[2])
+    assert torch.equal(z, dX)
