@@ -161,7 +161,7 @@ __device__ __forceinline__ float row_sum(float v, int lanes) {
   return v;
 }
 // 1 / sqrt(mean of squares + eps) of a row whose values the lanes of a group hold.  Rows whose squares leave fp32 are summed
-// again scaled by 2^-70 (eps is far below their mean).
+// again scaled by 2^-70, and eps by its square (an eps that vanishes by that is far below their mean).
 template <int N, int PER>
 __device__ __forceinline__ float row_rms(const F2 (&a)[PER][N], const F2 (&b)[PER][N], int lanes, float inv_d, float eps) {
   const float ss = row_sum(dot<N, PER>(a, a, b, b), lanes);
@@ -174,7 +174,7 @@ __device__ __forceinline__ float row_rms(const F2 (&a)[PER][N], const F2 (&b)[PE
 #pragma unroll
     for (int c = 0; c < N; ++c) { sa[i][c] = mul(a[i][c], two(down, down)); sb[i][c] = mul(b[i][c], two(down, down)); }
   const float sc = row_sum(dot<N, PER>(sa, sa, sb, sb), lanes);
-  return big ? rsqrtf(sc * inv_d) * down : rsqrtf(ss * inv_d + eps);
+  return big ? rsqrtf(fmaf(sc, inv_d, eps * down * down)) * down : rsqrtf(ss * inv_d + eps);
 }
 
 // The chunks that lane `lig` of a row has: channels, whether there are any, whether they are turned.

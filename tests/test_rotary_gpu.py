@@ -380,3 +380,26 @@ def test_weight_gradient_without_keys(tokens):
     dwk.fill_(7.0)
     h.qk_norm_backward(x, None, w, None, g, None, dq, None, None, dwk)
     assert not dwk.any()
+
+
+@pytest.mark.parametrize("eps", (1e30, 1e38))
+def test_large_eps_beside_large_rows(eps):
+    """Rows whose squares leave fp32, with an eps of the size of their mean (1e38) or far below it; rows of ordinary size with the same
+    eps.  The mean and eps are added in fp32 as in any other row: the bounds of normed rows and of their gradients."""
+    cfg = RotaryConfig(64, 32, "fp32")
+    h = B.Rotary(cfg)
+    gen = torch.Generator("cuda").manual_seed(12)
+    x, g = (torch.randn(1, 2, 6, 64, generator=gen, device="cuda") for _ in range(2))
+    x[:, :, ::2] *= 1e19
+    y, dx, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(64, device="cuda")
+    h.qk_norm(x, None, None, None, y, None, eps=eps)
+    h.qk_norm_backward(x, None, None, None, g, None, dx, None, dw, eps=eps)
+    at = given(cfg, None, 1, 6)
+    r = 1 / torch.sqrt(x.double().square().mean(-1, keepdim=True) + eps)
+    n = x.double() * r
+    want = rotate(cfg, h, n, at)
+    within(y, want, half_step(x.dtype) * want.abs() + 3e-6 * rotate(cfg, h, n, at, absolute=True), "norm")
+    dz, big = rotate(cfg, h, g, at, inverse=True), rotate(cfg, h, g, at, absolute=True)
+    want = r * (dz - n * (dz * n).mean(-1, keepdim=True))
+    within(dx, want, half_step(x.dtype) * want.abs() + 1e-5 * r * (big + n.abs() * (big * n.abs()).mean(-1, keepdim=True)), "dx")
+    within(dw, (dz * n).sum((0, 1, 2)), 1e-5 * (big * n.abs()).sum((0, 1, 2)), "dw")
