@@ -1009,7 +1009,12 @@ extern "C" ff_status_t ff_ffn_create(const ff_ffn_config_t* cfg, ff_ffn_t** out)
         h->room[mats - 1][wide][split] = clusters * split * (int)(233472 / (smem + 1024));
       }
   if (e == cudaSuccess) e = cudaMalloc((void**)&h->status, 256);
-  if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);
+  // (cleared before the handle is out, on a stream of its own: the default stream may be busy, and others do not wait for it)
+  cudaStream_t st = nullptr;
+  if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+  if (e == cudaSuccess) e = cudaMemsetAsync(h->status, 0, 256, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (st) cudaStreamDestroy(st);
   if (e != cudaSuccess) {
     if (h->status) cudaFree(h->status);
     delete h;

@@ -387,3 +387,22 @@ def test_overlap():
     z = X.clone()
     ffn.backward(z, Wg, Wu, Wd, gate, up, dout, z, dWd=grads[2])
     assert torch.equal(z, dX)
+
+
+def test_status_of_a_new_handle():
+    """A handle's status word is clear for every stream from the start, also where the default stream is busy while it is made and the
+    word's memory held something else before."""
+    runtime = C.CDLL("libcudart.so.12")
+    blocks = [C.c_void_p() for _ in range(64)]
+    for b in blocks:
+        assert runtime.cudaMalloc(C.byref(b), C.c_size_t(256)) == 0
+        assert runtime.cudaMemset(b, 255, C.c_size_t(256)) == 0
+    torch.cuda.synchronize()
+    for b in blocks:
+        assert runtime.cudaFree(b) == 0
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(200_000_000)
+    ffn = B.GatedFFN(FFNConfig(64, 128))
+    with torch.cuda.stream(side):
+        assert ffn.device_status() == 0
+    torch.cuda.synchronize()
