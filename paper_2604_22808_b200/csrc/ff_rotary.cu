@@ -696,6 +696,8 @@ ff_status_t run(const ff_rotary_t* handle, int mode, int64_t batch, int64_t toke
     if (cells != tokens) return fail(h, FF_ERR_INVALID_ARG, "without positions the tokens are the grid's cells: T * H * W of them");
   }
   if (positions && (((uintptr_t)positions) & 3)) return fail(h, FF_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+  if ((((uintptr_t)w[0]) | ((uintptr_t)w[1]) | ((uintptr_t)dwq) | ((uintptr_t)dwk)) & 3)
+    return fail(h, FF_ERR_INVALID_ARG, "norm weights and their gradients must be 4-byte aligned");
   if (positions && position_stride < 0) return fail(h, FF_ERR_INVALID_ARG, "the positions' stride must not be negative");
   HeadsParams P{};
   Call call{h, batch, tokens, c.dtype == FF_FP32 ? 4 : 2, 0};

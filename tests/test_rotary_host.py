@@ -97,3 +97,21 @@ def test_refused_calls():
     assert back(g=None) == 1 and back(ws=None) == 3 and back(nbytes=64) == 3 and back(ws=4104) == 3
     assert lib.ff_rotary_create(None, None) == 1 and lib.ff_rotary_destroy(None) == 0
     assert lib.ff_qk_norm_workspace_bytes(None, None) == 1
+
+
+def test_refused_weight_addresses():
+    """Norm weights and their gradients that are not aligned to a float are turned down before a launch would read or write them."""
+    lib, h = B.library(), B.Rotary(RotaryConfig(64, 64))
+
+    def norm(wq, wk):
+        return lib.ff_qk_norm(h.handle, 1, 8, None, 0, _heads(), _heads(), wq, wk, 1e-6, _heads(), _heads(), None)
+
+    def back(*w):
+        return lib.ff_qk_norm_backward(h.handle, 1, 8, None, 0, _heads(), _heads(), *w[:2], 1e-6, _heads(), _heads(), _heads(), _heads(),
+                                       *w[2:], 4096, 1 << 24, None)
+    for bad in (4097, 4098, 4099):
+        assert norm(bad, None) == 1 and norm(4096, bad) == 1
+        for i in range(4):
+            w = [4096] * 4
+            w[i] = bad
+            assert back(*w) == 1 and b"aligned" in lib.ff_rotary_last_error(h.handle)
