@@ -804,7 +804,7 @@ extern "C" ff_status_t ff_rotary_create(const ff_rotary_config_t* cfg, ff_rotary
     return fail(nullptr, FF_ERR_INVALID_ARG, "rot_dim must be even and between 2 and head_dim");
   if (c.head_dim % 8 != 0 || c.head_dim > 256) return fail(nullptr, FF_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 and <= 256");
   if (!(c.base >= 1.0) || !(c.base < 1e300)) return fail(nullptr, FF_ERR_INVALID_ARG, "base must be finite and at least 1");
-  if (c.scaling != FF_ROTARY_SCALE_NONE && (!(c.factor >= 1.0) || !(c.factor < 1e9))) return fail(nullptr, FF_ERR_INVALID_ARG, "the scaling factor must be between 1 and 1e9");
+  if (c.scaling != FF_ROTARY_SCALE_NONE && (!(c.factor >= 1.0) || !(c.factor <= 1e9))) return fail(nullptr, FF_ERR_INVALID_ARG, "the scaling factor must be between 1 and 1e9");
   if (c.scaling == FF_ROTARY_SCALE_BY_PARTS && c.original_length < 1) return fail(nullptr, FF_ERR_INVALID_ARG, "scaling by parts needs the original length");
   const int32_t* a = c.axis_pairs;
   const bool axes = a[0] || a[1] || a[2];

@@ -115,3 +115,13 @@ def test_refused_weight_addresses():
             w = [4096] * 4
             w[i] = bad
             assert back(*w) == 1 and b"aligned" in lib.ff_rotary_last_error(h.handle)
+
+
+def test_largest_factor():
+    """The header's range of the scaling factor includes both ends."""
+    for scaling, length in (("linear", 0), ("ntk", 0), ("by_parts", 2048)):
+        plain, _ = B.Rotary(RotaryConfig(64, 64)).frequencies()
+        theta, _ = B.Rotary(RotaryConfig(64, 64, scaling=scaling, factor=1e9, original_length=length)).frequencies()
+        assert math.isclose(theta[-1], plain[-1] / 1e9, rel_tol=1e-12)
+        with pytest.raises(B.FFError):
+            B.Rotary(RotaryConfig(64, 64, scaling=scaling, factor=math.nextafter(1e9, 2e9), original_length=length))
