@@ -364,7 +364,8 @@ ff_status_t ff_forward_projected_rotary(ff_plan_t *plan, const void *X, const vo
  *   Wd              [hidden][dim]
  *   gate, up        [tokens][hidden]: X Wg and X Wu, kept by a training forward for the backward pass
  * The hidden activations (and, backward, the gradients of gate and up) are rounded to bf16 between the products; the
- * accumulators and the activation are fp32.  Any number of tokens, one and zero included.
+ * accumulators and the activation are fp32.  Any number of tokens, one and zero included, up to 2^31 - 256 and to 2^38 values
+ * in the widest tensor.
  *
  * A handle belongs to the device that was current at ff_ffn_create and holds a status word there; like a plan it is
  * not thread-safe, and it has to outlive the graphs its calls are captured into.  Calls are asynchronous on the
@@ -382,7 +383,7 @@ typedef struct {
 } ff_ffn_config_t;
 
 ff_status_t ff_ffn_validate(const ff_ffn_config_t *cfg);
-/* Workspace of a forward (training = 0) or backward (1) call with that many tokens. */
+/* Workspace of a forward (training = 0) or backward (1) call with that many tokens (FF_ERR_UNSUPPORTED: too many). */
 ff_status_t ff_ffn_workspace_bytes(const ff_ffn_config_t *cfg, int64_t tokens, int32_t training, size_t *bytes);
 ff_status_t ff_ffn_create(const ff_ffn_config_t *cfg, ff_ffn_t **out);
 ff_status_t ff_ffn_destroy(ff_ffn_t *ffn);            /* NULL is allowed */

@@ -932,10 +932,14 @@ bool overlap(std::initializer_list<Span> written, std::initializer_list<Span> re
   }
   return false;
 }
+// More tokens than the kernels' indexes and tensor maps take
+constexpr char MOST_TOKENS[] = "tokens must be at most 2^31 - 256, and tokens * hidden (or dim) at most 2^38";
+bool too_many(const ff_ffn_config_t& c, int64_t tokens) {
+  return tokens > 0x7fffff00 || tokens * (int64_t)(c.dim > c.hidden ? c.dim : c.hidden) > (1ll << 38);
+}
 ff_status_t check_call(ff_ffn* h, int64_t tokens, void* ws, size_t ws_bytes, int training, size_t* need) {
   if (tokens < 0) return fail(h, FF_ERR_INVALID_ARG, "tokens must not be negative");
-  const int64_t widest = h->cfg.dim > h->cfg.hidden ? h->cfg.dim : h->cfg.hidden;
-  if (tokens > 0x7fffff00 || tokens * widest > (1ll << 38)) return fail(h, FF_ERR_UNSUPPORTED, "tokens must be below 2^31 - 256, and tokens * hidden at most 2^38");
+  if (too_many(h->cfg, tokens)) return fail(h, FF_ERR_UNSUPPORTED, MOST_TOKENS);
   int device = -1;
   if (cudaGetDevice(&device) != cudaSuccess || device != h->device) return fail(h, FF_ERR_INVALID_ARG, "the handle belongs to another device than the current one");
   *need = 0;
@@ -969,6 +973,7 @@ extern "C" ff_status_t ff_ffn_workspace_bytes(const ff_ffn_config_t* c, int64_t 
   const ff_status_t s = ff_ffn_validate(c);
   if (s != FF_OK) return s;
   if (!bytes || tokens < 0) return fail(nullptr, FF_ERR_INVALID_ARG, "bytes is NULL or tokens negative");
+  if (too_many(*c, tokens)) return fail(nullptr, FF_ERR_UNSUPPORTED, MOST_TOKENS);
   // H;  backward: dG, dU, H;  behind them the sums of products whose K is cut
   *bytes = (training ? 3 : 1) * hidden_bytes(*c, tokens);
   if (tokens > 0 && training) {

@@ -41,3 +41,15 @@ def test_null_handles():
     assert lib.ff_ffn_backward(None, 1, *[None] * 12, 0, None) == 1
     assert lib.ff_ffn_device_status(None, None) == 1
     assert lib.ff_ffn_create(C.byref(B.ff_ffn_config_t(64, 64, 0)), None) == 1
+
+
+@pytest.mark.parametrize("training", (0, 1))
+def test_workspace_of_too_many_tokens(training):
+    """More tokens than a call takes: refused as the call refuses them, instead of a size that has left its type."""
+    lib, n = B.library(), C.c_size_t()
+    for cfg, most in (((8, 8, 0), 0x7fffff00), ((64, 1 << 20, 0), 1 << 18)):
+        c = B.ff_ffn_config_t(*cfg)
+        assert lib.ff_ffn_workspace_bytes(C.byref(c), most, training, C.byref(n)) == 0 and n.value >= (3 if training else 1) * most * cfg[1] * 2
+        for tokens in (most + 1, 1 << 40, (1 << 63) - 1):
+            assert lib.ff_ffn_workspace_bytes(C.byref(c), tokens, training, C.byref(n)) == 2
+            assert lib.ff_last_error(None)
