@@ -634,7 +634,8 @@ class GatedFFN:
         return dX, dWg, dWu, dWd
 
     def device_status(self) -> int:
-        return library().ff_ffn_device_status(self.handle, self._raw_stream(self.device.index))
+        with self._torch.cuda.device(self.device):               # (its default stream is 0, as every device's is)
+            return library().ff_ffn_device_status(self.handle, self._raw_stream(self.device.index))
 
 
 # Same names as the C entry points, for callers that prefer the flat API.

@@ -1,5 +1,6 @@
 """The gated feed-forward block, host side: checks of the configuration and workspace sizes (no GPU)."""
 import ctypes as C
+from types import SimpleNamespace
 
 import pytest
 
@@ -53,3 +54,26 @@ def test_workspace_of_too_many_tokens(training):
         for tokens in (most + 1, 1 << 40, (1 << 63) - 1):
             assert lib.ff_ffn_workspace_bytes(C.byref(c), tokens, training, C.byref(n)) == 2
             assert lib.ff_last_error(None)
+
+
+@pytest.mark.parametrize("current", (0, 1))
+def test_status_is_read_on_the_handles_device(monkeypatch, current):
+    """device_status names its device's current stream, which may be the default one: 0 on any device.  So the call is made with that device
+    current, whichever was before (a fake of torch's device functions and of the library)."""
+    at, seen = [current], []
+
+    class Device:
+        def __init__(self, device):
+            self.index = device.index
+
+        def __enter__(self):
+            self.before, at[0] = at[0], self.index
+
+        def __exit__(self, *_):
+            at[0] = self.before
+    ffn = B.GatedFFN.__new__(B.GatedFFN)
+    ffn.device, ffn.handle = SimpleNamespace(index=1), None
+    ffn._torch = SimpleNamespace(cuda=SimpleNamespace(device=Device, current_device=lambda: at[0]))
+    ffn._raw_stream = lambda index: 0
+    monkeypatch.setattr(B, "library", lambda: SimpleNamespace(ff_ffn_device_status=lambda handle, stream: seen.append(at[0]) or 0))
+    assert ffn.device_status() == 0 and seen == [1] and at == [current]
