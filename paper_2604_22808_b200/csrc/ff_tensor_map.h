@@ -30,20 +30,25 @@ inline bool ff_encode_map(CUtensorMap* map, CUtensorMapDataType type, int rank, 
 }
 
 // Tensor maps kept between calls: encoding the two dozen of a forward took longer on the host than the launches they are
-// for.  An entry is known by what the plan's configuration makes of it (the encoder's own code and the number of slices),
+// for.  An entry is known by what the handle's configuration makes of it (the encoder's own code and the number of slices or rows),
 // never by an address: every use puts in the address it is for, so new tensors cost what old ones do.
 struct FFMapCache {
-  static constexpr int N = 48;             // (a plan has at most 40 kinds; with more, the last ones are encoded every time)
-  CUtensorMap map[N];
+  static constexpr int N = 48;             // (a plan has at most 40 kinds; a feed-forward handle some more with every number of tokens:
+  CUtensorMap map[N];                      //  the one that was not used for longest then makes room)
   int code[N], slices[N];
+  unsigned long long use[N], uses;         // when an entry was last used; uses so far
   int used;
   template <class Encode>
   bool get(CUtensorMap* out, const void* base, int c, int s, Encode encode) {
     const auto replace = ff_tensor_map_driver().replace_address;
-    for (int i = 0; replace && i < used; ++i)
-      if (code[i] == c && slices[i] == s) { *out = map[i]; return replace(out, const_cast<void*>(base)) == CUDA_SUCCESS; }
+    int at = 0;                            // the oldest
+    for (int i = 0; replace && i < used; ++i) {
+      if (code[i] == c && slices[i] == s) { use[i] = ++uses; *out = map[i]; return replace(out, const_cast<void*>(base)) == CUDA_SUCCESS; }
+      if (use[i] < use[at]) at = i;
+    }
     if (!encode()) return false;
-    if (used < N) { map[used] = *out; code[used] = c; slices[used] = s; ++used; }
+    if (used < N) at = used++;
+    map[at] = *out; code[at] = c; slices[at] = s; use[at] = ++uses;
     return true;
   }
 };
