@@ -304,7 +304,10 @@ typedef struct {
 
 /* One tensor of head rows: element (b, h, n, c) lies at data[b stride_batch + h stride_head + n stride_token
  * + c].  Strides in elements, >= 0, any order; rows that are wider aligned move in wider pieces (16 bytes at
- * most).  An output may be its own input (the same address and strides); otherwise outputs overlap nothing. */
+ * most).  Pairs of the interleaved layout move as one piece: addresses and strides (of dimensions longer than one) that are
+ * not multiples of two elements are refused with FF_ERR_UNSUPPORTED; the half layout takes any.  An output may be its own
+ * input (the same address and strides); otherwise outputs overlap nothing.  At most 65536 heads, and batch * tokens below
+ * 2^31 in a call. */
 typedef struct {
   void *data;              /* device */
   int64_t stride_batch, stride_head, stride_token;

@@ -125,3 +125,17 @@ def test_largest_factor():
         assert math.isclose(theta[-1], plain[-1] / 1e9, rel_tol=1e-12)
         with pytest.raises(B.FFError):
             B.Rotary(RotaryConfig(64, 64, scaling=scaling, factor=math.nextafter(1e9, 2e9), original_length=length))
+
+
+@pytest.mark.parametrize("dtype,size", (("bf16", 2), ("fp32", 4)))
+def test_interleaved_rows_of_odd_alignment(dtype, size):
+    """A pair of the interleaved layout moves as one piece: an address or a stride, in use, that is not a multiple of two elements is refused
+    in every call, as the header says."""
+    lib, h = B.library(), B.Rotary(RotaryConfig(64, 64, dtype, "interleaved"))
+    for odd in (_heads(ptr=4096 + size), _heads(st=65), _heads(sh=513)):
+        for q, g, y in ((odd, _heads(), _heads()), (_heads(), odd, _heads()), (_heads(), _heads(), odd)):
+            assert lib.ff_qk_norm_backward(h.handle, 1, 8, None, 0, q, None, None, None, 1e-6, g, None, y, None, None, None, 4096, 1 << 24, None) == 2
+        assert lib.ff_rotary_apply(h.handle, 1, 8, None, 0, odd, None, 0, _heads(), None, None) == 2
+        assert lib.ff_qk_norm(h.handle, 1, 8, None, 0, _heads(), odd, None, None, 1e-6, _heads(), _heads(), None) == 2
+        assert b"aligned to two elements" in lib.ff_rotary_last_error(h.handle)
+    assert lib.ff_rotary_apply(h.handle, 2, 8, None, 0, _heads(sb=1025), None, 0, _heads(), None, None) == 2
