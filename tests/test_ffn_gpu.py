@@ -406,3 +406,63 @@ def test_status_of_a_new_handle():
     with torch.cuda.stream(side):
         assert ffn.device_status() == 0
     torch.cuda.synchronize()
+
+
+def exact_inputs(M, D, F, live=None, seed=0):
+    """Small whole numbers for which every sum of the block is exact in fp32 and H, dG and dU are exact in bf16, whatever the order of
+    the sums: X is 1 in the first column and -1, 0 or 1 elsewhere; a column of Wg is 32 in the first row and has four more ones, one of Wu
+    four; so gates are 28 .. 36, where each activation is the gate itself and its slope 1 (e^-28 is below half a step of 1 in fp32), up is
+    -4 .. 4 and |H| <= 144.  dout has four ones a row (none but in the last `live` rows): |dH| <= 4 times the columns' chance of meeting."""
+    gen = torch.Generator("cuda").manual_seed(seed)
+
+    def three(*shape):
+        return torch.randint(-1, 2, shape, generator=gen, device="cuda", dtype=torch.int8).to(torch.bfloat16)
+
+    def four_ones(rows, cols, first=0):
+        """[rows][cols] with +-1 in four random places (or fewer, where two meet) of each row, from column `first` on"""
+        t = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+        at = torch.randint(first, cols, (rows, 4), generator=gen, device="cuda")
+        return t.scatter_(1, at, (2 * torch.randint(0, 2, (rows, 4), generator=gen, device="cuda") - 1).to(torch.bfloat16))
+    X, Wd, dout = three(M, D), three(F, D), four_ones(M, D)
+    X[:, 0] = 1
+    Wg, Wu = (four_ones(F, D, 1).t().contiguous() for _ in range(2))
+    Wg[0] = 32
+    if live is not None:
+        dout[:M - live] = 0
+    return X, Wg, Wu, Wd, dout
+
+
+def check_exact(M, D, F, activation, rows=None):
+    """Every output is the exact number rounded once, bit for bit: no part of a sum is left out or added twice.  With `rows`, what belongs to
+    tokens is compared for that many at the end, the only ones with a gradient."""
+    X, Wg, Wu, Wd, dout = exact_inputs(M, D, F, rows)
+    ffn = B.GatedFFN(FFNConfig(D, F, activation))
+    out, dX, gate, up = torch.empty_like(X), torch.empty_like(X), *(torch.empty(M, F, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ffn.forward(X, Wg, Wu, Wd, out, gate, up)
+    alone = torch.empty_like(X)
+    ffn.forward(X, Wg, Wu, Wd, alone)
+    grads = [torch.empty_like(t) for t in (Wg, Wu, Wd)]
+    ffn.backward(X, Wg, Wu, Wd, gate, up, dout, dX, *grads)
+    assert ffn.device_status() == 0
+    end = slice(M - (rows or M), M)
+    x, do, wg, wu, wd = (t.double() for t in (X[end], dout[end], Wg, Wu, Wd))
+    g, u = x @ wg, x @ wu
+    h, dh = g * u, do @ wd.T
+    dg, du = dh * u, dh * g
+    for t in (g, u, h, dg, du):
+        assert torch.equal(t, t.to(torch.bfloat16).double())
+    for got, want, name in ((gate[end], g, "gate"), (up[end], u, "up"), (out[end], h @ wd, "out"), (alone[end], h @ wd, "out alone"),
+                            (dX[end], dg @ wg.T + du @ wu.T, "dX"), (grads[0], x.T @ dg, "dWg"), (grads[1], x.T @ du, "dWu"), (grads[2], h.T @ do, "dWd")):
+        assert want.abs().max() < 2 ** 24, name
+        assert torch.equal(got, want.to(torch.bfloat16)), f"{name}: {int((got != want.to(torch.bfloat16)).sum())} of {want.numel()}"
+
+
+@pytest.mark.parametrize("M,D,F", [(1, 256, 520), (1, 1032, 40000), (13, 2048, 5632), (37, 1032, 4104), (100, 1032, 40000), (300, 520, 648), (513, 256, 136),
+                                   (700, 136, 2056), (4100, 64, 72), (5000, 1032, 1544), (20000, 264, 520)])
+def test_exact_sums(M, D, F):
+    check_exact(M, D, F, ("silu", "gelu_tanh", "gelu")[M % 3])
+
+
+def test_far_rows_exact():
+    """Hidden activations and their gradients beyond 2^31 elements: the last tokens' outputs and all gradients, which only these tokens have."""
+    check_exact(70000, 8, 31000, "silu", 300)
