@@ -403,3 +403,43 @@ def test_large_eps_beside_large_rows(eps):
     want = r * (dz - n * (dz * n).mean(-1, keepdim=True))
     within(dx, want, half_step(x.dtype) * want.abs() + 1e-5 * r * (big + n.abs() * (big * n.abs()).mean(-1, keepdim=True)), "dx")
     within(dw, (dz * n).sum((0, 1, 2)), 1e-5 * (big * n.abs()).sum((0, 1, 2)), "dw")
+
+
+def test_special_values_backward():
+    """A row of x or of the gradient that holds an infinity or a NaN spoils its own dx and, in the channels that the formula says, dw;
+    the other rows keep their bits.  Rows whose squares leave fp32 have the gradient of the same rows scaled, divided by the scale."""
+    cfg = RotaryConfig(64, 32, "fp32")
+    h = B.Rotary(cfg)
+    gen = torch.Generator("cuda").manual_seed(13)
+    x, g = (torch.randn(1, 2, 70, 64, generator=gen, device="cuda") for _ in range(2))
+    w = torch.rand(64, generator=gen, device="cuda") + 0.5
+    at = given(cfg, None, 1, 70)
+
+    def call(x, g, eps=EPS):
+        dx, dw = torch.full_like(x, 7.0), torch.full_like(w, 7.0)
+        h.qk_norm_backward(x, None, w, None, g, None, dx, None, dw, eps=eps)
+        return dx, dw
+    clean, _ = call(x, g)
+    for into_x, value, channel in ((True, math.nan, 3), (True, math.inf, 40), (False, math.nan, 5), (False, -math.inf, 50), (False, math.inf, 20)):
+        bad = [x.clone(), g.clone()]
+        bad[0 if into_x else 1][0, 1, 66, channel] = value
+        dx, dw = call(*bad)
+        n, wd = normed(bad[0], w)
+        r = 1 / torch.sqrt(bad[0].double().square().mean(-1, keepdim=True) + EPS)
+        dz, big = rotate(cfg, h, bad[1], at, inverse=True), rotate(cfg, h, bad[1], at, absolute=True)
+        want = r * (dz * wd - n * (dz * wd * n).mean(-1, keepdim=True))
+        others = torch.ones(1, 2, 70, dtype=torch.bool, device="cuda")
+        others[0, 1, 66] = False
+        assert torch.equal(dx[others], clean[others])
+        assert torch.equal(dx[0, 1, 66].isfinite(), want[0, 1, 66].isfinite())
+        want, bound = (dz * n).sum((0, 1, 2)), 1e-5 * (big * n.abs()).sum((0, 1, 2))
+        fine = want.isfinite()
+        assert torch.equal(dw.isfinite(), fine)
+        if fine.any():
+            within(dw[fine], want[fine], bound[fine], "dw")
+    plain, scaled = call(x, g, 1e-30), call(x * 2.0 ** 100, g, 1e-30)
+    n, wd = normed(x, w)
+    r = 1 / torch.sqrt(x.double().square().mean(-1, keepdim=True))
+    big = rotate(cfg, h, g, at, absolute=True)
+    within(scaled[0].double() * 2.0 ** 100, plain[0].double(), 2e-5 * r * (big * wd + n.abs() * (big * wd * n.abs()).mean(-1, keepdim=True)), "dx of large rows")
+    within(scaled[1], plain[1].double(), 2e-5 * (big * n.abs()).sum((0, 1, 2)), "dw of large rows")
