@@ -404,10 +404,11 @@ class Rotary:
     """Rotary positions of queries and keys, alone or with the norm of every head row in the same pass.
 
     q, k and the tensors written are CUDA tensors [batch][heads][tokens][head_dim] of the configuration's type, with
-    contiguous channels and any strides for the rest (a transposed view of [batch][tokens][heads][head_dim] is one; for interleaved
-    pairs addresses and strides have to be multiples of two elements); q and k may have different numbers of heads, and k and its output may be None.  An output may be its own input.  positions: an
-    int32 CUDA tensor [tokens] or [batch][tokens], with a last dimension of 3 (t, h, w) where the configuration divides the
-    pairs over axes; None: the token's index, or its cell in the configuration's grid."""
+    contiguous channels and any strides for the rest (a transposed view of [batch][tokens][heads][head_dim] is one; for
+    interleaved pairs addresses and strides have to be multiples of two elements); q and k may have different numbers of heads,
+    and k and its output may be None.  An output may be its own input.  positions: an int32 CUDA tensor [tokens] or
+    [batch][tokens], with a last dimension of 3 (t, h, w) where the configuration divides the pairs over axes; None: the token's
+    index, or its cell in the configuration's grid."""
 
     def __init__(self, cfg: RotaryConfig):
         import torch
