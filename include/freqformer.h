@@ -366,7 +366,8 @@ ff_status_t ff_forward_projected_rotary(ff_plan_t *plan, const void *X, const vo
  *   Wg, Wu          [dim][hidden]
  *   Wd              [hidden][dim]
  *   gate, up        [tokens][hidden]: X Wg and X Wu, kept by a training forward for the backward pass
- * The hidden activations (and, backward, the gradients of gate and up) are rounded to bf16 between the products; the
+ * The hidden activations (and, backward, the gradients of gate and up) are rounded to bf16 between the products: the
+ * forward pass makes them from gate and up in fp32, the backward pass again from the kept, rounded ones.  The
  * accumulators and the activation are fp32.  Any number of tokens, one and zero included, up to 2^31 - 256 and to 2^38 values
  * in the widest tensor.
  *

@@ -3,8 +3,8 @@
 //   dH = dout Wd^T, dG = dH U act'(G), dU = dH act(G), dX = dG Wg^T + dU Wu^T,
 //   dWg = X^T dG, dWu = X^T dU, dWd = H^T dout
 //
-// Three launches of one kernel: gate and up (then out), dH (then all gradients together).  It is a persistent GEMM on CTA pairs (tcgen05,
-// cta_group::2) with tiles of 256 x 256 (128 rows of A and 128 columns of B in either CTA's shared memory), K in chunks of 64, a ring of
+// One kernel makes all products: forward in two launches (gate and up; out), backward in two (dH; all gradients together), and where K was
+// cut a small one joins the parts.  It is a persistent GEMM on CTA pairs (tcgen05, cta_group::2) with tiles of 256 x 256 (128 rows of A and 128 columns of B in either CTA's shared memory), K in chunks of 64, a ring of
 // six stages filled by TMA, and two accumulators of 256 tensor-memory columns, so that the epilogue of a tile overlaps the main loop of
 // the next.  Operands are read as they lie in memory, K-major or MN-major, so nothing is transposed.
 //   gate and up   one tile is 128 columns of G (the even CTA's half of B) beside the same 128 columns of U (the odd CTA's), so
@@ -101,7 +101,8 @@ __device__ __forceinline__ float activation(float g, float* slope) {
     return g * s;
   } else {
     // 1 - Phi(|g|) = e^(-x^2) (a1 t + .. + a5 t^5) / 2, x = |g| / sqrt 2, t = 1 / (1 + 0.3275911 x), to 0.75e-7: Abramowitz and
-    // Stegun, "Handbook of Mathematical Functions", 7.1.26.  Its exponential is the one of the derivative.  (With erfcf the launches
+    // Stegun, "Handbook of Mathematical Functions", 7.1.26.  Relative to 1 - Phi that is 5e-4 at |g| = 4, 1.6e-3 at 5 and 3.6e-3 at 6,
+    // below half a step of bf16 (3.9e-3) where the result is above 1e-9 g.  Its exponential is the one of the derivative.  (With erfcf the launches
     // of dH and dWd took 276 us instead of 249: 16384 tokens, dim and hidden 2048.)
     const float x = 0.70710678118654752f * fabsf(g), t = rcp(fmaf(0.3275911f, x, 1.f)), e = exponential(-x * x);
     const float h = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
@@ -713,8 +714,12 @@ int split_of(long long tiles, int k, double values, double* us = nullptr) {
 }
 // The same for a product with an epilogue, whose K stays whole: tiles of 256 columns or narrow ones, of which there are twice as many.
 // A chunk of a narrow tile takes 0.22 us (three quarters of the bytes for half the products), the epilogue of a tile, which overlaps the
-// next tile's products, `epilogue` us of a wide one and of a narrow one.  Measured, wide / narrow, us: backward of 200 tokens, dim 1264, hidden 2464 44.7 / 38.1,
-// of 4000 165 / 175; forward of 128 tokens, dim 512, hidden 1408 13.5 / 12.0, of 1000 tokens, dim 1024, hidden 2816 28.6 / 30.2.
+// next tile's products, `epilogue` us of a wide one and of a narrow one.  Measured in captured rows of calls, wide / narrow, us: backward of
+// 200 tokens, dim 1264, hidden 2464 36.6 / 31.4, of 4000 152 / 158 (estimated the other way round, dH 32 / 26), of 4000 tokens, dim 1024,
+// hidden 2816 132 / 135; forward of 128 tokens, dim 512, hidden 1408 16.0 / 12.8, of 1000 tokens, dim 1024, hidden 2816 28.2 / 28.6.
+// A forward that keeps G and U has a longer epilogue (10,500 cycles a wide tile, about 5.5 us) than the estimate knows of; its choice was the
+// faster one all the same: 128 tokens, dim 512, hidden 1408 14.0 / 11.9, 4000 tokens, dim 768, hidden 2056 43.0 / 46.8, 16384 159 / 174,
+// 2000 tokens, dim 2048, hidden 5632 106 / 124.
 struct Tiling { bool narrow; double us; };
 Tiling tiling_of(long long rows, int cols, int width, int k, const double (&epilogue)[2]) {
   constexpr int pairs = FF_B200_SMS / 2;
@@ -1068,9 +1073,9 @@ extern "C" ff_status_t ff_ffn_forward(ff_ffn_t* h, int64_t tokens, const void* X
     return fail(h, FF_ERR_INVALID_ARG, "gate, up or the workspace overlaps another tensor, or out overlaps Wd");
   cudaStream_t st = (cudaStream_t)stream;
   const Matrix x{X, tokens, D}, hid{ws, tokens, F}, wg{Wg, D, F}, wu{Wu, D, F}, wd{Wd, F, D};
-  // Either product runs on the kernel whose estimate is lower (2 us more for start and end of the larger one).  Measured, dim 2048, hidden 5632, both products on tiles of 256
-  // tokens / on the few-token kernel, us: 1 token 34.0 / 21.1, 64 tokens 31.6 / 25.2, 128 32.7 / 35.9, 512 46.5 / 64.3; dim 1024, hidden
-  // 2816, product with Wd: 400 tokens 25.9 / 21.5, 768 27.8 / 32.4.
+  // Either product runs on the kernel whose estimate is lower (2 us more for start and end of the larger one).  Measured in captured rows of
+  // calls, dim 2048, hidden 5632, both products on the tiles that tiling_of gives / on the few-token kernel, us: 1 token 36.9 / 18.9,
+  // 64 tokens 29.3 / 23.6, 128 30.0 / 26.9, 512 42.9 / 62.4; dim 1024, hidden 2816, product with Wd: 400 tokens 22.2 / 19.3, 768 24.2 / 23.6.
   const FewShape up_few = few_shape(h, tokens, F, chunks(D), 2), down_few = few_shape(h, tokens, D, chunks(F), 1);
   const Product down = down_product(h->cfg, tokens);
   double down_us;

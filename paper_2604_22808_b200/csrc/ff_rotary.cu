@@ -10,9 +10,9 @@
 // token and pair; they do not depend on the head, so a thread that owns the same pairs of one token computes them once and
 // keeps them in registers while it walks over the heads.
 //
-// Angles: theta_p / 2 pi is kept as a 64-bit fraction of a turn.  position * fraction modulo 2^64 is then the angle modulo a
-// whole turn, exact to 2^-33 turns for any 32-bit position: its high word gives the quadrant and a remainder of at most an eighth of a
-// turn, whose sine and cosine are short Taylor polynomials (two values an instruction: the pair of them), and no floating-point
+// Angles: theta_p / 2 pi is kept as a 64-bit fraction of a turn, cut off.  position * fraction modulo 2^64 is then the angle modulo a
+// whole turn, less than 2^-33 turns off for any 32-bit position, and its high word, cut off again, less than 1.5 x 2^-32.  The word gives
+// the quadrant and a remainder of at most an eighth of a turn (as a float another 2^-28 turns off at most), whose sine and cosine are short Taylor polynomials (two values an instruction: the pair of them), and no floating-point
 // product of a far position ever has to be reduced.
 //
 // Threads: a row is cut in chunks of CH channels (16 bytes where strides, rot_dim and head_dim allow, else 8, 4 or 2), and a
