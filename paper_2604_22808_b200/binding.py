@@ -335,6 +335,8 @@ class Plan:
                 raise FFError(1, f"expected a contiguous bf16 tensor of shape {shape} on {self.device}")
         ts = _floats(timesteps, self.cfg.batch)
         if rotary is not None:
+            if eps and C.c_float(eps).value == 0:
+                raise FFError(1, "eps is 0 in fp32, which means no norm")
             w, (pos, stride) = [rotary._weight(t, self.device) for t in (wq, wk)], rotary._positions(positions, cfg.batch, cfg.N, self.device)
             _check(library().ff_forward_projected_rotary(self.handle, X.data_ptr(), Wqkv.data_ptr(), Wo.data_ptr(), rotary.handle, pos, stride,
                                                          *w, eps, self._check_masks(alloc), ts, out.data_ptr(), self._stream()), self.handle)

@@ -97,3 +97,26 @@ def test_stream_handle_with_and_without_the_private_name():
     assert B._stream_getter(SimpleNamespace(_C=SimpleNamespace(), cuda=public))(3) == 103
     private = SimpleNamespace(_cuda_getCurrentRawStream=lambda index: 200 + index)
     assert B._stream_getter(SimpleNamespace(_C=private, cuda=public))(3) == 203
+
+
+def test_eps_that_vanishes_in_fp32():
+    """eps reaches the library in fp32, where 0 means no norm: one that is above 0 only in 64 bits is refused, not taken for that."""
+    p = object.__new__(B.Plan)
+    p.cfg = C.TINY.scaled("bf16", dtype="bf16")
+    p._torch, p.device, p.handle = torch, torch.device("cpu"), None
+    p._stream = lambda: None
+    D = p.cfg.heads * p.cfg.head_dim
+
+    def tensor(*shape):                              # (what stands for one on a GPU)
+        return SimpleNamespace(shape=shape, dtype=torch.bfloat16, device=p.device, is_cuda=True, is_contiguous=lambda: True, data_ptr=lambda: 4096)
+    x, wqkv, wo = tensor(1, p.cfg.N, D), tensor(3, D, D), tensor(D, D)
+    rotary = B.Rotary(C.RotaryConfig(p.cfg.head_dim, p.cfg.head_dim))
+
+    def call(eps):
+        p.forward_projected(x, wqkv, wo, x, timesteps=[1.0], rotary=rotary, eps=eps)
+    for eps in (0.0, 2.0 ** -149, 1e-6):
+        with pytest.raises(B.FFError, match="plan is NULL"):
+            call(eps)
+    for eps in (1e-50, 2.0 ** -151):
+        with pytest.raises(B.FFError, match="eps"):
+            call(eps)
