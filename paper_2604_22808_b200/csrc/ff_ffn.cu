@@ -3,10 +3,11 @@
 //   dH = dout Wd^T, dG = dH U act'(G), dU = dH act(G), dX = dG Wg^T + dU Wu^T,
 //   dWg = X^T dG, dWu = X^T dU, dWd = H^T dout
 //
-// One kernel makes all products: forward in two launches (gate and up; out), backward in two (dH; all gradients together), and where K was
-// cut a small one joins the parts.  It is a persistent GEMM on CTA pairs (tcgen05, cta_group::2) with tiles of 256 x 256 (128 rows of A and 128 columns of B in either CTA's shared memory), K in chunks of 64, a ring of
-// six stages filled by TMA, and two accumulators of 256 tensor-memory columns, so that the epilogue of a tile overlaps the main loop of
-// the next.  Operands are read as they lie in memory, K-major or MN-major, so nothing is transposed.
+// One kernel makes all products: forward in two launches (gate and up; out), backward in two (dH; all gradients together), and where K
+// was cut a small one joins the parts.  It is a persistent GEMM on CTA pairs (tcgen05, cta_group::2) with tiles of 256 x 256 (128 rows of
+// A and 128 columns of B in either CTA's shared memory), K in chunks of 64, a ring of six stages filled by TMA, and two accumulators of
+// 256 tensor-memory columns, so that the epilogue of a tile overlaps the main loop of the next.  Operands are read as they lie in memory,
+// K-major or MN-major, so nothing is transposed.
 //   gate and up   one tile is 128 columns of G (the even CTA's half of B) beside the same 128 columns of U (the odd CTA's), so
 //                 that both values of an element lie in one lane of tensor memory and H leaves without G and U reaching memory
 //   dH            its epilogue reads G and U and writes dG, dU and H (needed for dWd; made again rather than kept)

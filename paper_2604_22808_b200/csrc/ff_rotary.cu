@@ -12,8 +12,9 @@
 //
 // Angles: theta_p / 2 pi is kept as a 64-bit fraction of a turn, cut off.  position * fraction modulo 2^64 is then the angle modulo a
 // whole turn, less than 2^-33 turns off for any 32-bit position, and its high word, cut off again, less than 1.5 x 2^-32.  The word gives
-// the quadrant and a remainder of at most an eighth of a turn (as a float another 2^-28 turns off at most), whose sine and cosine are short Taylor polynomials (two values an instruction: the pair of them), and no floating-point
-// product of a far position ever has to be reduced.
+// the quadrant and a remainder of at most an eighth of a turn (as a float another 2^-28 turns off at most), whose sine and cosine are
+// short Taylor polynomials (two values an instruction: the pair of them), and no floating-point product of a far position ever has to be
+// reduced.
 //
 // Threads: a row is cut in chunks of CH channels (16 bytes where strides, rot_dim and head_dim allow, else 8, 4 or 2), and a
 // thread owns two chunks of it so that both channels of a pair are its own: no exchange between threads for the rotation.
