@@ -409,6 +409,103 @@ ff_status_t ff_ffn_backward(ff_ffn_t *ffn, int64_t tokens, const void *X, const 
 /* Synchronises the stream, returns the device status word (FF_OK or FF_ERR_TIMEOUT) and clears it. */
 ff_status_t ff_ffn_device_status(ff_ffn_t *ffn, void *cuda_stream);
 
+/* ---- layer norm ------------------------------------------------------------------------------------------
+ *
+ * The norm in front of a layer's attention, cross attention and feed-forward block (no counterpart in the paper):
+ *     y = (x - mean) r w + b,   r = 1 / sqrt(variance + eps),   mean and variance over the dim values of a row
+ * with weights and bias of the model, [dim], or of each sample, [batch][dim] (the scale and shift that a diffusion
+ * model makes from the timestep; unit_offset then counts the weight from one: 1 + w).
+ *
+ * A handle holds host memory only and serves any device; calls run on the current one.  Like a plan it is not
+ * thread-safe (its error message), and its calls are asynchronous on the given stream. */
+typedef struct ff_layer_norm ff_layer_norm_t; /* opaque */
+
+typedef struct {
+  int32_t dim;             /* 1 .. 8192 */
+  int32_t dtype;           /* FF_BF16 or FF_FP32: x, y and their gradients; weights and all arithmetic are fp32 */
+  int32_t unit_offset;     /* non-zero: y = (x - mean) r (1 + w) + b */
+  float eps;               /* > 0, finite */
+} ff_layer_norm_config_t;
+
+/* Rows of dim neighbouring values: value c of token n of sample b lies at data[b stride_batch + n stride_token + c].
+ * Strides in elements, >= 0; rows whose addresses, strides and dim are multiples of 16 bytes move in pieces of that size,
+ * others value by value (or two bf16 at a time). */
+typedef struct {
+  void *data;              /* device */
+  int64_t stride_batch, stride_token;
+} ff_rows_t;
+
+ff_status_t ff_layer_norm_create(const ff_layer_norm_config_t *cfg, ff_layer_norm_t **out);
+ff_status_t ff_layer_norm_destroy(ff_layer_norm_t *norm);   /* NULL is allowed */
+const char *ff_layer_norm_last_error(const ff_layer_norm_t *norm);   /* as ff_last_error */
+
+/* weight, bias: device, float: [dim] where per_sample is 0, else [batch][dim]; NULL: ones (whatever unit_offset is), zeros.  y may be x (the same address
+ * and strides), otherwise it overlaps no input.  batch * tokens below 2^31. */
+ff_status_t ff_layer_norm_forward(const ff_layer_norm_t *norm, int64_t batch, int64_t tokens, const ff_rows_t *x, const float *weight,
+                                  const float *bias, int32_t per_sample, const ff_rows_t *y, void *cuda_stream);
+
+/* From the forward pass's input x and the gradient dy of its output: dx (which may be dy or x, or NULL: not wanted) and the
+ * gradients of weight and bias in their layout (device, float; NULL: not wanted; their sums over no tokens are zeros).  The sums
+ * run in an order that depends on the sizes alone: the same call gives the same bits.
+ *   workspace  device, 16-byte aligned, ff_layer_norm_workspace_bytes; calls that may run at the same time need one each */
+ff_status_t ff_layer_norm_backward(const ff_layer_norm_t *norm, int64_t batch, int64_t tokens, const ff_rows_t *x, const float *weight,
+                                   int32_t per_sample, const ff_rows_t *dy, const ff_rows_t *dx, float *dweight, float *dbias, void *workspace,
+                                   size_t workspace_bytes, void *cuda_stream);
+ff_status_t ff_layer_norm_workspace_bytes(const ff_layer_norm_t *norm, int64_t batch, int64_t tokens, int32_t per_sample, size_t *bytes);
+
+/* ---- cross attention ----------------------------------------------------------------------------------------
+ *
+ * The layer's tokens attend to the states of an encoder (a text's, an image's) of another length (no counterpart in the
+ * paper, whose layer is unconditional):
+ *     out = softmax_j(scale q k_j) v   over the keys j that count,     lse = ln sum_j e^(scale q k_j)
+ * bf16 head rows of any strides (ff_heads_t), fp32 scores, softmax and sums; probabilities and, backward, the gradients of the scores
+ * are rounded to bf16 where they enter a matrix product.  Head h reads key head h / (heads / kv_heads).
+ *   lengths  device, int32 [batch]: keys from there on do not count (as if within 0 .. keys); NULL: all count
+ *   mask     device, bytes [batch][keys], 0: the key does not count; NULL: all count.  Both: a key has to pass both
+ * What stands in the rows of keys that do not count, infinities and NaN among it, touches no result.  A row for which no key
+ * counts gives zeros, an lse of -infinity and no gradients; the gradients of keys that do not count are zeros.
+ *
+ * A handle belongs to the device that was current at ff_cross_attention_create and holds a status word there; like a plan it
+ * is not thread-safe, and it has to outlive the graphs its calls are captured into.  Calls are asynchronous on the given
+ * stream, which has to be one of that device, the current one.  The caller owns the workspace (device, 256-byte aligned);
+ * calls that may run at the same time need one each. */
+typedef struct ff_cross_attention ff_cross_attention_t; /* opaque */
+
+typedef struct {
+  int32_t head_dim;        /* multiple of 8, 8 .. 128 */
+  int32_t heads, kv_heads; /* heads a multiple of kv_heads, at most 65536 */
+  float scale;             /* > 0, finite; 0: 1 / sqrt(head_dim) */
+} ff_cross_attention_config_t;
+
+ff_status_t ff_cross_attention_validate(const ff_cross_attention_config_t *cfg);
+/* Workspace of a forward (training = 0) or backward (1) call of these sizes (FF_ERR_UNSUPPORTED: too large). */
+ff_status_t ff_cross_attention_workspace_bytes(const ff_cross_attention_config_t *cfg, int64_t batch, int64_t queries, int64_t keys,
+                                               int32_t training, size_t *bytes);
+ff_status_t ff_cross_attention_create(const ff_cross_attention_config_t *cfg, ff_cross_attention_t **out);
+ff_status_t ff_cross_attention_destroy(ff_cross_attention_t *attention);            /* NULL is allowed */
+const char *ff_cross_attention_last_error(const ff_cross_attention_t *attention);   /* as ff_last_error */
+
+/* q, out: heads of `queries` tokens; k, v: kv_heads of `keys` tokens.  Addresses and strides (of dimensions longer than one) are
+ * multiples of 16 bytes; k and v may have a batch or head stride of 0 (the same states for all).  out may be q (the same
+ * address and strides), otherwise it overlaps no input.
+ *   lse  device, float [batch][heads][queries], kept for the backward pass; or NULL
+ * Sizes: batch * heads and the number of 128-row tiles of queries below 2^31, queries and keys at most 2^31 - 256. */
+ff_status_t ff_cross_attention_forward(ff_cross_attention_t *attention, int64_t batch, int64_t queries, int64_t keys, const ff_heads_t *q,
+                                       const ff_heads_t *k, const ff_heads_t *v, const int32_t *lengths, const uint8_t *mask,
+                                       const ff_heads_t *out, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* The gradients of q, k and v from that of out and what the forward pass kept; dq, or dk and dv together, may be NULL.  They
+ * overwrite what was there, sum over the heads that share a key head, overlap no input and not one another, and are the same
+ * bits in every call with the same inputs. */
+ff_status_t ff_cross_attention_backward(ff_cross_attention_t *attention, int64_t batch, int64_t queries, int64_t keys, const ff_heads_t *q,
+                                        const ff_heads_t *k, const ff_heads_t *v, const int32_t *lengths, const uint8_t *mask,
+                                        const ff_heads_t *out, const float *lse, const ff_heads_t *dout, const ff_heads_t *dq,
+                                        const ff_heads_t *dk, const ff_heads_t *dv, void *workspace, size_t workspace_bytes,
+                                        void *cuda_stream);
+
+/* Synchronises the stream, returns the device status word (FF_OK or FF_ERR_TIMEOUT) and clears it. */
+ff_status_t ff_cross_attention_device_status(ff_cross_attention_t *attention, void *cuda_stream);
+
 /* ---- for callers that cannot allocate device memory ---------------------------------------------
  *
  * The paper has no counterpart of this entry point; it exists for integration reasons only.

@@ -13,7 +13,7 @@ from typing import Optional, Sequence
 
 import numpy as np
 
-from .configs import FFConfig, FFNConfig, RotaryConfig
+from .configs import CrossAttentionConfig, FFConfig, FFNConfig, LayerNormConfig, RotaryConfig
 
 # FF_LIBRARY_VARIANT=debug loads the build with device-side range checks (python -m paper_2604_22808_b200.build --debug),
 # =clocks the one with cycle sums (--clocks)
@@ -36,7 +36,10 @@ EXPORTS = ("ff_config_validate", "ff_band_sizes", "ff_band_rank", "ff_workspace_
            "ff_plan_selftest_bounded_wait", "ff_rotary_create", "ff_rotary_destroy", "ff_rotary_last_error", "ff_rotary_frequencies",
            "ff_rotary_apply", "ff_qk_norm", "ff_qk_norm_backward", "ff_qk_norm_workspace_bytes", "ff_forward_projected_rotary", "ff_ffn_validate",
            "ff_ffn_workspace_bytes", "ff_ffn_create", "ff_ffn_destroy", "ff_ffn_last_error", "ff_ffn_forward", "ff_ffn_backward",
-           "ff_ffn_device_status")
+           "ff_ffn_device_status", "ff_layer_norm_create", "ff_layer_norm_destroy", "ff_layer_norm_last_error", "ff_layer_norm_forward",
+           "ff_layer_norm_backward", "ff_layer_norm_workspace_bytes", "ff_cross_attention_validate", "ff_cross_attention_workspace_bytes",
+           "ff_cross_attention_create", "ff_cross_attention_destroy", "ff_cross_attention_last_error", "ff_cross_attention_forward",
+           "ff_cross_attention_backward", "ff_cross_attention_device_status")
 STAGES = ("transform", "router", "attention", "summary", "inverse")
 
 
@@ -62,6 +65,18 @@ class ff_ffn_config_t(C.Structure):
     _fields_ = [("dim", C.c_int32), ("hidden", C.c_int32), ("activation", C.c_int32)]
 
 
+class ff_layer_norm_config_t(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("dtype", C.c_int32), ("unit_offset", C.c_int32), ("eps", C.c_float)]
+
+
+class ff_cross_attention_config_t(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("scale", C.c_float)]
+
+
+class ff_rows_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_batch", C.c_int64), ("stride_token", C.c_int64)]
+
+
 class ff_heads_t(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride_batch", C.c_int64), ("stride_head", C.c_int64), ("stride_token", C.c_int64),
                 ("heads", C.c_int32)]
@@ -83,7 +98,7 @@ def library() -> C.CDLL:
         lib = C.CDLL(_LIB_PATH)
         lib.ff_last_error.restype = C.c_char_p
         lib.ff_last_error.argtypes = [C.c_void_p]
-        for name in ("ff_rotary_last_error", "ff_ffn_last_error"):
+        for name in ("ff_rotary_last_error", "ff_ffn_last_error", "ff_layer_norm_last_error", "ff_cross_attention_last_error"):
             getattr(lib, name).restype = C.c_char_p
             getattr(lib, name).argtypes = [C.c_void_p]
         for name in EXPORTS:
@@ -124,6 +139,20 @@ def library() -> C.CDLL:
         lib.ff_ffn_forward.argtypes = [C.c_void_p, C.c_int64] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
         lib.ff_ffn_backward.argtypes = [C.c_void_p, C.c_int64] + [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p]
         lib.ff_ffn_device_status.argtypes = [C.c_void_p, C.c_void_p]
+        lib.ff_layer_norm_create.argtypes = [C.POINTER(ff_layer_norm_config_t), C.POINTER(C.c_void_p)]
+        lib.ff_layer_norm_destroy.argtypes = [C.c_void_p]
+        lib.ff_layer_norm_workspace_bytes.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
+        lib.ff_layer_norm_forward.argtypes = [C.c_void_p, C.c_int64, C.c_int64] + [C.c_void_p] * 3 + [C.c_int32, C.c_void_p, C.c_void_p]
+        lib.ff_layer_norm_backward.argtypes = ([C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 5
+                                               + [C.c_size_t, C.c_void_p])
+        lib.ff_cross_attention_validate.argtypes = [C.POINTER(ff_cross_attention_config_t)]
+        lib.ff_cross_attention_workspace_bytes.argtypes = ([C.POINTER(ff_cross_attention_config_t)] + [C.c_int64] * 3
+                                                           + [C.c_int32, C.POINTER(C.c_size_t)])
+        lib.ff_cross_attention_create.argtypes = [C.POINTER(ff_cross_attention_config_t), C.POINTER(C.c_void_p)]
+        lib.ff_cross_attention_destroy.argtypes = [C.c_void_p]
+        lib.ff_cross_attention_forward.argtypes = [C.c_void_p] + [C.c_int64] * 3 + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
+        lib.ff_cross_attention_backward.argtypes = [C.c_void_p] + [C.c_int64] * 3 + [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p]
+        lib.ff_cross_attention_device_status.argtypes = [C.c_void_p, C.c_void_p]
         lib.ff_config_validate.argtypes = [C.POINTER(ff_config_t)]
         lib.ff_band_sizes.argtypes = [C.POINTER(ff_config_t), C.POINTER(C.c_int64)]
         lib.ff_band_rank.argtypes = [C.POINTER(ff_config_t), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32),
@@ -641,6 +670,219 @@ class GatedFFN:
             return library().ff_ffn_device_status(self.handle, self._raw_stream(self.device.index))
 
 
+# ---- layer norm ----------------------------------------------------------------------------------------
+class LayerNorm:
+    """y = (x - mean) / sqrt(variance + eps) * weight + bias on CUDA tensors [batch][tokens][dim] (or [tokens][dim]) of any strides whose
+    rows are contiguous; weight, bias: contiguous fp32, [dim], or [batch][dim] for each sample its own, or None."""
+
+    def __init__(self, cfg: LayerNormConfig):
+        import torch
+        self.cfg = cfg
+        self._torch = torch
+        self.handle = C.c_void_p()
+        c = ff_layer_norm_config_t(cfg.dim, {"bf16": 0, "fp32": 1}.get(cfg.dtype, -1), int(cfg.unit_offset), cfg.eps)
+        _check(library().ff_layer_norm_create(C.byref(c), C.byref(self.handle)))
+        self._dtype = torch.float32 if cfg.dtype == "fp32" else torch.bfloat16
+        self._float32, self._model, self._lib = torch.float32, torch.Size((cfg.dim,)), library()
+        self._sized, self._bytes = None, 0                       # the workspace's size for the last sizes of a backward call
+        self._raw_stream = _stream_getter(torch)
+
+    def destroy(self):
+        if self.handle:
+            library().ff_layer_norm_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def _status(self, status: int):
+        if status != FF_OK:
+            raise FFError(status, library().ff_layer_norm_last_error(self.handle).decode())
+
+    def _rows(self, x, *others):
+        """Checks the tensors of a call: (batch, tokens), the addresses of their ff_rows_t (None for None), the array that holds those."""
+        dtype, device, shape, rank = self._dtype, x.device, x.shape, x.dim()
+        if rank not in (2, 3) or shape[-1] != self.cfg.dim or not x.is_cuda or x.dtype != dtype:
+            raise FFError(1, f"expected x a {dtype} tensor [batch][tokens][{self.cfg.dim}] or [tokens][{self.cfg.dim}] on a GPU")
+        rows, at = [], []
+        for t in (x,) + others:
+            if t is None:
+                at.append(None)
+                continue
+            if t.shape != shape or t.dtype != dtype or t.device != device:
+                raise FFError(1, f"expected a {dtype} tensor of shape {tuple(shape)} on {device}")
+            st = t.stride()
+            if st[-1] != 1 and shape[-1] > 1:
+                raise FFError(1, "the values of a row must be contiguous")
+            at.append(8 * len(rows))
+            rows += (t.data_ptr(), st[0] if rank == 3 else 0, st[-2])
+        rows = array("q", rows)
+        base = rows.buffer_info()[0]
+        return (shape[0] if rank == 3 else 1, shape[-2]), [None if o is None else base + o for o in at], rows
+
+    def _weights(self, batch, device, *weights):
+        """Whether they are each sample's, and their addresses."""
+        per_sample, shape, at = 0, None, []
+        for w in weights:
+            if w is None:
+                at.append(None)
+                continue
+            if shape is None:
+                shape = self._model if w.shape == self._model else self._torch.Size((batch, self.cfg.dim))
+                per_sample = int(shape is not self._model)
+            if w.dtype != self._float32 or w.shape != shape or not w.is_contiguous() or w.device != device:
+                raise FFError(1, f"expected contiguous fp32 weights and biases, all [{self.cfg.dim}] or all [{batch}][{self.cfg.dim}], on {device}")
+            at.append(w.data_ptr())
+        return per_sample, at
+
+    def _call(self, device, fn, *args):
+        """The call on the tensors' device (made current for it where another one is) and its current stream."""
+        torch = self._torch
+        if torch.cuda.current_device() == device.index:
+            return self._status(fn(self.handle, *args, self._raw_stream(device.index)))
+        with torch.cuda.device(device):
+            return self._status(fn(self.handle, *args, self._raw_stream(device.index)))
+
+    def forward(self, x, weight, bias, y):
+        """y may be x."""
+        size, (ax, ay), keep = self._rows(x, y)
+        per_sample, (w, b) = self._weights(size[0], x.device, weight, bias)
+        self._call(x.device, self._lib.ff_layer_norm_forward, *size, ax, w, b, per_sample, ay)
+        return y
+
+    def backward(self, x, weight, dy, dx, dweight=None, dbias=None):
+        """Gradients of x (dx may be dy or x, or None) and, where given, of weight and bias, from the input x and the gradient of y."""
+        size, (ax, ag, ad), keep = self._rows(x, dy, dx)
+        per_sample, (w, dw, db) = self._weights(size[0], x.device, weight, dweight, dbias)
+        if self._sized != (size, per_sample):
+            n = C.c_size_t()
+            self._status(self._lib.ff_layer_norm_workspace_bytes(self.handle, *size, per_sample, C.byref(n)))
+            self._sized, self._bytes = (size, per_sample), n.value
+        # (a workspace per call: calls on different streams and captured graphs share none)
+        ws = self._torch.empty(self._bytes, dtype=self._torch.uint8, device=x.device)
+        self._call(x.device, self._lib.ff_layer_norm_backward, *size, ax, w, per_sample, ag, ad, dw, db, ws.data_ptr(), self._bytes)
+        return dx, dweight, dbias
+
+
+# ---- cross attention -----------------------------------------------------------------------------------
+class CrossAttention:
+    """out = softmax(scale q k^T) v over the keys that count, on bf16 CUDA tensors [batch][heads][tokens][head_dim] of any strides (16-byte
+    multiples) whose channels are contiguous; k and v have kv_heads heads and the encoder's number of states.
+    lengths: int32 [batch], keys from there on do not count;  mask: bool or uint8 [batch][keys], false: the key does not count."""
+
+    def __init__(self, cfg: CrossAttentionConfig, device: str = "cuda:0"):
+        import torch
+        self.cfg = cfg
+        self._torch = torch
+        self.handle = C.c_void_p()
+        self._c = c = ff_cross_attention_config_t(cfg.head_dim, cfg.heads, cfg.kv_heads, cfg.scale)
+        _check(library().ff_cross_attention_validate(C.byref(c)))
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        with torch.cuda.device(self.device):
+            _check(library().ff_cross_attention_create(C.byref(c), C.byref(self.handle)))
+        self._sized, self._bytes = None, 0                       # the workspace's size for the last sizes of a call
+        self._lib, self._bf16, self._uint8, self._float32, self._int32 = library(), torch.bfloat16, torch.uint8, torch.float32, torch.int32
+        self._mask_types = (torch.bool, torch.uint8)
+        self._raw_stream = _stream_getter(torch)
+
+    def destroy(self):
+        if self.handle:
+            library().ff_cross_attention_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+    def _status(self, status: int):
+        if status != FF_OK:
+            raise FFError(status, library().ff_cross_attention_last_error(self.handle).decode())
+
+    def _heads(self, q, k, *others):
+        """Checks the tensors of a call, `others` as (tensor or None, is it like k) in turns: (batch, queries, keys), the addresses of
+        their ff_heads_t (None for None), and the array that holds those."""
+        c, bf16, device = self.cfg, self._bf16, self.device
+        qs, ks = q.shape, k.shape
+        if len(qs) != 4 or qs[1] != c.heads or qs[3] != c.head_dim:
+            raise FFError(1, f"expected q a tensor [batch][{c.heads}][queries][{c.head_dim}]")
+        if len(ks) != 4 or ks[0] != qs[0] or ks[1] != c.kv_heads or ks[3] != c.head_dim:
+            raise FFError(1, f"expected k a tensor [{qs[0]}][{c.kv_heads}][keys][{c.head_dim}]")
+        rows, at = [], []
+        for t, like_k in ((q, False), (k, True)) + tuple(zip(others[::2], others[1::2])):
+            if t is None:
+                at.append(None)
+                continue
+            if t.shape != (ks if like_k else qs) or t.dtype != bf16 or t.device != device:
+                raise FFError(1, f"expected a bf16 tensor of shape {tuple(ks if like_k else qs)} on {device}")
+            sb, sh, st, sc = t.stride()
+            if sc != 1:
+                raise FFError(1, "the channels of a head must be contiguous")
+            at.append(8 * len(rows))
+            rows += (t.data_ptr(), sb, sh, st, t.shape[1])           # (the layout of ff_heads_t, heads in its low half word)
+        rows = array("q", rows)
+        base = rows.buffer_info()[0]
+        return (qs[0], qs[2], ks[2]), [None if o is None else base + o for o in at], rows
+
+    def _keys(self, size, lengths, mask):
+        """Addresses of the lengths and the mask, checked."""
+        at = []
+        for t, types, shape, what in ((lengths, (self._int32,), size[:1], "int32 lengths"), (mask, self._mask_types, size[::2], "a bool mask")):
+            if t is None:
+                at.append(None)
+                continue
+            if t.dtype not in types or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+                raise FFError(1, f"expected {what}, contiguous, of shape {tuple(shape)} on {self.device}")
+            at.append(t.data_ptr())
+        return at
+
+    def _lse(self, size, lse):
+        if lse is None:
+            return None
+        shape = (size[0], self.cfg.heads, size[1])
+        if lse.dtype != self._float32 or lse.shape != shape or not lse.is_contiguous() or lse.device != self.device:
+            raise FFError(1, f"expected lse a contiguous fp32 tensor of shape {shape} on {self.device}")
+        return lse.data_ptr()
+
+    def _call(self, fn, training, size, *args):
+        torch, dev = self._torch, self.device
+        if self._sized != (size, training):
+            n = C.c_size_t()
+            _check(self._lib.ff_cross_attention_workspace_bytes(C.byref(self._c), *size, training, C.byref(n)))
+            self._sized, self._bytes = (size, training), n.value
+        n = self._bytes
+        # (a workspace per call: calls on different streams and captured graphs share none)
+        ws = torch.empty(n, dtype=self._uint8, device=dev)
+        if torch.cuda.current_device() == dev.index:
+            return self._status(fn(self.handle, *size, *args, ws.data_ptr(), n, self._raw_stream(dev.index)))
+        with torch.cuda.device(dev):
+            return self._status(fn(self.handle, *size, *args, ws.data_ptr(), n, self._raw_stream(dev.index)))
+
+    def forward(self, q, k, v, out, lse=None, lengths=None, mask=None):
+        """lse (fp32 [batch][heads][queries]): the logarithms of the rows' sums are written there, for backward.  out may be q."""
+        size, (aq, ak, av, ao), keep = self._heads(q, k, v, True, out, False)
+        self._call(self._lib.ff_cross_attention_forward, False, size, aq, ak, av, *self._keys(size, lengths, mask), ao, self._lse(size, lse))
+        return out
+
+    def backward(self, q, k, v, out, lse, dout, dq=None, dk=None, dv=None, lengths=None, mask=None):
+        """Gradients of q, k and v, where given (dk and dv together), from that of out and what forward left in out and lse.  They
+        overlap no other tensor."""
+        size, (aq, ak, av, ao, ag, adq, adk, adv), keep = self._heads(q, k, v, True, out, False, dout, False, dq, False, dk, True, dv, True)
+        self._call(self._lib.ff_cross_attention_backward, True, size, aq, ak, av, *self._keys(size, lengths, mask), ao, self._lse(size, lse), ag, adq,
+                   adk, adv)
+        return dq, dk, dv
+
+    def device_status(self) -> int:
+        with self._torch.cuda.device(self.device):               # (its default stream is 0, as every device's is)
+            return library().ff_cross_attention_device_status(self.handle, self._raw_stream(self.device.index))
+
+
 # Same names as the C entry points, for callers that prefer the flat API.
 def ff_plan_create(cfg: FFConfig, weights=None, U=None, host_staging=False, device="cuda:0") -> Plan:
     return Plan(cfg, weights, U, host_staging, device)
@@ -693,6 +935,30 @@ def ff_ffn_forward(ffn: GatedFFN, X, Wg, Wu, Wd, out, gate=None, up=None):
 
 def ff_ffn_backward(ffn: GatedFFN, X, Wg, Wu, Wd, gate, up, dout, dX=None, dWg=None, dWu=None, dWd=None):
     return ffn.backward(X, Wg, Wu, Wd, gate, up, dout, dX, dWg, dWu, dWd)
+
+
+def ff_layer_norm_create(cfg: LayerNormConfig) -> LayerNorm:
+    return LayerNorm(cfg)
+
+
+def ff_layer_norm_forward(norm: LayerNorm, x, weight, bias, y):
+    return norm.forward(x, weight, bias, y)
+
+
+def ff_layer_norm_backward(norm: LayerNorm, x, weight, dy, dx, dweight=None, dbias=None):
+    return norm.backward(x, weight, dy, dx, dweight, dbias)
+
+
+def ff_cross_attention_create(cfg: CrossAttentionConfig, device="cuda:0") -> CrossAttention:
+    return CrossAttention(cfg, device)
+
+
+def ff_cross_attention_forward(attention: CrossAttention, q, k, v, out, lse=None, lengths=None, mask=None):
+    return attention.forward(q, k, v, out, lse, lengths, mask)
+
+
+def ff_cross_attention_backward(attention: CrossAttention, q, k, v, out, lse, dout, dq=None, dk=None, dv=None, lengths=None, mask=None):
+    return attention.backward(q, k, v, out, lse, dout, dq, dk, dv, lengths, mask)
 
 
 def ff_high_attention_noalloc(q, k, v, y, radius: int, sync: bool = True):

@@ -83,6 +83,24 @@ class FFNConfig:
     activation: str = "silu"                        # "silu", "gelu_tanh" or "gelu"
 
 
+@dataclass(frozen=True)
+class LayerNormConfig:
+    """Layer norm (include/freqformer.h, ff_layer_norm_config_t)."""
+    dim: int
+    dtype: str = "bf16"                             # "bf16" or "fp32"; weights are fp32
+    eps: float = 1e-6
+    unit_offset: bool = False                       # the weight counts from one
+
+
+@dataclass(frozen=True)
+class CrossAttentionConfig:
+    """Attention to an encoder's states (include/freqformer.h, ff_cross_attention_config_t)."""
+    head_dim: int
+    heads: int
+    kv_heads: int
+    scale: float = 0.0                              # 0: 1 / sqrt(head_dim)
+
+
 def _cuts(grid, c_low_num, c_low_den):
     """L_a = n_a * c_low, M_a = n_a * (c_low + 1/2), both exact integers here."""
     low = tuple(n * c_low_num // c_low_den for n in grid)

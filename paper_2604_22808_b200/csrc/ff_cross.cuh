@@ -1,0 +1,108 @@
+// Cross attention: what the forward and backward launches share.
+//
+// Work is laid out by tiles of 128 query rows.  The heads of a group (those that read one key head) read the same keys, so a
+// tile's rows may be of any of them: with at least 65 query tokens a tile is 128 tokens of one head, with fewer as many whole heads
+// of the group as fit.  A tile of keys is 128 keys of one key head.
+#pragma once
+#include "ff_internal.h"
+#include "ff_sm100.cuh"
+
+struct ff_cross_attention {
+  ff_cross_attention_config_t cfg;
+  int device;
+  float scale;
+  int* status;                 // device
+  char err[512];
+};
+
+constexpr int CX_TILE = 128;
+
+struct CrossDims {
+  int B, H, G, group;          // samples, heads, key heads, heads of a key head
+  int N, K, d;                 // query tokens, keys, channels
+  int bn, bh;                  // tokens and heads of a tile of queries
+  int n_tiles, tiles;          // tiles along the tokens, tiles of a key head of a sample
+  int once[3][2];              // q, k, v: coordinate factors (0: the same rows for all) of batch and head
+  const int* lengths;
+  const uint8_t* mask;
+  float scale, sl2;            // scale; scale * log2(e)
+  int* status;
+};
+
+#if defined(__CUDACC__)
+// Keys of sample b that may count, and tiles of them.
+__device__ __forceinline__ int cx_keys(const CrossDims& D, int b) {
+  if (!D.lengths) return D.K;
+  const int n = __ldg(D.lengths + b);
+  return n < 0 ? 0 : n < D.K ? n : D.K;
+}
+// Does tile j of a sample with `keys` keys hold rows that do not count, yet have been loaded?
+__device__ __forceinline__ bool cx_unclean(const CrossDims& D, int keys, int j) {
+  return D.mask || (keys < D.K && (j + 1) * CX_TILE > keys);
+}
+// The keys of a tile that count, as the bits of four words: bit l of word k is key 4 l + k.  All 32 lanes.
+struct CxValid { uint32_t w[4]; };
+__device__ __forceinline__ CxValid cx_valid(const CrossDims& D, int b, int keys, int j, int lane) {
+  CxValid v;
+  const long long at = (long long)b * D.K;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int key = j * CX_TILE + 4 * lane + k;
+    const bool on = key < keys && (!D.mask || __ldg(D.mask + at + key) != 0);
+    v.w[k] = __ballot_sync(0xffffffffu, on);
+  }
+  return v;
+}
+// First head and token of tile t of key head g.
+__device__ __forceinline__ void cx_place(const CrossDims& D, int g, int t, int& h0, int& n0) {
+  const int pack = t / D.n_tiles;
+  h0 = g * D.group + pack * D.bh;
+  n0 = (t - pack * D.n_tiles) * D.bn;
+}
+// Loads a tile of rows (halves of 64 channels, `bytes` apart in shared memory); the caller has announced its bytes.
+__device__ __forceinline__ void cx_load(uint8_t* dst, int bytes, int halves, const CUtensorMap* map, uint64_t* bar, int n, int h, int b) {
+  sm100::tma_load_4d(dst, map, bar, 0, n, h, b);
+  if (halves > 1) sm100::tma_load_4d(dst + bytes, map, bar, 64, n, h, b);
+}
+// Zeros in the rows of a tile in shared memory (rows of 128 bytes, halves `bytes` apart) whose keys do not count: in the product they
+// meet probabilities of zero, and zero times what may stand there need not be zero.  All 32 lanes.
+__device__ __forceinline__ void cx_clean(uint8_t* tile, int bytes, int halves, const CxValid& v, int lane) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t gone = ~v.w[k];
+    while (gone) {
+      // four rows at a time, eight lanes of 16 bytes each
+      uint32_t rest = gone;
+      int row = -1;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int l = __ffs(rest) - 1;
+        if (i == (lane >> 3)) row = l < 0 ? -1 : 4 * l + k;
+        rest &= rest - 1;
+      }
+      gone = rest;
+      if (row >= 0)
+        for (int h = 0; h < halves; ++h) *(uint4*)(tile + h * bytes + row * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+    }
+  }
+  sm100::fence_proxy_async();
+}
+// Puts 32 consecutive fp32 values of a row (columns 32 c .. of the 64 of a swizzled half in shared memory) there as bf16.
+__device__ __forceinline__ void cx_stage(uint8_t* half, int row, int c, const uint32_t (&r)[32], float factor) {
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = sm100::bf16_pair(__float_as_uint(__uint_as_float(r[v * 8 + 2 * i]) * factor), __float_as_uint(__uint_as_float(r[v * 8 + 2 * i + 1]) * factor));
+    *(uint4*)(half + row * 128 + (((c * 4 + v) ^ (row & 7)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+#endif
+
+// A map over the rows of head rows: [batch][heads][tokens][head_dim] with boxes of 64 channels, `rows` tokens and `heads` heads.
+bool cx_map(CUtensorMap* map, const ff_heads_t* t, int64_t batch, int64_t tokens, int d, int rows, int heads);
+cudaError_t cx_backward_init();
+cudaError_t cx_backward(const ff_cross_attention* h, const CrossDims& D, const ff_heads_t* q, const ff_heads_t* k, const ff_heads_t* v, const ff_heads_t* out,
+                        const float* lse, const ff_heads_t* dout, const ff_heads_t* dq, const ff_heads_t* dk, const ff_heads_t* dv, void* ws, cudaStream_t st);
+size_t cx_backward_bytes(const CrossDims& D);
