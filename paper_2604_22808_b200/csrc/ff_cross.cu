@@ -461,7 +461,7 @@ void shape_of(const ff_cross_attention_config_t& c, int64_t batch, int64_t queri
   D->B = (int)batch; D->H = c.heads; D->G = c.kv_heads; D->group = c.heads / c.kv_heads;
   D->N = (int)queries; D->K = (int)keys; D->d = c.head_dim;
   D->bn = TILE; D->bh = 1;
-  if (queries <= TILE / 2)
+  if (queries >= 1 && queries <= TILE / 2)
     for (int n = 2; n <= D->group && n * queries <= TILE; ++n)
       if (D->group % n == 0) { D->bn = (int)queries; D->bh = n; }
   D->n_tiles = (int)((queries + D->bn - 1) / D->bn);
@@ -563,7 +563,7 @@ extern "C" ff_status_t ff_cross_attention_workspace_bytes(const ff_cross_attenti
   if (!bytes || batch < 0 || queries < 0 || keys < 0) return fail(nullptr, FF_ERR_INVALID_ARG, "bytes is NULL, or batch, queries or keys negative");
   if (too_large(*c, batch, queries, keys)) return fail(nullptr, FF_ERR_UNSUPPORTED, MOST);
   *bytes = 0;
-  if (batch == 0 || queries == 0) return FF_OK;
+  if (batch == 0 || (queries == 0 && !training)) return FF_OK;
   CrossDims D;
   shape_of(*c, batch, queries, keys, &D);
   if (training) {
@@ -674,5 +674,36 @@ extern "C" ff_status_t ff_cross_attention_backward(ff_cross_attention_t* h, int6
                                                    const ff_heads_t* out, const float* lse, const ff_heads_t* dout, const ff_heads_t* dq,
                                                    const ff_heads_t* dk, const ff_heads_t* dv, void* ws, size_t ws_bytes, void* stream) {
   if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "the handle is NULL");
-  return fail(h, FF_ERR_UNSUPPORTED, "not there yet");
+  ff_status_t s = check_call(h, batch, queries, keys, ws, ws_bytes, 1);
+  if (s != FF_OK) return s;
+  if (!dk != !dv) return fail(h, FF_ERR_INVALID_ARG, "dk and dv are made together, or neither is");
+  if (batch == 0 || (!dq && !dk)) return FF_OK;
+  const ff_cross_attention_config_t& c = h->cfg;
+  const ff_heads_t none = {h->status, 8, 8, 8, c.kv_heads}, no_query = {h->status, 8, 8, 8, c.heads};   // (no rows: none is read)
+  if (keys == 0) k = v = &none;
+  if (queries == 0) q = out = dout = &no_query;
+  if (!(queries == 0 || lse)) return fail(h, FF_ERR_INVALID_ARG, "lse is NULL");
+  s = check_heads(h, q, c.heads, queries ? batch : 1, queries, false, false);
+  if (s == FF_OK) s = check_heads(h, k, c.kv_heads, batch, keys, false, true);
+  if (s == FF_OK) s = check_heads(h, v, c.kv_heads, batch, keys, false, true);
+  if (s == FF_OK) s = check_heads(h, out, c.heads, queries ? batch : 1, queries, false, false);
+  if (s == FF_OK) s = check_heads(h, dout, c.heads, queries ? batch : 1, queries, false, false);
+  if (s == FF_OK && dq && queries) s = check_heads(h, dq, c.heads, batch, queries, true, false);
+  if (s == FF_OK && dk && keys) s = check_heads(h, dk, c.kv_heads, batch, keys, true, false);
+  if (s == FF_OK && dv && keys) s = check_heads(h, dv, c.kv_heads, batch, keys, true, false);
+  if (s != FF_OK) return s;
+  if ((((uintptr_t)lse) | ((uintptr_t)lengths)) & 3) return fail(h, FF_ERR_INVALID_ARG, "lse and lengths must be 4-byte aligned");
+  // (dq is written while other tiles still read q, dout and out; dk and dv while others read k and v, and the other launch's inputs)
+  const ff_heads_t *in[5] = {q, k, v, out, dout}, *made[3] = {queries ? dq : nullptr, keys ? dk : nullptr, keys ? dv : nullptr};
+  for (int i = 0; i < 3; ++i) {
+    for (int j = 0; j < 5; ++j)
+      if (made[i] && made[i]->data == in[j]->data) return fail(h, FF_ERR_INVALID_ARG, "a gradient lies over an input");
+    for (int j = 0; j < i; ++j)
+      if (made[i] && made[j] && made[i]->data == made[j]->data) return fail(h, FF_ERR_INVALID_ARG, "a gradient lies over another one");
+  }
+  CrossDims D;
+  shape_of(c, batch, queries, keys, &D);
+  keys_of(&D, h, q, k, v, lengths, mask);
+  CX_CUDA(h, cx_backward(D, q, k, v, out, lse, dout, queries ? dq : nullptr, keys ? dk : nullptr, dv, ws, (cudaStream_t)stream));
+  return FF_OK;
 }
