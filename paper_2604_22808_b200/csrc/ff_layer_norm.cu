@@ -7,12 +7,13 @@
 // The mean is subtracted before the squares are summed (the values are in registers, a second sum costs no memory traffic), so
 // rows whose mean is far from zero lose nothing.
 //
-// Forward, up to 2048 bf16 or 1024 fp32 values: a warp has a row (at most 64 values a thread) and the sums are shuffles alone.
-// Longer rows, and all rows of the backward pass, where a thread also keeps the weights and both gradients' sums of its channels,
-// go to a block with 16 values a thread.
+// A team of threads, a warp or a block, takes rows in turns, every thread the same channels of each (16 at most), so that weights, bias and,
+// backward, the gradients' sums of those channels stay in its registers; the next rows are on their way while these are summed.
 #include <stdio.h>
 
+#include <initializer_list>
 #include <new>
+#include <type_traits>
 
 #include "ff_chunks.cuh"
 #include "ff_internal.h"
@@ -26,7 +27,10 @@ namespace {
 
 constexpr int VALUES = 16;                        // values of a row that a thread of a block has
 constexpr int MAX_DIM = 8192, MAX_THREADS = MAX_DIM / VALUES;
-constexpr int ROW_WARPS = 4;                      // rows at a time in a block whose warps have a row each
+constexpr int BLOCK_WARPS = 8;
+constexpr int SM_THREADS = 512;                   // threads of an SM that one wave of blocks counts on
+template <class T> constexpr int STAGES = sizeof(T) == 4 ? 3 : 4;   // sets of rows of a team on their way or being read (two blocks fit an SM)
+constexpr int ROWS = 2;                           // rows of a team at a time, forward
 
 struct RowsView { char* p; long long sb, st; };   // strides in bytes
 struct NormParams {
@@ -38,7 +42,7 @@ struct NormParams {
   long long part_stride;            // ... and how far those of the blocks are apart
   unsigned tokens, segment, parts;  // tokens of a sample; rows whose gradients are summed together, blocks that do it
   FFFastDiv by_tokens;
-  int rows, d, pieces;
+  int rows, d, pieces, team_warps;
   float inv_d, eps;
 };
 
@@ -48,16 +52,57 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int m = 16; m; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
   return v;
 }
-// Sum over the threads that have a row: the warp, or the block, whose warps' sums meet in one of several places in turns.
+// A team: `warps` neighbouring warps of a block, which holds several.
+struct Team { int warps, index, teams, thread, threads; };
 template <bool WARP>
-__device__ __forceinline__ float row_sum(float v, float* place) {
-  v = warp_sum(v);
-  if constexpr (WARP) return v;
-  const int warps = blockDim.x >> 5;
-  if ((threadIdx.x & 31) == 0) place[threadIdx.x >> 5] = v;
-  __syncthreads();
-  const int lane = threadIdx.x & 31;
-  return warp_sum(lane < warps ? place[lane] : 0.f);
+__device__ __forceinline__ Team team_of(const NormParams& P) {
+  Team t;
+  t.warps = WARP ? 1 : P.team_warps;
+  const int warp = threadIdx.x >> 5;
+  t.teams = (blockDim.x >> 5) / t.warps;
+  t.index = warp / t.warps;
+  t.threads = t.warps * 32;
+  t.thread = threadIdx.x - t.index * t.threads;
+  return t;
+}
+// Sums over a team, whose warps' sums meet in a place of their own: four at a time are read (one after the other they took
+// longer than the rest of the row).
+constexpr int PLACE = MAX_THREADS / 32;
+using Place = float[BLOCK_WARPS][PLACE];                       // [team][warp]
+template <bool WARP, int K>
+__device__ __forceinline__ void team_sum(const Team& t, float (&v)[K], Place* place) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
+  if constexpr (!WARP) {
+    const int lane = threadIdx.x & 31;
+    if (lane < K) {
+      float mine = v[0];
+#pragma unroll
+      for (int k = 1; k < K; ++k)
+        if (lane == k) mine = v[k];
+      place[lane][t.index][t.thread >> 5] = mine;
+    }
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + t.index), "r"(t.threads) : "memory");
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float4 s = *(const float4*)place[k][t.index];
+#pragma unroll
+      for (int w = 4; w < PLACE; w += 4)
+        if (w < t.warps) {
+          const float4 u = *(const float4*)(place[k][t.index] + w);
+          s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
+        }
+      v[k] = (s.x + s.y) + (s.z + s.w);
+    }
+  }
+}
+// (the places of warps that a team does not have)
+template <bool WARP, int K>
+__device__ __forceinline__ void clear(Place (&place)[K]) {
+  if constexpr (!WARP) {
+    for (int i = threadIdx.x; i < K * BLOCK_WARPS * PLACE; i += blockDim.x) (&place[0][0][0])[i] = 0.f;
+    __syncthreads();
+  }
 }
 
 // A thread's pieces of a row: piece `first + i * step`.
@@ -65,19 +110,20 @@ template <class T, int CH, int PER>
 struct Row {
   static constexpr int N = pairs_of(CH);
   using C = Chunk<T, CH>;
-  static __device__ __forceinline__ void load(C (&raw)[PER], const char* row, int first, int step, int pieces) {
+  using V = F2[PER][N];
+  static __device__ __forceinline__ void load(V& v, const char* row, int first, int step, int pieces) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const C none{};
-      raw[i] = first + i * step < pieces ? *(const C*)(row + (long long)(first + i * step) * sizeof(C)) : none;
+      unpack<T, CH>(first + i * step < pieces ? *(const C*)(row + (long long)(first + i * step) * sizeof(C)) : none, v[i]);
     }
   }
-  static __device__ __forceinline__ void store(char* row, const F2 (&v)[PER][N], int first, int step, int pieces) {
+  static __device__ __forceinline__ void store(char* row, const V& v, int first, int step, int pieces) {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
       if (first + i * step < pieces) *(C*)(row + (long long)(first + i * step) * sizeof(C)) = pack<T, CH>(v[i]);
   }
-  static __device__ __forceinline__ float sum(const F2 (&v)[PER][N]) {
+  static __device__ __forceinline__ float sum(const V& v) {
     F2 s = two(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < PER; ++i)
@@ -85,7 +131,7 @@ struct Row {
       for (int c = 0; c < N; ++c) s = __fadd2_rn(s, v[i][c]);
     return low(s) + high(s);
   }
-  static __device__ __forceinline__ float dot(const F2 (&u)[PER][N], const F2 (&v)[PER][N]) {
+  static __device__ __forceinline__ float dot(const V& u, const V& v) {
     F2 s = two(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < PER; ++i)
@@ -93,154 +139,272 @@ struct Row {
       for (int c = 0; c < N; ++c) s = fma(u[i][c], v[i][c], s);
     return low(s) + high(s);
   }
-  // Values minus `m`, and zeros where the row has none.
-  static __device__ __forceinline__ void centre(F2 (&v)[PER][N], float m, int first, int step, int pieces) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const bool have = first + i * step < pieces;
-#pragma unroll
-      for (int c = 0; c < N; ++c) v[i][c] = have ? two(low(v[i][c]) - m, CH > 1 ? high(v[i][c]) - m : 0.f) : two(0.f, 0.f);
-    }
-  }
-  // raw -> n = (x - mean) r; the result is r.  Rows whose squares (or sum) leave fp32 are taken again, scaled by 2^-80, and eps by its
-  // square (which is far below their variance).  The sums meet in places 0 and 1, 2 and 3.
-  template <bool WARP>
-  static __device__ __forceinline__ float normalise(const C (&raw)[PER], F2 (&n)[PER][N], const NormParams& P, int first, int step, float (*place)[32]) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) unpack<T, CH>(raw[i], n[i]);
-    centre(n, row_sum<WARP>(sum(n), place[0]) * P.inv_d, first, step, P.pieces);
-    const float var = row_sum<WARP>(dot(n, n), place[1]) * P.inv_d;
-    float r = rsqrtf(var + P.eps), scale = r;
-    if (!(var < 3.0e38f)) {
-      const float down = 8.2718061255302767e-25f;              // 2^-80
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        unpack<T, CH>(raw[i], n[i]);
-#pragma unroll
-        for (int c = 0; c < N; ++c) n[i][c] = mul(n[i][c], two(down, down));
-      }
-      centre(n, row_sum<WARP>(sum(n), place[2]) * P.inv_d, first, step, P.pieces);
-      scale = rsqrtf(row_sum<WARP>(dot(n, n), place[3]) * P.inv_d + P.eps * down * down);
-      r = scale * down;
-    }
+  static __device__ __forceinline__ void times(V& v, float f) {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
 #pragma unroll
-      for (int c = 0; c < N; ++c) n[i][c] = mul(n[i][c], two(scale, scale));
-    return r;
+      for (int c = 0; c < N; ++c) v[i][c] = mul(v[i][c], two(f, f));
   }
-  // Neighbouring weights of a piece as they multiply, or ones.
-  static __device__ __forceinline__ F2 weight(const NormParams& P, const float* w, int piece, int c) {
-    if (!w || piece >= P.pieces) return two(1.f, 1.f);
-    return two(w[piece * CH + 2 * c] + P.plus, CH > 1 ? w[piece * CH + 2 * c + 1] + P.plus : 0.f);
+  // Values minus `m`, and zeros where the row has none.
+  static __device__ __forceinline__ void centre(V& v, float m, int first, int step, int pieces) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const float mine = first + i * step < pieces ? -m : 0.f;
+#pragma unroll
+      for (int c = 0; c < N; ++c) v[i][c] = __fadd2_rn(v[i][c], two(mine, CH > 1 ? mine : 0.f));
+    }
+  }
+  // Neighbouring weights of a piece, `plus` more, or `none` where there are none.
+  static __device__ __forceinline__ void weights(V& w, const float* from, float plus, float none, int first, int step, int pieces) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        const int at = (first + i * step) * CH + 2 * c;
+        w[i][c] = from && first + i * step < pieces ? two(from[at] + plus, CH > 1 ? from[at + 1] + plus : 0.f) : two(none, none);
+      }
   }
 };
-
-__device__ __forceinline__ const char* row_at(const RowsView& v, unsigned b, unsigned n) { return v.p + (long long)b * v.sb + (long long)n * v.st; }
-
-// Forward.  The next row is on its way while this one is summed.
-template <class T, int CH, int PER, bool WARP>
-__global__ void __launch_bounds__(WARP ? ROW_WARPS * 32 : MAX_THREADS) norm_forward_kernel(const __grid_constant__ NormParams P) {
+// A team's rows on their way: every thread copies its own pieces of them into places of its own in shared memory, STAGES - 1 sets of rows
+// ahead.  (Pieces of two bytes cannot be copied that way: one set ahead, in registers.)
+template <class T, int CH, int PER, int SET>
+struct Ring {
   using R = Row<T, CH, PER>;
-  constexpr int N = R::N;
-  __shared__ float place[WARP ? 1 : 4][32];
-  const int first = WARP ? threadIdx.x & 31 : threadIdx.x, step = WARP ? 32 : blockDim.x;
-  const int teams = WARP ? gridDim.x * ROW_WARPS : gridDim.x;
-  int row = WARP ? blockIdx.x * ROW_WARPS + (threadIdx.x >> 5) : blockIdx.x;
-  ff_pdl_wait();
-  if (row >= P.rows) return;
-  typename R::C raw[PER];
-  unsigned b = divide(row, P.by_tokens), n = row - b * P.tokens;
-  R::load(raw, row_at(P.x, b, n), first, step, P.pieces);
-#pragma unroll 1
-  while (true) {
-    F2 v[PER][N];
-    R::template normalise<WARP>(raw, v, P, first, step, place);
-    char* to = (char*)row_at(P.y, b, n);
-    const float *w = P.w ? P.w + b * P.w_stride : nullptr, *bias = P.bias ? P.bias + b * P.w_stride : nullptr;
-    row += teams;
-    const bool more = row < P.rows;
-    if (more) {
-      b = divide(row, P.by_tokens), n = row - b * P.tokens;
-      R::load(raw, row_at(P.x, b, n), first, step, P.pieces);
-    }
+  using C = typename R::C;
+  static constexpr bool SHARED = sizeof(C) >= 4;
+  C* places;                                                   // [stage][row of the set][piece][thread of the block]
+  int stage;
+  C raw[SHARED ? 1 : SET][SHARED ? 1 : PER];
+  __device__ __forceinline__ Ring(void* shared) : places((C*)shared + threadIdx.x), stage(0) {}
+  __device__ __forceinline__ C* place(int s, int row, int piece) const { return places + ((s * SET + row) * PER + piece) * blockDim.x; }
+  // Row `k` of the set that goes into stage `to` (the row is there or not).
+  __device__ __forceinline__ void ask(int to, int k, const char* row, bool there, int first, int step, int pieces) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int piece = first + i * step;
-      if (piece >= P.pieces) break;
-#pragma unroll
-      for (int c = 0; c < N; ++c) {
-        const F2 add = bias ? two(bias[piece * CH + 2 * c], CH > 1 ? bias[piece * CH + 2 * c + 1] : 0.f) : two(0.f, 0.f);
-        v[i][c] = fma(v[i][c], R::weight(P, w, piece, c), add);
+      const bool on = there && first + i * step < pieces;
+      const char* from = row + (long long)(first + i * step) * sizeof(C);
+      if constexpr (SHARED) {
+        copy_async<sizeof(C)>(place(to, k, i), on ? from : row, on);
+      } else {
+        const C none{};
+        raw[k][i] = on ? *(const C*)from : none;
       }
     }
-    R::store(to, v, first, step, P.pieces);
-    if (!more) break;
   }
+  __device__ __forceinline__ void asked() { if constexpr (SHARED) copy_commit(); }
+  __device__ __forceinline__ void arrived() { if constexpr (SHARED) copy_wait<STAGES<T> - 2>(); }
+  __device__ __forceinline__ void take(int k, typename R::V& v) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if constexpr (SHARED) unpack<T, CH>(*place(stage, k, i), v[i]);
+      else unpack<T, CH>(raw[k][i], v[i]);
+    }
+  }
+  // The stage that has just been read is asked for again, and the next one follows.
+  __device__ __forceinline__ int next() {
+    const int was = stage;
+    stage = stage + 1 == STAGES<T> ? 0 : stage + 1;
+    return was;
+  }
+};
+template <class T, int CH, int PER, int SET>
+constexpr size_t ring_bytes(int threads) { return sizeof(T) * CH >= 4 ? (size_t)STAGES<T> * SET * PER * sizeof(T) * CH * threads : 0; }
+constexpr float DOWN = 8.2718061255302767e-25f;                // 2^-80, for rows whose squares (or sum) leave fp32
+
+__device__ __forceinline__ char* row_at(const RowsView& v, const NormParams& P, unsigned segment, unsigned at) {
+  const unsigned row = segment * P.segment + at, b = divide(row, P.by_tokens), n = row - b * P.tokens;
+  return v.p + (long long)b * v.sb + (long long)n * v.st;
 }
 
-// Backward: a block has a row at a time; block s * parts + i takes every parts-th row of segment s.
-template <class T, int CH, int PER>
-__global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const __grid_constant__ NormParams P) {
+// Forward: the teams of blocks s * parts .. (s + 1) * parts - 1 take the rows of segment s in turns, ROWS at a time.
+template <class T, int CH, int PER, bool WARP>
+__global__ void __launch_bounds__(MAX_THREADS) norm_forward_kernel(const __grid_constant__ NormParams P) {
   using R = Row<T, CH, PER>;
   constexpr int N = R::N;
-  __shared__ float place[6][32];
-  const int first = threadIdx.x, step = blockDim.x;
+  __shared__ __align__(16) Place place[2 * ROWS];
+  const Team team = team_of<WARP>(P);
+  const int first = team.thread, step = team.threads;
   const unsigned segment = blockIdx.x / P.parts, part = blockIdx.x - segment * P.parts;
+  const unsigned stride = P.parts * team.teams;
+  unsigned at = part * team.teams + team.index;
+  clear<WARP>(place);
   ff_pdl_wait();
-  F2 w[PER][N], dw[PER][N], db[PER][N];
+  extern __shared__ __align__(16) unsigned char shared[];
+  Ring<T, CH, PER, ROWS> ring(shared);
+  unsigned asked = at;
+  auto ask = [&](int stage) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-      w[i][c] = R::weight(P, P.w ? P.w + segment * P.w_stride : nullptr, first + i * step, c);
-      dw[i][c] = db[i][c] = two(0.f, 0.f);
+    for (int k = 0; k < ROWS; ++k, asked += stride) {
+      const bool there = asked < P.segment;
+      ring.ask(stage, k, row_at(P.x, P, segment, there ? asked : 0), there, first, step, P.pieces);
     }
-  typename R::C x[PER], g[PER];
-  unsigned at = part, b, n;
-  auto ask = [&] {
-    const unsigned row = segment * P.segment + at;
-    b = divide(row, P.by_tokens), n = row - b * P.tokens;
-    R::load(x, row_at(P.x, b, n), first, step, P.pieces);
-    R::load(g, row_at(P.g, b, n), first, step, P.pieces);
+    ring.asked();
   };
-  if (at < P.segment) ask();
+#pragma unroll
+  for (int i = 0; i < (ring.SHARED ? STAGES<T> - 1 : 1); ++i) ask(i);
+  typename R::V w, b;
+  R::weights(w, P.w ? P.w + segment * P.w_stride : nullptr, P.plus, 1.f, first, step, P.pieces);
+  R::weights(b, P.bias ? P.bias + segment * P.w_stride : nullptr, 0.f, 0.f, first, step, P.pieces);
 #pragma unroll 1
   while (at < P.segment) {
-    F2 v[PER][N], dy[PER][N];
-    const float r = R::template normalise<false>(x, v, P, first, step, place);
-    char* to = P.y.p ? (char*)row_at(P.y, b, n) : nullptr;
+    typename R::V v[ROWS];
+    float s[ROWS], r[ROWS];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      unpack<T, CH>(g[i], dy[i]);
+    ring.arrived();
 #pragma unroll
-      for (int c = 0; c < N; ++c) {
-        dw[i][c] = fma(dy[i][c], v[i][c], dw[i][c]);
-        db[i][c] = __fadd2_rn(db[i][c], dy[i][c]);
-        dy[i][c] = mul(dy[i][c], w[i][c]);                     // g
+    for (int k = 0; k < ROWS; ++k) { ring.take(k, v[k]); s[k] = R::sum(v[k]); }
+    ask((ring.next() + STAGES<T> - 1) % STAGES<T>);
+    team_sum<WARP>(team, s, place);
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) { R::centre(v[k], s[k] * P.inv_d, first, step, P.pieces); s[k] = R::dot(v[k], v[k]); }
+    team_sum<WARP>(team, s, place + ROWS);
+    bool big = false;
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) { r[k] = rsqrtf(fmaf(s[k], P.inv_d, P.eps)); big |= !(s[k] < 3.0e38f); }
+    if (big) {                                                 // (the same in the whole team)
+      // taken again scaled, and eps by the scale's square, which is far below the variance of such a row
+#pragma unroll 1
+      for (int k = 0; k < ROWS; ++k) {
+        typename R::V u;
+        const float f = !(s[k] < 3.0e38f) ? DOWN : 1.f;
+        float t[1];
+        R::load(u, row_at(P.x, P, segment, at + k * stride), first, step, at + k * stride < P.segment ? P.pieces : 0);
+        R::times(u, f);
+        t[0] = R::sum(u);
+        team_sum<WARP>(team, t, place);
+        R::centre(u, t[0] * P.inv_d, first, step, P.pieces);
+        t[0] = R::dot(u, u);
+        team_sum<WARP>(team, t, place + ROWS);
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j)
+          if (j == k) {
+            r[j] = rsqrtf(fmaf(t[0], P.inv_d, P.eps * f * f));
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+              for (int c = 0; c < N; ++c) v[j][i][c] = u[i][c];
+          }
       }
     }
-    at += P.parts;
-    if (at < P.segment) ask();
-    const float m = row_sum<false>(R::sum(dy), place[4]) * P.inv_d, k = row_sum<false>(R::dot(dy, v), place[5]) * P.inv_d;
-    if (to) {
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      if (at + k * stride >= P.segment) break;
 #pragma unroll
       for (int i = 0; i < PER; ++i)
 #pragma unroll
-        for (int c = 0; c < N; ++c)
-          dy[i][c] = mul(fma(v[i][c], two(-k, -k), two(low(dy[i][c]) - m, high(dy[i][c]) - m)), two(r, r));
-      R::store(to, dy, first, step, P.pieces);
+        for (int c = 0; c < N; ++c) v[k][i][c] = fma(mul(v[k][i][c], two(r[k], r[k])), w[i][c], b[i][c]);
+      R::store(row_at(P.y, P, segment, at + k * stride), v[k], first, step, P.pieces);
     }
+    at += ROWS * stride;
   }
+}
+
+// Backward: the teams' rows as in the forward pass, one at a time.  The sums of dweight and dbias of a block's teams are joined and go to its
+// place among the parts.
+template <class T, int CH, int PER, bool WARP>
+__global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const __grid_constant__ NormParams P) {
+  using R = Row<T, CH, PER>;
+  constexpr int N = R::N;
+  __shared__ __align__(16) Place place[4];
+  extern __shared__ __align__(16) unsigned char shared[];
+  float* joined = (float*)shared;                              // at the end: [teams][d]
+  const Team team = team_of<WARP>(P);
+  const int first = team.thread, step = team.threads;
+  const unsigned segment = blockIdx.x / P.parts, part = blockIdx.x - segment * P.parts;
+  const unsigned stride = P.parts * team.teams;
+  unsigned at = part * team.teams + team.index;
+  clear<WARP>(place);
+  ff_pdl_wait();
+  Ring<T, CH, PER, 2> ring(shared);                            // (a row of x, one of dy)
+  unsigned asked = at;
+  auto ask = [&](int stage) {
+    const bool there = asked < P.segment;
+    const unsigned row = there ? asked : 0;
+    ring.ask(stage, 0, row_at(P.x, P, segment, row), there, first, step, P.pieces);
+    ring.ask(stage, 1, row_at(P.g, P, segment, row), there, first, step, P.pieces);
+    ring.asked();
+    asked += stride;
+  };
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int piece = first + i * step;
-    if (piece >= P.pieces) break;
+  for (int i = 0; i < (ring.SHARED ? STAGES<T> - 1 : 1); ++i) ask(i);
+  typename R::V w, dw, db;
+  R::weights(w, P.w ? P.w + segment * P.w_stride : nullptr, P.plus, 1.f, first, step, P.pieces);
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const long long to = blockIdx.x * P.part_stride + piece * CH + c;
-      if (P.dw) P.dw[to] = c & 1 ? high(dw[i][c / 2]) : low(dw[i][c / 2]);
-      if (P.db) P.db[to] = c & 1 ? high(db[i][c / 2]) : low(db[i][c / 2]);
+  for (int i = 0; i < PER; ++i)
+#pragma unroll
+    for (int c = 0; c < N; ++c) dw[i][c] = db[i][c] = two(0.f, 0.f);
+#pragma unroll 1
+  while (at < P.segment) {
+    typename R::V v, dy;
+    ring.arrived();
+    ring.take(0, v);
+    ring.take(1, dy);
+    ask((ring.next() + STAGES<T> - 1) % STAGES<T>);
+    float m[1] = {R::sum(v)};
+    team_sum<WARP>(team, m, place);
+    R::centre(v, m[0] * P.inv_d, first, step, P.pieces);
+    // sums of c^2, of g = dy w and of g c
+    auto sums = [&](float (&s)[3]) {
+      s[0] = R::dot(v, v);
+      F2 u = two(0.f, 0.f), t = u;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          const F2 gw = mul(dy[i][c], w[i][c]);
+          u = __fadd2_rn(u, gw);
+          t = fma(gw, v[i][c], t);
+        }
+      s[1] = low(u) + high(u);
+      s[2] = low(t) + high(t);
+      team_sum<WARP>(team, s, place + 1);
+    };
+    float s[3];
+    sums(s);
+    float r = rsqrtf(fmaf(s[0], P.inv_d, P.eps)), scale = r;
+    if (!(s[0] < 3.0e38f)) {                                   // (as in the forward pass)
+      R::load(v, row_at(P.x, P, segment, at), first, step, P.pieces);
+      R::times(v, DOWN);
+      m[0] = R::sum(v);
+      team_sum<WARP>(team, m, place);
+      R::centre(v, m[0] * P.inv_d, first, step, P.pieces);
+      sums(s);
+      scale = rsqrtf(fmaf(s[0], P.inv_d, P.eps * DOWN * DOWN));
+      r = scale * DOWN;
+    }
+    const float mean_g = -s[1] * P.inv_d, mean_gn = -s[2] * scale * P.inv_d;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        const F2 n = mul(v[i][c], two(scale, scale));
+        dw[i][c] = fma(dy[i][c], n, dw[i][c]);
+        db[i][c] = __fadd2_rn(db[i][c], dy[i][c]);
+        dy[i][c] = mul(fma(n, two(mean_gn, mean_gn), fma(dy[i][c], w[i][c], two(mean_g, mean_g))), two(r, r));
+      }
+    if (P.y.p) R::store(row_at(P.y, P, segment, at), dy, first, step, P.pieces);
+    at += stride;
+  }
+  if constexpr (ring.SHARED) copy_wait<0>();
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float* out = which ? P.db : P.dw;
+    if (!out) continue;
+    out += blockIdx.x * P.part_stride;
+    const typename R::V& v = which ? db : dw;
+    __syncthreads();                                           // (the other one has been read)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int piece = first + i * step;
+      if (piece < P.pieces)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) joined[team.index * P.d + piece * CH + c] = c & 1 ? high(v[i][c / 2]) : low(v[i][c / 2]);
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < P.d; c += blockDim.x) {
+      float s = 0.f;
+      for (int k = 0; k < team.teams; ++k) s += joined[k * P.d + c];
+      out[c] = s;
     }
   }
 }
@@ -299,41 +463,76 @@ int piece_of(int d, int e, uint64_t bits) {
     if (d % ch == 0 && bits % ((uint64_t)ch * e) == 0 && (ch == 16 / e || e == 2)) return ch;
   return 1;
 }
-int block_threads(int pieces, int per) { return ((pieces + per - 1) / per + 31) / 32 * 32; }
-
-// Blocks whose sums are joined: enough for every SM, and no more than rows.
-constexpr int PART_BLOCKS = 4 * FF_B200_SMS;
+// A block: teams of as many warps as a row takes, BLOCK_WARPS warps in all unless a team has more.
+struct Block { int team_warps, teams, threads; };
+Block block_of(int pieces, int per) {
+  Block b;
+  b.team_warps = (pieces + per * 32 - 1) / (per * 32);
+  b.teams = b.team_warps < BLOCK_WARPS ? BLOCK_WARPS / b.team_warps : 1;
+  b.threads = b.teams * b.team_warps * 32;
+  return b;
+}
+// The rows whose gradients are summed together (the model's, or each sample's) and the blocks they are divided between: one wave of
+// them, and at most one for every `each` rows.
 struct Parts { unsigned segments, rows, parts; };
-Parts parts_of(int64_t batch, int64_t tokens, int per_sample) {
+Parts parts_of(int64_t batch, int64_t tokens, int per_sample, int threads, long long each) {
   Parts p;
   p.segments = per_sample ? (unsigned)batch : 1;
   p.rows = (unsigned)(per_sample ? tokens : batch * tokens);
-  p.parts = PART_BLOCKS / (p.segments ? p.segments : 1);
-  if (p.parts > p.rows) p.parts = p.rows;
+  const long long most = ((long long)p.rows + each - 1) / each, wave = (long long)FF_B200_SMS * (SM_THREADS / threads) / (p.segments ? p.segments : 1);
+  p.parts = (unsigned)(wave < most ? wave : most);
   if (p.parts < 1) p.parts = 1;
   return p;
 }
 
+// More than the default limit of shared memory, with every call that needs it (a handle serves any device), and always as much as the longest
+// row takes, so that calls of several threads do not lower each other's.
+constexpr int MOST_SMEM = STAGES<float> * ROWS * MAX_DIM * (int)sizeof(float);
+cudaError_t allow(void (*kernel)(NormParams), size_t smem) {
+  return smem <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST_SMEM);
+}
+
 template <class T, int CH, int PER, bool WARP>
-cudaError_t forward(NormParams& P, cudaStream_t st) {
-  // Blocks of one wave take the rows in turns.
-  const int threads = WARP ? ROW_WARPS * 32 : block_threads(P.pieces, PER);
-  const long long blocks = WARP ? (P.rows + ROW_WARPS - 1) / ROW_WARPS : P.rows, wave = (long long)FF_B200_SMS * (2048 / threads);
-  return ff_launch(norm_forward_kernel<T, CH, PER, WARP>, dim3((unsigned)(blocks < 4 * wave ? blocks : 4 * wave)), dim3(threads), 0, st, P);
+cudaError_t forward(NormParams& P, int64_t batch, int64_t tokens, int per_sample, cudaStream_t st) {
+  const Block b = block_of(P.pieces, PER);
+  const Parts p = parts_of(batch, tokens, per_sample, b.threads, b.teams);
+  P.segment = p.rows; P.parts = p.parts; P.team_warps = b.team_warps;
+  const size_t smem = ring_bytes<T, CH, PER, ROWS>(b.threads);
+  const cudaError_t e = allow(norm_forward_kernel<T, CH, PER, WARP>, smem);
+  return e != cudaSuccess ? e : ff_launch(norm_forward_kernel<T, CH, PER, WARP>, dim3(p.segments * p.parts), dim3(b.threads), smem, st, P);
 }
-template <class T, int CH, int PER>
+template <class T, int CH, int PER, bool WARP>
 cudaError_t backward(NormParams& P, unsigned blocks, cudaStream_t st) {
-  return ff_launch(norm_backward_kernel<T, CH, PER>, dim3(blocks), dim3(block_threads(P.pieces, PER)), 0, st, P);
+  const Block b = block_of(P.pieces, PER);
+  P.team_warps = b.team_warps;
+  const size_t ring = ring_bytes<T, CH, PER, 2>(b.threads), joined = (size_t)b.teams * P.d * sizeof(float), smem = ring > joined ? ring : joined;
+  const cudaError_t e = allow(norm_backward_kernel<T, CH, PER, WARP>, smem);
+  return e != cudaSuccess ? e : ff_launch(norm_backward_kernel<T, CH, PER, WARP>, dim3(blocks), dim3(b.threads), smem, st, P);
 }
-template <class T, int CH>
-cudaError_t forward_of(NormParams& P, cudaStream_t st) {
-  if constexpr (CH * sizeof(T) == 16) {
-    if (P.pieces <= 32) return forward<T, CH, 1, true>(P, st);
-    if (P.pieces <= 64) return forward<T, CH, 2, true>(P, st);
-    if (P.pieces <= 128) return forward<T, CH, 4, true>(P, st);
-    if (P.pieces <= 256) return forward<T, CH, 8, true>(P, st);
-  }
-  return forward<T, CH, VALUES / CH, false>(P, st);
+// The team and the pieces of a thread: a warp where it has room for the row, else a block with 16 values a thread (8 in pieces of one
+// value, where more of them have to be on their way and fewer fit).
+template <class T, int CH, class Run>
+cudaError_t with_team(int pieces, Run run) {
+  using std::integral_constant;
+  using True = integral_constant<bool, true>;
+  using False = integral_constant<bool, false>;
+  constexpr int MOST = CH == 1 ? 8 : VALUES / CH;
+  if (pieces <= 32 * MOST / 2) return run(integral_constant<int, MOST / 2>(), True());
+  if (pieces <= 32 * MOST) return run(integral_constant<int, MOST>(), True());
+  if (pieces <= MAX_THREADS * MOST) return run(integral_constant<int, MOST>(), False());
+  return run(integral_constant<int, VALUES / CH>(), False());
+}
+template <class Run>
+cudaError_t with_piece(int e, int ch, Run run) {
+  if (e == 4) return ch == 4 ? run(float(), std::integral_constant<int, 4>()) : run(float(), std::integral_constant<int, 1>());
+  return ch == 8 ? run(__nv_bfloat16(), std::integral_constant<int, 8>())
+                 : ch == 2 ? run(__nv_bfloat16(), std::integral_constant<int, 2>()) : run(__nv_bfloat16(), std::integral_constant<int, 1>());
+}
+
+// Backward: the same blocks whatever the tensors' alignment, so that the workspace does not depend on it.
+Parts backward_parts(const ff_layer_norm_config_t& c, int64_t batch, int64_t tokens, int per_sample) {
+  const Block b = block_of(c.dim, VALUES);
+  return parts_of(batch, tokens, per_sample, b.threads, b.teams);
 }
 
 ff_status_t check_call(ff_layer_norm* h, int64_t batch, int64_t tokens, std::initializer_list<const float*> weights) {
@@ -398,8 +597,13 @@ extern "C" ff_status_t ff_layer_norm_forward(const ff_layer_norm_t* handle, int6
   P.x = view(x, e); P.y = view(y, e);
   P.bias = bias;
   cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t err = e == 4 ? (ch == 4 ? forward_of<float, 4>(P, st) : forward_of<float, 1>(P, st))
-                                 : ch == 8 ? forward_of<__nv_bfloat16, 8>(P, st) : ch == 2 ? forward_of<__nv_bfloat16, 2>(P, st) : forward_of<__nv_bfloat16, 1>(P, st);
+  const cudaError_t err = with_piece(e, ch, [&](auto t, auto piece) {
+    using T = decltype(t);
+    constexpr int CH = decltype(piece)::value;
+    return with_team<T, CH>(P.pieces, [&](auto per, auto warp) {
+      return forward<T, CH, decltype(per)::value, decltype(warp)::value>(P, batch, tokens, per_sample, st);
+    });
+  });
   return err == cudaSuccess ? FF_OK : cuda_fail(h, err);
 }
 
@@ -408,7 +612,7 @@ extern "C" ff_status_t ff_layer_norm_workspace_bytes(const ff_layer_norm_t* hand
   if (!h || !bytes) return fail(h, FF_ERR_INVALID_ARG, "handle or bytes is NULL");
   const ff_status_t s = check_call(h, batch, tokens, {});
   if (s != FF_OK) return s;
-  const Parts p = parts_of(batch, tokens, per_sample);
+  const Parts p = backward_parts(h->cfg, batch, tokens, per_sample);
   *bytes = batch * tokens == 0 || p.parts == 1 ? 0 : (size_t)p.segments * p.parts * 2 * h->cfg.dim * sizeof(float);
   return FF_OK;
 }
@@ -441,7 +645,7 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
   if (need && (((uintptr_t)ws) & 15)) return fail(h, FF_ERR_WORKSPACE, "the workspace must be 16-byte aligned");
   if (!dx && !dweight && !dbias) return FF_OK;
   const int ch = piece_of(d, e, bits);
-  const Parts parts = parts_of(batch, tokens, per_sample);
+  const Parts parts = backward_parts(h->cfg, batch, tokens, per_sample);
   NormParams P = common(h, batch, tokens, weight, per_sample, ch);
   P.x = view(x, e); P.g = view(dy, e);
   if (dx) P.y = view(dx, e);
@@ -456,9 +660,11 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
     P.part_stride = 2 * d;
   }
   const unsigned blocks = parts.segments * parts.parts;
-  cudaError_t err = e == 4 ? (ch == 4 ? backward<float, 4, VALUES / 4>(P, blocks, st) : backward<float, 1, VALUES>(P, blocks, st))
-                           : ch == 8 ? backward<__nv_bfloat16, 8, VALUES / 8>(P, blocks, st)
-                           : ch == 2 ? backward<__nv_bfloat16, 2, VALUES / 2>(P, blocks, st) : backward<__nv_bfloat16, 1, VALUES>(P, blocks, st);
+  cudaError_t err = with_piece(e, ch, [&](auto t, auto piece) {
+    using T = decltype(t);
+    constexpr int CH = decltype(piece)::value;
+    return with_team<T, CH>(P.pieces, [&](auto per, auto warp) { return backward<T, CH, decltype(per)::value, decltype(warp)::value>(P, blocks, st); });
+  });
   if (err == cudaSuccess && parts.parts > 1 && (dweight || dbias)) {
     const int columns = (d + 31) / 32;
     err = ff_launch(norm_join_kernel, dim3(parts.segments * columns, 2), dim3(1024), 0, st, (const float*)ws, (int)parts.parts, d, columns, dweight, dbias);

@@ -227,16 +227,6 @@ __device__ __forceinline__ bool token_of(const HeadsParams& P, int group, int wa
   return row < P.rows;
 }
 
-// A thread's own piece of memory into its own place in shared memory, asynchronously (`on` false: zeros).
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* to, const void* from, bool on) {
-  const unsigned at = (unsigned)__cvta_generic_to_shared(to), n = on ? BYTES : 0;
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(n) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(at), "l"(from), "r"(n), "n"(BYTES) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
-
 // A block's way through the units (group of 8 x 32 / lanes tokens, head or two): a run of them, those of a group following one another, all
 // blocks' runs equally long.  (Whole groups in turns over all blocks and shares of what is left measured no better.)
 struct Walk {
