@@ -25,12 +25,15 @@ struct ff_layer_norm {
 
 namespace {
 
-constexpr int VALUES = 16;                        // values of a row that a thread of a block has
-constexpr int MAX_DIM = 8192, MAX_THREADS = MAX_DIM / VALUES;
-constexpr int BLOCK_WARPS = 8;
-constexpr int SM_THREADS = 512;                   // threads of an SM that one wave of blocks counts on
-template <class T> constexpr int STAGES = sizeof(T) == 4 ? 3 : 4;   // sets of rows of a team on their way or being read (two blocks fit an SM)
-constexpr int ROWS = 2;                           // rows of a team at a time, forward
+// Values of a row that a thread has (in pieces of one value 8, where more of them have to be on their way, or 16).  With 32 instead of 16 the
+// shuffles, barriers and addresses of a row are shared by twice the values: 16384 x 1024 bf16 backward 24 us instead of 30, 32768 x 5120
+// forward 114 instead of 148 (65536 x 2048 forward: 100, with 16 and two rows at a time 89).  Weights and both sums then leave room for
+// one block of eight warps on an SM backward; three blocks of four, which spill, took 36 to 60 us for the former.
+constexpr int VALUES = 32;
+constexpr int MAX_DIM = 8192, MAX_THREADS = 512;
+constexpr int BLOCK_WARPS = 8;                    // warps of a block, unless a team has more
+constexpr int FORWARD_BLOCKS = 2, BACKWARD_BLOCKS = 1;   // such blocks on an SM
+template <class T> constexpr int STAGES = sizeof(T) == 4 ? 3 : 4;   // rows of a team on their way or being read
 
 struct RowsView { char* p; long long sb, st; };   // strides in bytes
 struct NormParams {
@@ -40,6 +43,7 @@ struct NormParams {
   float plus;                       // added to the weight
   float *dw, *db;                   // backward: where a block's sums go (or NULL) ...
   long long part_stride;            // ... and how far those of the blocks are apart
+  int even;                         // the rows of a segment lie at one distance
   unsigned tokens, segment, parts;  // tokens of a sample; rows whose gradients are summed together, blocks that do it
   FFFastDiv by_tokens;
   int rows, d, pieces, team_warps;
@@ -47,11 +51,6 @@ struct NormParams {
 };
 
 __device__ __forceinline__ unsigned divide(unsigned n, const FFFastDiv& f) { return (unsigned)(((unsigned long long)__umulhi(n, f.m) + n) >> f.s); }
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int m = 16; m; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
-  return v;
-}
 // A team: `warps` neighbouring warps of a block, which holds several.
 struct Team { int warps, index, teams, thread, threads; };
 template <bool WARP>
@@ -67,21 +66,32 @@ __device__ __forceinline__ Team team_of(const NormParams& P) {
 }
 // Sums over a team, whose warps' sums meet in a place of their own: four at a time are read (one after the other they took
 // longer than the rest of the row).
-constexpr int PLACE = MAX_THREADS / 32;
-using Place = float[BLOCK_WARPS][PLACE];                       // [team][warp]
-template <bool WARP, int K>
-__device__ __forceinline__ void team_sum(const Team& t, float (&v)[K], Place* place) {
+template <int WARPS> using Place = float[BLOCK_WARPS][WARPS];  // [team][warp]
+template <bool WARP, int K, int PLACE>
+__device__ __forceinline__ void team_sum(const Team& t, float (&v)[K], float (*place)[BLOCK_WARPS][PLACE]) {
+  static_assert(K <= 4, "");
+  const int lane = threadIdx.x & 31;
+  // With several sums a lane gives away half of them at the first exchanges and goes on with the others.
+  float mine = v[0];
+  int which = 0;
+  if constexpr (K > 2) {
+    const bool h = lane & 16, g = lane & 8;
+    const float v3 = K > 3 ? v[K - 1] : 0.f;
+    const float k0 = (h ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, h ? v[0] : v[2], 16), k1 = (h ? v3 : v[1]) + __shfl_xor_sync(0xffffffffu, h ? v[1] : v3, 16);
+    mine = (g ? k1 : k0) + __shfl_xor_sync(0xffffffffu, g ? k0 : k1, 8);
+    which = (lane >> 3) & 3;
+  } else if constexpr (K == 2) {
+    const bool h = lane & 16;
+    mine = (h ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, h ? v[0] : v[1], 16);
+    which = lane >> 4;
+  }
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
-  if constexpr (!WARP) {
-    const int lane = threadIdx.x & 31;
-    if (lane < K) {
-      float mine = v[0];
+  for (int m = K > 2 ? 4 : K == 2 ? 8 : 16; m; m >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, m);
+  if constexpr (WARP) {
 #pragma unroll
-      for (int k = 1; k < K; ++k)
-        if (lane == k) mine = v[k];
-      place[lane][t.index][t.thread >> 5] = mine;
-    }
+    for (int k = 0; k < K; ++k) v[k] = K == 1 ? mine : __shfl_sync(0xffffffffu, mine, K == 2 ? 16 * k : 8 * k);
+  } else {
+    if ((lane & (K > 2 ? 7 : K == 2 ? 15 : 31)) == 0 && which < K) place[which][t.index][t.thread >> 5] = mine;
     asm volatile("bar.sync %0, %1;" ::"r"(1 + t.index), "r"(t.threads) : "memory");
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -97,31 +107,47 @@ __device__ __forceinline__ void team_sum(const Team& t, float (&v)[K], Place* pl
   }
 }
 // (the places of warps that a team does not have)
-template <bool WARP, int K>
-__device__ __forceinline__ void clear(Place (&place)[K]) {
+template <bool WARP, int K, int PLACE>
+__device__ __forceinline__ void clear(float (&place)[K][BLOCK_WARPS][PLACE]) {
   if constexpr (!WARP) {
     for (int i = threadIdx.x; i < K * BLOCK_WARPS * PLACE; i += blockDim.x) (&place[0][0][0])[i] = 0.f;
     __syncthreads();
   }
 }
 
-// A thread's pieces of a row: piece `first + i * step`.
-template <class T, int CH, int PER>
+// A thread's pieces of a row, every `threads`-th of the team: their first channels, and whether the row has them.
+// FULL: it has them all.
+template <int CH, int PER, bool FULL>
+struct Mine {
+  int at[PER];
+  bool on[PER];
+  __device__ __forceinline__ Mine(const Team& t, int pieces) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int piece = t.thread + i * t.threads;
+      on[i] = piece < pieces;
+      at[i] = FULL || on[i] ? piece * CH : 0;
+    }
+  }
+  __device__ __forceinline__ bool have(int i) const { return FULL || on[i]; }
+};
+template <class T, int CH, int PER, bool FULL>
 struct Row {
   static constexpr int N = pairs_of(CH);
   using C = Chunk<T, CH>;
   using V = F2[PER][N];
-  static __device__ __forceinline__ void load(V& v, const char* row, int first, int step, int pieces) {
+  using M = Mine<CH, PER, FULL>;
+  static __device__ __forceinline__ void load(V& v, const char* row, const M& m) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const C none{};
-      unpack<T, CH>(first + i * step < pieces ? *(const C*)(row + (long long)(first + i * step) * sizeof(C)) : none, v[i]);
+      unpack<T, CH>(m.have(i) ? *(const C*)(row + m.at[i] * sizeof(T)) : none, v[i]);
     }
   }
-  static __device__ __forceinline__ void store(char* row, const V& v, int first, int step, int pieces) {
+  static __device__ __forceinline__ void store(char* row, const V& v, const M& m) {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      if (first + i * step < pieces) *(C*)(row + (long long)(first + i * step) * sizeof(C)) = pack<T, CH>(v[i]);
+      if (m.have(i)) *(C*)(row + m.at[i] * sizeof(T)) = pack<T, CH>(v[i]);
   }
   static __device__ __forceinline__ float sum(const V& v) {
     F2 s = two(0.f, 0.f);
@@ -146,48 +172,45 @@ struct Row {
       for (int c = 0; c < N; ++c) v[i][c] = mul(v[i][c], two(f, f));
   }
   // Values minus `m`, and zeros where the row has none.
-  static __device__ __forceinline__ void centre(V& v, float m, int first, int step, int pieces) {
+  static __device__ __forceinline__ void centre(V& v, float mean, const M& m) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const float mine = first + i * step < pieces ? -m : 0.f;
+      const float mine = m.have(i) ? -mean : 0.f;
 #pragma unroll
       for (int c = 0; c < N; ++c) v[i][c] = __fadd2_rn(v[i][c], two(mine, CH > 1 ? mine : 0.f));
     }
   }
   // Neighbouring weights of a piece, `plus` more, or `none` where there are none.
-  static __device__ __forceinline__ void weights(V& w, const float* from, float plus, float none, int first, int step, int pieces) {
+  static __device__ __forceinline__ void weights(V& w, const float* from, float plus, float none, const M& m) {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
 #pragma unroll
-      for (int c = 0; c < N; ++c) {
-        const int at = (first + i * step) * CH + 2 * c;
-        w[i][c] = from && first + i * step < pieces ? two(from[at] + plus, CH > 1 ? from[at + 1] + plus : 0.f) : two(none, none);
-      }
+      for (int c = 0; c < N; ++c)
+        w[i][c] = from && m.have(i) ? two(from[m.at[i] + 2 * c] + plus, CH > 1 ? from[m.at[i] + 2 * c + 1] + plus : 0.f) : two(none, none);
   }
 };
 // A team's rows on their way: every thread copies its own pieces of them into places of its own in shared memory, STAGES - 1 sets of rows
 // ahead.  (Pieces of two bytes cannot be copied that way: one set ahead, in registers.)
-template <class T, int CH, int PER, int SET>
+template <class T, int CH, int PER, bool FULL, int SET>
 struct Ring {
-  using R = Row<T, CH, PER>;
+  using R = Row<T, CH, PER, FULL>;
   using C = typename R::C;
   static constexpr bool SHARED = sizeof(C) >= 4;
-  C* places;                                                   // [stage][row of the set][piece][thread of the block]
-  int stage;
+  unsigned char* places;                                       // [stage][row of the set][piece][thread of the block]
+  int stage, stage_bytes;
   C raw[SHARED ? 1 : SET][SHARED ? 1 : PER];
-  __device__ __forceinline__ Ring(void* shared) : places((C*)shared + threadIdx.x), stage(0) {}
-  __device__ __forceinline__ C* place(int s, int row, int piece) const { return places + ((s * SET + row) * PER + piece) * blockDim.x; }
+  __device__ __forceinline__ Ring(void* shared) : places((unsigned char*)shared + threadIdx.x * sizeof(C)), stage(0), stage_bytes(SET * PER * (int)sizeof(C) * (int)blockDim.x) {}
+  __device__ __forceinline__ C* place(int s, int row, int piece) const { return (C*)(places + s * stage_bytes + (row * PER + piece) * (int)sizeof(C) * (int)blockDim.x); }
   // Row `k` of the set that goes into stage `to` (the row is there or not).
-  __device__ __forceinline__ void ask(int to, int k, const char* row, bool there, int first, int step, int pieces) {
+  __device__ __forceinline__ void ask(int to, int k, const char* row, bool there, const typename R::M& m) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const bool on = there && first + i * step < pieces;
-      const char* from = row + (long long)(first + i * step) * sizeof(C);
+      const char* from = row + m.at[i] * sizeof(T);
       if constexpr (SHARED) {
-        copy_async<sizeof(C)>(place(to, k, i), on ? from : row, on);
+        copy_async<sizeof(C)>(place(to, k, i), from, there && m.have(i));
       } else {
         const C none{};
-        raw[k][i] = on ? *(const C*)from : none;
+        raw[k][i] = there && m.have(i) ? *(const C*)from : none;
       }
     }
   }
@@ -211,124 +234,115 @@ template <class T, int CH, int PER, int SET>
 constexpr size_t ring_bytes(int threads) { return sizeof(T) * CH >= 4 ? (size_t)STAGES<T> * SET * PER * sizeof(T) * CH * threads : 0; }
 constexpr float DOWN = 8.2718061255302767e-25f;                // 2^-80, for rows whose squares (or sum) leave fp32
 
+// Row `at` of a segment, and the team's way from one to the next.  (Rows that follow one another at one distance, of a sample or of a whole
+// contiguous batch, need no division.)
 __device__ __forceinline__ char* row_at(const RowsView& v, const NormParams& P, unsigned segment, unsigned at) {
-  const unsigned row = segment * P.segment + at, b = divide(row, P.by_tokens), n = row - b * P.tokens;
+  if (P.even) return v.p + (long long)segment * v.sb + (long long)at * v.st;
+  const unsigned b = divide(at, P.by_tokens), n = at - b * P.tokens;          // (then there is one segment)
   return v.p + (long long)b * v.sb + (long long)n * v.st;
 }
+struct Way {
+  char* p;
+  long long step;
+  __device__ __forceinline__ Way(const RowsView& v, const NormParams& P, unsigned segment, unsigned at, unsigned stride)
+      : p(row_at(v, P, segment, at)), step((long long)stride * v.st) {}
+  __device__ __forceinline__ void to(const RowsView& v, const NormParams& P, unsigned at) {
+    if (P.even) p += step;
+    else p = row_at(v, P, 0, at);
+  }
+};
 
-// Forward: the teams of blocks s * parts .. (s + 1) * parts - 1 take the rows of segment s in turns, ROWS at a time.
-template <class T, int CH, int PER, bool WARP>
-__global__ void __launch_bounds__(MAX_THREADS) norm_forward_kernel(const __grid_constant__ NormParams P) {
-  using R = Row<T, CH, PER>;
+// Forward: the teams of blocks s * parts .. (s + 1) * parts - 1 take the rows of segment s in turns.
+template <class T, int CH, int PER, bool FULL, bool WARP, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD_BLOCKS : 1) norm_forward_kernel(const __grid_constant__ NormParams P) {
+  using R = Row<T, CH, PER, FULL>;
   constexpr int N = R::N;
-  __shared__ __align__(16) Place place[2 * ROWS];
+  __shared__ __align__(16) Place<THREADS / 32> place[2];
+  extern __shared__ __align__(16) unsigned char shared[];
   const Team team = team_of<WARP>(P);
-  const int first = team.thread, step = team.threads;
+  const typename R::M mine(team, P.pieces);
   const unsigned segment = blockIdx.x / P.parts, part = blockIdx.x - segment * P.parts;
   const unsigned stride = P.parts * team.teams;
   unsigned at = part * team.teams + team.index;
   clear<WARP>(place);
   ff_pdl_wait();
-  extern __shared__ __align__(16) unsigned char shared[];
-  Ring<T, CH, PER, ROWS> ring(shared);
+  Ring<T, CH, PER, FULL, 1> ring(shared);
   unsigned asked = at;
+  Way from(P.x, P, segment, at, stride), to(P.y, P, segment, at, stride);
   auto ask = [&](int stage) {
-#pragma unroll
-    for (int k = 0; k < ROWS; ++k, asked += stride) {
-      const bool there = asked < P.segment;
-      ring.ask(stage, k, row_at(P.x, P, segment, there ? asked : 0), there, first, step, P.pieces);
-    }
+    ring.ask(stage, 0, from.p, asked < P.segment, mine);
     ring.asked();
+    asked += stride;
+    if (asked < P.segment) from.to(P.x, P, asked);
   };
 #pragma unroll
   for (int i = 0; i < (ring.SHARED ? STAGES<T> - 1 : 1); ++i) ask(i);
   typename R::V w, b;
-  R::weights(w, P.w ? P.w + segment * P.w_stride : nullptr, P.plus, 1.f, first, step, P.pieces);
-  R::weights(b, P.bias ? P.bias + segment * P.w_stride : nullptr, 0.f, 0.f, first, step, P.pieces);
+  R::weights(w, P.w ? P.w + segment * P.w_stride : nullptr, P.plus, 1.f, mine);
+  R::weights(b, P.bias ? P.bias + segment * P.w_stride : nullptr, 0.f, 0.f, mine);
 #pragma unroll 1
   while (at < P.segment) {
-    typename R::V v[ROWS];
-    float s[ROWS], r[ROWS];
-#pragma unroll
+    typename R::V v;
     ring.arrived();
-#pragma unroll
-    for (int k = 0; k < ROWS; ++k) { ring.take(k, v[k]); s[k] = R::sum(v[k]); }
+    ring.take(0, v);
+    float s[1] = {R::sum(v)};
     ask((ring.next() + STAGES<T> - 1) % STAGES<T>);
     team_sum<WARP>(team, s, place);
-#pragma unroll
-    for (int k = 0; k < ROWS; ++k) { R::centre(v[k], s[k] * P.inv_d, first, step, P.pieces); s[k] = R::dot(v[k], v[k]); }
-    team_sum<WARP>(team, s, place + ROWS);
-    bool big = false;
-#pragma unroll
-    for (int k = 0; k < ROWS; ++k) { r[k] = rsqrtf(fmaf(s[k], P.inv_d, P.eps)); big |= !(s[k] < 3.0e38f); }
-    if (big) {                                                 // (the same in the whole team)
+    R::centre(v, s[0] * P.inv_d, mine);
+    s[0] = R::dot(v, v);
+    team_sum<WARP>(team, s, place + 1);
+    float r = rsqrtf(fmaf(s[0], P.inv_d, P.eps));
+    if (!(s[0] < 3.0e38f)) {                                   // (the same in the whole team)
       // taken again scaled, and eps by the scale's square, which is far below the variance of such a row
-#pragma unroll 1
-      for (int k = 0; k < ROWS; ++k) {
-        typename R::V u;
-        const float f = !(s[k] < 3.0e38f) ? DOWN : 1.f;
-        float t[1];
-        R::load(u, row_at(P.x, P, segment, at + k * stride), first, step, at + k * stride < P.segment ? P.pieces : 0);
-        R::times(u, f);
-        t[0] = R::sum(u);
-        team_sum<WARP>(team, t, place);
-        R::centre(u, t[0] * P.inv_d, first, step, P.pieces);
-        t[0] = R::dot(u, u);
-        team_sum<WARP>(team, t, place + ROWS);
-#pragma unroll
-        for (int j = 0; j < ROWS; ++j)
-          if (j == k) {
-            r[j] = rsqrtf(fmaf(t[0], P.inv_d, P.eps * f * f));
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-#pragma unroll
-              for (int c = 0; c < N; ++c) v[j][i][c] = u[i][c];
-          }
-      }
+      R::load(v, row_at(P.x, P, segment, at), mine);
+      R::times(v, DOWN);
+      s[0] = R::sum(v);
+      team_sum<WARP>(team, s, place);
+      R::centre(v, s[0] * P.inv_d, mine);
+      s[0] = R::dot(v, v);
+      team_sum<WARP>(team, s, place + 1);
+      r = rsqrtf(fmaf(s[0], P.inv_d, P.eps * DOWN * DOWN));
     }
 #pragma unroll
-    for (int k = 0; k < ROWS; ++k) {
-      if (at + k * stride >= P.segment) break;
+    for (int i = 0; i < PER; ++i)
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-#pragma unroll
-        for (int c = 0; c < N; ++c) v[k][i][c] = fma(mul(v[k][i][c], two(r[k], r[k])), w[i][c], b[i][c]);
-      R::store(row_at(P.y, P, segment, at + k * stride), v[k], first, step, P.pieces);
-    }
-    at += ROWS * stride;
+      for (int c = 0; c < N; ++c) v[i][c] = fma(mul(v[i][c], two(r, r)), w[i][c], b[i][c]);
+    R::store(to.p, v, mine);
+    at += stride;
+    if (at < P.segment) to.to(P.y, P, at);
   }
 }
 
 // Backward: the teams' rows as in the forward pass, one at a time.  The sums of dweight and dbias of a block's teams are joined and go to its
 // place among the parts.
-template <class T, int CH, int PER, bool WARP>
-__global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const __grid_constant__ NormParams P) {
-  using R = Row<T, CH, PER>;
+template <class T, int CH, int PER, bool FULL, bool WARP, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWARD_BLOCKS : 1) norm_backward_kernel(const __grid_constant__ NormParams P) {
+  using R = Row<T, CH, PER, FULL>;
   constexpr int N = R::N;
-  __shared__ __align__(16) Place place[4];
+  __shared__ __align__(16) Place<THREADS / 32> place[4];
   extern __shared__ __align__(16) unsigned char shared[];
   float* joined = (float*)shared;                              // at the end: [teams][d]
   const Team team = team_of<WARP>(P);
-  const int first = team.thread, step = team.threads;
+  const typename R::M mine(team, P.pieces);
   const unsigned segment = blockIdx.x / P.parts, part = blockIdx.x - segment * P.parts;
   const unsigned stride = P.parts * team.teams;
   unsigned at = part * team.teams + team.index;
   clear<WARP>(place);
   ff_pdl_wait();
-  Ring<T, CH, PER, 2> ring(shared);                            // (a row of x, one of dy)
+  Ring<T, CH, PER, FULL, 2> ring(shared);                            // (a row of x, one of dy)
   unsigned asked = at;
+  Way x(P.x, P, segment, at, stride), g(P.g, P, segment, at, stride), to(P.y, P, segment, at, stride);
   auto ask = [&](int stage) {
-    const bool there = asked < P.segment;
-    const unsigned row = there ? asked : 0;
-    ring.ask(stage, 0, row_at(P.x, P, segment, row), there, first, step, P.pieces);
-    ring.ask(stage, 1, row_at(P.g, P, segment, row), there, first, step, P.pieces);
+    ring.ask(stage, 0, x.p, asked < P.segment, mine);
+    ring.ask(stage, 1, g.p, asked < P.segment, mine);
     ring.asked();
     asked += stride;
+    if (asked < P.segment) { x.to(P.x, P, asked); g.to(P.g, P, asked); }
   };
 #pragma unroll
   for (int i = 0; i < (ring.SHARED ? STAGES<T> - 1 : 1); ++i) ask(i);
   typename R::V w, dw, db;
-  R::weights(w, P.w ? P.w + segment * P.w_stride : nullptr, P.plus, 1.f, first, step, P.pieces);
+  R::weights(w, P.w ? P.w + segment * P.w_stride : nullptr, P.plus, 1.f, mine);
 #pragma unroll
   for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -342,7 +356,7 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const __grid
     ask((ring.next() + STAGES<T> - 1) % STAGES<T>);
     float m[1] = {R::sum(v)};
     team_sum<WARP>(team, m, place);
-    R::centre(v, m[0] * P.inv_d, first, step, P.pieces);
+    R::centre(v, m[0] * P.inv_d, mine);
     // sums of c^2, of g = dy w and of g c
     auto sums = [&](float (&s)[3]) {
       s[0] = R::dot(v, v);
@@ -363,11 +377,11 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const __grid
     sums(s);
     float r = rsqrtf(fmaf(s[0], P.inv_d, P.eps)), scale = r;
     if (!(s[0] < 3.0e38f)) {                                   // (as in the forward pass)
-      R::load(v, row_at(P.x, P, segment, at), first, step, P.pieces);
+      R::load(v, row_at(P.x, P, segment, at), mine);
       R::times(v, DOWN);
       m[0] = R::sum(v);
       team_sum<WARP>(team, m, place);
-      R::centre(v, m[0] * P.inv_d, first, step, P.pieces);
+      R::centre(v, m[0] * P.inv_d, mine);
       sums(s);
       scale = rsqrtf(fmaf(s[0], P.inv_d, P.eps * DOWN * DOWN));
       r = scale * DOWN;
@@ -382,8 +396,9 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const __grid
         db[i][c] = __fadd2_rn(db[i][c], dy[i][c]);
         dy[i][c] = mul(fma(n, two(mean_gn, mean_gn), fma(dy[i][c], w[i][c], two(mean_g, mean_g))), two(r, r));
       }
-    if (P.y.p) R::store(row_at(P.y, P, segment, at), dy, first, step, P.pieces);
+    if (P.y.p) R::store(to.p, dy, mine);
     at += stride;
+    if (at < P.segment) to.to(P.y, P, at);
   }
   if constexpr (ring.SHARED) copy_wait<0>();
 #pragma unroll
@@ -395,10 +410,9 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const __grid
     __syncthreads();                                           // (the other one has been read)
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int piece = first + i * step;
-      if (piece < P.pieces)
+      if (mine.have(i))
 #pragma unroll
-        for (int c = 0; c < CH; ++c) joined[team.index * P.d + piece * CH + c] = c & 1 ? high(v[i][c / 2]) : low(v[i][c / 2]);
+        for (int c = 0; c < CH; ++c) joined[team.index * P.d + mine.at[i] + c] = c & 1 ? high(v[i][c / 2]) : low(v[i][c / 2]);
     }
     __syncthreads();
     for (int c = threadIdx.x; c < P.d; c += blockDim.x) {
@@ -456,6 +470,11 @@ ff_status_t check_rows(ff_layer_norm* h, const ff_rows_t* v, int64_t batch, int6
   return FF_OK;
 }
 RowsView view(const ff_rows_t* v, int e) { return RowsView{(char*)v->data, (long long)v->stride_batch * e, (long long)v->stride_token * e}; }
+// Do the rows of a batch follow one another at one distance?  (With one token a sample at that of the samples, which is then the tokens'.)
+bool even(RowsView* v, int64_t batch, int64_t tokens) {
+  if (tokens == 1) v->st = v->sb;
+  return batch == 1 || tokens == 1 || v->sb == tokens * v->st;
+}
 
 // Values of a piece that dim and the tensors' alignment allow.
 int piece_of(int d, int e, uint64_t bits) {
@@ -463,23 +482,26 @@ int piece_of(int d, int e, uint64_t bits) {
     if (d % ch == 0 && bits % ((uint64_t)ch * e) == 0 && (ch == 16 / e || e == 2)) return ch;
   return 1;
 }
-// A block: teams of as many warps as a row takes, BLOCK_WARPS warps in all unless a team has more.
+// A block: teams of as many warps as a row takes, BLOCK_WARPS warps in all unless a team has more, or there are few rows: then every SM
+// gets some of them (8 rows of 2048: 4.6 us in two blocks, 2.9 in eight).
 struct Block { int team_warps, teams, threads; };
-Block block_of(int pieces, int per) {
+Block block_of(int pieces, int per, long long rows) {
   Block b;
   b.team_warps = (pieces + per * 32 - 1) / (per * 32);
   b.teams = b.team_warps < BLOCK_WARPS ? BLOCK_WARPS / b.team_warps : 1;
+  const long long fair = (rows + FF_B200_SMS - 1) / FF_B200_SMS;
+  if (b.teams > fair) b.teams = (int)(fair < 1 ? 1 : fair);
   b.threads = b.teams * b.team_warps * 32;
   return b;
 }
 // The rows whose gradients are summed together (the model's, or each sample's) and the blocks they are divided between: one wave of
 // them, and at most one for every `each` rows.
 struct Parts { unsigned segments, rows, parts; };
-Parts parts_of(int64_t batch, int64_t tokens, int per_sample, int threads, long long each) {
+Parts parts_of(int64_t batch, int64_t tokens, int per_sample, int threads, int blocks, long long each) {
   Parts p;
   p.segments = per_sample ? (unsigned)batch : 1;
   p.rows = (unsigned)(per_sample ? tokens : batch * tokens);
-  const long long most = ((long long)p.rows + each - 1) / each, wave = (long long)FF_B200_SMS * (SM_THREADS / threads) / (p.segments ? p.segments : 1);
+  const long long most = ((long long)p.rows + each - 1) / each, wave = (long long)FF_B200_SMS * (threads > BLOCK_WARPS * 32 ? 1 : blocks) / (p.segments ? p.segments : 1);
   p.parts = (unsigned)(wave < most ? wave : most);
   if (p.parts < 1) p.parts = 1;
   return p;
@@ -487,40 +509,47 @@ Parts parts_of(int64_t batch, int64_t tokens, int per_sample, int threads, long 
 
 // More than the default limit of shared memory, with every call that needs it (a handle serves any device), and always as much as the longest
 // row takes, so that calls of several threads do not lower each other's.
-constexpr int MOST_SMEM = STAGES<float> * ROWS * MAX_DIM * (int)sizeof(float);
+constexpr int MOST_SMEM = STAGES<float> * 2 * MAX_DIM * (int)sizeof(float);
 cudaError_t allow(void (*kernel)(NormParams), size_t smem) {
   return smem <= 40 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST_SMEM);
 }
 
-template <class T, int CH, int PER, bool WARP>
+template <class T, int CH, int PER, bool WARP, int THREADS>
 cudaError_t forward(NormParams& P, int64_t batch, int64_t tokens, int per_sample, cudaStream_t st) {
-  const Block b = block_of(P.pieces, PER);
-  const Parts p = parts_of(batch, tokens, per_sample, b.threads, b.teams);
+  const Block b = block_of(P.pieces, PER, P.rows);
+  const Parts p = parts_of(batch, tokens, per_sample, b.threads, FORWARD_BLOCKS, b.teams);
   P.segment = p.rows; P.parts = p.parts; P.team_warps = b.team_warps;
-  const size_t smem = ring_bytes<T, CH, PER, ROWS>(b.threads);
-  const cudaError_t e = allow(norm_forward_kernel<T, CH, PER, WARP>, smem);
-  return e != cudaSuccess ? e : ff_launch(norm_forward_kernel<T, CH, PER, WARP>, dim3(p.segments * p.parts), dim3(b.threads), smem, st, P);
+  const size_t smem = ring_bytes<T, CH, PER, 1>(b.threads);
+  const bool full = P.pieces == PER * 32 * b.team_warps;
+  const auto kernel = full && CH > 1 ? norm_forward_kernel<T, CH, PER, (CH > 1), WARP, THREADS> : norm_forward_kernel<T, CH, PER, false, WARP, THREADS>;
+  const cudaError_t e = allow(kernel, smem);
+  return e != cudaSuccess ? e : ff_launch(kernel, dim3(p.segments * p.parts), dim3(b.threads), smem, st, P);
 }
-template <class T, int CH, int PER, bool WARP>
+template <class T, int CH, int PER, bool WARP, int THREADS>
 cudaError_t backward(NormParams& P, unsigned blocks, cudaStream_t st) {
-  const Block b = block_of(P.pieces, PER);
+  const Block b = block_of(P.pieces, PER, P.rows);
   P.team_warps = b.team_warps;
   const size_t ring = ring_bytes<T, CH, PER, 2>(b.threads), joined = (size_t)b.teams * P.d * sizeof(float), smem = ring > joined ? ring : joined;
-  const cudaError_t e = allow(norm_backward_kernel<T, CH, PER, WARP>, smem);
-  return e != cudaSuccess ? e : ff_launch(norm_backward_kernel<T, CH, PER, WARP>, dim3(blocks), dim3(b.threads), smem, st, P);
+  const bool full = P.pieces == PER * 32 * b.team_warps;
+  const auto kernel = full && CH > 1 ? norm_backward_kernel<T, CH, PER, (CH > 1), WARP, THREADS> : norm_backward_kernel<T, CH, PER, false, WARP, THREADS>;
+  const cudaError_t e = allow(kernel, smem);
+  return e != cudaSuccess ? e : ff_launch(kernel, dim3(blocks), dim3(b.threads), smem, st, P);
 }
-// The team and the pieces of a thread: a warp where it has room for the row, else a block with 16 values a thread (8 in pieces of one
-// value, where more of them have to be on their way and fewer fit).
+// The team and the pieces of a thread: a warp where it has room for the row, with as few pieces a thread as do, else several warps.
 template <class T, int CH, class Run>
 cudaError_t with_team(int pieces, Run run) {
   using std::integral_constant;
   using True = integral_constant<bool, true>;
   using False = integral_constant<bool, false>;
+  using Small = integral_constant<int, BLOCK_WARPS * 32>;
+  using Large = integral_constant<int, CH == 1 ? MAX_THREADS : MAX_DIM / VALUES>;
   constexpr int MOST = CH == 1 ? 8 : VALUES / CH;
-  if (pieces <= 32 * MOST / 2) return run(integral_constant<int, MOST / 2>(), True());
-  if (pieces <= 32 * MOST) return run(integral_constant<int, MOST>(), True());
-  if (pieces <= MAX_THREADS * MOST) return run(integral_constant<int, MOST>(), False());
-  return run(integral_constant<int, VALUES / CH>(), False());
+  if constexpr (MOST >= 4) if (pieces <= 32 * (MOST / 4)) return run(integral_constant<int, MOST / 4>(), True(), Small());
+  if (pieces <= 32 * (MOST / 2)) return run(integral_constant<int, MOST / 2>(), True(), Small());
+  if (pieces <= 32 * MOST) return run(integral_constant<int, MOST>(), True(), Small());
+  if (pieces <= 32 * BLOCK_WARPS * MOST) return run(integral_constant<int, MOST>(), False(), Small());
+  if constexpr (CH == 1 && MOST < 16) if (pieces > MAX_THREADS * MOST) return run(integral_constant<int, 16>(), False(), Large());
+  return run(integral_constant<int, MOST>(), False(), Large());
 }
 template <class Run>
 cudaError_t with_piece(int e, int ch, Run run) {
@@ -531,8 +560,8 @@ cudaError_t with_piece(int e, int ch, Run run) {
 
 // Backward: the same blocks whatever the tensors' alignment, so that the workspace does not depend on it.
 Parts backward_parts(const ff_layer_norm_config_t& c, int64_t batch, int64_t tokens, int per_sample) {
-  const Block b = block_of(c.dim, VALUES);
-  return parts_of(batch, tokens, per_sample, b.threads, b.teams);
+  const Block b = block_of(c.dim, VALUES, batch * tokens);
+  return parts_of(batch, tokens, per_sample, b.threads, BACKWARD_BLOCKS, b.teams);
 }
 
 ff_status_t check_call(ff_layer_norm* h, int64_t batch, int64_t tokens, std::initializer_list<const float*> weights) {
@@ -554,6 +583,7 @@ NormParams common(const ff_layer_norm* h, int64_t batch, int64_t tokens, const f
   P.pieces = P.d / ch;
   P.inv_d = 1.f / (float)P.d;
   P.eps = h->cfg.eps;
+  P.even = 1;                                // (each sample's rows are)
   return P;
 }
 
@@ -595,13 +625,14 @@ extern "C" ff_status_t ff_layer_norm_forward(const ff_layer_norm_t* handle, int6
   const int ch = piece_of(h->cfg.dim, e, bits);
   NormParams P = common(h, batch, tokens, weight, per_sample, ch);
   P.x = view(x, e); P.y = view(y, e);
+  if (!per_sample) P.even = even(&P.x, batch, tokens) & even(&P.y, batch, tokens);
   P.bias = bias;
   cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t err = with_piece(e, ch, [&](auto t, auto piece) {
     using T = decltype(t);
     constexpr int CH = decltype(piece)::value;
-    return with_team<T, CH>(P.pieces, [&](auto per, auto warp) {
-      return forward<T, CH, decltype(per)::value, decltype(warp)::value>(P, batch, tokens, per_sample, st);
+    return with_team<T, CH>(P.pieces, [&](auto per, auto warp, auto threads) {
+      return forward<T, CH, decltype(per)::value, decltype(warp)::value, decltype(threads)::value>(P, batch, tokens, per_sample, st);
     });
   });
   return err == cudaSuccess ? FF_OK : cuda_fail(h, err);
@@ -649,6 +680,7 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
   NormParams P = common(h, batch, tokens, weight, per_sample, ch);
   P.x = view(x, e); P.g = view(dy, e);
   if (dx) P.y = view(dx, e);
+  if (!per_sample) P.even = even(&P.x, batch, tokens) & even(&P.g, batch, tokens) & (!dx || even(&P.y, batch, tokens));
   P.segment = parts.rows;
   P.parts = parts.parts;
   if (parts.parts == 1) {
@@ -663,7 +695,9 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
   cudaError_t err = with_piece(e, ch, [&](auto t, auto piece) {
     using T = decltype(t);
     constexpr int CH = decltype(piece)::value;
-    return with_team<T, CH>(P.pieces, [&](auto per, auto warp) { return backward<T, CH, decltype(per)::value, decltype(warp)::value>(P, blocks, st); });
+    return with_team<T, CH>(P.pieces, [&](auto per, auto warp, auto threads) {
+      return backward<T, CH, decltype(per)::value, decltype(warp)::value, decltype(threads)::value>(P, blocks, st);
+    });
   });
   if (err == cudaSuccess && parts.parts > 1 && (dweight || dbias)) {
     const int columns = (d + 31) / 32;
