@@ -7,14 +7,18 @@
 //
 // A CTA takes items (sample, key head, one or two neighbouring tiles of queries, part of the keys); the two tiles, "streams" A and
 // B, share every tile of keys and values, and while the softmax of one works the tensor core runs the products of the other.
-//   warp 0       TMA producer: the query tiles, tiles of keys and values (two stages each)
-//   warp 1       tcgen05.mma issuer: S_x = Q_x K^T (both from shared memory), O_x += P_x V (P from tensor memory), in the order
-//                PV_A[j], QK_A[j+1], PV_B[j], QK_B[j+1]; owns the tensor memory
+//   warp 0       TMA producer: the query tiles; tiles of 64 keys and of their values, each through a ring of its own
+//   warps 1, 3   tcgen05.mma issuers of A and B: S_x = Q_x K^T (both from shared memory) into one of two places in turns, O_x += P_x V (P from
+//                tensor memory), in the order QK[j+1], PV[j], on through the items.  (One warp for both was the limit: some 32 cycles an
+//                instruction, 150 a commit or wait.)  Warp 1 owns the tensor memory
 //   warp 2       zeros in rows of V whose keys do not count, in tiles that may hold such rows
-//   warps 4..11  softmax: a thread per query row; P goes back to tensor memory as bf16 over the scores; O accumulates in tensor memory
-//                and is rescaled only when a row's maximum grows by more than 2^8.  At the end O / l goes out through
-//                shared memory by TMA.
-// Tensor memory (512 columns): S/P of A, S/P of B, O of A, O of B.  Every wait is bounded; when one runs out the CTA raises
+//   warps 4..11  softmax: a thread per query row; P goes back to tensor memory as bf16 over the scores, while the next tile's scores are
+//                made in the other place.  O accumulates in tensor memory and is rescaled only when a row's maximum
+//                grows by more than 2^8.  At the end O / l goes out through shared memory by TMA.
+// With tiles of 128 keys there is room for one place of scores a stream: the next ones had to wait for the product with the last P, and
+// 64K queries, 24 heads of 128, 512 keys took 578 us; P in shared memory freed that place, but the products then read more from shared memory
+// than it gives (589 us).
+// Tensor memory (512 columns): S/P of A and of B, twice 64 each, O of A, O of B.  Every wait is bounded; when one runs out the CTA raises
 // FF_ERR_TIMEOUT in the handle's status word, takes no more work and returns.
 #include <math.h>
 #include <stdio.h>
@@ -31,7 +35,11 @@ namespace {
 constexpr int TILE = CX_TILE;
 constexpr int TILE_BYTES = TILE * 128 * 2, HALF_BYTES = TILE_BYTES / 2;
 constexpr int THREADS = 128 + 2 * 128;
+constexpr int KEYS = 64;       // of a tile
 constexpr float LAZY_LOG2 = 8.0f;
+#ifndef CX_FMA
+#define CX_FMA 0
+#endif
 
 struct CrossParams {
   CrossDims dm;
@@ -41,14 +49,23 @@ struct CrossParams {
   float *part, *part_lse;      // splits > 1: [part][batch][heads][tokens][d] O / l, and the sums' log2
 };
 
+template <int HD> constexpr int PLACES = HD == 64 ? 4 : 3;              // of the rings
 struct Shared {
-  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t v_raw[2];           // in place of v_full for a tile that has to be cleaned first
-  uint64_t s_full[2], p_half[2], p_full[2], o_full[2], o_empty[2];      // per stream
+  uint64_t q_full[2], q_empty[2];                                       // per stream
+  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];                // per place
+  uint64_t v_raw[4];                                                    // in place of v_full for a tile that has to be cleaned first
+  uint64_t s_full[2][2], p_full[2][2];                                  // per stream and place of its scores
+  uint64_t o_full[2], o_empty[2];                                       // per stream
   uint32_t tmem_base;
   int abort_flag;
 };
 constexpr size_t SMEM = 7 * TILE_BYTES + sizeof(Shared) + 1024;
+// The place of a ring that a tile has, and the parity of its turn there.
+template <int N> struct Place {
+  unsigned at = 0, turn = 0;
+  __device__ __forceinline__ void next() { if (++at == N) { at = 0; turn ^= 1; } }
+  __device__ __forceinline__ void skip(unsigned n) { n += at; at = n % N; turn ^= n / N & 1; }
+};
 
 struct Item { int b, g, part, tile, has_b, keys, j0, j1; };
 __device__ __forceinline__ Item item_of(const CrossParams& P, int it) {
@@ -61,33 +78,78 @@ __device__ __forceinline__ Item item_of(const CrossParams& P, int it) {
   x.b = bg / P.dm.G;
   x.g = bg - x.b * P.dm.G;
   x.keys = cx_keys(P.dm, x.b);
-  const long long nk = (x.keys + TILE - 1) / TILE;
+  const long long nk = (x.keys + KEYS - 1) / KEYS;
   x.j0 = (int)(nk * x.part / P.splits);
   x.j1 = (int)(nk * (x.part + 1) / P.splits);
   return x;
 }
+
+// The tiles of keys of a CTA's items, one after the other.
+struct Steps {
+  const CrossParams& P;
+  int it, j;
+  Item x;
+  bool there;
+  __device__ __forceinline__ Steps(const CrossParams& P_) : P(P_), it((int)blockIdx.x - (int)gridDim.x), there(true) { item(); }
+  __device__ __forceinline__ void item() {                   // (items without keys have none)
+    do {
+      it += gridDim.x;
+      if (it >= P.items) { there = false; return; }
+      x = item_of(P, it);
+    } while (x.j0 == x.j1);
+    j = x.j0;
+  }
+  __device__ __forceinline__ void next() { if (++j == x.j1) item(); }
+  __device__ __forceinline__ bool first() const { return j == x.j0; }
+};
+
+// The same with what the issuers need alone.
+struct Cursor {
+  int it, left, keys;          // item; tiles of it from here on; keys from the tile's first one on
+  bool has_b, first, there;    // is it the item's first tile?
+  __device__ __forceinline__ Cursor(const CrossParams& P) : it((int)blockIdx.x - (int)gridDim.x) { item(P); }
+  __device__ __forceinline__ void item(const CrossParams& P) {
+    do {
+      it += gridDim.x;
+      there = it < P.items;
+      if (!there) return;
+      const Item x = item_of(P, it);
+      left = cx_uniform(x.j1 - x.j0); keys = cx_uniform(x.keys - x.j0 * KEYS); has_b = x.has_b;
+    } while (left == 0);
+    first = true;
+  }
+  __device__ __forceinline__ void next(const CrossParams& P) {
+    keys -= KEYS; first = false;
+    if (--left == 0) item(P);
+  }
+  __device__ __forceinline__ bool last() const { return left == 1; }
+  __device__ __forceinline__ int sixteens() const { return keys >= KEYS ? KEYS / 16 : (keys + 15) / 16; }      // of the tile's keys
+};
 
 template <int HD>
 __global__ void __launch_bounds__(THREADS, 1)
 cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_o, const __grid_constant__ CrossParams P) {
   extern __shared__ uint8_t smem_raw[];
+  constexpr int HALVES = HD / 64, BYTES = TILE * HD * 2, NP = PLACES<HD>, KV_BYTES = KEYS * HD * 2, KV_HALF = KEYS * 128;
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* sQ = smem;                       // streams A and B
-  uint8_t* sK = smem + 2 * TILE_BYTES;      // two stages
-  uint8_t* sV = smem + 4 * TILE_BYTES;      // two stages
-  uint8_t* sO = smem + 6 * TILE_BYTES;      // half a tile for either stream's output
+  uint8_t* sQ = smem;                       // queries of streams A and B
+  uint8_t* sO = sQ + 2 * BYTES;             // outputs of A and B
+  uint8_t* sK = sO + 2 * BYTES;             // NP places
+  uint8_t* sV = sK + NP * KV_BYTES;         // NP places
   Shared& sh = *(Shared*)(smem + 7 * TILE_BYTES);
+  static_assert(4 * BYTES + 2 * NP * KV_BYTES <= 7 * TILE_BYTES, "");
   const CrossDims& D = P.dm;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int HALVES = HD / 64;
 
   if (threadIdx.x == 0) {
-    mbar_init(&sh.q_full, 1); mbar_init(&sh.q_empty, 1);
+    for (int i = 0; i < NP; ++i) {
+      mbar_init(&sh.k_full[i], 1); mbar_init(&sh.k_empty[i], 2);
+      mbar_init(&sh.v_full[i], 1); mbar_init(&sh.v_empty[i], 2); mbar_init(&sh.v_raw[i], 1);
+    }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.k_full[i], 1); mbar_init(&sh.k_empty[i], 1);
-      mbar_init(&sh.v_full[i], 1); mbar_init(&sh.v_empty[i], 1); mbar_init(&sh.v_raw[i], 1);
-      mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_half[i], 128); mbar_init(&sh.p_full[i], 128);
+      mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1);
+      for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[i][k], 1); mbar_init(&sh.p_full[i][k], 128); }
       mbar_init(&sh.o_full[i], 1); mbar_init(&sh.o_empty[i], 128);
     }
     sh.abort_flag = 0;
@@ -108,122 +170,138 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       // ------------------------------------------------------------------ TMA producer
       if (lane == 0) {
         const int q_bytes = D.bn * D.bh * HD * 2;
-        unsigned iter = 0, g = 0;
+        unsigned items[2] = {0, 0}, g = 0;
+        Place<NP> kp, vp;
         bool ok = true;
-        for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
-          const Item x = item_of(P, it);
-          if (x.j0 == x.j1) continue;
-          if (iter >= 1) ok = mbar_wait(&sh.q_empty, (iter - 1) & 1, abort_flag);
-          if (!ok) break;
-          mbar_arrive_expect_tx(&sh.q_full, x.has_b ? 2 * q_bytes : q_bytes);
-          for (int sx = 0; sx <= x.has_b; ++sx) {
-            int h0, n0;
-            cx_place(D, x.g, x.tile + sx, h0, n0);
-            cx_load(sQ + sx * TILE_BYTES, HALF_BYTES, HALVES, &map_q, &sh.q_full, n0, h0 * D.once[0][1], x.b * D.once[0][0]);
-          }
-          ++iter;
-          for (int j = x.j0; j < x.j1; ++j, ++g) {
-            const int st = g & 1;
-            if (g >= 2) ok = mbar_wait(&sh.k_empty[st], ((g >> 1) - 1) & 1, abort_flag);
-            if (!ok) break;
-            mbar_arrive_expect_tx(&sh.k_full[st], TILE * HD * 2);
-            cx_load(sK + st * TILE_BYTES, HALF_BYTES, HALVES, &map_k, &sh.k_full[st], j * TILE, x.g * D.once[1][1], x.b * D.once[1][0]);
-            if (g >= 2) ok = mbar_wait(&sh.v_empty[st], ((g >> 1) - 1) & 1, abort_flag);
-            if (!ok) break;
-            uint64_t* full = cx_unclean(D, x.keys, j) ? &sh.v_raw[st] : &sh.v_full[st];
-            mbar_arrive_expect_tx(full, TILE * HD * 2);
-            cx_load(sV + st * TILE_BYTES, HALF_BYTES, HALVES, &map_v, full, j * TILE, x.g * D.once[2][1], x.b * D.once[2][0]);
-          }
+        // the keys of tile gt, ahead of them the queries of its item where that begins
+        auto load_keys = [&](const Steps& w, unsigned gt) {
+          const Item& x = w.x;
+          if (w.first())
+            for (int sx = 0; sx <= x.has_b && ok; ++sx) {
+              if (items[sx] >= 1) ok = mbar_wait(&sh.q_empty[sx], (items[sx] - 1) & 1, abort_flag);
+              if (!ok) break;
+              ++items[sx];
+              int h0, n0;
+              cx_place(D, x.g, x.tile + sx, h0, n0);
+              mbar_arrive_expect_tx(&sh.q_full[sx], q_bytes);
+              cx_load(sQ + sx * BYTES, HALF_BYTES, HALVES, &map_q, &sh.q_full[sx], n0, h0 * D.once[0][1], x.b * D.once[0][0]);
+            }
+          if (ok && gt >= NP) ok = mbar_wait(&sh.k_empty[kp.at], kp.turn ^ 1, abort_flag);
+          if (!ok) return;
+          mbar_arrive_expect_tx(&sh.k_full[kp.at], KV_BYTES);
+          cx_load(sK + kp.at * KV_BYTES, KV_HALF, HALVES, &map_k, &sh.k_full[kp.at], w.j * KEYS, x.g * D.once[1][1], x.b * D.once[1][0]);
+          kp.next();
+        };
+        Steps ahead(P);
+        // the values of the tile behind it
+        int j = 0, h = 0, b = 0;
+        bool clean = false;
+        auto load_values = [&] {
+          if (g >= NP) ok = mbar_wait(&sh.v_empty[vp.at], vp.turn ^ 1, abort_flag);
+          if (!ok) return;
+          uint64_t* bar = clean ? &sh.v_raw[vp.at] : &sh.v_full[vp.at];
+          mbar_arrive_expect_tx(bar, KV_BYTES);
+          cx_load(sV + vp.at * KV_BYTES, KV_HALF, HALVES, &map_v, bar, j * KEYS, h, b);
+          vp.next();
+        };
+        bool there = ahead.there;
+        if (there) load_keys(ahead, 0);
+        for (; there && ok; ++g) {
+          j = ahead.j; h = ahead.x.g * D.once[2][1]; b = ahead.x.b * D.once[2][0];
+          clean = cx_unclean<KEYS>(D, ahead.x.keys, j);
+          ahead.next();
+          there = ahead.there;
+          // Values first where their place is free, else the next keys, whose place is free sooner.
+          const bool first = g < NP || mbar_try_wait(&sh.v_empty[vp.at], vp.turn ^ 1);
+          if (first) load_values();
+          if (ok && there) load_keys(ahead, g + 1);
+          if (ok && !first) load_values();
         }
       }
-    } else if (warp == 1) {
-      // ------------------------------------------------------------------ MMA issuer
-      const uint32_t idesc_qk = idesc_bf16_f32(TILE, TILE, false, false);
+    } else if (warp == 1 || warp == 3) {
+      // ------------------------------------------------------------------ MMA issuers, one for either stream
+      const int sx = warp >> 1;
+      const uint32_t idesc_qk = idesc_bf16_f32(TILE, 0, false, false);
       const uint32_t idesc_pv = idesc_bf16_f32(TILE, HD, false, true);
-      unsigned iter = 0, g = 0;
-      unsigned cp[2] = {0, 0};          // P phases consumed per stream
-      unsigned ce[2] = {0, 0};          // items seen per stream (for the hand-back of O)
+      unsigned asked = 0, done = 0;           // steps whose scores have been asked for, whose P has been consumed
+      unsigned begun = 0, ended = 0;          // items whose scores have begun, whose outputs are complete
       bool ok = true;
-      const uint64_t q_desc = smem_desc_sw128(smem_u32(sQ), 16, 1024), k_desc = smem_desc_sw128(smem_u32(sK), 16, 1024);
-      const uint64_t v_desc = smem_desc_sw128(smem_u32(sV), HALF_BYTES, 1024);
-      auto issue_qk = [&](int sx, unsigned gt, bool last, bool release_q) {
-        const int st = gt & 1;
-        const uint64_t qd = q_desc + (uint64_t)(sx * (TILE_BYTES >> 4)), kd = k_desc + (uint64_t)(st * (TILE_BYTES >> 4));
+      const uint64_t q_desc = smem_desc_sw128(smem_u32(sQ + sx * BYTES), 16, 1024), k_desc = smem_desc_sw128(smem_u32(sK), 16, 1024);
+      const uint64_t v_desc = smem_desc_sw128(smem_u32(sV), KV_HALF, 1024);
+      const uint32_t s_tm = tm + sx * 128, o_tm = s_tm + 256;
+      Place<NP> kp, vp;
+      auto mine = [&](const Cursor& w) { return sx == 0 || w.has_b; };
+      // the scores of a tile (their place has been read: the P in it by the product two tiles before, issued by then)
+      auto scores = [&](const Cursor& w) -> bool {
+        if (!mbar_wait_warp(&sh.k_full[kp.at], kp.turn, abort_flag)) return false;
+        if (mine(w)) {
+          if (w.first && !mbar_wait_warp(&sh.q_full[sx], begun++ & 1, abort_flag)) return false;
+          tc_fence_after();
+          const uint32_t idesc = idesc_qk | (uint32_t)(w.sixteens() * 2) << 17;              // (N in eights)
+          const uint64_t kd = k_desc + (uint64_t)(kp.at * (KV_BYTES >> 4));
+          const int place = asked++ & 1;
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint64_t off = (uint64_t)(((k >> 2) * HALF_BYTES + (k & 3) * 32) >> 4);
-          umma_ss(tm + sx * 128, qd + off, kd + off, idesc_qk, k > 0 ? 1u : 0u);
+          for (int k = 0; k < HALVES; ++k)
+            umma_ss4(s_tm + place * 64, q_desc + (uint64_t)(k * (HALF_BYTES >> 4)), kd + (uint64_t)(k * (KV_HALF >> 4)), idesc, k > 0 ? 1u : 0u);
+          umma_commit(&sh.s_full[sx][place]);
+          if (w.last()) umma_commit(&sh.q_empty[sx]);
+          umma_commit(&sh.k_empty[kp.at]);
+        } else if (lane == 0) {
+          mbar_arrive(&sh.k_empty[kp.at]);
         }
-        umma_commit(&sh.s_full[sx]);
-        if (last) umma_commit(&sh.k_empty[st]);
-        if (release_q) umma_commit(&sh.q_empty);
-      };
-      auto issue_pv = [&](int sx, unsigned gt, bool first, bool last, bool last_of_item) -> bool {
-        const int st = gt & 1;
-        if (!mbar_wait_warp(&sh.p_half[sx], cp[sx] & 1, abort_flag)) return false;
-        if (first && ce[sx] >= 1 && !mbar_wait_warp(&sh.o_empty[sx], (ce[sx] - 1) & 1, abort_flag)) return false;
-        tc_fence_after();
-        const uint64_t vd = v_desc + (uint64_t)(st * (TILE_BYTES >> 4));
-        const uint32_t p_tm = tm + sx * 128, d_tm = p_tm + 256;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          if (k == 4) {
-            if (!mbar_wait_warp(&sh.p_full[sx], cp[sx] & 1, abort_flag)) return false;
-            ++cp[sx];
-            tc_fence_after();
-          }
-          umma_ts(d_tm, p_tm + k * 8, vd + (uint64_t)(k * (2048 >> 4)), idesc_pv, k == 0 && first ? 0u : 1u);
-        }
-        if (last_of_item) umma_commit(&sh.o_full[sx]);
-        if (last) umma_commit(&sh.v_empty[st]);
+        kp.next();
         return true;
       };
-      for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
-        const Item x = item_of(P, it);
-        if (x.j0 == x.j1) continue;
-        ok = mbar_wait_warp(&sh.q_full, iter & 1, abort_flag) && mbar_wait_warp(&sh.k_full[g & 1], (g >> 1) & 1, abort_flag);
-        if (!ok) break;
-        ++iter;
-        tc_fence_after();
-        const int nk = x.j1 - x.j0;
-        issue_qk(0, g, !x.has_b, nk == 1 && !x.has_b);
-        if (x.has_b) issue_qk(1, g, true, nk == 1);
-        for (int i = 0; i < nk && ok; ++i) {
-          const unsigned gt = g + i;
-          const bool more = i + 1 < nk;
-          ok = mbar_wait_warp(&sh.v_full[gt & 1], (gt >> 1) & 1, abort_flag);
-          for (int sx = 0; sx <= x.has_b && ok; ++sx) {
-            const bool last = sx == x.has_b;
-            ok = issue_pv(sx, gt, i == 0, last, !more);
-            if (!ok || !more) continue;
-            if (sx == 0) {
-              ok = mbar_wait_warp(&sh.k_full[(gt + 1) & 1], ((gt + 1) >> 1) & 1, abort_flag);
-              if (!ok) break;
-              tc_fence_after();
-            }
-            issue_qk(sx, gt + 1, last, last && i + 2 == nk);
+      auto product = [&](const Cursor& w) -> bool {
+        if (!mbar_wait_warp(&sh.v_full[vp.at], vp.turn, abort_flag)) return false;
+        if (mine(w)) {
+          const int place = done & 1, steps = w.sixteens();
+          if (!mbar_wait_warp(&sh.p_full[sx][place], done >> 1 & 1, abort_flag)) return false;
+          if (w.first && ended >= 1 && !mbar_wait_warp(&sh.o_empty[sx], (ended - 1) & 1, abort_flag)) return false;
+          tc_fence_after();
+          const uint64_t vd = v_desc + (uint64_t)(vp.at * (KV_BYTES >> 4));
+          const uint32_t p_tm = s_tm + place * 64, on = w.first ? 0u : 1u;
+          if (steps == KEYS / 16) {
+            umma_ts4(o_tm, p_tm, vd, idesc_pv, on);
+          } else {
+            for (int k = 0; k < steps; ++k) umma_ts(o_tm, p_tm + k * 8, vd + (uint64_t)(k * (2048 >> 4)), idesc_pv, k == 0 ? on : 1u);
           }
+          ++done;
+          if (w.last()) { umma_commit(&sh.o_full[sx]); ++ended; }
+          umma_commit(&sh.v_empty[vp.at]);
+        } else if (lane == 0) {
+          mbar_arrive(&sh.v_empty[vp.at]);
         }
-        g += nk;
-        ce[0] += 1;
-        if (x.has_b) ce[1] += 1;
+        vp.next();
+        return true;
+      };
+      Cursor now(P);
+      if (now.there) ok = scores(now);
+      while (now.there && ok) {
+        Cursor ahead = now;
+        ahead.next(P);
+        // The next tile's scores first, unless they are of an item whose queries are still on their way.
+        bool early = ahead.there;
+        if (early && ahead.first && mine(ahead)) early = __all_sync(0xffffffffu, mbar_try_wait(&sh.q_full[sx], begun & 1));
+        if (early) ok = scores(ahead);
+        if (ok) ok = product(now);
+        if (ok && ahead.there && !early) ok = scores(ahead);
+        now = ahead;
       }
     } else if (warp == 2) {
       // ------------------------------------------------------------------ rows of V that do not count
-      unsigned g = 0, raw[2] = {0, 0};                      // tiles; those cleaned, per stage
+      unsigned turns = 0;                                   // whether each place has been cleaned an odd number of times
+      Place<NP> vp;
       bool ok = true;
-      for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
-        const Item x = item_of(P, it);
-        for (int j = x.j0; j < x.j1 && ok; ++j, ++g) {
-          if (!cx_unclean(D, x.keys, j)) continue;
-          const int st = g & 1;
-          const CxValid valid = cx_valid(D, x.b, x.keys, j, lane);
-          ok = mbar_wait_warp(&sh.v_raw[st], raw[st]++ & 1, abort_flag);
-          if (!ok) break;
-          cx_clean(sV + st * TILE_BYTES, HALF_BYTES, HALVES, valid, lane);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.v_full[st]);
-        }
+      for (Steps w(P); w.there && ok; w.next(), vp.next()) {
+        if (!cx_unclean<KEYS>(D, w.x.keys, w.j)) continue;
+        const CxValid64 valid = cx_valid64(D, w.x.b, w.x.keys, w.j * KEYS, lane);
+        ok = mbar_wait_warp(&sh.v_raw[vp.at], turns >> vp.at & 1, abort_flag);
+        if (!ok) break;
+        turns ^= 1u << vp.at;
+        cx_clean(sV + vp.at * KV_BYTES, KV_HALF, HALVES, valid.w, lane);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.v_full[vp.at]);
       }
     }
   } else {
@@ -235,112 +313,123 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_addr = tm + lane_addr + sx * 128;
     const uint32_t o_addr = tm + lane_addr + 256 + sx * 128;
-    uint8_t* stage = sO + sx * HALF_BYTES;
+    uint8_t* stage = sO + sx * BYTES;
     const float sl2 = D.sl2;
-    const int rows = D.bn * D.bh;
-    const int row_h = row / D.bn, row_n = row - row_h * D.bn;
-    unsigned cs = 0;                  // tiles of keys this stream has processed (phases of s_full / p_full)
-    unsigned co = 0;                  // phases of o_full consumed: one per item with keys
+    unsigned n = 0, items = 0;        // tiles this stream has taken, items (with keys) it has ended
+    Place<NP> vp;                     // of the tile's values
     bool ok = true, staged = false;
     for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
-      const Item x = item_of(P, it);
-      if (sx == 1 && !x.has_b) continue;
-      int h0, n0;
-      cx_place(D, x.g, x.tile + sx, h0, n0);
-      const bool here = row < rows && n0 + row_n < D.N;
-      const bool work = __any_sync(0xffffffffu, here);      // (rows that a tile does not have take no time)
+      int b, keys, from;
+      bool work;                                            // (rows that a tile does not have take no time)
+      {
+        const Item x = item_of(P, it);
+        if (sx == 1 && !x.has_b) {
+          vp.skip(x.j1 - x.j0);
+          continue;
+        }
+        int h0, n0;
+        cx_place(D, x.g, x.tile + sx, h0, n0);
+        work = __any_sync(0xffffffffu, row / D.bn < D.bh && n0 + row % D.bn < D.N);
+        b = x.b; from = x.j0 * KEYS; keys = x.keys < x.j1 * KEYS ? x.keys : x.j1 * KEYS;       // (of this part)
+      }
+      const bool some = from < keys;
       float m_ref = -INFINITY, mb = 0.f, l = 0.f;
       bool counts = false;                                  // has a key counted?
-      for (int j = x.j0; j < x.j1 && ok; ++j) {
-        const bool full = !D.mask && (j + 1) * TILE <= x.keys;
-        CxValid valid = {};
-        if (!full) valid = cx_valid(D, x.b, x.keys, j, lane);
-        ok = mbar_wait_warp(&sh.s_full[sx], cs & 1, abort_flag);
+      for (int first = from; first < keys && ok; first += KEYS, ++n, vp.next()) {
+        const bool full = !D.mask && first + KEYS <= keys;
+        CxValid64 valid = {};
+        if (!full) valid = cx_valid64(D, b, keys, first, lane);
+        const uint32_t at = s_addr + (n & 1) * 64;
+        ok = mbar_wait_warp(&sh.s_full[sx][n & 1], n >> 1 & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
         if (work) {
-          uint32_t r[4][32];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, r[c]);
+          uint32_t r[2][32];
+          // scores into registers, those of keys that do not count as -infinity; their maximum
+          tmem_ld32(at, r[0]);
+          tmem_ld32(at + 32, r[1]);
           tmem_wait_ld();
           if (!full) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
               for (int i = 0; i < 32; ++i)
-                if (!(valid.w[i & 3] >> (c * 8 + (i >> 2)) & 1)) r[c][i] = 0xff800000u;
+                if (!(valid.w[i & 1] >> (c * 16 + (i >> 1)) & 1)) r[c][i] = 0xff800000u;
           }
-          counts |= full || (valid.w[0] | valid.w[1] | valid.w[2] | valid.w[3]);
+          counts |= full || (valid.w[0] | valid.w[1]);
           float t4[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) t4[c] = fmaxf(__uint_as_float(r[c][0]), __uint_as_float(r[c][1]));
+          for (int c = 0; c < 4; ++c) t4[c] = fmaxf(__uint_as_float(r[c >> 1][(c & 1) * 16]), __uint_as_float(r[c >> 1][(c & 1) * 16 + 1]));
 #pragma unroll
-          for (int i = 2; i < 32; i += 2)
+          for (int i = 2; i < 16; i += 2)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) t4[c] = max3f(t4[c], __uint_as_float(r[c][i]), __uint_as_float(r[c][i + 1]));
+            for (int c = 0; c < 4; ++c) t4[c] = max3f(t4[c], __uint_as_float(r[c >> 1][(c & 1) * 16 + i]), __uint_as_float(r[c >> 1][(c & 1) * 16 + i + 1]));
           const float m_new = fmaxf(m_ref, fmaxf(max3f(t4[0], t4[1], t4[2]), t4[3]));
           const bool need = (m_new - m_ref) * sl2 > LAZY_LOG2;          // (no: NaN, where no key has counted yet)
-          // The previous PV of this stream has completed: the scores of this tile, which s_full announces, were issued
-          // behind it by the same warp.  So O may be rescaled in place.
-          if (j > x.j0 && __any_sync(0xffffffffu, need)) {
-            const float alpha = need ? ex2((m_ref - m_new) * sl2) : 1.f;
+          if (__any_sync(0xffffffffu, need)) {
+            if (first > from) {
+              // O is rescaled in place, behind the product of the tile before, which frees that tile's values (once they have arrived: till
+              // then the barrier may be two turns away, which looks the same).
+              const unsigned place = vp.at == 0 ? NP - 1 : vp.at - 1, turn = vp.turn ^ (vp.at == 0);
+              if (!mbar_wait_warp(&sh.v_full[place], turn, abort_flag) || !mbar_wait_warp(&sh.v_empty[place], turn, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+              const float alpha = need ? ex2((m_ref - m_new) * sl2) : 1.f;
 #pragma unroll
-            for (int c = 0; c < HD / 16; ++c) {
-              uint32_t v[16];
-              tmem_ld16(o_addr + c * 16, v);
-              tmem_wait_ld();
+              for (int c = 0; c < HD / 16; ++c) {
+                uint32_t v[16];
+                tmem_ld16(o_addr + c * 16, v);
+                tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
-              tmem_st16(o_addr + c * 16, v);
+                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                tmem_st16(o_addr + c * 16, v);
+              }
+              l *= alpha;
             }
-            tmem_wait_st();
-            l *= alpha;
+            if (need) { m_ref = m_new; mb = m_new * sl2; }
           }
-          if (need) { m_ref = m_new; mb = m_new * sl2; }
           // P = 2^(s scale log2(e) - m) as bf16 over the scores; the row's sum is of the unrounded ones
-          float2 sum2 = make_float2(0.f, 0.f);
+          float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
           const float2 sl22 = make_float2(sl2, sl2), nmb2 = make_float2(-mb, -mb);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             uint32_t pk[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const float2 arg = __ffma2_rn(make_float2(__uint_as_float(r[c][2 * i]), __uint_as_float(r[c][2 * i + 1])), sl22, nmb2);
-              const float2 pp = make_float2(ex2(arg.x), ex2(arg.y));
-              sum2 = __fadd2_rn(sum2, pp);
-              const __nv_bfloat162 v = __floats2bfloat162_rn(pp.x, pp.y);
-              pk[i] = *(const uint32_t*)&v;
+              const float2 pp = i % 16 < CX_FMA ? cx_exp2_fma(arg) : make_float2(ex2(arg.x), ex2(arg.y));
+              sum2[i & 1] = __fadd2_rn(sum2[i & 1], pp);
+              pk[i] = bf16_pair(__float_as_uint(pp.x), __float_as_uint(pp.y));
             }
-            tmem_st16(s_addr + c * 16, pk);
-            if (c & 1) {                                    // 64 keys are there
-              tmem_wait_st();
-              tc_fence_before();
-              mbar_arrive(c == 1 ? &sh.p_half[sx] : &sh.p_full[sx]);
-            }
+            tmem_st16(at + c * 16, pk);
           }
-          l += sum2.x + sum2.y;
-        } else {
-          tc_fence_before();
-          mbar_arrive(&sh.p_half[sx]);
-          mbar_arrive(&sh.p_full[sx]);
+          l += (sum2[0].x + sum2[1].x) + (sum2[0].y + sum2[1].y);
+          tmem_wait_st();
         }
-        ++cs;
+        tc_fence_before();
+        mbar_arrive(&sh.p_full[sx][n & 1]);
       }
       if (!ok) break;
-      if (x.j0 < x.j1) {
-        ok = mbar_wait_warp(&sh.o_full[sx], co & 1, abort_flag);
-        ++co;
+      if (some) {
+        ok = mbar_wait_warp(&sh.o_full[sx], items++ & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
       }
+      // (worked out again: kept through the loop it would take registers from the scores)
+      int again = it, h0, n0;
+      asm volatile("" : "+r"(again));
+      const Item x = item_of(P, again);
+      cx_place(D, x.g, x.tile + sx, h0, n0);
+      const int row_h = row / D.bn, row_n = row - row_h * D.bn;
+      const bool here = row_h < D.bh && n0 + row_n < D.N;
       const float inv = 1.f / l;
       const long long at = ((long long)x.b * D.H + h0 + row_h) * D.N + n0 + row_n;
       const float lse2 = counts ? mb + log2f(l) : -INFINITY;
       if (P.splits > 1) {
         const long long pat = (long long)x.part * D.B * D.H * D.N + at;
         if (here) P.part_lse[pat] = lse2;
-        if (x.j0 < x.j1) {
+        if (some && work) {
           float* to = P.part + pat * D.d;
+#pragma unroll 1
           for (int c = 0; c < HD / 32; ++c) {
             uint32_t r[32];
             tmem_ld32(o_addr + c * 32, r);
@@ -356,35 +445,33 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
       } else {
         if (P.lse && here) P.lse[at] = lse2 * 0.69314718055994531f;
-#pragma unroll 1
-        for (int half = 0; half < HALVES; ++half) {
-          if (staged) {                                     // the store before has read the stage
-            if (row == 0) bulk_wait_read0();
-            bar_sync(1 + sx, 128);
-          }
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            uint32_t r[32];
-            if (x.j0 < x.j1) {
-              tmem_ld32(o_addr + half * 64 + c * 32, r);
-              tmem_wait_ld();
-            }
-            if (!counts) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) r[i] = 0;
-            }
-            cx_stage(stage, row, c, r, counts ? inv : 1.f);
-          }
-          fence_proxy_async();
+        if (staged) {                                       // the item before has left the stage
+          if (row == 0) bulk_wait_read0();
           bar_sync(1 + sx, 128);
-          if (row == 0) {
-            tma_store_4d(stage, &map_o, half * 64, n0, h0, x.b);
-            bulk_commit();
-          }
-          staged = true;
         }
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t r[32];
+          if (some) {
+            tmem_ld32(o_addr + c * 32, r);
+            tmem_wait_ld();
+          }
+          if (!counts) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = 0;
+          }
+          cx_stage(stage + (c / 2) * HALF_BYTES, row, c & 1, r, counts ? inv : 1.f);
+        }
+        fence_proxy_async();
+        bar_sync(1 + sx, 128);
+        if (row == 0) {
+          tma_store_4d(stage, &map_o, 0, n0, h0, x.b);
+          if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_o, 64, n0, h0, x.b);
+          bulk_commit();
+        }
+        staged = true;
       }
-      if (x.j0 < x.j1) {
+      if (some) {
         tc_fence_before();
         mbar_arrive(&sh.o_empty[sx]);
       }
@@ -475,7 +562,7 @@ struct Forward { int pair, pairs, splits; };
 Forward forward_of(const CrossDims& D) {
   Forward best = {1, D.tiles, 1};
   double least = 1e30;
-  const long long nk = (D.K + TILE - 1) / TILE;
+  const long long nk = (D.K + KEYS - 1) / KEYS;
   for (int pair = 1; pair <= 2; ++pair) {
     const int pairs = (D.tiles + pair - 1) / pair;
     for (int splits = 1; splits <= 64 && splits <= (nk > 1 ? nk : 1); ++splits) {
@@ -584,8 +671,8 @@ extern "C" ff_status_t ff_cross_attention_create(const ff_cross_attention_config
   if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "out of host memory");
   h->cfg = *cfg;
   cudaError_t e = cudaGetDevice(&h->device);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(cross_forward_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(cross_forward_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM);
+  for (const void* kernel : {(const void*)cross_forward_kernel<128>, (const void*)cross_forward_kernel<64>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM);
   if (e == cudaSuccess) e = cx_backward_init();
   if (e == cudaSuccess) e = cudaMalloc((void**)&h->status, 256);
   // (cleared before the handle is out, on a stream of its own: the default stream may be busy, and others do not wait for it)
@@ -655,12 +742,12 @@ extern "C" ff_status_t ff_cross_attention_forward(ff_cross_attention_t* h, int64
   P.part_lse = (float*)((char*)ws + part_bytes(P.dm, f.splits));
   CUtensorMap mq, mk, mv, mo;
   const int64_t kn = keys > 0 ? keys : 1;
-  if (!cx_map(&mq, q, batch, queries, c.head_dim, P.dm.bn, P.dm.bh) || !cx_map(&mk, k, keys > 0 ? batch : 1, kn, c.head_dim, TILE, 1) ||
-      !cx_map(&mv, v, keys > 0 ? batch : 1, kn, c.head_dim, TILE, 1) || !cx_map(&mo, out, batch, queries, c.head_dim, P.dm.bn, P.dm.bh))
+  if (!cx_map(&mq, q, batch, queries, c.head_dim, P.dm.bn, P.dm.bh) || !cx_map(&mk, k, keys > 0 ? batch : 1, kn, c.head_dim, KEYS, 1) ||
+      !cx_map(&mv, v, keys > 0 ? batch : 1, kn, c.head_dim, KEYS, 1) || !cx_map(&mo, out, batch, queries, c.head_dim, P.dm.bn, P.dm.bh))
     return fail(h, FF_ERR_CUDA, "could not encode the tensor maps");
   const dim3 grid((unsigned)(P.items < FF_B200_SMS ? P.items : FF_B200_SMS));
-  CX_CUDA(h, c.head_dim > 64 ? ff_launch(cross_forward_kernel<128>, grid, dim3(THREADS), SMEM, st, mq, mk, mv, mo, P)
-                             : ff_launch(cross_forward_kernel<64>, grid, dim3(THREADS), SMEM, st, mq, mk, mv, mo, P));
+  const auto kernel = c.head_dim > 64 ? cross_forward_kernel<128> : cross_forward_kernel<64>;
+  CX_CUDA(h, ff_launch(kernel, grid, dim3(THREADS), SMEM, st, mq, mk, mv, mo, P));
   if (f.splits > 1) {
     JoinParams J{P.part, P.part_lse, lse, (long long)batch * c.heads * queries, f.splits, c.heads, (int)queries, c.head_dim, (char*)out->data,
                  (long long)out->stride_batch * 2, (long long)out->stride_head * 2, (long long)out->stride_token * 2};

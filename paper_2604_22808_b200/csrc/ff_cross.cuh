@@ -36,9 +36,13 @@ __device__ __forceinline__ int cx_keys(const CrossDims& D, int b) {
   const int n = __ldg(D.lengths + b);
   return n < 0 ? 0 : n < D.K ? n : D.K;
 }
+// A value that all lanes have, from the first of them: so the compiler knows that they do, and keeps what follows from it (loops over tiles,
+// operands of the tensor core's instructions) in registers of the warp.  Otherwise each operand is moved there for each instruction.
+__device__ __forceinline__ int cx_uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 // Does tile j of a sample with `keys` keys hold rows that do not count, yet have been loaded?
+template <int KEYS>
 __device__ __forceinline__ bool cx_unclean(const CrossDims& D, int keys, int j) {
-  return D.mask || (keys < D.K && (j + 1) * CX_TILE > keys);
+  return D.mask || (keys < D.K && (j + 1) * KEYS > keys);
 }
 // The keys of a tile that count, as the bits of four words: bit l of word k is key 4 l + k.  All 32 lanes.
 struct CxValid { uint32_t w[4]; };
@@ -50,6 +54,33 @@ __device__ __forceinline__ CxValid cx_valid(const CrossDims& D, int b, int keys,
     const int key = j * CX_TILE + 4 * lane + k;
     const bool on = key < keys && (!D.mask || __ldg(D.mask + at + key) != 0);
     v.w[k] = __ballot_sync(0xffffffffu, on);
+  }
+  return v;
+}
+// 2^x of two values on the FMA units, x up to 120: 2^n p(f) with n the nearest whole number and |f| <= 1/2, p the polynomial of degree 5 of the
+// least relative error (7.5e-8; found with Remez's exchange), x below -126 taken as that, NaN kept.
+__device__ __forceinline__ float2 cx_exp2_fma(float2 x) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
+  const float2 big = make_float2(12582912.f, 12582912.f);     // 1.5 x 2^23: adding it rounds to whole numbers, kept in the low bits
+  const float2 t = __fadd2_rn(x, big);
+  const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
+  const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
+  float2 p = __ffma2_rn(f, make_float2(1.327647263e-3f, 1.327647263e-3f), make_float2(9.675541343e-3f, 9.675541343e-3f));
+  p = __ffma2_rn(p, f, make_float2(5.550713272e-2f, 5.550713272e-2f));
+  p = __ffma2_rn(p, f, make_float2(2.402211972e-1f, 2.402211972e-1f));
+  p = __ffma2_rn(p, f, make_float2(6.931469671e-1f, 6.931469671e-1f));
+  p = __ffma2_rn(p, f, make_float2(1.000000072f, 1.000000072f));
+  return __fmul2_rn(p, make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3f800000u)));
+}
+// Of 64 keys from `first` on, those that count: bit l of word k is key first + 2 l + k.  All 32 lanes.
+struct CxValid64 { uint32_t w[2]; };
+__device__ __forceinline__ CxValid64 cx_valid64(const CrossDims& D, int b, int keys, int first, int lane) {
+  CxValid64 v;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int key = first + 2 * lane + k;
+    v.w[k] = __ballot_sync(0xffffffffu, key < keys && (!D.mask || __ldg(D.mask + (long long)b * D.K + key) != 0));
   }
   return v;
 }
@@ -65,11 +96,13 @@ __device__ __forceinline__ void cx_load(uint8_t* dst, int bytes, int halves, con
   if (halves > 1) sm100::tma_load_4d(dst + bytes, map, bar, 64, n, h, b);
 }
 // Zeros in the rows of a tile in shared memory (rows of 128 bytes, halves `bytes` apart) whose keys do not count: in the product they
-// meet probabilities of zero, and zero times what may stand there need not be zero.  All 32 lanes.
-__device__ __forceinline__ void cx_clean(uint8_t* tile, int bytes, int halves, const CxValid& v, int lane) {
+// meet probabilities of zero, and zero times what may stand there need not be zero.  W words of valid bits: bit l of word k is row
+// W l + k.  All 32 lanes.
+template <int W>
+__device__ __forceinline__ void cx_clean(uint8_t* tile, int bytes, int halves, const uint32_t (&valid)[W], int lane) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    uint32_t gone = ~v.w[k];
+  for (int k = 0; k < W; ++k) {
+    uint32_t gone = ~valid[k];
     while (gone) {
       // four rows at a time, eight lanes of 16 bytes each
       uint32_t rest = gone;
@@ -77,7 +110,7 @@ __device__ __forceinline__ void cx_clean(uint8_t* tile, int bytes, int halves, c
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int l = __ffs(rest) - 1;
-        if (i == (lane >> 3)) row = l < 0 ? -1 : 4 * l + k;
+        if (i == (lane >> 3)) row = l < 0 ? -1 : W * l + k;
         rest &= rest - 1;
       }
       gone = rest;

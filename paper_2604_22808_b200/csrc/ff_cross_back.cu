@@ -134,7 +134,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             const int st = g % 3;
             if (g >= 3) ok = mbar_wait(&sh.k_empty[st], (g / 3 - 1) & 1, abort_flag);
             if (!ok) break;
-            uint64_t* full = cx_unclean(D, x.keys, j) ? &sh.k_raw[st] : &sh.k_full[st];
+            uint64_t* full = cx_unclean<TILE>(D, x.keys, j) ? &sh.k_raw[st] : &sh.k_full[st];
             mbar_arrive_expect_tx(full, TILE * HD * 2);
             cx_load(sK + st * TILE_BYTES, HALF_BYTES, HALVES, &map_k, full, j * TILE, x.g * D.once[1][1], x.b * D.once[1][0]);
             if (!out_asked) {                                // (behind the first keys: the stage may still be on its way out)
@@ -216,13 +216,13 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
         const QueryItem x = query_item(P, it);
         for (int j = x.j0; j < x.j1 && ok; ++j, ++g) {
-          if (!cx_unclean(D, x.keys, j)) continue;
+          if (!cx_unclean<TILE>(D, x.keys, j)) continue;
           const int st = g % 3;
           const CxValid valid = cx_valid(D, x.b, x.keys, j, lane);
           const unsigned n = st == 0 ? raw[0]++ : st == 1 ? raw[1]++ : raw[2]++;
           ok = mbar_wait_warp(&sh.k_raw[st], n & 1, abort_flag);
           if (!ok) break;
-          cx_clean(sK + st * TILE_BYTES, HALF_BYTES, HALVES, valid, lane);
+          cx_clean(sK + st * TILE_BYTES, HALF_BYTES, HALVES, valid.w, lane);
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.k_full[st]);
         }
