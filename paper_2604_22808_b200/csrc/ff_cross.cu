@@ -9,8 +9,9 @@
 // B, share every tile of keys and values, and while the softmax of one works the tensor core runs the products of the other.
 //   warp 0       TMA producer: the query tiles; tiles of 64 keys and of their values, each through a ring of its own
 //   warps 1, 3   tcgen05.mma issuers of A and B: S_x = Q_x K^T (both from shared memory) into one of two places in turns, O_x += P_x V (P from
-//                tensor memory), in the order QK[j+1], PV[j], on through the items.  (One warp for both was the limit: some 32 cycles an
-//                instruction, 150 a commit or wait.)  Warp 1 owns the tensor memory
+//                tensor memory), in the order QK[j+1], PV[j], on through the items.  (One warp for both was the limit, and so were more commits
+//                than the one for the scores: some 32 cycles an instruction, 150 a commit or wait.  What else waits for a product
+//                within an item is told by the softmax warps, when they see scores that were asked for behind it.)  Warp 1 owns the tensor memory
 //   warp 2       zeros in rows of V whose keys do not count, in tiles that may hold such rows
 //   warps 4..11  softmax: a thread per query row; P goes back to tensor memory as bf16 over the scores, while the next tile's scores are
 //                made in the other place.  O accumulates in tensor memory and is rescaled only when a row's maximum
@@ -55,7 +56,7 @@ struct Shared {
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];                // per place
   uint64_t v_raw[4];                                                    // in place of v_full for a tile that has to be cleaned first
   uint64_t s_full[2][2], p_full[2][2];                                  // per stream and place of its scores
-  uint64_t o_full[2], o_empty[2];                                       // per stream
+  uint64_t pv_done[2], o_full[2], o_empty[2];                           // per stream
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -64,6 +65,7 @@ constexpr size_t SMEM = 7 * TILE_BYTES + sizeof(Shared) + 1024;
 template <int N> struct Place {
   unsigned at = 0, turn = 0;
   __device__ __forceinline__ void next() { if (++at == N) { at = 0; turn ^= 1; } }
+  __device__ __forceinline__ unsigned back(unsigned n) const { return at >= n ? at - n : at + N - n; }
   __device__ __forceinline__ void skip(unsigned n) { n += at; at = n % N; turn ^= n / N & 1; }
 };
 
@@ -150,7 +152,7 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1);
       for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[i][k], 1); mbar_init(&sh.p_full[i][k], 128); }
-      mbar_init(&sh.o_full[i], 1); mbar_init(&sh.o_empty[i], 128);
+      mbar_init(&sh.pv_done[i], 1); mbar_init(&sh.o_full[i], 1); mbar_init(&sh.o_empty[i], 128);
     }
     sh.abort_flag = 0;
     fence_mbar_init();
@@ -245,7 +247,6 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             umma_ss4(s_tm + place * 64, q_desc + (uint64_t)(k * (HALF_BYTES >> 4)), kd + (uint64_t)(k * (KV_HALF >> 4)), idesc, k > 0 ? 1u : 0u);
           umma_commit(&sh.s_full[sx][place]);
           if (w.last()) umma_commit(&sh.q_empty[sx]);
-          umma_commit(&sh.k_empty[kp.at]);
         } else if (lane == 0) {
           mbar_arrive(&sh.k_empty[kp.at]);
         }
@@ -267,8 +268,8 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             for (int k = 0; k < steps; ++k) umma_ts(o_tm, p_tm + k * 8, vd + (uint64_t)(k * (2048 >> 4)), idesc_pv, k == 0 ? on : 1u);
           }
           ++done;
-          if (w.last()) { umma_commit(&sh.o_full[sx]); ++ended; }
-          umma_commit(&sh.v_empty[vp.at]);
+          if (w.left == 2) umma_commit(&sh.pv_done[sx]);
+          if (w.last()) { umma_commit(&sh.o_full[sx]); umma_commit(&sh.v_empty[vp.at]); ++ended; }
         } else if (lane == 0) {
           mbar_arrive(&sh.v_empty[vp.at]);
         }
@@ -315,8 +316,8 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const uint32_t o_addr = tm + lane_addr + 256 + sx * 128;
     uint8_t* stage = sO + sx * BYTES;
     const float sl2 = D.sl2;
-    unsigned n = 0, items = 0;        // tiles this stream has taken, items (with keys) it has ended
-    Place<NP> vp;                     // of the tile's values
+    unsigned n = 0, items = 0, ends = 0;      // tiles this stream has taken, items (with keys; with more than one tile of them) it has ended
+    Place<NP> vp;                     // of the tile's keys and values
     bool ok = true, staged = false;
     for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
       int b, keys, from;
@@ -343,6 +344,10 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         ok = mbar_wait_warp(&sh.s_full[sx][n & 1], n >> 1 & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
+        if (row == 0) {                                     // what has been read by now: the keys, and the values two tiles back
+          mbar_arrive(&sh.k_empty[vp.at]);
+          if (first >= from + 2 * KEYS) mbar_arrive(&sh.v_empty[vp.back(2)]);
+        }
         if (work) {
           uint32_t r[2][32];
           // scores into registers, those of keys that do not count as -infinity; their maximum
@@ -368,10 +373,10 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           const bool need = (m_new - m_ref) * sl2 > LAZY_LOG2;          // (no: NaN, where no key has counted yet)
           if (__any_sync(0xffffffffu, need)) {
             if (first > from) {
-              // O is rescaled in place, behind the product of the tile before, which frees that tile's values (once they have arrived: till
-              // then the barrier may be two turns away, which looks the same).
-              const unsigned place = vp.at == 0 ? NP - 1 : vp.at - 1, turn = vp.turn ^ (vp.at == 0);
-              if (!mbar_wait_warp(&sh.v_full[place], turn, abort_flag) || !mbar_wait_warp(&sh.v_empty[place], turn, abort_flag)) { ok = false; break; }
+              // O is rescaled in place, behind the product of the tile before: it is done when the next scores are, which were asked for behind
+              // it, or, at an item's last tile, when the issuer says so.
+              if (!(first + KEYS < keys ? mbar_wait_warp(&sh.s_full[sx][~n & 1], (n + 1) >> 1 & 1, abort_flag)
+                                        : mbar_wait_warp(&sh.pv_done[sx], ends & 1, abort_flag))) { ok = false; break; }
               tc_fence_after();
               const float alpha = need ? ex2((m_ref - m_new) * sl2) : 1.f;
 #pragma unroll
@@ -413,6 +418,10 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         ok = mbar_wait_warp(&sh.o_full[sx], items++ & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
+        if (keys - from > KEYS) {                           // (the last values: the issuer)
+          if (row == 0) mbar_arrive(&sh.v_empty[vp.back(2)]);
+          ++ends;
+        }
       }
       // (worked out again: kept through the loop it would take registers from the scores)
       int again = it, h0, n0;
