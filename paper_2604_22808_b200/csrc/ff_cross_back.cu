@@ -9,10 +9,9 @@
 //
 // dq: a CTA takes a tile of queries (of a part of the keys, where tiles are few).
 //   warp 0       TMA producer: Q, dout, out (into the stage), tiles of K (three stages) and V (one)
-//   warp 1       tcgen05.mma issuer: S = Q K^T into two buffers in turns, dP = dout V^T, dQ += dS K (dS from tensor memory, K as an
-//                MN-major operand), in the order S[j+1], dP[j+1], dQ[j]
+//   warp 1       tcgen05.mma issuer: S = Q K^T into two buffers in turns, dP = dout V^T
 //   warp 2       zeros in rows of K whose keys do not count, in tiles that may hold such rows
-//   warp 3       stores the finished tile from the stage
+//   warp 3       tcgen05.mma issuer: dQ += dS K (dS from tensor memory, K as an MN-major operand)
 //   warps 4..11  a thread per query row, two warpgroups that take the tiles of keys in turns: P, then dS as bf16 over the scores; D at the
 //                item's start, from dout and out in shared memory
 //   tensor memory: S (twice), dP, dQ
@@ -54,7 +53,7 @@ struct KeyParams {
 
 // ---- dq -------------------------------------------------------------------------------------------------------------------
 struct QueryShared {
-  uint64_t q_full, q_empty, o_full, stage_full, stage_free;
+  uint64_t q_full, q_empty, o_full, stage_free;
   uint64_t k_full[3], k_empty[3], k_raw[3], v_full, v_empty;
   uint64_t s_full[2], ds_full[2], dp_full, dp_empty, dq_full, dq_empty;
   uint32_t tmem_base;
@@ -93,7 +92,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 
   if (threadIdx.x == 0) {
     mbar_init(&sh.q_full, 1); mbar_init(&sh.q_empty, 1 + 8); mbar_init(&sh.o_full, 1);
-    mbar_init(&sh.stage_full, 256); mbar_init(&sh.stage_free, 1);
+    mbar_init(&sh.stage_free, 1);
     for (int i = 0; i < 3; ++i) { mbar_init(&sh.k_full[i], 1); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.k_raw[i], 1); }
     mbar_init(&sh.v_full, 1); mbar_init(&sh.v_empty, 1);
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.ds_full[i], 128); }
@@ -155,24 +154,20 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     } else if (warp == 1) {
       // ------------------------------------------------------------------ MMA issuer
       const uint32_t idesc_s = idesc_bf16_f32(TILE, TILE, false, false);
-      const uint32_t idesc_q = idesc_bf16_f32(TILE, HD, false, true);
       const uint64_t q_desc = smem_desc_sw128(smem_u32(sQ), 16, 1024), g_desc = smem_desc_sw128(smem_u32(sG), 16, 1024);
       const uint64_t k_desc = smem_desc_sw128(smem_u32(sK), 16, 1024), v_desc = smem_desc_sw128(smem_u32(sV), 16, 1024);
-      const uint64_t km_desc = smem_desc_sw128(smem_u32(sK), HALF_BYTES, 1024);
       unsigned iter = 0, g = 0;
       bool ok = true;
       auto score = [&](uint32_t d_tm, uint64_t a, uint64_t b) {
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint64_t off = (uint64_t)(((k >> 2) * HALF_BYTES + (k & 3) * 32) >> 4);
-          umma_ss(d_tm, a + off, b + off, idesc_s, k > 0 ? 1u : 0u);
-        }
+        for (int k = 0; k < HALVES; ++k) umma_ss4(d_tm, a + (uint64_t)(k * (HALF_BYTES >> 4)), b + (uint64_t)(k * (HALF_BYTES >> 4)), idesc_s, k > 0 ? 1u : 0u);
       };
-      auto issue_s = [&](unsigned gt) -> bool {              // (the buffer's dS has been read by dQ[gt - 2], issued before)
-        const int st = gt % 3;
-        if (!mbar_wait_warp(&sh.k_full[st], (gt / 3) & 1, abort_flag)) return false;
+      // (the buffer's dS has been read when the keys of two tiles before are free; their place was filled, so that turn has ended)
+      auto issue_s = [&](unsigned gt) -> bool {
+        if (!mbar_wait_warp(&sh.k_full[gt % 3], (gt / 3) & 1, abort_flag)) return false;
+        if (gt >= 2 && !mbar_wait_warp(&sh.k_empty[(gt - 2) % 3], ((gt - 2) / 3) & 1, abort_flag)) return false;
         tc_fence_after();
-        score(tm + (gt & 1) * 128, q_desc, k_desc + (uint64_t)(st * (TILE_BYTES >> 4)));
+        score(tm + (gt & 1) * 128, q_desc, k_desc + (uint64_t)((gt % 3) * (TILE_BYTES >> 4)));
         umma_commit(&sh.s_full[gt & 1]);
         return true;
       };
@@ -188,25 +183,34 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       };
       for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
         const QueryItem x = query_item(P, it);
-        if (x.j0 == x.j1) continue;
-        const int nk = x.j1 - x.j0;
-        ok = mbar_wait_warp(&sh.q_full, iter & 1, abort_flag) && issue_s(g) && issue_dp(g, nk == 1);
-        for (int i = 0; i < nk && ok; ++i) {
-          const unsigned gt = g + i;
-          if (i + 1 < nk) ok = issue_s(gt + 1) && issue_dp(gt + 1, i + 2 == nk);
-          if (!ok) break;
-          ok = mbar_wait_warp(&sh.ds_full[gt & 1], (gt >> 1) & 1, abort_flag);
-          if (ok && i == 0 && iter >= 1) ok = mbar_wait_warp(&sh.dq_empty, (iter - 1) & 1, abort_flag);
+        const int nk = cx_uniform(x.j1 - x.j0);
+        if (nk == 0) continue;
+        ok = mbar_wait_warp(&sh.q_full, iter & 1, abort_flag);
+        for (int i = 0; i < nk && ok; ++i) ok = issue_s(g + i) && issue_dp(g + i, i + 1 == nk);
+        g += nk;
+        ++iter;
+      }
+    } else if (warp == 3) {
+      // ------------------------------------------------------------------ dQ += dS K
+      const uint32_t idesc_q = idesc_bf16_f32(TILE, HD, false, true);
+      const uint64_t km_desc = smem_desc_sw128(smem_u32(sK), HALF_BYTES, 1024);
+      unsigned iter = 0, g = 0;
+      bool ok = true;
+      for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
+        const QueryItem x = query_item(P, it);
+        const int nk = cx_uniform(x.j1 - x.j0);
+        if (nk == 0) continue;
+        if (iter >= 1) ok = mbar_wait_warp(&sh.dq_empty, (iter - 1) & 1, abort_flag);
+        for (int i = 0; i < nk && ok; ++i, ++g) {
+          ok = mbar_wait_warp(&sh.ds_full[g & 1], (g >> 1) & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
-          const uint64_t kd = km_desc + (uint64_t)((gt % 3) * (TILE_BYTES >> 4));
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            umma_ts(tm + 384, tm + (gt & 1) * 128 + k * 8, kd + (uint64_t)(k * (2048 >> 4)), idesc_q, k == 0 && i == 0 ? 0u : 1u);
-          umma_commit(&sh.k_empty[gt % 3]);
-          if (i + 1 == nk) umma_commit(&sh.dq_full);
+          const uint64_t kd = km_desc + (uint64_t)((g % 3) * (TILE_BYTES >> 4));
+          umma_ts4(tm + 384, tm + (g & 1) * 128, kd, idesc_q, i == 0 ? 0u : 1u);
+          umma_ts4(tm + 384, tm + (g & 1) * 128 + 32, kd + (uint64_t)(4 * (2048 >> 4)), idesc_q, 1u);
+          umma_commit(&sh.k_empty[g % 3]);
         }
-        g += nk;
+        if (ok) umma_commit(&sh.dq_full);
         ++iter;
       }
     } else if (warp == 2) {
@@ -227,28 +231,6 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           if (lane == 0) mbar_arrive(&sh.k_full[st]);
         }
       }
-    } else {
-      // ------------------------------------------------------------------ finished tiles
-      if (lane == 0) {
-        unsigned iter = 0;
-        bool ok = true;
-        for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
-          const QueryItem x = query_item(P, it);
-          if (x.j0 == x.j1) continue;
-          ok = mbar_wait(&sh.stage_full, iter++ & 1, abort_flag);
-          if (!ok) break;
-          if (P.splits == 1) {
-            int h0, n0;
-            cx_place(D, x.g, x.tile, h0, n0);
-            tma_store_4d(stage, &map_dq, 0, n0, h0, x.b);
-            if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_dq, 64, n0, h0, x.b);
-            bulk_commit();
-            bulk_wait_read0();
-          }
-          mbar_arrive(&sh.stage_free);
-        }
-        bulk_wait0();
-      }
     }
   } else {
     reg_inc<200>();
@@ -261,7 +243,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     const int rows = D.bn * D.bh;
     const int row_h = row / D.bn, row_n = row - row_h * D.bn;
     unsigned iter = 0, g = 0;
-    bool ok = true;
+    bool ok = true, stored = false;
     for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
       const QueryItem x = query_item(P, it);
       int h0, n0;
@@ -281,6 +263,10 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             }
           }
         continue;
+      }
+      if (stored) {                                          // the item before has left the stage
+        if (wg == 0 && row == 0) { bulk_wait_read0(); mbar_arrive(&sh.stage_free); }
+        stored = false;
       }
       const float nlse2 = here ? -P.lse[at] * LOG2E : -INFINITY;        // (rows that are not there: P = 0)
       // D = dout out of this row
@@ -374,11 +360,18 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                                                          __uint_as_float(r[v * 4 + 2]) * D.scale, __uint_as_float(r[v * 4 + 3]) * D.scale);
         }
       }
-      fence_proxy_async();
-      mbar_arrive(&sh.stage_full);
       tc_fence_before();
       mbar_arrive(&sh.dq_empty);
+      fence_proxy_async();
+      bar_sync(2, 256);
+      if (!part && wg == 0 && row == 0) {
+        tma_store_4d(stage, &map_dq, 0, n0, h0, x.b);
+        if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_dq, 64, n0, h0, x.b);
+        bulk_commit();
+      }
+      stored = true;
     }
+    if (wg == 0 && row == 0) bulk_wait0();
   }
 
   // ------------------------------------------------------------------ teardown
@@ -506,10 +499,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       bool ok = true;
       auto score = [&](uint32_t d_tm, uint64_t a, uint64_t b) {
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint64_t off = (uint64_t)(((k >> 2) * HALF_BYTES + (k & 3) * 32) >> 4);
-          umma_ss(d_tm, a + off, b + off, idesc_s, k > 0 ? 1u : 0u);
-        }
+        for (int k = 0; k < HALVES; ++k) umma_ss4(d_tm, a + (uint64_t)(k * (HALF_BYTES >> 4)), b + (uint64_t)(k * (HALF_BYTES >> 4)), idesc_s, k > 0 ? 1u : 0u);
       };
       auto issue_s = [&](unsigned gt) -> bool {              // (P^T in its place has been read by dV, issued before)
         const int st = gt & 1;
@@ -530,19 +520,17 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       // D += A^T-tile times rows of the stage; either warpgroup's half of A (queries 0 .. 63 and 64 .. 127) lies in its own 64 columns
       auto issue_sum = [&](uint32_t d_tm, uint32_t a_tm, uint64_t b, uint64_t* half, unsigned parity, bool first) -> bool {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          if ((k & 3) == 0) {
-            if (!mbar_wait_warp(&half[k >> 2], parity, abort_flag)) return false;
-            tc_fence_after();
-          }
-          umma_ts(d_tm, a_tm + (k >> 2) * 64 + (k & 3) * 8, b + (uint64_t)(k * (2048 >> 4)), idesc_d, k == 0 && first ? 0u : 1u);
+        for (int h = 0; h < 2; ++h) {
+          if (!mbar_wait_warp(&half[h], parity, abort_flag)) return false;
+          tc_fence_after();
+          umma_ts4(d_tm, a_tm + h * 64, b + (uint64_t)(h * 4 * (2048 >> 4)), idesc_d, h == 0 && first ? 0u : 1u);
         }
         return true;
       };
       for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
         const KeyItem x = key_item(P, it);
-        if (x.t0 == x.t1) continue;
-        const int nt = x.t1 - x.t0;
+        const int nt = cx_uniform(x.t1 - x.t0);
+        if (nt == 0) continue;
         ok = mbar_wait_warp(&sh.kv_full, iter & 1, abort_flag) && issue_s(g) && issue_dp(g);
         if (ok && iter >= 1) ok = mbar_wait_warp(&sh.sum_empty, (iter - 1) & 1, abort_flag);
         for (int i = 0; i < nt && ok; ++i) {
