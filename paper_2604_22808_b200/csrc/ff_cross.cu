@@ -38,9 +38,6 @@ constexpr int TILE_BYTES = TILE * 128 * 2, HALF_BYTES = TILE_BYTES / 2;
 constexpr int THREADS = 128 + 2 * 128;
 constexpr int KEYS = 64;       // of a tile
 constexpr float LAZY_LOG2 = 8.0f;
-#ifndef CX_FMA
-#define CX_FMA 0
-#endif
 
 struct CrossParams {
   CrossDims dm;
@@ -401,7 +398,7 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const float2 arg = __ffma2_rn(make_float2(__uint_as_float(r[c][2 * i]), __uint_as_float(r[c][2 * i + 1])), sl22, nmb2);
-              const float2 pp = i % 16 < CX_FMA ? cx_exp2_fma(arg) : make_float2(ex2(arg.x), ex2(arg.y));
+              const float2 pp = make_float2(ex2(arg.x), ex2(arg.y));
               sum2[i & 1] = __fadd2_rn(sum2[i & 1], pp);
               pk[i] = bf16_pair(__float_as_uint(pp.x), __float_as_uint(pp.y));
             }

@@ -57,22 +57,6 @@ __device__ __forceinline__ CxValid cx_valid(const CrossDims& D, int b, int keys,
   }
   return v;
 }
-// 2^x of two values on the FMA units, x up to 120: 2^n p(f) with n the nearest whole number and |f| <= 1/2, p the polynomial of degree 5 of the
-// least relative error (7.5e-8; found with Remez's exchange), x below -126 taken as that, NaN kept.
-__device__ __forceinline__ float2 cx_exp2_fma(float2 x) {
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
-  const float2 big = make_float2(12582912.f, 12582912.f);     // 1.5 x 2^23: adding it rounds to whole numbers, kept in the low bits
-  const float2 t = __fadd2_rn(x, big);
-  const float2 n = __fadd2_rn(t, make_float2(-12582912.f, -12582912.f));
-  const float2 f = __fadd2_rn(x, make_float2(-n.x, -n.y));
-  float2 p = __ffma2_rn(f, make_float2(1.327647263e-3f, 1.327647263e-3f), make_float2(9.675541343e-3f, 9.675541343e-3f));
-  p = __ffma2_rn(p, f, make_float2(5.550713272e-2f, 5.550713272e-2f));
-  p = __ffma2_rn(p, f, make_float2(2.402211972e-1f, 2.402211972e-1f));
-  p = __ffma2_rn(p, f, make_float2(6.931469671e-1f, 6.931469671e-1f));
-  p = __ffma2_rn(p, f, make_float2(1.000000072f, 1.000000072f));
-  return __fmul2_rn(p, make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3f800000u)));
-}
 // Of 64 keys from `first` on, those that count: bit l of word k is key first + 2 l + k.  All 32 lanes.
 struct CxValid64 { uint32_t w[2]; };
 __device__ __forceinline__ CxValid64 cx_valid64(const CrossDims& D, int b, int keys, int first, int lane) {
@@ -95,29 +79,26 @@ __device__ __forceinline__ void cx_load(uint8_t* dst, int bytes, int halves, con
   sm100::tma_load_4d(dst, map, bar, 0, n, h, b);
   if (halves > 1) sm100::tma_load_4d(dst + bytes, map, bar, 64, n, h, b);
 }
+// The same tile on its way into L2.
+__device__ __forceinline__ void cx_prefetch(int halves, const CUtensorMap* map, int n, int h, int b) {
+  sm100::tma_prefetch_4d(map, 0, n, h, b);
+  if (halves > 1) sm100::tma_prefetch_4d(map, 64, n, h, b);
+}
 // Zeros in the rows of a tile in shared memory (rows of 128 bytes, halves `bytes` apart) whose keys do not count: in the product they
 // meet probabilities of zero, and zero times what may stand there need not be zero.  W words of valid bits: bit l of word k is row
 // W l + k.  All 32 lanes.
 template <int W>
 __device__ __forceinline__ void cx_clean(uint8_t* tile, int bytes, int halves, const uint32_t (&valid)[W], int lane) {
+  const int sub = lane >> 3;                                 // four rows at a time, eight lanes of 16 bytes each
+  uint32_t mine = valid[0];
 #pragma unroll
-  for (int k = 0; k < W; ++k) {
-    uint32_t gone = ~valid[k];
-    while (gone) {
-      // four rows at a time, eight lanes of 16 bytes each
-      uint32_t rest = gone;
-      int row = -1;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int l = __ffs(rest) - 1;
-        if (i == (lane >> 3)) row = l < 0 ? -1 : W * l + k;
-        rest &= rest - 1;
-      }
-      gone = rest;
-      if (row >= 0)
-        for (int h = 0; h < halves; ++h) *(uint4*)(tile + h * bytes + row * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
-    }
-  }
+  for (int k = 1; k < W; ++k)
+    if (sub % W == k) mine = valid[k];
+  uint8_t* to = tile + lane * 16;
+#pragma unroll 8
+  for (int i = 0; i < 8 * W; ++i)                            // rows 4 i + sub
+    if (!(mine >> (i * 4 / W + sub / W) & 1))
+      for (int h = 0; h < halves; ++h) *(uint4*)(to + h * bytes + i * 512) = make_uint4(0, 0, 0, 0);
   sm100::fence_proxy_async();
 }
 // Puts 32 consecutive fp32 values of a row (columns 32 c .. of the 64 of a swizzled half in shared memory) there as bf16.

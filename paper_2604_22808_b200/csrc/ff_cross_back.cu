@@ -12,8 +12,9 @@
 //   warp 1       tcgen05.mma issuer: S = Q K^T into two buffers in turns, dP = dout V^T
 //   warp 2       zeros in rows of K whose keys do not count, in tiles that may hold such rows
 //   warp 3       tcgen05.mma issuer: dQ += dS K (dS from tensor memory, K as an MN-major operand)
-//   warps 4..11  a thread per query row, two warpgroups that take the tiles of keys in turns: P, then dS as bf16 over the scores; D at the
-//                item's start, from dout and out in shared memory
+//   warps 4..11  a thread per query row and half of the keys: P, then dS as bf16 over the scores; D at the item's first tile, from dout
+//                and out in shared memory.  (Warpgroups that took whole tiles in turns: 70 instead of 60 us for 16K queries, 6 heads of
+//                128, 512 keys.)
 //   tensor memory: S (twice), dP, dQ
 //
 // dk, dv: a CTA takes a tile of keys and a run of the query tiles of its group.
@@ -53,8 +54,9 @@ struct KeyParams {
 
 // ---- dq -------------------------------------------------------------------------------------------------------------------
 struct QueryShared {
-  uint64_t q_full, q_empty, o_full, stage_free;
-  uint64_t k_full[3], k_empty[3], k_raw[3], v_full, v_empty;
+  uint64_t q_full[2], q_empty[2], o_full, stage_free;
+  uint64_t k_full[3], k_empty[3], k_raw[3], v_full[2], v_empty[2];
+  float d[2][TILE];                                          // sums of either half of the channels
   uint64_t s_full[2], ds_full[2], dp_full, dp_empty, dq_full, dq_empty;
   uint32_t tmem_base;
   int abort_flag;
@@ -84,19 +86,21 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const __grid_constant__ QueryParams P) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t *sQ = smem, *sG = smem + TILE_BYTES, *sK = smem + 2 * TILE_BYTES, *sV = smem + 5 * TILE_BYTES, *stage = smem + 6 * TILE_BYTES;
+  constexpr int BYTES = TILE * HD * 2, NQ = HD == 64 ? 2 : 1;         // places of queries (with dout) and of values
+  uint8_t *sQ = smem, *sG = sQ + NQ * BYTES, *sK = sG + NQ * BYTES, *sV = sK + 3 * BYTES, *stage = sV + NQ * BYTES;
+  static_assert((3 * NQ + 4) * BYTES <= 7 * TILE_BYTES, "");
   QueryShared& sh = *(QueryShared*)(smem + 7 * TILE_BYTES);
   const CrossDims& D = P.dm;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int HALVES = HD / 64;
 
   if (threadIdx.x == 0) {
-    mbar_init(&sh.q_full, 1); mbar_init(&sh.q_empty, 1 + 8); mbar_init(&sh.o_full, 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1 + 8); mbar_init(&sh.v_full[i], 1); mbar_init(&sh.v_empty[i], 1); }
+    mbar_init(&sh.o_full, 1);
     mbar_init(&sh.stage_free, 1);
     for (int i = 0; i < 3; ++i) { mbar_init(&sh.k_full[i], 1); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.k_raw[i], 1); }
-    mbar_init(&sh.v_full, 1); mbar_init(&sh.v_empty, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.ds_full[i], 128); }
-    mbar_init(&sh.dp_full, 1); mbar_init(&sh.dp_empty, 128); mbar_init(&sh.dq_full, 1); mbar_init(&sh.dq_empty, 256);
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.ds_full[i], 256); }
+    mbar_init(&sh.dp_full, 1); mbar_init(&sh.dp_empty, 256); mbar_init(&sh.dq_full, 1); mbar_init(&sh.dq_empty, 256);
     sh.abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&map_q); tma_prefetch_desc(&map_k); tma_prefetch_desc(&map_v);
@@ -118,35 +122,51 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         const int q_bytes = D.bn * D.bh * HD * 2;
         unsigned iter = 0, g = 0;
         bool ok = true;
+        auto load_keys = [&](const QueryItem& x, int j) {
+          const int st = g % 3;
+          if (g >= 3) ok = mbar_wait(&sh.k_empty[st], (g / 3 - 1) & 1, abort_flag);
+          if (!ok) return;
+          uint64_t* full = cx_unclean<TILE>(D, x.keys, j) ? &sh.k_raw[st] : &sh.k_full[st];
+          mbar_arrive_expect_tx(full, BYTES);
+          cx_load(sK + st * BYTES, HALF_BYTES, HALVES, &map_k, full, j * TILE, x.g * D.once[1][1], x.b * D.once[1][0]);
+        };
+        auto load_values = [&](const QueryItem& x, int j) {
+          const int vp = g % NQ;
+          if (g >= NQ) ok = mbar_wait(&sh.v_empty[vp], (g / NQ - 1) & 1, abort_flag);
+          if (!ok) return;
+          mbar_arrive_expect_tx(&sh.v_full[vp], BYTES);
+          cx_load(sV + vp * BYTES, HALF_BYTES, HALVES, &map_v, &sh.v_full[vp], j * TILE, x.g * D.once[2][1], x.b * D.once[2][0]);
+          ++g;
+        };
         for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
           const QueryItem x = query_item(P, it);
           if (x.j0 == x.j1) continue;
           int h0, n0;
           cx_place(D, x.g, x.tile, h0, n0);
-          if (iter >= 1) ok = mbar_wait(&sh.q_empty, (iter - 1) & 1, abort_flag);
+          load_keys(x, x.j0);                                // (their place is free before that of the queries)
+          const int qb = iter % NQ;
+          if (ok && iter >= NQ) ok = mbar_wait(&sh.q_empty[qb], (iter / NQ - 1) & 1, abort_flag);
           if (!ok) break;
-          mbar_arrive_expect_tx(&sh.q_full, 2 * q_bytes);
-          cx_load(sQ, HALF_BYTES, HALVES, &map_q, &sh.q_full, n0, h0 * D.once[0][1], x.b * D.once[0][0]);
-          cx_load(sG, HALF_BYTES, HALVES, &map_dout, &sh.q_full, n0, h0, x.b);
-          bool out_asked = false;
-          for (int j = x.j0; j < x.j1; ++j, ++g) {
-            const int st = g % 3;
-            if (g >= 3) ok = mbar_wait(&sh.k_empty[st], (g / 3 - 1) & 1, abort_flag);
-            if (!ok) break;
-            uint64_t* full = cx_unclean<TILE>(D, x.keys, j) ? &sh.k_raw[st] : &sh.k_full[st];
-            mbar_arrive_expect_tx(full, TILE * HD * 2);
-            cx_load(sK + st * TILE_BYTES, HALF_BYTES, HALVES, &map_k, full, j * TILE, x.g * D.once[1][1], x.b * D.once[1][0]);
-            if (!out_asked) {                                // (behind the first keys: the stage may still be on its way out)
-              out_asked = true;
-              if (iter >= 1) ok = mbar_wait(&sh.stage_free, (iter - 1) & 1, abort_flag);
-              if (!ok) break;
-              mbar_arrive_expect_tx(&sh.o_full, q_bytes);
-              cx_load(stage, HALF_BYTES, HALVES, &map_out, &sh.o_full, n0, h0, x.b);
-            }
-            if (g >= 1) ok = mbar_wait(&sh.v_empty, (g - 1) & 1, abort_flag);
-            if (!ok) break;
-            mbar_arrive_expect_tx(&sh.v_full, TILE * HD * 2);
-            cx_load(sV, HALF_BYTES, HALVES, &map_v, &sh.v_full, j * TILE, x.g * D.once[2][1], x.b * D.once[2][0]);
+          mbar_arrive_expect_tx(&sh.q_full[qb], 2 * q_bytes);
+          cx_load(sQ + qb * BYTES, HALF_BYTES, HALVES, &map_q, &sh.q_full[qb], n0, h0 * D.once[0][1], x.b * D.once[0][0]);
+          cx_load(sG + qb * BYTES, HALF_BYTES, HALVES, &map_dout, &sh.q_full[qb], n0, h0, x.b);
+          load_values(x, x.j0);
+          if (it + (int)gridDim.x < P.items) {               // what the next item reads first, from memory into L2
+            const QueryItem y = query_item(P, it + gridDim.x);
+            int h1, n1;
+            cx_place(D, y.g, y.tile, h1, n1);
+            cx_prefetch(HALVES, &map_q, n1, h1 * D.once[0][1], y.b * D.once[0][0]);
+            cx_prefetch(HALVES, &map_dout, n1, h1, y.b);
+            cx_prefetch(HALVES, &map_out, n1, h1, y.b);
+          }
+          // (behind the first keys and values: the stage may still be on its way out)
+          if (ok && iter >= 1) ok = mbar_wait(&sh.stage_free, (iter - 1) & 1, abort_flag);
+          if (!ok) break;
+          mbar_arrive_expect_tx(&sh.o_full, q_bytes);
+          cx_load(stage, HALF_BYTES, HALVES, &map_out, &sh.o_full, n0, h0, x.b);
+          for (int j = x.j0 + 1; j < x.j1 && ok; ++j) {
+            load_keys(x, j);
+            if (ok) load_values(x, j);
           }
           ++iter;
         }
@@ -167,25 +187,25 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         if (!mbar_wait_warp(&sh.k_full[gt % 3], (gt / 3) & 1, abort_flag)) return false;
         if (gt >= 2 && !mbar_wait_warp(&sh.k_empty[(gt - 2) % 3], ((gt - 2) / 3) & 1, abort_flag)) return false;
         tc_fence_after();
-        score(tm + (gt & 1) * 128, q_desc, k_desc + (uint64_t)((gt % 3) * (TILE_BYTES >> 4)));
+        score(tm + (gt & 1) * 128, q_desc + (uint64_t)(iter % NQ * (BYTES >> 4)), k_desc + (uint64_t)((gt % 3) * (BYTES >> 4)));
         umma_commit(&sh.s_full[gt & 1]);
         return true;
       };
       auto issue_dp = [&](unsigned gt, bool last) -> bool {
-        if (!mbar_wait_warp(&sh.v_full, gt & 1, abort_flag)) return false;
+        if (!mbar_wait_warp(&sh.v_full[gt % NQ], (gt / NQ) & 1, abort_flag)) return false;
         if (gt >= 1 && !mbar_wait_warp(&sh.dp_empty, (gt - 1) & 1, abort_flag)) return false;
         tc_fence_after();
-        score(tm + 256, g_desc, v_desc);
+        score(tm + 256, g_desc + (uint64_t)(iter % NQ * (BYTES >> 4)), v_desc + (uint64_t)(gt % NQ * (BYTES >> 4)));
         umma_commit(&sh.dp_full);
-        umma_commit(&sh.v_empty);
-        if (last) umma_commit(&sh.q_empty);
+        umma_commit(&sh.v_empty[gt % NQ]);
+        if (last) umma_commit(&sh.q_empty[iter % NQ]);
         return true;
       };
       for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
         const QueryItem x = query_item(P, it);
         const int nk = cx_uniform(x.j1 - x.j0);
         if (nk == 0) continue;
-        ok = mbar_wait_warp(&sh.q_full, iter & 1, abort_flag);
+        ok = mbar_wait_warp(&sh.q_full[iter % NQ], (iter / NQ) & 1, abort_flag);
         for (int i = 0; i < nk && ok; ++i) ok = issue_s(g + i) && issue_dp(g + i, i + 1 == nk);
         g += nk;
         ++iter;
@@ -205,9 +225,9 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           ok = mbar_wait_warp(&sh.ds_full[g & 1], (g >> 1) & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
-          const uint64_t kd = km_desc + (uint64_t)((g % 3) * (TILE_BYTES >> 4));
+          const uint64_t kd = km_desc + (uint64_t)((g % 3) * (BYTES >> 4));
           umma_ts4(tm + 384, tm + (g & 1) * 128, kd, idesc_q, i == 0 ? 0u : 1u);
-          umma_ts4(tm + 384, tm + (g & 1) * 128 + 32, kd + (uint64_t)(4 * (2048 >> 4)), idesc_q, 1u);
+          umma_ts4(tm + 384, tm + (g & 1) * 128 + 64, kd + (uint64_t)(4 * (2048 >> 4)), idesc_q, 1u);    // (dS of either half of the keys)
           umma_commit(&sh.k_empty[g % 3]);
         }
         if (ok) umma_commit(&sh.dq_full);
@@ -226,7 +246,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           const unsigned n = st == 0 ? raw[0]++ : st == 1 ? raw[1]++ : raw[2]++;
           ok = mbar_wait_warp(&sh.k_raw[st], n & 1, abort_flag);
           if (!ok) break;
-          cx_clean(sK + st * TILE_BYTES, HALF_BYTES, HALVES, valid.w, lane);
+          cx_clean(sK + st * BYTES, HALF_BYTES, HALVES, valid.w, lane);
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.k_full[st]);
         }
@@ -239,7 +259,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     const int wg = (warp - 4) >> 2;
     const int row = quarter * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
-    const uint32_t s_addr = tm + lane_addr + wg * 128, dp_addr = tm + lane_addr + 256, dq_addr = tm + lane_addr + 384;
+    const uint32_t s_addr = tm + lane_addr + wg * 64, dp_addr = s_addr + 256, dq_addr = tm + lane_addr + 384;
     const int rows = D.bn * D.bh;
     const int row_h = row / D.bn, row_n = row - row_h * D.bn;
     unsigned iter = 0, g = 0;
@@ -269,83 +289,87 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         stored = false;
       }
       const float nlse2 = here ? -P.lse[at] * LOG2E : -INFINITY;        // (rows that are not there: P = 0)
-      // D = dout out of this row
-      ok = mbar_wait_warp(&sh.q_full, iter & 1, abort_flag) && mbar_wait_warp(&sh.o_full, iter & 1, abort_flag);
-      if (!ok) break;
-      float2 d2 = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const int off = h * HALF_BYTES + row * 128 + ((c ^ (row & 7)) * 16);
-          const uint4 a = *(const uint4*)(sG + off), b = *(const uint4*)(stage + off);
-          const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            d2 = __ffma2_rn(make_float2(__uint_as_float(av[i] << 16), __uint_as_float(av[i] & 0xffff0000u)),
-                            make_float2(__uint_as_float(bv[i] << 16), __uint_as_float(bv[i] & 0xffff0000u)), d2);
-        }
-      const float delta = d2.x + d2.y;
-      if (wg == 0 && x.j0 == 0 && here) P.delta[at] = delta;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.q_empty);
+      float delta = 0.f;
       for (int j = x.j0; j < x.j1 && ok; ++j, ++g) {
-        if ((int)(g & 1) != wg) continue;
         const bool full = !D.mask && (j + 1) * TILE <= x.keys;
         CxValid valid = {};
         if (!full) valid = cx_valid(D, x.b, x.keys, j, lane);
-        ok = mbar_wait_warp(&sh.s_full[wg], (g >> 1) & 1, abort_flag);
+        const uint32_t at_s = s_addr + (g & 1) * 128;
+        ok = mbar_wait_warp(&sh.s_full[g & 1], (g >> 1) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        uint32_t p[4][32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, p[c]);
+        uint32_t p[2][32];
+        tmem_ld32(at_s, p[0]);
+        tmem_ld32(at_s + 32, p[1]);
         tmem_wait_ld();
         const float2 sl22 = make_float2(D.sl2, D.sl2), nl2 = make_float2(nlse2, nlse2);
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float2 arg = __ffma2_rn(make_float2(__uint_as_float(p[c][2 * i]), __uint_as_float(p[c][2 * i + 1])), sl22, nl2);
             p[c][2 * i] = __float_as_uint(ex2(arg.x));
             p[c][2 * i + 1] = __float_as_uint(ex2(arg.y));
           }
+        if (j == x.j0) {                                     // D = dout out of this row, half of the channels each
+          ok = mbar_wait_warp(&sh.q_full[iter % NQ], (iter / NQ) & 1, abort_flag) && mbar_wait_warp(&sh.o_full, iter & 1, abort_flag);
+          if (!ok) break;
+          const uint8_t* g_row = sG + iter % NQ * BYTES + (HALVES > 1 ? wg * HALF_BYTES : 0) + row * 128;
+          const uint8_t* o_row = stage + (HALVES > 1 ? wg * HALF_BYTES : 0) + row * 128;
+          float2 d2 = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int c = 0; c < 4 * HALVES; ++c) {
+            const int off = ((HALVES > 1 ? c : wg * 4 + c) ^ (row & 7)) * 16;
+            const uint4 a = *(const uint4*)(g_row + off), b = *(const uint4*)(o_row + off);
+            const uint32_t av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              d2 = __ffma2_rn(make_float2(__uint_as_float(av[i] << 16), __uint_as_float(av[i] & 0xffff0000u)),
+                              make_float2(__uint_as_float(bv[i] << 16), __uint_as_float(bv[i] & 0xffff0000u)), d2);
+          }
+          sh.d[wg][row] = d2.x + d2.y;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.q_empty[iter % NQ]);
+          bar_sync(1, 256);                                  // (and out in the stage has been read by all)
+          delta = sh.d[0][row] + sh.d[1][row];
+          if (wg == 0 && x.j0 == 0 && here) P.delta[at] = delta;
+        }
         ok = mbar_wait_warp(&sh.dp_full, g & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
         const float2 nd2 = make_float2(-delta, -delta);
+        uint32_t r[2][32];
+        tmem_ld32(dp_addr, r[0]);
+        tmem_ld32(dp_addr + 32, r[1]);
+        tmem_wait_ld();
+        tc_fence_before();
+        mbar_arrive(&sh.dp_empty);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t r[32], pk[16];
-          tmem_ld32(dp_addr + c * 32, r);
-          tmem_wait_ld();
-          if (c == 3) {                                      // dP has been read
-            tc_fence_before();
-            mbar_arrive(&sh.dp_empty);
-          }
+        for (int c = 0; c < 2; ++c) {
+          uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float2 v = __fmul2_rn(make_float2(__uint_as_float(p[c][2 * i]), __uint_as_float(p[c][2 * i + 1])),
-                                        __fadd2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), nd2));
+                                        __fadd2_rn(make_float2(__uint_as_float(r[c][2 * i]), __uint_as_float(r[c][2 * i + 1])), nd2));
             float lo = v.x, hi = v.y;
             if (!full) {
-              if (!(valid.w[(2 * i) & 3] >> (c * 8 + (i >> 1)) & 1)) lo = 0.f;
-              if (!(valid.w[(2 * i + 1) & 3] >> (c * 8 + (i >> 1)) & 1)) hi = 0.f;
+              const int bit = wg * 16 + c * 8 + (i >> 1);
+              if (!(valid.w[(2 * i) & 3] >> bit & 1)) lo = 0.f;
+              if (!(valid.w[(2 * i + 1) & 3] >> bit & 1)) hi = 0.f;
             }
             pk[i] = bf16_pair(__float_as_uint(lo), __float_as_uint(hi));
           }
-          tmem_st16(s_addr + c * 16, pk);
+          tmem_st16(at_s + c * 16, pk);
         }
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(&sh.ds_full[wg]);
+        mbar_arrive(&sh.ds_full[g & 1]);
       }
       if (!ok) break;
       ok = mbar_wait_warp(&sh.dq_full, iter & 1, abort_flag);
       if (!ok) break;
       tc_fence_after();
       ++iter;
-      if (!part) bar_sync(1, 256);                           // (out in the stage has been read by all)
       for (int c = c0; c < c0 + HD / 2; c += 32) {
         uint32_t r[32];
         tmem_ld32(dq_addr + c, r);
@@ -593,7 +617,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       const int key = x.j * TILE + row;
       const bool here = key < D.K;
       const bool counts = key < x.keys && (!D.mask || __ldg(D.mask + (long long)x.b * D.K + key) != 0);
-      const bool empty = x.t0 == x.t1;
+      const bool empty = x.t0 == x.t1, all = __all_sync(0xffffffffu, counts);
       for (int t = x.t0; t < x.t1 && ok; ++t, ++g) {
         const int st = g & 1;
         const float4 *nlse = (const float4*)(sh.nlse2[st] + wg * 64), *nd = (const float4*)(sh.ndelta[st] + wg * 64);
@@ -607,19 +631,20 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const float2 sl22 = make_float2(D.sl2, D.sl2);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float4 n4 = nlse[c * 8 + i];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              uint32_t &lo = p[c][4 * i + 2 * e], &hi = p[c][4 * i + 2 * e + 1];
-              const float2 arg = __ffma2_rn(make_float2(__uint_as_float(lo), __uint_as_float(hi)), sl22, e ? make_float2(n4.z, n4.w) : make_float2(n4.x, n4.y));
-              lo = counts ? __float_as_uint(ex2(arg.x)) : 0u;
-              hi = counts ? __float_as_uint(ex2(arg.y)) : 0u;
-              pk[2 * i + e] = bf16_pair(lo, hi);
-            }
+            const float2 a = __ffma2_rn(make_float2(__uint_as_float(p[c][4 * i]), __uint_as_float(p[c][4 * i + 1])), sl22, make_float2(n4.x, n4.y));
+            const float2 b = __ffma2_rn(make_float2(__uint_as_float(p[c][4 * i + 2]), __uint_as_float(p[c][4 * i + 3])), sl22, make_float2(n4.z, n4.w));
+            p[c][4 * i] = __float_as_uint(ex2(a.x)); p[c][4 * i + 1] = __float_as_uint(ex2(a.y));
+            p[c][4 * i + 2] = __float_as_uint(ex2(b.x)); p[c][4 * i + 3] = __float_as_uint(ex2(b.y));
           }
+          if (!all)                                          // (rows of zeros, whatever stands in K)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) p[c][i] = counts ? p[c][i] : 0u;
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pk[i] = bf16_pair(p[c][2 * i], p[c][2 * i + 1]);
           tmem_st16(s_addr + c * 16, pk);
         }
         tmem_wait_st();
@@ -628,27 +653,28 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         ok = mbar_wait_warp(&sh.dp_full, g & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
+        uint32_t r[2][32];
+        tmem_ld32(dp_addr, r[0]);
+        tmem_ld32(dp_addr + 32, r[1]);
+        tmem_wait_ld();
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          uint32_t r[32], pk[16];
-          tmem_ld32(dp_addr + c * 32, r);
-          tmem_wait_ld();
+          uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float4 n4 = nd[c * 8 + i];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const float2 v = __fmul2_rn(make_float2(__uint_as_float(p[c][4 * i + 2 * e]), __uint_as_float(p[c][4 * i + 2 * e + 1])),
-                                          __fadd2_rn(make_float2(__uint_as_float(r[4 * i + 2 * e]), __uint_as_float(r[4 * i + 2 * e + 1])),
+                                          __fadd2_rn(make_float2(__uint_as_float(r[c][4 * i + 2 * e]), __uint_as_float(r[c][4 * i + 2 * e + 1])),
                                                      e ? make_float2(n4.z, n4.w) : make_float2(n4.x, n4.y)));
-              pk[2 * i + e] = counts ? bf16_pair(__float_as_uint(v.x), __float_as_uint(v.y)) : 0u;
+              pk[2 * i + e] = bf16_pair(__float_as_uint(v.x), __float_as_uint(v.y));
             }
           }
-          if (c == 0) {                                      // (the second half of dP^T lies beyond what is written here)
-            tmem_st16(dp_addr, pk);
-          } else {
-            tmem_st16(dp_addr + 16, pk);
-          }
+          if (!all)                                          // (... and in V)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pk[i] = counts ? pk[i] : 0u;
+          tmem_st16(dp_addr + c * 16, pk);
         }
         tmem_wait_st();
         tc_fence_before();
