@@ -563,9 +563,10 @@ void shape_of(const ff_cross_attention_config_t& c, int64_t batch, int64_t queri
   D->sl2 = (float)(D->scale * 1.4426950408889634);
 }
 // Items of the forward launch: one or two tiles, all keys or parts of them, by the estimated time.  A tile of keys takes a pair of query
-// tiles 1.6 us and a single one 1.0, an item 2 us more; joining the parts takes 3 us and what they write and read.
+// tiles 1.2 us and a single one 0.75, an item 2 us more; joining the parts takes 3 us and what they write and read.  With lengths, which the host does
+// not know, two thirds of the keys are expected, unevenly over the items, so that more and shorter ones are better.
 struct Forward { int pair, pairs, splits; };
-Forward forward_of(const CrossDims& D) {
+Forward forward_of(const CrossDims& D, bool lengths) {
   Forward best = {1, D.tiles, 1};
   double least = 1e30;
   const long long nk = (D.K + KEYS - 1) / KEYS;
@@ -573,9 +574,9 @@ Forward forward_of(const CrossDims& D) {
     const int pairs = (D.tiles + pair - 1) / pair;
     for (int splits = 1; splits <= 64 && splits <= (nk > 1 ? nk : 1); ++splits) {
       const double items = (double)D.B * D.G * pairs * splits;
-      if (splits > 1 && items > 2 * FF_B200_SMS) break;
-      const double waves = ceil(items / FF_B200_SMS);
-      const double us = waves * ((double)((nk + splits - 1) / splits) * (pair == 2 ? 1.6 : 1.0) + 2) +
+      if (splits > 1 && items > 4 * FF_B200_SMS) break;
+      const double even = items / FF_B200_SMS, waves = !lengths ? ceil(even) : even * 2 / 3 + 0.35 > 1 ? even * 2 / 3 + 0.35 : 1;
+      const double us = waves * ((double)((nk + splits - 1) / splits) * (pair == 2 ? 1.2 : 0.75) + 2) +
                         (splits > 1 ? 3 + (double)splits * D.B * D.H * D.N * D.d * 8 / 4e6 : 0);
       if (us < least) { least = us; best = {pair, pairs, splits}; }
     }
@@ -662,8 +663,8 @@ extern "C" ff_status_t ff_cross_attention_workspace_bytes(const ff_cross_attenti
   if (training) {
     *bytes = cx_backward_bytes(D);
   } else {
-    const Forward f = forward_of(D);
-    if (f.splits > 1) *bytes = part_bytes(D, f.splits) + part_lse_bytes(D, f.splits);
+    const int a = forward_of(D, false).splits, b = forward_of(D, true).splits, most = a > b ? a : b;      // (whether there are lengths, the call says)
+    if (most > 1) *bytes = part_bytes(D, most) + part_lse_bytes(D, most);
   }
   return FF_OK;
 }
@@ -738,7 +739,7 @@ extern "C" ff_status_t ff_cross_attention_forward(ff_cross_attention_t* h, int64
   CrossParams P{};
   shape_of(c, batch, queries, keys, &P.dm);
   keys_of(&P.dm, h, q, k, v, lengths, mask);
-  const Forward f = forward_of(P.dm);
+  const Forward f = forward_of(P.dm, lengths != nullptr);
   P.pair = f.pair; P.pairs = f.pairs; P.splits = f.splits;
   const long long items = (long long)P.dm.B * P.dm.G * f.pairs * f.splits;
   if (items >= 0x7fffffff - FF_B200_SMS) return fail(h, FF_ERR_UNSUPPORTED, MOST);
