@@ -489,7 +489,7 @@ const char *ff_cross_attention_last_error(const ff_cross_attention_t *attention)
  * multiples of 16 bytes; k and v may have a batch or head stride of 0 (the same states for all).  out may be q (the same
  * address and strides), otherwise it overlaps no input.
  *   lse  device, float [batch][heads][queries], kept for the backward pass; or NULL
- * Sizes: batch * heads and the number of 128-row tiles of queries below 2^31, queries and keys at most 2^31 - 256. */
+ * Sizes: the 128-row tiles of all heads' queries, and as many of keys, below 2^31 - 1024, queries and keys at most 2^31 - 256. */
 ff_status_t ff_cross_attention_forward(ff_cross_attention_t *attention, int64_t batch, int64_t queries, int64_t keys, const ff_heads_t *q,
                                        const ff_heads_t *k, const ff_heads_t *v, const int32_t *lengths, const uint8_t *mask,
                                        const ff_heads_t *out, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream);

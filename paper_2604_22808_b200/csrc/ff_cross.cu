@@ -53,7 +53,7 @@ struct Shared {
   uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];                // per place
   uint64_t v_raw[4];                                                    // in place of v_full for a tile that has to be cleaned first
   uint64_t s_full[2][2], p_full[2][2];                                  // per stream and place of its scores
-  uint64_t pv_done[2], o_full[2], o_empty[2];                           // per stream
+  uint64_t pv_done[2], o_full[2], o_empty[2], staged[2], sent[2];       // per stream
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -150,6 +150,7 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1);
       for (int k = 0; k < 2; ++k) { mbar_init(&sh.s_full[i][k], 1); mbar_init(&sh.p_full[i][k], 128); }
       mbar_init(&sh.pv_done[i], 1); mbar_init(&sh.o_full[i], 1); mbar_init(&sh.o_empty[i], 128);
+      mbar_init(&sh.staged[i], 128); mbar_init(&sh.sent[i], 1);
     }
     sh.abort_flag = 0;
     fence_mbar_init();
@@ -315,7 +316,8 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const float sl2 = D.sl2;
     unsigned n = 0, items = 0, ends = 0;      // tiles this stream has taken, items (with keys; with more than one tile of them) it has ended
     Place<NP> vp;                     // of the tile's keys and values
-    bool ok = true, staged = false;
+    unsigned staged = 0;              // items it has put on the stage
+    bool ok = true;
     for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
       int b, keys, from;
       bool work;                                            // (rows that a tile does not have take no time)
@@ -451,9 +453,10 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
       } else {
         if (P.lse && here) P.lse[at] = lse2 * 0.69314718055994531f;
-        if (staged) {                                       // the item before has left the stage
-          if (row == 0) bulk_wait_read0();
-          bar_sync(1 + sx, 128);
+        if (staged >= 1) {                                  // the item before has left the stage
+          if (row == 0) { bulk_wait_read0(); mbar_arrive(&sh.sent[sx]); }
+          ok = mbar_wait_warp(&sh.sent[sx], (staged - 1) & 1, abort_flag);
+          if (!ok) break;
         }
 #pragma unroll
         for (int c = 0; c < HD / 32; ++c) {
@@ -469,13 +472,17 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
           cx_stage(stage + (c / 2) * HALF_BYTES, row, c & 1, r, counts ? inv : 1.f);
         }
         fence_proxy_async();
-        bar_sync(1 + sx, 128);
-        if (row == 0) {
-          tma_store_4d(stage, &map_o, 0, n0, h0, x.b);
-          if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_o, 64, n0, h0, x.b);
-          bulk_commit();
+        mbar_arrive(&sh.staged[sx]);
+        if (quarter == 0) {
+          ok = mbar_wait_warp(&sh.staged[sx], staged & 1, abort_flag);
+          if (!ok) break;
+          if (row == 0) {
+            tma_store_4d(stage, &map_o, 0, n0, h0, x.b);
+            if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_o, 64, n0, h0, x.b);
+            bulk_commit();
+          }
         }
-        staged = true;
+        ++staged;
       }
       if (some) {
         tc_fence_before();
@@ -586,12 +593,13 @@ Forward forward_of(const CrossDims& D, bool lengths) {
 size_t part_bytes(const CrossDims& D, int splits) { return (size_t)splits * D.B * D.H * D.N * D.d * sizeof(float); }
 size_t part_lse_bytes(const CrossDims& D, int splits) { return (size_t)splits * D.B * D.H * D.N * sizeof(float); }
 
-// Sizes that the kernels' indexes and tensor maps take
-constexpr char MOST[] = "queries and keys must be at most 2^31 - 256, batch * heads and their tiles of queries (and of keys) below 2^31, all values below 2^42";
+// Sizes that the kernels' indexes (items, and a grid more) and tensor maps take
+constexpr double MOST_TILES = 2147483648.0 - 1024;
+constexpr char MOST[] = "queries and keys must be at most 2^31 - 256, the 128-row tiles of all heads' queries (and of keys) below 2^31 - 1024, all values below 2^42";
 bool too_large(const ff_cross_attention_config_t& c, int64_t batch, int64_t queries, int64_t keys) {
   if (batch > 0x7fffffff || queries > 0x7fffff00 || keys > 0x7fffff00) return true;
   const double bh = (double)batch * c.heads;
-  return bh >= 2147483648.0 || bh * (double)((queries + TILE - 1) / TILE) >= 2147483648.0 || bh * (double)((keys + TILE - 1) / TILE) >= 2147483648.0 ||
+  return bh >= MOST_TILES || bh * (double)((queries + TILE - 1) / TILE) >= MOST_TILES || bh * (double)((keys + TILE - 1) / TILE) >= MOST_TILES ||
          bh * (double)queries * c.head_dim >= 4398046511104.0;
 }
 
@@ -742,7 +750,6 @@ extern "C" ff_status_t ff_cross_attention_forward(ff_cross_attention_t* h, int64
   const Forward f = forward_of(P.dm, lengths != nullptr);
   P.pair = f.pair; P.pairs = f.pairs; P.splits = f.splits;
   const long long items = (long long)P.dm.B * P.dm.G * f.pairs * f.splits;
-  if (items >= 0x7fffffff - FF_B200_SMS) return fail(h, FF_ERR_UNSUPPORTED, MOST);
   P.items = (int)items;
   P.lse = lse;
   P.part = (float*)ws;

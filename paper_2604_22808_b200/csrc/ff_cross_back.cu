@@ -54,7 +54,7 @@ struct KeyParams {
 
 // ---- dq -------------------------------------------------------------------------------------------------------------------
 struct QueryShared {
-  uint64_t q_full[2], q_empty[2], o_full, stage_free;
+  uint64_t q_full[2], q_empty[2], o_full, d_full, staged, stage_free;
   uint64_t k_full[3], k_empty[3], k_raw[3], v_full[2], v_empty[2];
   float d[2][TILE];                                          // sums of either half of the channels
   uint64_t s_full[2], ds_full[2], dp_full, dp_empty, dq_full, dq_empty;
@@ -97,7 +97,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1 + 8); mbar_init(&sh.v_full[i], 1); mbar_init(&sh.v_empty[i], 1); }
     mbar_init(&sh.o_full, 1);
-    mbar_init(&sh.stage_free, 1);
+    mbar_init(&sh.d_full, 256); mbar_init(&sh.staged, 256); mbar_init(&sh.stage_free, 1);
     for (int i = 0; i < 3; ++i) { mbar_init(&sh.k_full[i], 1); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.k_raw[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.ds_full[i], 256); }
     mbar_init(&sh.dp_full, 1); mbar_init(&sh.dp_empty, 256); mbar_init(&sh.dq_full, 1); mbar_init(&sh.dq_empty, 256);
@@ -330,7 +330,9 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           sh.d[wg][row] = d2.x + d2.y;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.q_empty[iter % NQ]);
-          bar_sync(1, 256);                                  // (and out in the stage has been read by all)
+          mbar_arrive(&sh.d_full);                           // (and out in the stage has been read by all)
+          ok = mbar_wait_warp(&sh.d_full, iter & 1, abort_flag);
+          if (!ok) break;
           delta = sh.d[0][row] + sh.d[1][row];
           if (wg == 0 && x.j0 == 0 && here) P.delta[at] = delta;
         }
@@ -387,11 +389,15 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       tc_fence_before();
       mbar_arrive(&sh.dq_empty);
       fence_proxy_async();
-      bar_sync(2, 256);
-      if (!part && wg == 0 && row == 0) {
-        tma_store_4d(stage, &map_dq, 0, n0, h0, x.b);
-        if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_dq, 64, n0, h0, x.b);
-        bulk_commit();
+      mbar_arrive(&sh.staged);
+      if (warp == 4) {
+        ok = mbar_wait_warp(&sh.staged, (iter - 1) & 1, abort_flag);
+        if (!ok) break;
+        if (!part && lane == 0) {
+          tma_store_4d(stage, &map_dq, 0, n0, h0, x.b);
+          if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_dq, 64, n0, h0, x.b);
+          bulk_commit();
+        }
       }
       stored = true;
     }
@@ -416,7 +422,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 // ---- dk, dv ---------------------------------------------------------------------------------------------------------------
 struct KeyShared {
   uint64_t kv_full, kv_empty, q_full[2], q_empty[2], g_full[2], g_empty[2], row_full[2], row_empty[2];
-  uint64_t s_full, dp_full, p_full[2], ds_full[2], sum_full, sum_empty;
+  uint64_t s_full, dp_full, p_full[2], ds_full[2], sum_full, sum_empty, staged[2];
   uint32_t tmem_base;
   int abort_flag;
   alignas(16) float nlse2[2][TILE];     // (read four at a time)
@@ -459,7 +465,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.q_full[i], 1); mbar_init(&sh.q_empty[i], 1); mbar_init(&sh.g_full[i], 1); mbar_init(&sh.g_empty[i], 1);
       mbar_init(&sh.row_full[i], 32); mbar_init(&sh.row_empty[i], 8);
-      mbar_init(&sh.p_full[i], 128); mbar_init(&sh.ds_full[i], 128);
+      mbar_init(&sh.p_full[i], 128); mbar_init(&sh.ds_full[i], 128); mbar_init(&sh.staged[i], 128);
     }
     mbar_init(&sh.s_full, 1); mbar_init(&sh.dp_full, 1); mbar_init(&sh.sum_full, 1); mbar_init(&sh.sum_empty, 256);
     sh.abort_flag = 0;
@@ -722,7 +728,9 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
           cx_stage(stage + (c / 64) * HALF_BYTES, row, (c % 64) / 32, r, factor);
         }
         fence_proxy_async();
-        bar_sync(1 + wg, 128);
+        mbar_arrive(&sh.staged[wg]);
+        if (quarter == 0) ok = mbar_wait_warp(&sh.staged[wg], (iter - 1) & 1, abort_flag);
+        if (!ok) break;
         if (row == 0) {
           const CUtensorMap* map = wg ? &map_dk : &map_dv;
           tma_store_4d(stage, map, 0, x.j * TILE, x.g, x.b);
