@@ -42,6 +42,7 @@ constexpr float LAZY_LOG2 = 8.0f;
 struct CrossParams {
   CrossDims dm;
   int pair, pairs, splits;     // tiles of an item (1 or 2), items of a key head of a sample, parts of the keys
+  CxDiv by_pairs, by_splits;
   int items;
   float* lse;                  // or NULL
   float *part, *part_lse;      // splits > 1: [part][batch][heads][tokens][d] O / l, and the sums' log2
@@ -69,17 +70,17 @@ template <int N> struct Place {
 struct Item { int b, g, part, tile, has_b, keys, j0, j1; };
 __device__ __forceinline__ Item item_of(const CrossParams& P, int it) {
   Item x;
-  int rest = it / P.pairs;
+  const int rest = P.by_pairs(it);
   x.tile = (it - rest * P.pairs) * P.pair;
   x.has_b = P.pair == 2 && x.tile + 1 < P.dm.tiles;
-  const int bg = rest / P.splits;
+  const int bg = P.by_splits(rest);
   x.part = rest - bg * P.splits;
-  x.b = bg / P.dm.G;
+  x.b = P.dm.by_G(bg);
   x.g = bg - x.b * P.dm.G;
   x.keys = cx_keys(P.dm, x.b);
-  const long long nk = (x.keys + KEYS - 1) / KEYS;
-  x.j0 = (int)(nk * x.part / P.splits);
-  x.j1 = (int)(nk * (x.part + 1) / P.splits);
+  const int nk = (x.keys + KEYS - 1) / KEYS;
+  x.j0 = cx_first(nk, x.part, P.splits, P.by_splits);
+  x.j1 = cx_first(nk, x.part + 1, P.splits, P.by_splits);
   return x;
 }
 
@@ -566,6 +567,7 @@ void shape_of(const ff_cross_attention_config_t& c, int64_t batch, int64_t queri
       if (D->group % n == 0) { D->bn = (int)queries; D->bh = n; }
   D->n_tiles = (int)((queries + D->bn - 1) / D->bn);
   D->tiles = D->n_tiles * (D->group / D->bh);
+  D->by_n_tiles = cx_div(D->n_tiles); D->by_tiles = cx_div(D->tiles); D->by_G = cx_div(D->G);
   D->scale = c.scale > 0.f ? c.scale : (float)(1.0 / sqrt((double)c.head_dim));
   D->sl2 = (float)(D->scale * 1.4426950408889634);
 }
@@ -748,7 +750,7 @@ extern "C" ff_status_t ff_cross_attention_forward(ff_cross_attention_t* h, int64
   shape_of(c, batch, queries, keys, &P.dm);
   keys_of(&P.dm, h, q, k, v, lengths, mask);
   const Forward f = forward_of(P.dm, lengths != nullptr);
-  P.pair = f.pair; P.pairs = f.pairs; P.splits = f.splits;
+  P.pair = f.pair; P.pairs = f.pairs; P.splits = f.splits; P.by_pairs = cx_div(f.pairs); P.by_splits = cx_div(f.splits);
   const long long items = (long long)P.dm.B * P.dm.G * f.pairs * f.splits;
   P.items = (int)items;
   P.lse = lse;

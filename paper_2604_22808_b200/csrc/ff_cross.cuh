@@ -17,12 +17,29 @@ struct ff_cross_attention {
 
 constexpr int CX_TILE = 128;
 
+// x / d for 0 <= x < 2^31 as a product (Granlund and Montgomery 1994): with 2^s >= d > 2^(s-1) and m = (2^(31+s) + e) / d, 0 < e <= d, the product
+// x m / 2^(31+s) is above x / d by less than 1 / d.  A kernel's roles each find their items' places by four or five divisions one after the other:
+// 1200 cycles for each item as plain divisions.
+struct CxDiv {
+  unsigned m;
+  int shift;
+#if defined(__CUDACC__)
+  __device__ __forceinline__ int operator()(int x) const { return (int)((unsigned long long)(unsigned)x * m >> shift); }
+#endif
+};
+inline CxDiv cx_div(int d) {
+  int s = 0;
+  while (s < 31 && (1ll << s) < d) ++s;
+  return CxDiv{d > 0 ? (unsigned)((1ull << (31 + s)) / (unsigned)d + 1) : 0u, 31 + s};
+}
+
 struct CrossDims {
   int B, H, G, group;          // samples, heads, key heads, heads of a key head
   int N, K, d;                 // query tokens, keys, channels
   int bn, bh;                  // tokens and heads of a tile of queries
   int n_tiles, tiles;          // tiles along the tokens, tiles of a key head of a sample
   int once[3][2];              // q, k, v: coordinate factors (0: the same rows for all) of batch and head
+  CxDiv by_n_tiles, by_tiles, by_G;
   const int* lengths;
   const uint8_t* mask;
   float scale, sl2;            // scale; scale * log2(e)
@@ -35,6 +52,11 @@ __device__ __forceinline__ int cx_keys(const CrossDims& D, int b) {
   if (!D.lengths) return D.K;
   const int n = __ldg(D.lengths + b);
   return n < 0 ? 0 : n < D.K ? n : D.K;
+}
+// The first of n steps that part `part` of `parts` has: n part / parts.
+__device__ __forceinline__ int cx_first(int n, int part, int parts, const CxDiv& by_parts) {
+  const int each = by_parts(n);
+  return each * part + by_parts((n - each * parts) * part);
 }
 // A value that all lanes have, from the first of them: so the compiler knows that they do, and keeps what follows from it (loops over tiles,
 // operands of the tensor core's instructions) in registers of the warp.  Otherwise each operand is moved there for each instruction.
@@ -70,7 +92,7 @@ __device__ __forceinline__ CxValid64 cx_valid64(const CrossDims& D, int b, int k
 }
 // First head and token of tile t of key head g.
 __device__ __forceinline__ void cx_place(const CrossDims& D, int g, int t, int& h0, int& n0) {
-  const int pack = t / D.n_tiles;
+  const int pack = D.by_n_tiles(t);
   h0 = g * D.group + pack * D.bh;
   n0 = (t - pack * D.n_tiles) * D.bn;
 }

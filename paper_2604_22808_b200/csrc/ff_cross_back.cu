@@ -8,10 +8,10 @@
 // one launch would need), and in return every sum has one owner and one order.
 //
 // dq: a CTA takes a tile of queries (of a part of the keys, where tiles are few).
-//   warp 0       TMA producer: Q, dout, out (into the stage), tiles of K (three stages) and V (one)
+//   warp 0       TMA producer: Q, dout, out (with 128 channels into the stage), tiles of K (three places) and V (one, or two of 64 channels)
 //   warp 1       tcgen05.mma issuer: S = Q K^T into two buffers in turns, dP = dout V^T
 //   warp 2       zeros in rows of K whose keys do not count, in tiles that may hold such rows
-//   warp 3       tcgen05.mma issuer: dQ += dS K (dS from tensor memory, K as an MN-major operand)
+//   warp 3       tcgen05.mma issuer: dQ += dS K (dS from tensor memory, K as an MN-major operand); sends dQ out of the stage
 //   warps 4..11  a thread per query row and half of the keys: P, then dS as bf16 over the scores; D at the item's first tile, from dout
 //                and out in shared memory.  (Warpgroups that took whole tiles in turns: 70 instead of 60 us for 16K queries, 6 heads of
 //                128, 512 keys.)
@@ -38,6 +38,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 struct QueryParams {
   CrossDims dm;
   int splits, items;           // parts of the keys
+  CxDiv by_splits;
   const float* lse;
   float* delta;                // [batch][heads][queries]: D, for the other launch
   float* part;                 // splits > 1: [part][batch][heads][tokens][d]
@@ -46,6 +47,7 @@ struct QueryParams {
 struct KeyParams {
   CrossDims dm;
   int key_tiles, chunks, items;  // parts of the query tiles
+  CxDiv by_key_tiles, by_chunks;
   const float *lse, *delta;
   float *part_k, *part_v;      // chunks > 1: [part][batch][kv_heads][keys][d]
   char *dk, *dv;               // and strides in bytes, for tiles whose keys do not count
@@ -57,7 +59,7 @@ struct QueryShared {
   uint64_t q_full[2], q_empty[2], o_full, d_full, staged, stage_free;
   uint64_t k_full[3], k_empty[3], k_raw[3], v_full[2], v_empty[2];
   float d[2][TILE];                                          // sums of either half of the channels
-  uint64_t s_full[2], ds_full[2], dp_full, dp_empty, dq_full, dq_empty;
+  uint64_t s_full[2], ds_full[2], dp_full, dp_empty, dq_full;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -66,16 +68,16 @@ constexpr size_t QUERY_SMEM = 7 * TILE_BYTES + sizeof(QueryShared) + 1024;
 struct QueryItem { int b, g, part, tile, keys, j0, j1; };
 __device__ __forceinline__ QueryItem query_item(const QueryParams& P, int it) {
   QueryItem x;
-  int rest = it / P.dm.tiles;
+  const int rest = P.dm.by_tiles(it);
   x.tile = it - rest * P.dm.tiles;
-  const int bg = rest / P.splits;
+  const int bg = P.by_splits(rest);
   x.part = rest - bg * P.splits;
-  x.b = bg / P.dm.G;
+  x.b = P.dm.by_G(bg);
   x.g = bg - x.b * P.dm.G;
   x.keys = cx_keys(P.dm, x.b);
-  const long long nk = (x.keys + TILE - 1) / TILE;
-  x.j0 = (int)(nk * x.part / P.splits);
-  x.j1 = (int)(nk * (x.part + 1) / P.splits);
+  const int nk = (x.keys + TILE - 1) / TILE;
+  x.j0 = cx_first(nk, x.part, P.splits, P.by_splits);
+  x.j1 = cx_first(nk, x.part + 1, P.splits, P.by_splits);
   return x;
 }
 
@@ -88,7 +90,8 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
   uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   constexpr int BYTES = TILE * HD * 2, NQ = HD == 64 ? 2 : 1;         // places of queries (with dout) and of values
   uint8_t *sQ = smem, *sG = sQ + NQ * BYTES, *sK = sG + NQ * BYTES, *sV = sK + 3 * BYTES, *stage = sV + NQ * BYTES;
-  static_assert((3 * NQ + 4) * BYTES <= 7 * TILE_BYTES, "");
+  uint8_t* sO = HD == 64 ? stage + BYTES : stage;            // (128 channels leave no room beside the stage)
+  static_assert((3 * NQ + 4) * BYTES + (HD == 64 ? BYTES : 0) <= 7 * TILE_BYTES, "");
   QueryShared& sh = *(QueryShared*)(smem + 7 * TILE_BYTES);
   const CrossDims& D = P.dm;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -100,7 +103,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     mbar_init(&sh.d_full, 256); mbar_init(&sh.staged, 256); mbar_init(&sh.stage_free, 1);
     for (int i = 0; i < 3; ++i) { mbar_init(&sh.k_full[i], 1); mbar_init(&sh.k_empty[i], 1); mbar_init(&sh.k_raw[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.ds_full[i], 256); }
-    mbar_init(&sh.dp_full, 1); mbar_init(&sh.dp_empty, 256); mbar_init(&sh.dq_full, 1); mbar_init(&sh.dq_empty, 256);
+    mbar_init(&sh.dp_full, 1); mbar_init(&sh.dp_empty, 256); mbar_init(&sh.dq_full, 1);
     sh.abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&map_q); tma_prefetch_desc(&map_k); tma_prefetch_desc(&map_v);
@@ -159,11 +162,11 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             cx_prefetch(HALVES, &map_dout, n1, h1, y.b);
             cx_prefetch(HALVES, &map_out, n1, h1, y.b);
           }
-          // (behind the first keys and values: the stage may still be on its way out)
-          if (ok && iter >= 1) ok = mbar_wait(&sh.stage_free, (iter - 1) & 1, abort_flag);
+          // (behind the first keys and values: their place may be the stage, and still be on its way out)
+          if (ok && iter >= 1) ok = mbar_wait(HD == 64 ? &sh.d_full : &sh.stage_free, (iter - 1) & 1, abort_flag);
           if (!ok) break;
           mbar_arrive_expect_tx(&sh.o_full, q_bytes);
-          cx_load(stage, HALF_BYTES, HALVES, &map_out, &sh.o_full, n0, h0, x.b);
+          cx_load(sO, HALF_BYTES, HALVES, &map_out, &sh.o_full, n0, h0, x.b);
           for (int j = x.j0 + 1; j < x.j1 && ok; ++j) {
             load_keys(x, j);
             if (ok) load_values(x, j);
@@ -220,7 +223,6 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         const QueryItem x = query_item(P, it);
         const int nk = cx_uniform(x.j1 - x.j0);
         if (nk == 0) continue;
-        if (iter >= 1) ok = mbar_wait_warp(&sh.dq_empty, (iter - 1) & 1, abort_flag);
         for (int i = 0; i < nk && ok; ++i, ++g) {
           ok = mbar_wait_warp(&sh.ds_full[g & 1], (g >> 1) & 1, abort_flag);
           if (!ok) break;
@@ -230,9 +232,25 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           umma_ts4(tm + 384, tm + (g & 1) * 128 + 64, kd + (uint64_t)(4 * (2048 >> 4)), idesc_q, 1u);    // (dS of either half of the keys)
           umma_commit(&sh.k_empty[g % 3]);
         }
-        if (ok) umma_commit(&sh.dq_full);
+        if (!ok) break;
+        umma_commit(&sh.dq_full);
+        // dQ has been read and lies in the stage: out with it, which takes less time than the next item's first dS
+        ok = mbar_wait_warp(&sh.staged, iter & 1, abort_flag);
+        if (ok && lane == 0) {
+          if (P.splits == 1) {
+            int h0, n0;
+            cx_place(D, x.g, x.tile, h0, n0);
+            tma_store_4d(stage, &map_dq, 0, n0, h0, x.b);
+            if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_dq, 64, n0, h0, x.b);
+            bulk_commit();
+            bulk_wait_read0();
+          }
+          mbar_arrive(&sh.stage_free);
+        }
+        __syncwarp();
         ++iter;
       }
+      if (lane == 0) bulk_wait0();
     } else if (warp == 2) {
       // ------------------------------------------------------------------ rows of K that do not count
       unsigned g = 0, raw[3] = {0, 0, 0};
@@ -263,11 +281,20 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     const int rows = D.bn * D.bh;
     const int row_h = row / D.bn, row_n = row - row_h * D.bn;
     unsigned iter = 0, g = 0;
-    bool ok = true, stored = false;
+    bool ok = true;
+    auto nlse2_of = [&](int it) {                            // (rows that are not there: P = 0)
+      if (it >= P.items) return 0.f;
+      const QueryItem x = query_item(P, it);
+      int h0, n0;
+      cx_place(D, x.g, x.tile, h0, n0);
+      return row < rows && n0 + row_n < D.N ? -P.lse[((long long)x.b * D.H + h0 + row_h) * D.N + n0 + row_n] * LOG2E : -INFINITY;
+    };
+    float next = nlse2_of(blockIdx.x);
     for (int it = blockIdx.x; it < P.items && ok; it += gridDim.x) {
       const QueryItem x = query_item(P, it);
       int h0, n0;
       cx_place(D, x.g, x.tile, h0, n0);
+      const float nlse2 = next;
       const bool here = row < rows && n0 + row_n < D.N;
       const long long at = ((long long)x.b * D.H + h0 + row_h) * D.N + n0 + row_n;
       const int c0 = wg * (HD / 2);                          // at the end each warpgroup has half of the columns
@@ -282,13 +309,9 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
               *(uint4*)(P.dq + x.b * P.sb + (h0 + row_h) * P.sh + (long long)(n0 + row_n) * P.sn + c * 2) = make_uint4(0, 0, 0, 0);
             }
           }
+        next = nlse2_of(it + gridDim.x);
         continue;
       }
-      if (stored) {                                          // the item before has left the stage
-        if (wg == 0 && row == 0) { bulk_wait_read0(); mbar_arrive(&sh.stage_free); }
-        stored = false;
-      }
-      const float nlse2 = here ? -P.lse[at] * LOG2E : -INFINITY;        // (rows that are not there: P = 0)
       float delta = 0.f;
       for (int j = x.j0; j < x.j1 && ok; ++j, ++g) {
         const bool full = !D.mask && (j + 1) * TILE <= x.keys;
@@ -315,7 +338,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
           ok = mbar_wait_warp(&sh.q_full[iter % NQ], (iter / NQ) & 1, abort_flag) && mbar_wait_warp(&sh.o_full, iter & 1, abort_flag);
           if (!ok) break;
           const uint8_t* g_row = sG + iter % NQ * BYTES + (HALVES > 1 ? wg * HALF_BYTES : 0) + row * 128;
-          const uint8_t* o_row = stage + (HALVES > 1 ? wg * HALF_BYTES : 0) + row * 128;
+          const uint8_t* o_row = sO + (HALVES > 1 ? wg * HALF_BYTES : 0) + row * 128;
           float2 d2 = make_float2(0.f, 0.f);
 #pragma unroll
           for (int c = 0; c < 4 * HALVES; ++c) {
@@ -346,29 +369,34 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         tmem_wait_ld();
         tc_fence_before();
         mbar_arrive(&sh.dp_empty);
+        uint32_t pk[2][16];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t pk[16];
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float2 v = __fmul2_rn(make_float2(__uint_as_float(p[c][2 * i]), __uint_as_float(p[c][2 * i + 1])),
                                         __fadd2_rn(make_float2(__uint_as_float(r[c][2 * i]), __uint_as_float(r[c][2 * i + 1])), nd2));
-            float lo = v.x, hi = v.y;
-            if (!full) {
-              const int bit = wg * 16 + c * 8 + (i >> 1);
-              if (!(valid.w[(2 * i) & 3] >> bit & 1)) lo = 0.f;
-              if (!(valid.w[(2 * i + 1) & 3] >> bit & 1)) hi = 0.f;
-            }
-            pk[i] = bf16_pair(__float_as_uint(lo), __float_as_uint(hi));
+            pk[c][i] = bf16_pair(__float_as_uint(v.x), __float_as_uint(v.y));
           }
-          tmem_st16(at_s + c * 16, pk);
+        if (!full) {                                         // zeros, whatever stands in K and V there
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int bit = wg * 16 + c * 8 + (i >> 1);
+              if (!(valid.w[(2 * i) & 3] >> bit & 1)) pk[c][i] &= 0xffff0000u;
+              if (!(valid.w[(2 * i + 1) & 3] >> bit & 1)) pk[c][i] &= 0xffffu;
+            }
         }
+        tmem_st16(at_s, pk[0]);
+        tmem_st16(at_s + 16, pk[1]);
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&sh.ds_full[g & 1]);
       }
       if (!ok) break;
-      ok = mbar_wait_warp(&sh.dq_full, iter & 1, abort_flag);
+      next = nlse2_of(it + gridDim.x);
+      ok = (HD == 128 || iter == 0 || mbar_wait_warp(&sh.stage_free, (iter - 1) & 1, abort_flag)) && mbar_wait_warp(&sh.dq_full, iter & 1, abort_flag);
       if (!ok) break;
       tc_fence_after();
       ++iter;
@@ -387,21 +415,9 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
       }
       tc_fence_before();
-      mbar_arrive(&sh.dq_empty);
       fence_proxy_async();
       mbar_arrive(&sh.staged);
-      if (warp == 4) {
-        ok = mbar_wait_warp(&sh.staged, (iter - 1) & 1, abort_flag);
-        if (!ok) break;
-        if (!part && lane == 0) {
-          tma_store_4d(stage, &map_dq, 0, n0, h0, x.b);
-          if (HALVES > 1) tma_store_4d(stage + HALF_BYTES, &map_dq, 64, n0, h0, x.b);
-          bulk_commit();
-        }
-      }
-      stored = true;
     }
-    if (wg == 0 && row == 0) bulk_wait0();
   }
 
   // ------------------------------------------------------------------ teardown
@@ -433,15 +449,15 @@ constexpr size_t KEY_SMEM = 6 * TILE_BYTES + sizeof(KeyShared) + 1024;
 struct KeyItem { int b, g, chunk, j, keys, t0, t1; };
 __device__ __forceinline__ KeyItem key_item(const KeyParams& P, int it) {
   KeyItem x;
-  int rest = it / P.key_tiles;
+  const int rest = P.by_key_tiles(it);
   x.j = it - rest * P.key_tiles;
-  const int bg = rest / P.chunks;
+  const int bg = P.by_chunks(rest);
   x.chunk = rest - bg * P.chunks;
-  x.b = bg / P.dm.G;
+  x.b = P.dm.by_G(bg);
   x.g = bg - x.b * P.dm.G;
   x.keys = cx_keys(P.dm, x.b);
-  x.t0 = (int)((long long)P.dm.tiles * x.chunk / P.chunks);
-  x.t1 = (int)((long long)P.dm.tiles * (x.chunk + 1) / P.chunks);
+  x.t0 = cx_first(P.dm.tiles, x.chunk, P.chunks, P.by_chunks);
+  x.t1 = cx_first(P.dm.tiles, x.chunk + 1, P.chunks, P.by_chunks);
   if (x.j * TILE >= x.keys) x.t1 = x.t0;                     // no key of the tile counts
   return x;
 }
@@ -863,7 +879,7 @@ cudaError_t cx_backward(const CrossDims& D, const ff_heads_t* q, const ff_heads_
   if (dq) {
     if (!cx_map(&mdq, dq, D.B, D.N, D.d, D.bn, D.bh)) return cudaErrorInvalidValue;
     QueryParams P{};
-    P.dm = D; P.splits = z.splits;
+    P.dm = D; P.splits = z.splits; P.by_splits = cx_div(z.splits);
     P.items = D.B * D.G * D.tiles * z.splits;
     P.lse = lse; P.delta = delta; P.part = part_q;
     const Rows r = rows_of(dq);
@@ -882,7 +898,7 @@ cudaError_t cx_backward(const CrossDims& D, const ff_heads_t* q, const ff_heads_
   if (e != cudaSuccess || !dk || D.K == 0) return e;
   if (!cx_map(&mdk, dk, D.B, D.K, D.d, TILE, 1) || !cx_map(&mdv, dv, D.B, D.K, D.d, TILE, 1)) return cudaErrorInvalidValue;
   KeyParams P{};
-  P.dm = D; P.key_tiles = z.key_tiles; P.chunks = z.chunks;
+  P.dm = D; P.key_tiles = z.key_tiles; P.chunks = z.chunks; P.by_key_tiles = cx_div(z.key_tiles); P.by_chunks = cx_div(z.chunks);
   P.items = D.B * D.G * z.key_tiles * z.chunks;
   P.lse = lse; P.delta = delta; P.part_k = part_k; P.part_v = part_v;
   const Rows rk = rows_of(dk), rv = rows_of(dv);
