@@ -330,7 +330,8 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
         int h0, n0;
         cx_place(D, x.g, x.tile + sx, h0, n0);
-        work = __any_sync(0xffffffffu, row / D.bn < D.bh && n0 + row % D.bn < D.N);
+        const int row_h = D.by_bn(row);
+        work = __any_sync(0xffffffffu, row_h < D.bh && n0 + row - row_h * D.bn < D.N);
         b = x.b; from = x.j0 * KEYS; keys = x.keys < x.j1 * KEYS ? x.keys : x.j1 * KEYS;       // (of this part)
       }
       const bool some = from < keys;
@@ -428,7 +429,7 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       asm volatile("" : "+r"(again));
       const Item x = item_of(P, again);
       cx_place(D, x.g, x.tile + sx, h0, n0);
-      const int row_h = row / D.bn, row_n = row - row_h * D.bn;
+      const int row_h = D.by_bn(row), row_n = row - row_h * D.bn;
       const bool here = row_h < D.bh && n0 + row_n < D.N;
       const float inv = 1.f / l;
       const long long at = ((long long)x.b * D.H + h0 + row_h) * D.N + n0 + row_n;
@@ -567,7 +568,7 @@ void shape_of(const ff_cross_attention_config_t& c, int64_t batch, int64_t queri
       if (D->group % n == 0) { D->bn = (int)queries; D->bh = n; }
   D->n_tiles = (int)((queries + D->bn - 1) / D->bn);
   D->tiles = D->n_tiles * (D->group / D->bh);
-  D->by_n_tiles = cx_div(D->n_tiles); D->by_tiles = cx_div(D->tiles); D->by_G = cx_div(D->G);
+  D->by_bn = cx_div(D->bn); D->by_n_tiles = cx_div(D->n_tiles); D->by_tiles = cx_div(D->tiles); D->by_G = cx_div(D->G);
   D->scale = c.scale > 0.f ? c.scale : (float)(1.0 / sqrt((double)c.head_dim));
   D->sl2 = (float)(D->scale * 1.4426950408889634);
 }

@@ -39,7 +39,7 @@ struct CrossDims {
   int bn, bh;                  // tokens and heads of a tile of queries
   int n_tiles, tiles;          // tiles along the tokens, tiles of a key head of a sample
   int once[3][2];              // q, k, v: coordinate factors (0: the same rows for all) of batch and head
-  CxDiv by_n_tiles, by_tiles, by_G;
+  CxDiv by_bn, by_n_tiles, by_tiles, by_G;
   const int* lengths;
   const uint8_t* mask;
   float scale, sl2;            // scale; scale * log2(e)

@@ -279,7 +279,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_addr = tm + lane_addr + wg * 64, dp_addr = s_addr + 256, dq_addr = tm + lane_addr + 384;
     const int rows = D.bn * D.bh;
-    const int row_h = row / D.bn, row_n = row - row_h * D.bn;
+    const int row_h = D.by_bn(row), row_n = row - row_h * D.bn;
     unsigned iter = 0, g = 0;
     bool ok = true;
     auto nlse2_of = [&](int it) {                            // (rows that are not there: P = 0)
@@ -608,7 +608,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
           float l[4], d[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int row = lane + 32 * i, rh = row / D.bn, rn = row - rh * D.bn;
+            const int row = lane + 32 * i, rh = D.by_bn(row), rn = row - rh * D.bn;
             const bool here = row < rows && n0 + rn < D.N;
             const long long at = ((long long)x.b * D.H + h0 + rh) * D.N + n0 + rn;
             l[i] = here ? -P.lse[at] * LOG2E : -INFINITY;    // (rows that are not there: P = 0)
