@@ -138,6 +138,10 @@ __device__ __forceinline__ void cx_stage(uint8_t* half, int row, int c, const ui
 
 // A map over the rows of head rows: [batch][heads][tokens][head_dim] with boxes of 64 channels, `rows` tokens and `heads` heads.
 bool cx_map(CUtensorMap* map, const ff_heads_t* t, int64_t batch, int64_t tokens, int d, int rows, int heads);
+// At most eight query rows for a key head: a kernel of its own, and what it is expected to take (never where it cannot).
+cudaError_t cx_few_init();
+double cx_few_us(const CrossDims& D);
+cudaError_t cx_few_forward(const CrossDims& D, const ff_heads_t* q, const ff_heads_t* k, const ff_heads_t* v, const ff_heads_t* out, float* lse, cudaStream_t st);
 cudaError_t cx_backward_init();
 cudaError_t cx_backward(const CrossDims& D, const ff_heads_t* q, const ff_heads_t* k, const ff_heads_t* v, const ff_heads_t* out, const float* lse,
                         const ff_heads_t* dout, const ff_heads_t* dq, const ff_heads_t* dk, const ff_heads_t* dv, void* ws, cudaStream_t st);
