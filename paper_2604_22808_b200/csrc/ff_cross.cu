@@ -280,9 +280,8 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       while (now.there && ok) {
         Cursor ahead = now;
         ahead.next(P);
-        // The next tile's scores first, unless they are of an item whose queries are still on their way.
-        bool early = ahead.there;
-        if (early && ahead.first && mine(ahead)) early = __all_sync(0xffffffffu, mbar_try_wait(&sh.q_full[sx], begun & 1));
+        // The next tile's scores first, but those of another item behind this one's last product, for which the softmax warps wait.
+        const bool early = ahead.there && !ahead.first;
         if (early) ok = scores(ahead);
         if (ok) ok = product(now);
         if (ok && ahead.there && !early) ok = scores(ahead);
