@@ -176,6 +176,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       }
     } else if (warp == 1) {
       // ------------------------------------------------------------------ MMA issuer
+      const int sixteens = (D.d + 15) / 16;                  // of the channels: the products leave out what is zero behind them
       const uint32_t idesc_s = idesc_bf16_f32(TILE, TILE, false, false);
       const uint64_t q_desc = smem_desc_sw128(smem_u32(sQ), 16, 1024), g_desc = smem_desc_sw128(smem_u32(sG), 16, 1024);
       const uint64_t k_desc = smem_desc_sw128(smem_u32(sK), 16, 1024), v_desc = smem_desc_sw128(smem_u32(sV), 16, 1024);
@@ -183,7 +184,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       bool ok = true;
       auto score = [&](uint32_t d_tm, uint64_t a, uint64_t b) {
 #pragma unroll
-        for (int k = 0; k < HALVES; ++k) umma_ss4(d_tm, a + (uint64_t)(k * (HALF_BYTES >> 4)), b + (uint64_t)(k * (HALF_BYTES >> 4)), idesc_s, k > 0 ? 1u : 0u);
+        for (int k = 0; k < HALVES; ++k) umma_ss_up_to_4(d_tm, a + (uint64_t)(k * (HALF_BYTES >> 4)), b + (uint64_t)(k * (HALF_BYTES >> 4)), idesc_s, k > 0 ? 1u : 0u, sixteens - k * 4);
       };
       // (the buffer's dS has been read when the keys of two tiles before are free; their place was filled, so that turn has ended)
       auto issue_s = [&](unsigned gt) -> bool {
@@ -215,7 +216,7 @@ cross_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant
       }
     } else if (warp == 3) {
       // ------------------------------------------------------------------ dQ += dS K
-      const uint32_t idesc_q = idesc_bf16_f32(TILE, HD, false, true);
+      const uint32_t idesc_q = idesc_bf16_f32(TILE, (D.d + 15) / 16 * 16, false, true);
       const uint64_t km_desc = smem_desc_sw128(smem_u32(sK), HALF_BYTES, 1024);
       unsigned iter = 0, g = 0;
       bool ok = true;
@@ -536,8 +537,9 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       }
     } else if (warp == 1) {
       // ------------------------------------------------------------------ MMA issuer
+      const int sixteens = (D.d + 15) / 16;                  // of the channels: the products leave out what is zero behind them
       const uint32_t idesc_s = idesc_bf16_f32(TILE, TILE, false, false);
-      const uint32_t idesc_d = idesc_bf16_f32(TILE, HD, false, true);
+      const uint32_t idesc_d = idesc_bf16_f32(TILE, sixteens * 16, false, true);
       const uint64_t k_desc = smem_desc_sw128(smem_u32(sK), 16, 1024), v_desc = smem_desc_sw128(smem_u32(sV), 16, 1024);
       const uint64_t q_desc = smem_desc_sw128(smem_u32(sQ), 16, 1024), g_desc = smem_desc_sw128(smem_u32(sG), 16, 1024);
       const uint64_t qm_desc = smem_desc_sw128(smem_u32(sQ), HALF_BYTES, 1024), gm_desc = smem_desc_sw128(smem_u32(sG), HALF_BYTES, 1024);
@@ -545,7 +547,7 @@ cross_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
       bool ok = true;
       auto score = [&](uint32_t d_tm, uint64_t a, uint64_t b) {
 #pragma unroll
-        for (int k = 0; k < HALVES; ++k) umma_ss4(d_tm, a + (uint64_t)(k * (HALF_BYTES >> 4)), b + (uint64_t)(k * (HALF_BYTES >> 4)), idesc_s, k > 0 ? 1u : 0u);
+        for (int k = 0; k < HALVES; ++k) umma_ss_up_to_4(d_tm, a + (uint64_t)(k * (HALF_BYTES >> 4)), b + (uint64_t)(k * (HALF_BYTES >> 4)), idesc_s, k > 0 ? 1u : 0u, sixteens - k * 4);
       };
       auto issue_s = [&](unsigned gt) -> bool {              // (P^T in its place has been read by dV, issued before)
         const int st = gt & 1;

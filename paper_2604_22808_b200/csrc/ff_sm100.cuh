@@ -285,6 +285,22 @@ __device__ __forceinline__ void umma_ss4(uint32_t d_tmem, uint64_t a_desc, uint6
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// ... or the first n of the four.
+__device__ __forceinline__ void umma_ss_up_to_4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, int n) {
+  asm volatile(
+      "{\n\t.reg .pred p, q, q1, q2, q3;\n\t.reg .b32 al, ah, bl, bh;\n\t.reg .b64 a, b;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\telect.sync _|q, 0xffffffff;\n\tmov.b64 {al, ah}, %1;\n\tmov.b64 {bl, bh}, %2;\n\t"
+      "setp.gt.and.s32 q1, %5, 1, q;\n\tsetp.gt.and.s32 q2, %5, 2, q;\n\tsetp.gt.and.s32 q3, %5, 3, q;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t"
+      "add.u32 al, al, 2;\n\tadd.u32 bl, bl, 2;\n\tmov.b64 a, {al, ah};\n\tmov.b64 b, {bl, bh};\n\t"
+      "@q1 tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n\t"
+      "add.u32 al, al, 2;\n\tadd.u32 bl, bl, 2;\n\tmov.b64 a, {al, ah};\n\tmov.b64 b, {bl, bh};\n\t"
+      "@q2 tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n\t"
+      "add.u32 al, al, 2;\n\tadd.u32 bl, bl, 2;\n\tmov.b64 a, {al, ah};\n\tmov.b64 b, {bl, bh};\n\t"
+      "@q3 tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(n)
+      : "memory");
+}
 // ... with A in tensor memory and B MN-major (a step of 16 is 16 rows of 128 bytes).
 __device__ __forceinline__ void umma_ts4(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
