@@ -18,7 +18,7 @@
 #endif
 
 // Debug build (-DFF_DEBUG): every computed band rank, row offset and tile coordinate of the attention path is range-checked on the device
-// before it is used (the kernels of ff_rotary.cu and ff_ffn.cu have no such checks); a value out of range is not used for the access (the
+// before it is used (the kernels of ff_rotary.cu, ff_ffn.cu, ff_layer_norm.cu and ff_cross*.cu have none); a value out of range is not used for the access (the
 // store or copy is skipped) and FF_ERR_INVALID_ARG together with the kernel's id is raised in the plan's status word, where
 // ff_plan_device_status reports it.  The release build compiles the checks away.
 #if defined(FF_DEBUG) && defined(__CUDACC__)
