@@ -440,7 +440,7 @@ ff_status_t ff_layer_norm_destroy(ff_layer_norm_t *norm);   /* NULL is allowed *
 const char *ff_layer_norm_last_error(const ff_layer_norm_t *norm);   /* as ff_last_error */
 
 /* weight, bias: device, float: [dim] where per_sample is 0, else [batch][dim]; NULL: ones (whatever unit_offset is), zeros.  y may be x (the same address
- * and strides), otherwise it overlaps no input.  batch * tokens below 2^31. */
+ * and strides; with others the call is refused), otherwise it overlaps no input.  batch * tokens below 2^31. */
 ff_status_t ff_layer_norm_forward(const ff_layer_norm_t *norm, int64_t batch, int64_t tokens, const ff_rows_t *x, const float *weight,
                                   const float *bias, int32_t per_sample, const ff_rows_t *y, void *cuda_stream);
 
@@ -487,7 +487,8 @@ const char *ff_cross_attention_last_error(const ff_cross_attention_t *attention)
 
 /* q, out: heads of `queries` tokens; k, v: kv_heads of `keys` tokens.  Addresses and strides (of dimensions longer than one) are
  * multiples of 16 bytes; k and v may have a batch or head stride of 0 (the same states for all).  out may be q (the same
- * address and strides), otherwise it overlaps no input.
+ * address and strides), otherwise it overlaps no input (one that starts where
+ * k or v does, or q in other places, is refused).
  *   lse  device, float [batch][heads][queries], kept for the backward pass; or NULL
  * Sizes: the 128-row tiles of all heads' queries, and as many of keys, below 2^31 - 1024, queries and keys at most 2^31 - 256. */
 ff_status_t ff_cross_attention_forward(ff_cross_attention_t *attention, int64_t batch, int64_t queries, int64_t keys, const ff_heads_t *q,

@@ -9,7 +9,8 @@
 // B, share every tile of keys and values, and while the softmax of one works the tensor core runs the products of the other.
 //   warp 0       TMA producer: the query tiles; tiles of 64 keys and of their values, each through a ring of its own
 //   warps 1, 3   tcgen05.mma issuers of A and B: S_x = Q_x K^T (both from shared memory) into one of two places in turns, O_x += P_x V (P from
-//                tensor memory), in the order QK[j+1], PV[j], on through the items.  (One warp for both was the limit, and so were more commits
+//                tensor memory), in the order QK[j+1], PV[j], but an item's last PV before the next item's first QK, since its softmax warps
+//                wait for it (16K queries, 12 heads, 8192 keys 845 -> 788 us).  (One warp for both was the limit, and so were more commits
 //                than the one for the scores: some 32 cycles an instruction, 150 a commit or wait.  What else waits for a product
 //                within an item is told by the softmax warps, when they see scores that were asked for behind it.)  Warp 1 owns the tensor memory
 //   warp 2       zeros in rows of V whose keys do not count, in tiles that may hold such rows
@@ -18,7 +19,8 @@
 //                grows by more than 2^8.  At the end O / l goes out through shared memory by TMA.
 // With tiles of 128 keys there is room for one place of scores a stream: the next ones had to wait for the product with the last P, and
 // 64K queries, 24 heads of 128, 512 keys took 578 us; P in shared memory freed that place, but the products then read more from shared memory
-// than it gives (589 us).
+// than it gives (589 us).  Now 454 us (243 at the rate of a large matrix product).  The issuers are the limit, whose products with M = 128, N = 64
+// read more operand bytes a cycle than larger tiles, then the softmax (1070 cycles a tile of its own, 1024 of them the two streams' exponentials).
 // Tensor memory (512 columns): S/P of A and of B, twice 64 each, O of A, O of B.  Every wait is bounded; when one runs out the CTA raises
 // FF_ERR_TIMEOUT in the handle's status word, takes no more work and returns.
 #include <math.h>
@@ -745,6 +747,11 @@ extern "C" ff_status_t ff_cross_attention_forward(ff_cross_attention_t* h, int64
   if (s == FF_OK) s = check_heads(h, out, c.heads, batch, queries, true, false);
   if (s != FF_OK) return s;
   if ((((uintptr_t)lse) | ((uintptr_t)lengths)) & 3) return fail(h, FF_ERR_INVALID_ARG, "lse and lengths must be 4-byte aligned");
+  // (out is written while other tiles still read the keys and values, and queries of other places)
+  if (keys && (out->data == k->data || out->data == v->data)) return fail(h, FF_ERR_INVALID_ARG, "out lies over k or v");
+  if (out->data == q->data && ((batch > 1 && out->stride_batch != q->stride_batch) || (c.heads > 1 && out->stride_head != q->stride_head) ||
+                               (queries > 1 && out->stride_token != q->stride_token)))
+    return fail(h, FF_ERR_INVALID_ARG, "out lies over q with other strides");
   cudaStream_t st = (cudaStream_t)stream;
   CrossParams P{};
   shape_of(c, batch, queries, keys, &P.dm);

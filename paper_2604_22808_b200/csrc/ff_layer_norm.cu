@@ -587,6 +587,11 @@ NormParams common(const ff_layer_norm* h, int64_t batch, int64_t tokens, const f
   return P;
 }
 
+// Does an output lie over an input in other places than the input's own rows?
+bool misplaced(const ff_rows_t* y, const ff_rows_t* x, int64_t batch, int64_t tokens) {
+  return y->data == x->data && ((batch > 1 && y->stride_batch != x->stride_batch) || (tokens > 1 && y->stride_token != x->stride_token));
+}
+
 }  // namespace
 
 extern "C" ff_status_t ff_layer_norm_create(const ff_layer_norm_config_t* cfg, ff_layer_norm_t** out) {
@@ -622,6 +627,7 @@ extern "C" ff_status_t ff_layer_norm_forward(const ff_layer_norm_t* handle, int6
   s = check_rows(h, x, batch, tokens, false, e, &bits);
   if (s == FF_OK) s = check_rows(h, y, batch, tokens, true, e, &bits);
   if (s != FF_OK) return s;
+  if (misplaced(y, x, batch, tokens)) return fail(h, FF_ERR_INVALID_ARG, "y lies over x with other strides");
   const int ch = piece_of(h->cfg.dim, e, bits);
   NormParams P = common(h, batch, tokens, weight, per_sample, ch);
   P.x = view(x, e); P.y = view(y, e);
@@ -655,6 +661,8 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
   if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "the handle is NULL");
   ff_status_t s = check_call(h, batch, tokens, {weight, dweight, dbias});
   if (s != FF_OK) return s;
+  if ((dweight && (dweight == dbias || dweight == weight)) || (dbias && dbias == weight))
+    return fail(h, FF_ERR_INVALID_ARG, "a gradient lies over another one or over the weight");
   cudaStream_t st = (cudaStream_t)stream;
   const int d = h->cfg.dim;
   if (batch * tokens == 0) {                 // sums over no rows
@@ -670,6 +678,8 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
   if (s == FF_OK) s = check_rows(h, dy, batch, tokens, false, e, &bits);
   if (s == FF_OK && dx) s = check_rows(h, dx, batch, tokens, true, e, &bits);
   if (s != FF_OK) return s;
+  if (dx && (misplaced(dx, x, batch, tokens) || misplaced(dx, dy, batch, tokens)))
+    return fail(h, FF_ERR_INVALID_ARG, "dx lies over x or dy with other strides");
   size_t need = 0;
   ff_layer_norm_workspace_bytes(handle, batch, tokens, per_sample, &need);
   if (need && (!ws || ws_bytes < need)) return fail(h, FF_ERR_WORKSPACE, "the workspace is missing or smaller than ff_layer_norm_workspace_bytes");
