@@ -25,14 +25,18 @@ struct ff_layer_norm {
 
 namespace {
 
-// Values of a row that a thread has (in pieces of one value 8, where more of them have to be on their way, or 16).  With 32 instead of 16 the
+// Values of a row that a thread has (in pieces of one value 8, where more of them have to be on their way, or 16; forward in pieces of two 16: 20000 x
+// 1154 bf16 42 us instead of 48, 9999 x 6002 72 instead of 98, backward 45 and 175 instead of 41 and 143).  With 32 instead of 16 the
 // shuffles, barriers and addresses of a row are shared by twice the values: 16384 x 1024 bf16 backward 24 us instead of 30, 32768 x 5120
 // forward 114 instead of 148 (65536 x 2048 forward: 100, with 16 and two rows at a time 89).  Weights and both sums then leave room for
 // one block of eight warps on an SM backward; three blocks of four, which spill, took 36 to 60 us for the former.
 constexpr int VALUES = 32;
 constexpr int MAX_DIM = 8192, MAX_THREADS = 512;
 constexpr int BLOCK_WARPS = 8;                    // warps of a block, unless a team has more
-constexpr int FORWARD_BLOCKS = 2, BACKWARD_BLOCKS = 1;   // such blocks on an SM
+constexpr int BACKWARD_BLOCKS = 1;                // such blocks on an SM
+// Forward, warps on an SM by the registers of their kernels: 64 with up to 8 values a thread, 96 with 16 or with 8 that come one by one, else 128.
+// (16 for all: 11000 x 1155 fp32 33.5 us instead of 25.8, 20000 x 1155 bf16 54 instead of 38.)
+template <int CH, int PER> constexpr int FORWARD_WARPS = CH * PER <= (CH > 1 ? 8 : 4) ? 32 : CH * PER <= (CH > 1 ? 16 : 8) ? 20 : 16;
 template <class T> constexpr int STAGES = sizeof(T) == 4 ? 3 : 4;   // rows of a team on their way or being read
 
 struct RowsView { char* p; long long sb, st; };   // strides in bytes
@@ -254,7 +258,7 @@ struct Way {
 
 // Forward: the teams of blocks s * parts .. (s + 1) * parts - 1 take the rows of segment s in turns.
 template <class T, int CH, int PER, bool FULL, bool WARP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD_BLOCKS : 1) norm_forward_kernel(const __grid_constant__ NormParams P) {
+__global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD_WARPS<CH, PER> / BLOCK_WARPS : 1) norm_forward_kernel(const __grid_constant__ NormParams P) {
   using R = Row<T, CH, PER, FULL>;
   constexpr int N = R::N;
   __shared__ __align__(16) Place<THREADS / 32> place[2];
@@ -497,11 +501,11 @@ Block block_of(int pieces, int per, long long rows) {
 // The rows whose gradients are summed together (the model's, or each sample's) and the blocks they are divided between: one wave of
 // them, and at most one for every `each` rows.
 struct Parts { unsigned segments, rows, parts; };
-Parts parts_of(int64_t batch, int64_t tokens, int per_sample, int threads, int blocks, long long each) {
+Parts parts_of(int64_t batch, int64_t tokens, int per_sample, int blocks, long long each) {
   Parts p;
   p.segments = per_sample ? (unsigned)batch : 1;
   p.rows = (unsigned)(per_sample ? tokens : batch * tokens);
-  const long long most = ((long long)p.rows + each - 1) / each, wave = (long long)FF_B200_SMS * (threads > BLOCK_WARPS * 32 ? 1 : blocks) / (p.segments ? p.segments : 1);
+  const long long most = ((long long)p.rows + each - 1) / each, wave = (long long)FF_B200_SMS * blocks / (p.segments ? p.segments : 1);
   p.parts = (unsigned)(wave < most ? wave : most);
   if (p.parts < 1) p.parts = 1;
   return p;
@@ -517,7 +521,7 @@ cudaError_t allow(void (*kernel)(NormParams), size_t smem) {
 template <class T, int CH, int PER, bool WARP, int THREADS>
 cudaError_t forward(NormParams& P, int64_t batch, int64_t tokens, int per_sample, cudaStream_t st) {
   const Block b = block_of(P.pieces, PER, P.rows);
-  const Parts p = parts_of(batch, tokens, per_sample, b.threads, FORWARD_BLOCKS, b.teams);
+  const Parts p = parts_of(batch, tokens, per_sample, FORWARD_WARPS<CH, PER> * 32 / b.threads, b.teams);
   P.segment = p.rows; P.parts = p.parts; P.team_warps = b.team_warps;
   const size_t smem = ring_bytes<T, CH, PER, 1>(b.threads);
   const bool full = P.pieces == PER * 32 * b.team_warps;
@@ -536,14 +540,14 @@ cudaError_t backward(NormParams& P, unsigned blocks, cudaStream_t st) {
   return e != cudaSuccess ? e : ff_launch(kernel, dim3(blocks), dim3(b.threads), smem, st, P);
 }
 // The team and the pieces of a thread: a warp where it has room for the row, with as few pieces a thread as do, else several warps.
-template <class T, int CH, class Run>
+template <class T, int CH, bool FORWARD, class Run>
 cudaError_t with_team(int pieces, Run run) {
   using std::integral_constant;
+  constexpr int MOST = CH == 1 || (CH == 2 && FORWARD) ? 8 : VALUES / CH;
   using True = integral_constant<bool, true>;
   using False = integral_constant<bool, false>;
   using Small = integral_constant<int, BLOCK_WARPS * 32>;
-  using Large = integral_constant<int, CH == 1 ? MAX_THREADS : MAX_DIM / VALUES>;
-  constexpr int MOST = CH == 1 ? 8 : VALUES / CH;
+  using Large = integral_constant<int, MOST == 8 && CH <= 2 ? MAX_THREADS : MAX_DIM / VALUES>;
   if constexpr (MOST >= 4) if (pieces <= 32 * (MOST / 4)) return run(integral_constant<int, MOST / 4>(), True(), Small());
   if (pieces <= 32 * (MOST / 2)) return run(integral_constant<int, MOST / 2>(), True(), Small());
   if (pieces <= 32 * MOST) return run(integral_constant<int, MOST>(), True(), Small());
@@ -561,7 +565,7 @@ cudaError_t with_piece(int e, int ch, Run run) {
 // Backward: the same blocks whatever the tensors' alignment, so that the workspace does not depend on it.
 Parts backward_parts(const ff_layer_norm_config_t& c, int64_t batch, int64_t tokens, int per_sample) {
   const Block b = block_of(c.dim, VALUES, batch * tokens);
-  return parts_of(batch, tokens, per_sample, b.threads, BACKWARD_BLOCKS, b.teams);
+  return parts_of(batch, tokens, per_sample, BACKWARD_BLOCKS, b.teams);
 }
 
 ff_status_t check_call(ff_layer_norm* h, int64_t batch, int64_t tokens, std::initializer_list<const float*> weights) {
@@ -637,7 +641,7 @@ extern "C" ff_status_t ff_layer_norm_forward(const ff_layer_norm_t* handle, int6
   const cudaError_t err = with_piece(e, ch, [&](auto t, auto piece) {
     using T = decltype(t);
     constexpr int CH = decltype(piece)::value;
-    return with_team<T, CH>(P.pieces, [&](auto per, auto warp, auto threads) {
+    return with_team<T, CH, true>(P.pieces, [&](auto per, auto warp, auto threads) {
       return forward<T, CH, decltype(per)::value, decltype(warp)::value, decltype(threads)::value>(P, batch, tokens, per_sample, st);
     });
   });
@@ -705,7 +709,7 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
   cudaError_t err = with_piece(e, ch, [&](auto t, auto piece) {
     using T = decltype(t);
     constexpr int CH = decltype(piece)::value;
-    return with_team<T, CH>(P.pieces, [&](auto per, auto warp, auto threads) {
+    return with_team<T, CH, false>(P.pieces, [&](auto per, auto warp, auto threads) {
       return backward<T, CH, decltype(per)::value, decltype(warp)::value, decltype(threads)::value>(P, blocks, st);
     });
   });
