@@ -825,7 +825,7 @@ class CrossAttention:
             if sc != 1:
                 raise FFError(1, "the channels of a head must be contiguous")
             at.append(8 * len(rows))
-            rows += (t.data_ptr(), sb, sh, st, t.shape[1])           # (the layout of ff_heads_t, heads in its low half word)
+            rows += (t.data_ptr(), sb, sh, st, c.kv_heads if like_k else c.heads)         # (the layout of ff_heads_t, heads in its low half word)
         rows = array("q", rows)
         base = rows.buffer_info()[0]
         return (qs[0], qs[2], ks[2]), [None if o is None else base + o for o in at], rows
@@ -857,12 +857,13 @@ class CrossAttention:
             _check(self._lib.ff_cross_attention_workspace_bytes(C.byref(self._c), *size, training, C.byref(n)))
             self._sized, self._bytes = (size, training), n.value
         n = self._bytes
-        # (a workspace per call: calls on different streams and captured graphs share none)
-        ws = torch.empty(n, dtype=self._uint8, device=dev)
+        # (a workspace per call that takes one: calls on different streams and captured graphs share none)
+        ws = torch.empty(n, dtype=self._uint8, device=dev) if n else None
+        at = ws.data_ptr() if n else None
         if torch.cuda.current_device() == dev.index:
-            return self._status(fn(self.handle, *size, *args, ws.data_ptr(), n, self._raw_stream(dev.index)))
+            return self._status(fn(self.handle, *size, *args, at, n, self._raw_stream(dev.index)))
         with torch.cuda.device(dev):
-            return self._status(fn(self.handle, *size, *args, ws.data_ptr(), n, self._raw_stream(dev.index)))
+            return self._status(fn(self.handle, *size, *args, at, n, self._raw_stream(dev.index)))
 
     def forward(self, q, k, v, out, lse=None, lengths=None, mask=None):
         """lse (fp32 [batch][heads][queries]): the logarithms of the rows' sums are written there, for backward.  out may be q."""

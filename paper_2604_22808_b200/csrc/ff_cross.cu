@@ -25,6 +25,7 @@
 // FF_ERR_TIMEOUT in the handle's status word, takes no more work and returns.
 #include <math.h>
 #include <stdio.h>
+#include <string.h>
 
 #include <initializer_list>
 #include <new>
@@ -626,8 +627,12 @@ ff_status_t check_call(ff_cross_attention* h, int64_t batch, int64_t queries, in
   if (too_large(h->cfg, batch, queries, keys)) return fail(h, FF_ERR_UNSUPPORTED, MOST);
   int device = -1;
   if (cudaGetDevice(&device) != cudaSuccess || device != h->device) return fail(h, FF_ERR_INVALID_ARG, "the handle belongs to another device than the current one");
-  size_t need = 0;
-  ff_cross_attention_workspace_bytes(&h->cfg, batch, queries, keys, training, &need);
+  const int64_t sizes[4] = {batch, queries, keys, training};
+  if (memcmp(sizes, h->sizes, sizeof sizes)) {               // (estimates that take a microsecond)
+    ff_cross_attention_workspace_bytes(&h->cfg, batch, queries, keys, training, &h->need);
+    memcpy(h->sizes, sizes, sizeof sizes);
+  }
+  const size_t need = h->need;
   if (need && (!ws || ws_bytes < need)) return fail(h, FF_ERR_WORKSPACE, "the workspace is missing or smaller than ff_cross_attention_workspace_bytes");
   if (need && (((uintptr_t)ws) & 255)) return fail(h, FF_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
   return FF_OK;
@@ -688,6 +693,7 @@ extern "C" ff_status_t ff_cross_attention_create(const ff_cross_attention_config
   ff_cross_attention* h = new (std::nothrow) ff_cross_attention();
   if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "out of host memory");
   h->cfg = *cfg;
+  h->sizes[0] = -1;
   cudaError_t e = cudaGetDevice(&h->device);
   for (const void* kernel : {(const void*)cross_forward_kernel<128>, (const void*)cross_forward_kernel<64>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM);

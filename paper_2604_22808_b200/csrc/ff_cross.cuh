@@ -12,6 +12,8 @@ struct ff_cross_attention {
   int device;
   float scale;
   int* status;                 // device
+  int64_t sizes[4];            // batch, queries, keys and training of the last call, and the workspace that it takes
+  size_t need;
   char err[512];
 };
 

@@ -667,8 +667,6 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
   if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "the handle is NULL");
   ff_status_t s = check_call(h, batch, tokens, {weight, dweight, dbias});
   if (s != FF_OK) return s;
-  if ((dweight && (dweight == dbias || dweight == weight)) || (dbias && dbias == weight))
-    return fail(h, FF_ERR_INVALID_ARG, "a gradient lies over another one or over the weight");
   cudaStream_t st = (cudaStream_t)stream;
   const int d = h->cfg.dim;
   if (batch * tokens == 0) {                 // sums over no rows
@@ -690,6 +688,8 @@ extern "C" ff_status_t ff_layer_norm_backward(const ff_layer_norm_t* handle, int
   ff_layer_norm_workspace_bytes(handle, batch, tokens, per_sample, &need);
   if (need && (!ws || ws_bytes < need)) return fail(h, FF_ERR_WORKSPACE, "the workspace is missing or smaller than ff_layer_norm_workspace_bytes");
   if (need && (((uintptr_t)ws) & 15)) return fail(h, FF_ERR_WORKSPACE, "the workspace must be 16-byte aligned");
+  if ((dweight && (dweight == dbias || dweight == weight)) || (dbias && dbias == weight))
+    return fail(h, FF_ERR_INVALID_ARG, "a gradient lies over another one or over the weight");
   if (!dx && !dweight && !dbias) return FF_OK;
   const int ch = piece_of(d, e, bits);
   const Parts parts = backward_parts(h->cfg, batch, tokens, per_sample);
