@@ -7,7 +7,7 @@
 // The mean is subtracted before the squares are summed (the values are in registers, a second sum costs no memory traffic), so
 // rows whose mean is far from zero lose nothing.
 //
-// A team of threads, a warp or a block, takes rows in turns, every thread the same channels of each (16 at most), so that weights, bias and,
+// A team of threads, a warp or a block, takes rows in turns, every thread the same channels of each (32 at most), so that weights, bias and,
 // backward, the gradients' sums of those channels stay in its registers; the next rows are on their way while these are summed.
 #include <stdio.h>
 
