@@ -34,9 +34,9 @@ constexpr int VALUES = 32;
 constexpr int MAX_DIM = 8192, MAX_THREADS = 512;
 constexpr int BLOCK_WARPS = 8;                    // warps of a block, unless a team has more
 constexpr int BACKWARD_BLOCKS = 1;                // such blocks on an SM
-// Forward, warps on an SM by the registers of their kernels: 64 with up to 8 values a thread, 96 with 16 or with 8 that come one by one, else 128.
-// (16 for all: 11000 x 1155 fp32 33.5 us instead of 25.8, 20000 x 1155 bf16 54 instead of 38.)
-template <int CH, int PER> constexpr int FORWARD_WARPS = CH * PER <= (CH > 1 ? 8 : 4) ? 32 : CH * PER <= (CH > 1 ? 16 : 8) ? 20 : 16;
+// Forward, warps on an SM by the registers of their kernels: 64 with up to 8 values a thread (80 where they come one by one), 96 with 16, else 128.
+// (16 for all: 11000 x 1155 fp32 33.5 us instead of 25.6, 20000 x 1155 bf16 54 instead of 36.5.)
+template <int CH, int PER> constexpr int FORWARD_WARPS = CH * PER <= (CH > 1 ? 8 : 4) ? 32 : CH * PER <= (CH > 1 ? 16 : 8) ? (CH > 1 ? 20 : 24) : 16;
 template <class T> constexpr int STAGES = sizeof(T) == 4 ? 3 : 4;   // rows of a team on their way or being read
 
 struct RowsView { char* p; long long sb, st; };   // strides in bytes
@@ -139,24 +139,48 @@ template <class T, int CH, int PER, bool FULL>
 struct Row {
   static constexpr int N = pairs_of(CH);
   using C = Chunk<T, CH>;
-  using V = F2[PER][N];
+  // Pairs of a piece's neighbouring values; of two pieces' single ones (each beside a zero they took 40 registers and a third of the instructions
+  // more: 9999 x 3001 fp32 backward 173 us instead of 98).
+  static constexpr int GROUPS = CH > 1 ? PER : PER / 2;
+  static_assert(CH > 1 || PER % 2 == 0, "");
+  using V = F2[GROUPS][N];
   using M = Mine<CH, PER, FULL>;
+  static __device__ __forceinline__ void put(V& v, int i, const C& piece) {
+    if constexpr (CH > 1) {
+      unpack<T, CH>(piece, v[i]);
+    } else {
+      F2 one[1];
+      unpack<T, 1>(piece, one);
+      v[i / 2][0] = i & 1 ? two(low(v[i / 2][0]), low(one[0])) : two(low(one[0]), 0.f);
+    }
+  }
+  static __device__ __forceinline__ float value(const V& v, int i, int c) {
+    if constexpr (CH > 1) return c & 1 ? high(v[i][c / 2]) : low(v[i][c / 2]);
+    else return i & 1 ? high(v[i / 2][0]) : low(v[i / 2][0]);
+  }
   static __device__ __forceinline__ void load(V& v, const char* row, const M& m) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const C none{};
-      unpack<T, CH>(m.have(i) ? *(const C*)(row + m.at[i] * sizeof(T)) : none, v[i]);
+      put(v, i, m.have(i) ? *(const C*)(row + m.at[i] * sizeof(T)) : none);
     }
   }
   static __device__ __forceinline__ void store(char* row, const V& v, const M& m) {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      if (m.have(i)) *(C*)(row + m.at[i] * sizeof(T)) = pack<T, CH>(v[i]);
+      if (m.have(i)) {
+        if constexpr (CH > 1) {
+          *(C*)(row + m.at[i] * sizeof(T)) = pack<T, CH>(v[i]);
+        } else {
+          const F2 one[1] = {two(value(v, i, 0), 0.f)};
+          *(C*)(row + m.at[i] * sizeof(T)) = pack<T, 1>(one);
+        }
+      }
   }
   static __device__ __forceinline__ float sum(const V& v) {
     F2 s = two(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
       for (int c = 0; c < N; ++c) s = __fadd2_rn(s, v[i][c]);
     return low(s) + high(s);
@@ -164,33 +188,39 @@ struct Row {
   static __device__ __forceinline__ float dot(const V& u, const V& v) {
     F2 s = two(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
       for (int c = 0; c < N; ++c) s = fma(u[i][c], v[i][c], s);
     return low(s) + high(s);
   }
   static __device__ __forceinline__ void times(V& v, float f) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
       for (int c = 0; c < N; ++c) v[i][c] = mul(v[i][c], two(f, f));
   }
   // Values minus `m`, and zeros where the row has none.
   static __device__ __forceinline__ void centre(V& v, float mean, const M& m) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const float mine = m.have(i) ? -mean : 0.f;
+    for (int i = 0; i < GROUPS; ++i) {
+      if constexpr (CH > 1) {
+        const float mine = m.have(i) ? -mean : 0.f;
 #pragma unroll
-      for (int c = 0; c < N; ++c) v[i][c] = __fadd2_rn(v[i][c], two(mine, CH > 1 ? mine : 0.f));
+        for (int c = 0; c < N; ++c) v[i][c] = __fadd2_rn(v[i][c], two(mine, mine));
+      } else {
+        v[i][0] = __fadd2_rn(v[i][0], two(m.have(2 * i) ? -mean : 0.f, m.have(2 * i + 1) ? -mean : 0.f));
+      }
     }
   }
   // Neighbouring weights of a piece, `plus` more, or `none` where there are none.
   static __device__ __forceinline__ void weights(V& w, const float* from, float plus, float none, const M& m) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
-      for (int c = 0; c < N; ++c)
-        w[i][c] = from && m.have(i) ? two(from[m.at[i] + 2 * c] + plus, CH > 1 ? from[m.at[i] + 2 * c + 1] + plus : 0.f) : two(none, none);
+      for (int c = 0; c < N; ++c) {
+        if constexpr (CH > 1) w[i][c] = from && m.have(i) ? two(from[m.at[i] + 2 * c] + plus, from[m.at[i] + 2 * c + 1] + plus) : two(none, none);
+        else w[i][c] = two(from && m.have(2 * i) ? from[m.at[2 * i]] + plus : none, from && m.have(2 * i + 1) ? from[m.at[2 * i + 1]] + plus : none);
+      }
   }
 };
 // A team's rows on their way: every thread copies its own pieces of them into places of its own in shared memory, STAGES - 1 sets of rows
@@ -223,8 +253,8 @@ struct Ring {
   __device__ __forceinline__ void take(int k, typename R::V& v) const {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if constexpr (SHARED) unpack<T, CH>(*place(stage, k, i), v[i]);
-      else unpack<T, CH>(raw[k][i], v[i]);
+      if constexpr (SHARED) R::put(v, i, *place(stage, k, i));
+      else R::put(v, i, raw[k][i]);
     }
   }
   // The stage that has just been read is asked for again, and the next one follows.
@@ -308,7 +338,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD
       r = rsqrtf(fmaf(s[0], P.inv_d, P.eps * DOWN * DOWN));
     }
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int i = 0; i < R::GROUPS; ++i)
 #pragma unroll
       for (int c = 0; c < N; ++c) v[i][c] = fma(mul(v[i][c], two(r, r)), w[i][c], b[i][c]);
     R::store(to.p, v, mine);
@@ -348,7 +378,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWAR
   typename R::V w, dw, db;
   R::weights(w, P.w ? P.w + segment * P.w_stride : nullptr, P.plus, 1.f, mine);
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
+  for (int i = 0; i < R::GROUPS; ++i)
 #pragma unroll
     for (int c = 0; c < N; ++c) dw[i][c] = db[i][c] = two(0.f, 0.f);
 #pragma unroll 1
@@ -366,7 +396,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWAR
       s[0] = R::dot(v, v);
       F2 u = two(0.f, 0.f), t = u;
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
+      for (int i = 0; i < R::GROUPS; ++i)
 #pragma unroll
         for (int c = 0; c < N; ++c) {
           const F2 gw = mul(dy[i][c], w[i][c]);
@@ -392,7 +422,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWAR
     }
     const float mean_g = -s[1] * P.inv_d, mean_gn = -s[2] * scale * P.inv_d;
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int i = 0; i < R::GROUPS; ++i)
 #pragma unroll
       for (int c = 0; c < N; ++c) {
         const F2 n = mul(v[i][c], two(scale, scale));
@@ -416,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWAR
     for (int i = 0; i < PER; ++i) {
       if (mine.have(i))
 #pragma unroll
-        for (int c = 0; c < CH; ++c) joined[team.index * P.d + mine.at[i] + c] = c & 1 ? high(v[i][c / 2]) : low(v[i][c / 2]);
+        for (int c = 0; c < CH; ++c) joined[team.index * P.d + mine.at[i] + c] = R::value(v, i, c);
     }
     __syncthreads();
     for (int c = threadIdx.x; c < P.d; c += blockDim.x) {
@@ -562,12 +592,15 @@ cudaError_t with_piece(int e, int ch, Run run) {
                  : ch == 2 ? run(__nv_bfloat16(), std::integral_constant<int, 2>()) : run(__nv_bfloat16(), std::integral_constant<int, 1>());
 }
 
-// Backward: the same blocks whatever the tensors' alignment, so that the workspace does not depend on it.  Kernels of rows of up to 256 values (128 where
-// they come one by one) have 100 registers, and two blocks on an SM: 30000 x 128 bf16 13.6 us instead of 16.4.
+// Backward: the same blocks whatever the tensors' alignment, so that the workspace does not depend on it.  Kernels of rows of up to 256 values have
+// 100 to 130 registers, and two blocks on an SM: 30000 x 128 bf16 13.6 us instead of 16.4.  Longer ones that come one by one, 8 of a thread, have 140,
+// for 14 warps on an SM: 9999 x 1155 bf16 42 us instead of 73 with one block of a team of five.
 Parts backward_parts(const ff_layer_norm_config_t& c, int64_t batch, int64_t tokens, int per_sample) {
-  const Block b = block_of(c.dim, VALUES, batch * tokens);
-  const bool light = c.dim <= (c.dim % (c.dtype == FF_FP32 ? 4 : 2) ? 128 : 256);
-  return parts_of(batch, tokens, per_sample, light ? 2 * BACKWARD_BLOCKS : BACKWARD_BLOCKS, b.teams);
+  const bool single = c.dim % (c.dtype == FF_FP32 ? 4 : 2) != 0, light = c.dim <= 256;
+  const bool eights = single && !light && c.dim <= 8 * 32 * BLOCK_WARPS;
+  const Block b = block_of(c.dim, eights ? 8 : VALUES, batch * tokens);
+  const int blocks = light ? 2 : eights ? 14 * 32 / b.threads : 1;
+  return parts_of(batch, tokens, per_sample, blocks > 1 ? blocks : 1, b.teams);
 }
 
 ff_status_t check_call(ff_layer_norm* h, int64_t batch, int64_t tokens, std::initializer_list<const float*> weights) {
