@@ -266,7 +266,12 @@ struct Ring {
 };
 template <class T, int CH, int PER, int SET>
 constexpr size_t ring_bytes(int threads) { return sizeof(T) * CH >= 4 ? (size_t)STAGES<T> * SET * PER * sizeof(T) * CH * threads : 0; }
-constexpr float DOWN = 8.2718061255302767e-25f;                // 2^-80, for rows whose squares (or sum) leave fp32
+constexpr float DOWN = 8.2718061255302767e-25f;                // 2^-80, for rows whose squares (or sum) leave fp32 ...
+constexpr float MOST = 3.0e38f;                                // ... when they are beyond this
+template <class T> __device__ __forceinline__ float value_at(const char* row, int c) {
+  if constexpr (sizeof(T) == 4) return ((const float*)row)[c];
+  else return __uint_as_float((unsigned)((const unsigned short*)row)[c] << 16);
+}
 
 // Row `at` of a segment, and the team's way from one to the next.  (Rows that follow one another at one distance, of a sample or of a whole
 // contiguous batch, need no division.)
@@ -286,12 +291,45 @@ struct Way {
   }
 };
 
+// A row whose squares leave fp32, once more value by value from memory: DOWN times it and the mean, or, where all values are the same, the row itself
+// and the first of them: minus it they are zeros, or NaN, and eps counts as it is.
+struct Centre { float factor, mean; };
+template <class T, bool WARP, int PLACE>
+__device__ __forceinline__ Centre centre_again_here(const char* row, const NormParams& P, const Team& team, float (*place)[BLOCK_WARPS][PLACE]) {
+  const float first = value_at<T>(row, 0);
+  float s[2] = {0.f, 0.f};
+#pragma unroll 1
+  for (int c = team.thread; c < P.d; c += team.threads) {
+    const float x = value_at<T>(row, c);
+    s[0] = fmaf(x, DOWN, s[0]);
+    s[1] += x != first ? 1.f : 0.f;
+  }
+  team_sum<WARP>(team, s, place);
+  return s[1] == 0.f ? Centre{1.f, first} : Centre{DOWN, s[0] * P.inv_d};
+}
+// A call of its own, so that such rows, which are rare, take no registers from the others.
+template <class T, bool WARP, int PLACE>
+__device__ __noinline__ Centre centre_again_call(const char* row, const NormParams& P, const Team& team, float (*place)[BLOCK_WARPS][PLACE]) {
+  return centre_again_here<T, WARP>(row, P, team, place);
+}
+template <bool CALL, class R, class T, bool WARP, int PLACE>
+__device__ __forceinline__ float centre_again(typename R::V& v, const char* row, const NormParams& P, const Team& team, const typename R::M& mine,
+                                              float (*place)[BLOCK_WARPS][PLACE]) {
+  Centre to;
+  if constexpr (CALL) to = centre_again_call<T, WARP>(row, P, team, place);
+  else to = centre_again_here<T, WARP>(row, P, team, place);
+  R::load(v, row, mine);
+  R::times(v, to.factor);
+  R::centre(v, to.mean, mine);
+  return to.factor;
+}
+
 // Forward: the teams of blocks s * parts .. (s + 1) * parts - 1 take the rows of segment s in turns.
 template <class T, int CH, int PER, bool FULL, bool WARP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD_WARPS<CH, PER> / BLOCK_WARPS : 1) norm_forward_kernel(const __grid_constant__ NormParams P) {
   using R = Row<T, CH, PER, FULL>;
   constexpr int N = R::N;
-  __shared__ __align__(16) Place<THREADS / 32> place[2];
+  __shared__ __align__(16) Place<THREADS / 32> place[4];
   extern __shared__ __align__(16) unsigned char shared[];
   const Team team = team_of<WARP>(P);
   const typename R::M mine(team, P.pieces);
@@ -322,21 +360,17 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD
     float s[1] = {R::sum(v)};
     ask((ring.next() + STAGES<T> - 1) % STAGES<T>);
     team_sum<WARP>(team, s, place);
-    R::centre(v, s[0] * P.inv_d, mine);
+    const float mean = s[0] * P.inv_d;
+    R::centre(v, mean, mine);
     s[0] = R::dot(v, v);
     team_sum<WARP>(team, s, place + 1);
-    float r = rsqrtf(fmaf(s[0], P.inv_d, P.eps));
-    if (!(s[0] < 3.0e38f)) {                                   // (the same in the whole team)
-      // taken again scaled, and eps by the scale's square, which is far below the variance of such a row
-      R::load(v, row_at(P.x, P, segment, at), mine);
-      R::times(v, DOWN);
-      s[0] = R::sum(v);
-      team_sum<WARP>(team, s, place);
-      R::centre(v, s[0] * P.inv_d, mine);
+    float f = 1.f;
+    if (__builtin_expect(!(s[0] < MOST), 0)) {                 // (the same in the whole team)
+      f = centre_again<true, R, T, WARP>(v, row_at(P.x, P, segment, at), P, team, mine, place + 2);
       s[0] = R::dot(v, v);
       team_sum<WARP>(team, s, place + 1);
-      r = rsqrtf(fmaf(s[0], P.inv_d, P.eps * DOWN * DOWN));
     }
+    const float r = rsqrtf(fmaf(s[0], P.inv_d, P.eps * f * f));        // (a row that was scaled down: eps is far below its variance)
 #pragma unroll
     for (int i = 0; i < R::GROUPS; ++i)
 #pragma unroll
@@ -353,7 +387,7 @@ template <class T, int CH, int PER, bool FULL, bool WARP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWARD_BLOCKS : 1) norm_backward_kernel(const __grid_constant__ NormParams P) {
   using R = Row<T, CH, PER, FULL>;
   constexpr int N = R::N;
-  __shared__ __align__(16) Place<THREADS / 32> place[4];
+  __shared__ __align__(16) Place<THREADS / 32> place[6];
   extern __shared__ __align__(16) unsigned char shared[];
   float* joined = (float*)shared;                              // at the end: [teams][d]
   const Team team = team_of<WARP>(P);
@@ -390,7 +424,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWAR
     ask((ring.next() + STAGES<T> - 1) % STAGES<T>);
     float m[1] = {R::sum(v)};
     team_sum<WARP>(team, m, place);
-    R::centre(v, m[0] * P.inv_d, mine);
+    const float mean = m[0] * P.inv_d;
+    R::centre(v, mean, mine);
     // sums of c^2, of g = dy w and of g c
     auto sums = [&](float (&s)[3]) {
       s[0] = R::dot(v, v);
@@ -407,19 +442,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWAR
       s[2] = low(t) + high(t);
       team_sum<WARP>(team, s, place + 1);
     };
-    float s[3];
+    float s[3], f = 1.f;
     sums(s);
-    float r = rsqrtf(fmaf(s[0], P.inv_d, P.eps)), scale = r;
-    if (!(s[0] < 3.0e38f)) {                                   // (as in the forward pass)
-      R::load(v, row_at(P.x, P, segment, at), mine);
-      R::times(v, DOWN);
-      m[0] = R::sum(v);
-      team_sum<WARP>(team, m, place);
-      R::centre(v, m[0] * P.inv_d, mine);
+    if (__builtin_expect(!(s[0] < MOST), 0)) {                 // (as in the forward pass)
+      f = centre_again<CH != 1 || sizeof(T) != 4, R, T, WARP>(v, row_at(P.x, P, segment, at), P, team, mine, place + 4);
       sums(s);
-      scale = rsqrtf(fmaf(s[0], P.inv_d, P.eps * DOWN * DOWN));
-      r = scale * DOWN;
     }
+    const float scale = rsqrtf(fmaf(s[0], P.inv_d, P.eps * f * f)), r = scale * f;
     const float mean_g = -s[1] * P.inv_d, mean_gn = -s[2] * scale * P.inv_d;
 #pragma unroll
     for (int i = 0; i < R::GROUPS; ++i)
