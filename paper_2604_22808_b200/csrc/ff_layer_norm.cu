@@ -4,8 +4,9 @@
 //   backward   g = dy w;  dx = r (g - mean(g) - n mean(g n));  dweight = sum over rows of dy n;  dbias = sum over rows of dy
 //
 // One pass over the rows: a row is read once, stays in registers, and is written once, so memory bounds it: 2 (backward 3) tensors.
-// The mean is subtracted before the squares are summed (the values are in registers, a second sum costs no memory traffic), so
-// rows whose mean is far from zero lose nothing.
+// The mean is subtracted before the squares are summed (the values are in registers, a second sum costs no memory traffic).  A mean of
+// fp32 values is off by 2^-24 of itself for every addition in a chain, 32 at most.  Rows whose mean is above 16 deviations, where that
+// would count, are centred again (centre_again), so that n is off by less than 2^-14 however far from zero a row lies.
 //
 // A team of threads, a warp or a block, takes rows in turns, every thread the same channels of each (32 at most), so that weights, bias and,
 // backward, the gradients' sums of those channels stay in its registers; the next rows are on their way while these are summed.
@@ -33,7 +34,7 @@ namespace {
 constexpr int VALUES = 32;
 constexpr int MAX_DIM = 8192, MAX_THREADS = 512;
 constexpr int BLOCK_WARPS = 8;                    // warps of a block, unless a team has more
-constexpr int BACKWARD_BLOCKS = 1;                // such blocks on an SM
+constexpr int EIGHTS_WARPS = 16;                  // warps on an SM, backward, of the kernel whose threads have 8 values that come one by one
 // Forward, warps on an SM by the registers of their kernels: 64 with up to 8 values a thread (80 where they come one by one), 96 with 16, else 128.
 // (16 for all: 11000 x 1155 fp32 33.5 us instead of 25.6, 20000 x 1155 bf16 54 instead of 36.5.)
 template <int CH, int PER> constexpr int FORWARD_WARPS = CH * PER <= (CH > 1 ? 8 : 4) ? 32 : CH * PER <= (CH > 1 ? 16 : 8) ? (CH > 1 ? 20 : 24) : 16;
@@ -51,7 +52,7 @@ struct NormParams {
   unsigned tokens, segment, parts;  // tokens of a sample; rows whose gradients are summed together, blocks that do it
   FFFastDiv by_tokens;
   int rows, d, pieces, team_warps;
-  float inv_d, eps;
+  float inv_d, least, eps;          // 1 / d, d / 256
 };
 
 __device__ __forceinline__ unsigned divide(unsigned n, const FFFastDiv& f) { return (unsigned)(((unsigned long long)__umulhi(n, f.m) + n) >> f.s); }
@@ -268,6 +269,8 @@ template <class T, int CH, int PER, int SET>
 constexpr size_t ring_bytes(int threads) { return sizeof(T) * CH >= 4 ? (size_t)STAGES<T> * SET * PER * sizeof(T) * CH * threads : 0; }
 constexpr float DOWN = 8.2718061255302767e-25f;                // 2^-80, for rows whose squares (or sum) leave fp32 ...
 constexpr float MOST = 3.0e38f;                                // ... when they are beyond this
+// Squares beyond fp32, or below `least`: a mean of more than 16 deviations, whose rounding, and that of its sum, count among them.
+__device__ __forceinline__ bool far_from_centred(float squares, float least) { return !(squares < MOST && squares >= least); }
 template <class T> __device__ __forceinline__ float value_at(const char* row, int c) {
   if constexpr (sizeof(T) == 4) return ((const float*)row)[c];
   else return __uint_as_float((unsigned)((const unsigned short*)row)[c] << 16);
@@ -291,37 +294,56 @@ struct Way {
   }
 };
 
-// A row whose squares leave fp32, once more value by value from memory: DOWN times it and the mean, or, where all values are the same, the row itself
-// and the first of them: minus it they are zeros, or NaN, and eps counts as it is.
-struct Centre { float factor, mean; };
-template <class T, bool WARP, int PLACE>
-__device__ __forceinline__ Centre centre_again_here(const char* row, const NormParams& P, const Team& team, float (*place)[BLOCK_WARPS][PLACE]) {
+// A row that one mean does not centre (far_from_centred), once more from memory, `factor` times it where its squares leave fp32.  The mean of what the
+// mean left is taken away too, and that of what this left.  Where all values are the same, the mean is the first of them: minus it they are
+// zeros, or NaN, and eps counts as it is.
+// A call of its own, piece by piece, so that such rows, which are rare, take no registers from the others: in its place it cost 20000 x 1154 bf16 forward 47 us
+// in place of 45, 9999 x 3001 fp32 backward 103 in place of 99.  (A tensor of such rows alone takes two to three times as long: 65536 x 2048 bf16 283 us.)
+// AT_ONCE pieces at a time: one, but four backward where rows of several warps come value by value, whose kernel then spills nothing (8000 x 2051 bf16
+// 73 us in place of 93).
+struct Centre { float factor, mean[3], squares; };
+template <class T, int CH, int AT_ONCE, bool WARP, int PLACE>
+__device__ __noinline__ Centre centre_again(const char* row, float factor, const NormParams& P, const Team& team, float (*place)[BLOCK_WARPS][PLACE]) {
+  auto each = [&](auto&& use) {
+#pragma unroll(AT_ONCE)
+    for (int piece = team.thread; piece < P.pieces; piece += team.threads) {
+      F2 v[pairs_of(CH)];
+      unpack<T, CH>(*(const Chunk<T, CH>*)(row + piece * (int)sizeof(Chunk<T, CH>)), v);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) use(c & 1 ? high(v[c / 2]) : low(v[c / 2]));
+    }
+  };
   const float first = value_at<T>(row, 0);
   float s[2] = {0.f, 0.f};
-#pragma unroll 1
-  for (int c = team.thread; c < P.d; c += team.threads) {
-    const float x = value_at<T>(row, c);
-    s[0] = fmaf(x, DOWN, s[0]);
-    s[1] += x != first ? 1.f : 0.f;
-  }
+  each([&](float x) { s[0] = fmaf(x, factor, s[0]); s[1] += x != first ? 1.f : 0.f; });
   team_sum<WARP>(team, s, place);
-  return s[1] == 0.f ? Centre{1.f, first} : Centre{DOWN, s[0] * P.inv_d};
+  if (s[1] == 0.f) return Centre{1.f, {first, 0.f, 0.f}, first - first};
+  Centre to = {factor, {s[0] * P.inv_d, 0.f, 0.f}, 0.f};
+#pragma unroll 1
+  for (int again = 1; again < 3; ++again) {
+    s[0] = s[1] = 0.f;
+    each([&](float x) {
+      const float c = fmaf(x, factor, -to.mean[0]) - to.mean[1];
+      s[0] += c;
+      s[1] = fmaf(c, c, s[1]);
+    });
+    team_sum<WARP>(team, s, place + 2 * again);
+    const float left = s[0] * P.inv_d;
+    (again == 1 ? to.mean[1] : to.mean[2]) = left;
+    to.squares = fmaf(-left, s[0], s[1]);
+  }
+  return to;
 }
-// A call of its own, so that such rows, which are rare, take no registers from the others.
-template <class T, bool WARP, int PLACE>
-__device__ __noinline__ Centre centre_again_call(const char* row, const NormParams& P, const Team& team, float (*place)[BLOCK_WARPS][PLACE]) {
-  return centre_again_here<T, WARP>(row, P, team, place);
-}
-template <bool CALL, class R, class T, bool WARP, int PLACE>
-__device__ __forceinline__ float centre_again(typename R::V& v, const char* row, const NormParams& P, const Team& team, const typename R::M& mine,
-                                              float (*place)[BLOCK_WARPS][PLACE]) {
-  Centre to;
-  if constexpr (CALL) to = centre_again_call<T, WARP>(row, P, team, place);
-  else to = centre_again_here<T, WARP>(row, P, team, place);
+// The same, and the row's values minus all of these.
+template <class R, class T, int CH, int AT_ONCE, bool WARP, int PLACE>
+__device__ __forceinline__ Centre centre_again(typename R::V& v, float squares, const char* row, const NormParams& P, const Team& team, const typename R::M& mine,
+                                               float (*place)[BLOCK_WARPS][PLACE]) {
+  const Centre to = centre_again<T, CH, AT_ONCE, WARP>(row, squares < MOST ? 1.f : DOWN, P, team, place);
   R::load(v, row, mine);
   R::times(v, to.factor);
-  R::centre(v, to.mean, mine);
-  return to.factor;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) R::centre(v, to.mean[i], mine);
+  return to;
 }
 
 // Forward: the teams of blocks s * parts .. (s + 1) * parts - 1 take the rows of segment s in turns.
@@ -329,7 +351,7 @@ template <class T, int CH, int PER, bool FULL, bool WARP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD_WARPS<CH, PER> / BLOCK_WARPS : 1) norm_forward_kernel(const __grid_constant__ NormParams P) {
   using R = Row<T, CH, PER, FULL>;
   constexpr int N = R::N;
-  __shared__ __align__(16) Place<THREADS / 32> place[4];
+  __shared__ __align__(16) Place<THREADS / 32> place[8];
   extern __shared__ __align__(16) unsigned char shared[];
   const Team team = team_of<WARP>(P);
   const typename R::M mine(team, P.pieces);
@@ -360,15 +382,15 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD
     float s[1] = {R::sum(v)};
     ask((ring.next() + STAGES<T> - 1) % STAGES<T>);
     team_sum<WARP>(team, s, place);
-    const float mean = s[0] * P.inv_d;
+    const float mean = s[0] * P.inv_d, least = mean * mean * P.least;
     R::centre(v, mean, mine);
     s[0] = R::dot(v, v);
     team_sum<WARP>(team, s, place + 1);
     float f = 1.f;
-    if (__builtin_expect(!(s[0] < MOST), 0)) {                 // (the same in the whole team)
-      f = centre_again<true, R, T, WARP>(v, row_at(P.x, P, segment, at), P, team, mine, place + 2);
-      s[0] = R::dot(v, v);
-      team_sum<WARP>(team, s, place + 1);
+    if (__builtin_expect(far_from_centred(s[0], least), 0)) {  // (the same in the whole team)
+      const Centre to = centre_again<R, T, CH, 1, WARP>(v, s[0], row_at(P.x, P, segment, at), P, team, mine, place + 2);
+      s[0] = to.squares;
+      f = to.factor;
     }
     const float r = rsqrtf(fmaf(s[0], P.inv_d, P.eps * f * f));        // (a row that was scaled down: eps is far below its variance)
 #pragma unroll
@@ -384,10 +406,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? FORWARD
 // Backward: the teams' rows as in the forward pass, one at a time.  The sums of dweight and dbias of a block's teams are joined and go to its
 // place among the parts.
 template <class T, int CH, int PER, bool FULL, bool WARP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWARD_BLOCKS : 1) norm_backward_kernel(const __grid_constant__ NormParams P) {
+__global__ void __launch_bounds__(CH == 1 && PER == 8 && !WARP ? EIGHTS_WARPS * 32 : THREADS, 1) norm_backward_kernel(const __grid_constant__ NormParams P) {
   using R = Row<T, CH, PER, FULL>;
   constexpr int N = R::N;
-  __shared__ __align__(16) Place<THREADS / 32> place[6];
+  __shared__ __align__(16) Place<THREADS / 32> place[10];
   extern __shared__ __align__(16) unsigned char shared[];
   float* joined = (float*)shared;                              // at the end: [teams][d]
   const Team team = team_of<WARP>(P);
@@ -424,7 +446,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWAR
     ask((ring.next() + STAGES<T> - 1) % STAGES<T>);
     float m[1] = {R::sum(v)};
     team_sum<WARP>(team, m, place);
-    const float mean = m[0] * P.inv_d;
+    const float mean = m[0] * P.inv_d, least = mean * mean * P.least;
     R::centre(v, mean, mine);
     // sums of c^2, of g = dy w and of g c
     auto sums = [&](float (&s)[3]) {
@@ -444,8 +466,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == BLOCK_WARPS * 32 ? BACKWAR
     };
     float s[3], f = 1.f;
     sums(s);
-    if (__builtin_expect(!(s[0] < MOST), 0)) {                 // (as in the forward pass)
-      f = centre_again<CH != 1 || sizeof(T) != 4, R, T, WARP>(v, row_at(P.x, P, segment, at), P, team, mine, place + 4);
+    if (__builtin_expect(far_from_centred(s[0], least), 0)) {  // (as in the forward pass)
+      f = centre_again<R, T, CH, CH == 1 && !WARP ? 4 : 1, WARP>(v, s[0], row_at(P.x, P, segment, at), P, team, mine, place + 4).factor;
       sums(s);
     }
     const float scale = rsqrtf(fmaf(s[0], P.inv_d, P.eps * f * f)), r = scale * f;
@@ -622,13 +644,14 @@ cudaError_t with_piece(int e, int ch, Run run) {
 }
 
 // Backward: the same blocks whatever the tensors' alignment, so that the workspace does not depend on it.  Kernels of rows of up to 256 values have
-// 100 to 130 registers, and two blocks on an SM: 30000 x 128 bf16 13.6 us instead of 16.4.  Longer ones that come one by one, 8 of a thread, have 140,
-// for 14 warps on an SM: 9999 x 1155 bf16 42 us instead of 73 with one block of a team of five.
+// 100 to 130 registers, and two blocks on an SM: 30000 x 128 bf16 13.9 us instead of 16.4.  Longer ones that come one by one, 8 of a thread, are held to
+// 128, so that 16 warps fit, and get as many blocks: 9999 x 1155 bf16 36.5 us instead of 73 with one block of a team of five.  (With room for a block
+// more than there are, blocks come three to an SM and two to another: 9999 x 1155 fp32 53 us with ten warps instead of 41.)
 Parts backward_parts(const ff_layer_norm_config_t& c, int64_t batch, int64_t tokens, int per_sample) {
   const bool single = c.dim % (c.dtype == FF_FP32 ? 4 : 2) != 0, light = c.dim <= 256;
   const bool eights = single && !light && c.dim <= 8 * 32 * BLOCK_WARPS;
   const Block b = block_of(c.dim, eights ? 8 : VALUES, batch * tokens);
-  const int blocks = light ? 2 : eights ? 14 * 32 / b.threads : 1;
+  const int blocks = light ? 2 : eights ? EIGHTS_WARPS * 32 / b.threads : 1;
   return parts_of(batch, tokens, per_sample, blocks > 1 ? blocks : 1, b.teams);
 }
 
@@ -650,6 +673,7 @@ NormParams common(const ff_layer_norm* h, int64_t batch, int64_t tokens, const f
   P.d = h->cfg.dim;
   P.pieces = P.d / ch;
   P.inv_d = 1.f / (float)P.d;
+  P.least = (float)P.d / 256.f;
   P.eps = h->cfg.eps;
   P.even = 1;                                // (each sample's rows are)
   return P;
