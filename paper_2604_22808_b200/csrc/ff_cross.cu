@@ -19,7 +19,8 @@
 //                grows by more than 2^8.  At the end O / l goes out through shared memory by TMA.
 // With tiles of 128 keys there is room for one place of scores a stream: the next ones had to wait for the product with the last P, and
 // 64K queries, 24 heads of 128, 512 keys took 578 us; P in shared memory freed that place, but the products then read more from shared memory
-// than it gives (589 us).  Now 454 us (243 at the rate of a large matrix product).  The issuers are the limit, whose products with M = 128, N = 64
+// than it gives (589 us).  Now 457 us (243 at the rate of a large matrix product) for some 20 ms of calls, captured or not, at 1.9 GHz; 525 in a row for
+// seconds, when the board's power limit holds the clock at 1.7.  The issuers are the limit, whose products with M = 128, N = 64
 // read more operand bytes a cycle than larger tiles, then the softmax (1070 cycles a tile of its own, 1024 of them the two streams' exponentials).
 // Tensor memory (512 columns): S/P of A and of B, twice 64 each, O of A, O of B.  Every wait is bounded; when one runs out the CTA raises
 // FF_ERR_TIMEOUT in the handle's status word, takes no more work and returns.
@@ -395,7 +396,8 @@ cross_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             if (need) { m_ref = m_new; mb = m_new * sl2; }
           }
-          // P = 2^(s scale log2(e) - m) as bf16 over the scores; the row's sum is of the unrounded ones
+          // P = 2^(s scale log2(e) - m) as bf16 over the scores; the row's sum is of the unrounded ones.  (What the product takes: 1.3e-3 to 1.7e-3 of the
+          // result, beside 1.7e-3 by the result's own rounding.  Two bf16 parts of P would be a second product, where the products are the limit.)
           float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
           const float2 sl22 = make_float2(sl2, sl2), nmb2 = make_float2(-mb, -mb);
 #pragma unroll
@@ -763,7 +765,10 @@ extern "C" ff_status_t ff_cross_attention_forward(ff_cross_attention_t* h, int64
   shape_of(c, batch, queries, keys, &P.dm);
   keys_of(&P.dm, h, q, k, v, lengths, mask);
   const Forward f = forward_of(P.dm, lengths != nullptr);
-  // (a few rows wait longer for a tile than that estimate says: 31 us for 20000 keys of 8 heads of 128, in place of 24 by the other kernel)
+  // A few rows wait longer for a tile than that estimate says.  Few rows / tiles, us, one query: 1 head of 64, 16,000 keys 13 / 30, 64,000 46 / 39, 128,000
+  // 88 / 50; 8 heads of 128, 16,000 keys 20 / 28, 64,000 62 / 63, 128,000 116 / 110; 32 on 8 of 128, 64,000 keys 62 / 83; 32 samples, 16 heads on 8 of 128,
+  // 2000 keys 43 / 89 (with lengths from all of them to a quarter, where only the tiles' estimate counts fewer: 32 / 74).  Near the border the slower one
+  // may be chosen: 4 heads of 128, 16,000 keys 27 in place of 19, 1 of 64, 32,000 keys 33 in place of 22.
   if (cx_few_us(P.dm) < 1.3 * f.us + 4) {
     CX_CUDA(h, cx_few_forward(P.dm, q, k, v, out, lse, st));
     return FF_OK;

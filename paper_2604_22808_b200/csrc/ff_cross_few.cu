@@ -176,6 +176,7 @@ cross_few_kernel(const __grid_constant__ FewParams P) {
       sc[i] = ex2(sc[i] - (ref == -INFINITY ? 0.f : ref));
       l[i & 1] += sc[i];
     }
+    // (bf16 is what the product takes, the sum is of the unrounded: see the tiles' kernel)
     const uint32_t p0 = transposed(bf16_pair(__float_as_uint(sc[0]), __float_as_uint(sc[1])));
     const uint32_t p1 = transposed(bf16_pair(__float_as_uint(sc[2]), __float_as_uint(sc[3])));
     // V^T: rows of eight keys and channels, transposed; channels 0 .. 7 and 8 .. 15 of the first eight keys, then of the others

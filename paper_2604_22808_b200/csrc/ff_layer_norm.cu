@@ -620,7 +620,9 @@ cudaError_t backward(NormParams& P, unsigned blocks, cudaStream_t st) {
   const cudaError_t e = allow(kernel, smem);
   return e != cudaSuccess ? e : ff_launch(kernel, dim3(blocks), dim3(b.threads), smem, st, P);
 }
-// The team and the pieces of a thread: a warp where it has room for the row, with as few pieces a thread as do, else several warps.
+// The team and the pieces of a thread: a warp where it has room for the row, with as few pieces a thread as do, else several warps.  (Rows above 4096
+// values that come one by one, 16 of a thread: 512 threads leave it 128 registers, and backward 300 bytes go to memory with bf16, whose next
+// row waits in registers, 60 with fp32: 8000 x 4101 334 and 143 us.)
 template <class T, int CH, bool FORWARD, class Run>
 cudaError_t with_team(int pieces, Run run) {
   using std::integral_constant;

@@ -34,7 +34,8 @@ def check(dtype, dim, values, weights):
     wanted = EPS ** -0.5 * (g - g.mean(-1, keepdim=True))
     bound = 72 * 2.0 ** -24 * EPS ** -0.5 * (g.abs() + g.abs().mean(-1, keepdim=True)) + HALF[dtype] * wanted.abs()
     assert ((dx[1::2].double() - wanted).abs() <= bound).all()
-    # dweight is that of the other rows, sums of n + 1 terms; n is off by 190 x 2^-24 (|n| + 1) at most (tests/test_layer_norm_means_gpu.py)
+    # dweight is that of the other rows, sums of n + 1 terms; n is off by 190 x 2^-24 (|n| + 1) at most (tests/test_layer_norm_means_gpu.py: the mean of
+    # 96 values and more lies within half a deviation, that of one or two is a sum of as many)
     X, DY = x[0::2].double(), dy[0::2].double()
     c = X - X.mean(-1, keepdim=True)
     N = c * ((c * c).mean(-1, keepdim=True) + EPS).rsqrt()
