@@ -424,7 +424,7 @@ typedef struct {
   int32_t dim;             /* 1 .. 8192 */
   int32_t dtype;           /* FF_BF16 or FF_FP32: x, y and their gradients; weights and all arithmetic are fp32 */
   int32_t unit_offset;     /* non-zero: y = (x - mean) r (1 + w) + b */
-  float eps;               /* > 0, finite */
+  float eps;               /* 2^-126 (the smallest fp32 number of all digits) or more, finite */
 } ff_layer_norm_config_t;
 
 /* Rows of dim neighbouring values: value c of token n of sample b lies at data[b stride_batch + n stride_token + c].

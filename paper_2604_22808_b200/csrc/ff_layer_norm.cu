@@ -10,6 +10,7 @@
 //
 // A team of threads, a warp or a block, takes rows in turns, every thread the same channels of each (32 at most), so that weights, bias and,
 // backward, the gradients' sums of those channels stay in its registers; the next rows are on their way while these are summed.
+#include <float.h>
 #include <stdio.h>
 
 #include <initializer_list>
@@ -694,7 +695,8 @@ extern "C" ff_status_t ff_layer_norm_create(const ff_layer_norm_config_t* cfg, f
   if (cfg->dtype != FF_BF16 && cfg->dtype != FF_FP32) return fail(nullptr, FF_ERR_INVALID_ARG, "dtype must be FF_BF16 or FF_FP32");
   if (cfg->dim < 1) return fail(nullptr, FF_ERR_INVALID_ARG, "dim must be positive");
   if (cfg->dim > MAX_DIM) return fail(nullptr, FF_ERR_UNSUPPORTED, "dim must be at most 8192");
-  if (!(cfg->eps > 0.f && cfg->eps < 3.0e38f)) return fail(nullptr, FF_ERR_INVALID_ARG, "eps must be positive and finite");
+  // (below FLT_MIN eps, and the squares that it is added to, have lost digits)
+  if (!(cfg->eps >= FLT_MIN && cfg->eps < 3.0e38f)) return fail(nullptr, FF_ERR_INVALID_ARG, "eps must be at least 2^-126, and finite");
   ff_layer_norm* h = new (std::nothrow) ff_layer_norm();
   if (!h) return fail(nullptr, FF_ERR_INVALID_ARG, "out of host memory");
   h->cfg = *cfg;
