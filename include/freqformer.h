@@ -474,7 +474,7 @@ typedef struct ff_cross_attention ff_cross_attention_t; /* opaque */
 typedef struct {
   int32_t head_dim;        /* multiple of 8, 8 .. 128 */
   int32_t heads, kv_heads; /* heads a multiple of kv_heads, at most 65536 */
-  float scale;             /* > 0, finite; 0: 1 / sqrt(head_dim) */
+  float scale;             /* > 0, below 2.3e38; 0: 1 / sqrt(head_dim) */
 } ff_cross_attention_config_t;
 
 ff_status_t ff_cross_attention_validate(const ff_cross_attention_config_t *cfg);

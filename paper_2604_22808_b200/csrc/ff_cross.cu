@@ -662,7 +662,8 @@ extern "C" ff_status_t ff_cross_attention_validate(const ff_cross_attention_conf
   if (!c) return fail(nullptr, FF_ERR_INVALID_ARG, "cfg is NULL");
   if (c->head_dim < 1 || c->heads < 1 || c->kv_heads < 1) return fail(nullptr, FF_ERR_INVALID_ARG, "head_dim, heads and kv_heads must be positive");
   if (c->heads % c->kv_heads) return fail(nullptr, FF_ERR_INVALID_ARG, "heads must be a multiple of kv_heads");
-  if (!(c->scale >= 0.f && c->scale < 3.0e38f)) return fail(nullptr, FF_ERR_INVALID_ARG, "scale must be positive and finite, or 0 for 1 / sqrt(head_dim)");
+  // (times log2(e), as the kernels count, it is finite too)
+  if (!(c->scale >= 0.f && c->scale < 2.3e38f)) return fail(nullptr, FF_ERR_INVALID_ARG, "scale must be positive and below 2.3e38, or 0 for 1 / sqrt(head_dim)");
   if (c->head_dim % 8 || c->head_dim > 128) return fail(nullptr, FF_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 and at most 128");
   if (c->heads > 65536) return fail(nullptr, FF_ERR_UNSUPPORTED, "at most 65536 heads are supported");
   return FF_OK;

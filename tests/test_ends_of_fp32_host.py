@@ -18,3 +18,10 @@ def test_layer_norm_eps(status, eps):
     lib, c, h = B.library(), B.ff_layer_norm_config_t(64, 0, 0, eps), C.c_void_p()
     assert lib.ff_layer_norm_create(C.byref(c), C.byref(h)) == status and bool(h) == (status == 0)
     lib.ff_layer_norm_destroy(h)
+
+
+@pytest.mark.parametrize("status,scale", [(0, 2.0 ** -126), (0, 2e38), (1, 2.4e38), (1, 2.99e38)])
+def test_cross_attention_scale(status, scale):
+    """Times log2(e), as the kernels count, the scale has to be finite: else scores of zero are no numbers."""
+    lib, c = B.library(), B.ff_cross_attention_config_t(64, 8, 8, scale)
+    assert lib.ff_cross_attention_validate(C.byref(c)) == status
